@@ -90,6 +90,10 @@ typedef enum {
 #define BITLINEAR_F32 0
 #define BITLINEAR_BF16 1
 
+/* Element types of an 8-bit key/value cache. */
+#define BITLINEAR_KV_INT8 0 /* whole numbers -127 .. 127 */
+#define BITLINEAR_KV_E4M3 1 /* 8-bit floats with 4 bits of exponent and 3 of fraction, largest 448 */
+
 /* Layout of a packed weight matrix (field w_format of bitlinear_problem). */
 #define BITLINEAR_WEIGHTS_2BIT 0   /* four values per byte, from bitlinear_pack_weights */
 #define BITLINEAR_WEIGHTS_DENSE5 1 /* five values per byte, from bitlinear_pack_weights5 */
@@ -491,6 +495,90 @@ int bitlinear_attention_decode_append(const float* q, const float* k, const floa
                                       void* stream);
 int bitlinear_lm_head(const void* x_bf16, const void* table_bf16, int M, int V, int K, float* logits, void* stream);
 int bitlinear_embed(const int32_t* ids, const void* table_bf16, int M, int V, int K, void* out_bf16, void* stream);
+
+/*
+ * Serving many requests around the decode step: a paged key/value cache held in 8 bits, and the draw of the next token.
+ * (No counterpart in the paper, which times decode of one request; the definitions are stated here.)
+ *
+ * The cache is a pool of n_blocks blocks; a block holds block_rows rows of every KV head:
+ *   codes  [n_blocks][n_kv][block_rows][D], int8 or e4m3 (kv_dtype), one pool for keys and one for values;
+ *   scales [n_blocks][n_kv] fp32, one per block and head, for each pool: a value is code * scale.
+ * A sequence's row t lies in row t % block_rows of block tables[sequence][t / block_rows].  A slot is
+ * block * block_rows + row, the place of one token in the pool.
+ *
+ * bitlinear_block_tables: the bookkeeping of one step for n_requests requests, from their lengths.
+ *   lengths     in : [R] int32, rows each request has in the cache (one outside 0 .. max_blocks * block_rows counts as the
+ *                    nearest inside).
+ *   new_tokens  in : [R] int32, tokens the request brings in this step; 0: none; negative: the request has finished.
+ *   tables   in/out: [R][max_blocks] int32 block ids; the entries of blocks newly handed out are written, no others.
+ *   free_blocks i/o: [n_blocks] int32, a stack of free block ids; n_free [1] int32 its height.
+ *   A finished request's blocks are pushed (in the order of the requests, each table from its start), then blocks are
+ *   popped for the requests in order, each for its new rows in order.  A request is served whole or not at all: those
+ *   before the first that does not fit - whose blocks the stack no longer has, or whose tokens would pass t_cap - are
+ *   served, those behind it that bring tokens are not.  A request that would outgrow max_blocks blocks is not served
+ *   and does not hold up the others.
+ *   lengths_out [R], n_free_out [1]: the state after the step; may be lengths and n_free themselves, must not overlap them
+ *                    otherwise.
+ *   served      out: [R] int32, 1, or 0 for a request that brought tokens and was not served (its state is unchanged).
+ *   cu_tokens   out: [R + 1] int32, the number of tokens placed before each request, and in all.
+ *   seq_ids, positions, row_lengths, slots out: [t_cap] int32 each, 16-byte aligned: for every token placed its request, its
+ *                    position, position + 1 (the rows it attends to) and its slot (-1 where the table holds an id
+ *                    outside 0 .. n_blocks-1); behind the last token -1, -1, 0, -1.
+ *   One launch (two where lengths or n_free are updated in place and the tokens fill several CTAs).
+ *   block_rows >= 1, max_blocks * block_rows, n_blocks * block_rows and R * max_blocks below 2^31.
+ *
+ * bitlinear_rope_kv8: rotary embedding of q and k as bitlinear_rope_kv, and append of k, v to an 8-bit pool.
+ *   q [T][n_q*D], k, v [T][n_kv*D] fp32; positions, slots [T] int32; rope_table from bitlinear_rope_table with t_max rows;
+ *   q_out bf16 [T][n_q*D] (the fp32 operations of bitlinear_rope_kv; zeros for a position outside 0 .. t_max-1).
+ *   A token whose slot lies outside the pool or whose position lies outside the table is not stored.  The tokens of one block
+ *   must stand next to each other in the call (as bitlinear_block_tables lays them out) and name different slots; this
+ *   is not checked: otherwise the contents of such a block are unspecified.
+ *   For each block and head that receives rows, with a = max |value| over the new rows (keys rotated, not rounded before):
+ *     need  = fl32(a / 127) for int8, the smallest power of two with 448 * need >= a for e4m3;  a at least 1e-30;
+ *     scale = need if the first new row is the block's row 0, else max(old scale, need);
+ *     new rows : code = value / scale rounded to the nearest code, ties to even;
+ *     the rows of the block in front of the new ones, if the scale grew: code = code * old scale / scale, rounded the same way.
+ *   So a block's scale depends on nothing but its own rows, whatever an earlier owner left there, and rows behind the new ones
+ *   keep their bits.
+ *
+ * bitlinear_attention_decode_kv8: bitlinear_attention_decode over an 8-bit pool: query row m attends to rows
+ *   0 .. lengths[m]-1 of sequence seq_ids[m] (NULL: sequence m).  q, out bf16 [M][n_q*D]; tables [n_seq][max_blocks].  A row
+ *   whose length is <= 0 or whose sequence lies outside 0 .. n_seq-1 gives zeros; lengths past the table count as its end; rows
+ *   of a block id outside 0 .. n_blocks-1 are left out.  Codes and scales of rows past a length are never used, whatever
+ *   they hold.  Scores, softmax and sums in fp32; the weights enter the tensor cores as f16.
+ *   D = 64 or 128, n_q / n_kv <= 8, block_rows 16, 32, 64 or 128, n_blocks * n_kv * block_rows < 2^31 - 256,
+ *   max_blocks * block_rows <= 2^30, M <= 65535; pools, q, out 16-byte aligned.  ws (device, 16-byte aligned) at least
+ *   bitlinear_attention_kv8_workspace_bytes(...) bytes (0 for unsupported sizes); contents need not survive, calls that
+ *   share one must not overlap.  The status word as for bitlinear_attention_decode.
+ *
+ * bitlinear_sample: one token per row of logits.  logits [M][V] fp32 or bf16 (logits_dtype), rows row_stride elements apart;
+ *   u, temperature, top_p, min_p [M] fp32, top_k [M] int32, all on the device, all but u nullable (1, 1, 0 and 0).
+ *     w_i = exp((l_i - max l) / temperature);
+ *     top_k  (1 .. V-1, else off): the top_k largest stay; equal logits rank by id, lowest first;
+ *     top_p  (below 1, else off) : of those the shortest run from the largest down whose mass is at least top_p of their mass stays;
+ *     min_p  (above 0)           : of those the ones with w_i >= min_p stay; the largest always does;
+ *     ids[m]      = the first id whose running sum of kept weights, in the order of ids, exceeds u times their total;
+ *     logprobs[m] = log of the kept share of that token (nullable).
+ *   A temperature that is not above 0: the largest logit, lowest id first, logprob 0.  A NaN counts as -infinity; rows of -infinity
+ *   alone give id -1 and logprob -infinity; +infinity shares all weight.  u outside [0, 1): the nearest inside.
+ *   Weights are formed in fp64 and summed as integers in units of 2^-44, so the result does not depend on the order of a sum.
+ *   V <= BITLINEAR_SAMPLE_MAX_VOCAB.  One launch, no workspace.
+ */
+#define BITLINEAR_SAMPLE_MAX_VOCAB 360448
+int bitlinear_block_tables(const int32_t* lengths, const int32_t* new_tokens, int n_requests, int32_t* tables, int max_blocks,
+                           int32_t* free_blocks, const int32_t* n_free, int n_blocks, int block_rows, int t_cap, int32_t* lengths_out,
+                           int32_t* n_free_out, int32_t* served, int32_t* cu_tokens, int32_t* seq_ids, int32_t* positions,
+                           int32_t* row_lengths, int32_t* slots, void* stream);
+int bitlinear_rope_kv8(const float* q, const float* k, const float* v, const int32_t* positions, const int32_t* slots, const float* rope_table,
+                       int T, int t_max, int n_q_heads, int n_kv_heads, int head_dim, void* q_out_bf16, void* k_cache, void* v_cache,
+                       float* k_scale, float* v_scale, int kv_dtype, int n_blocks, int block_rows, void* stream);
+size_t bitlinear_attention_kv8_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim);
+int bitlinear_attention_decode_kv8(const void* q_bf16, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                   const int32_t* tables, const int32_t* lengths, const int32_t* seq_ids, int M, int n_q_heads,
+                                   int n_kv_heads, int head_dim, int kv_dtype, int n_blocks, int block_rows, int n_seq, int max_blocks,
+                                   void* out_bf16, void* ws, size_t ws_bytes, void* stream);
+int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long long row_stride, const float* u, const float* temperature,
+                     const int32_t* top_k, const float* top_p, const float* min_p, int32_t* ids, float* logprobs, void* stream);
 
 /*
  * Self-test of the bounded device-side waits (no counterpart in the paper: every kernel of this library waits on

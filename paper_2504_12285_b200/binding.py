@@ -61,6 +61,12 @@ _SIGNATURES = {
                                                    _c_void_p]),
     "bitlinear_lm_head": (_c_int, [_c_void_p, _c_void_p, _c_int, _c_int, _c_int, _c_void_p, _c_void_p]),
     "bitlinear_embed": (_c_int, [_c_void_p, _c_void_p, _c_int, _c_int, _c_int, _c_void_p, _c_void_p]),
+    "bitlinear_block_tables": (_c_int, [_c_void_p, _c_void_p, _c_int, _c_void_p, _c_int, _c_void_p, _c_void_p, _c_int, _c_int, _c_int] +
+                               [_c_void_p] * 9),
+    "bitlinear_rope_kv8": (_c_int, [_c_void_p] * 6 + [_c_int] * 5 + [_c_void_p] * 5 + [_c_int] * 3 + [_c_void_p]),
+    "bitlinear_attention_kv8_workspace_bytes": (_c_size_t, [_c_int, _c_int, _c_int]),
+    "bitlinear_attention_decode_kv8": (_c_int, [_c_void_p] * 8 + [_c_int] * 9 + [_c_void_p, _c_void_p, _c_size_t, _c_void_p]),
+    "bitlinear_sample": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 8),
     "bitlinear_poll_status": (_c_int, [_c_void_p]),
     "bitlinear_probe_int8_mma_rate": (_c_int, [_c_int, ctypes.POINTER(ctypes.c_double), _c_void_p]),
     "bitlinear_selftest_wait_timeout": (_c_int, [ctypes.c_uint, _c_void_p]),
@@ -617,6 +623,147 @@ def bitlinear_embed(ids, table, out=None):
         out = torch.empty(M, K, dtype=torch.bfloat16, device=table.device)
     _check(lib().bitlinear_embed(_ptr(ids), _ptr(table), M, V, K, _ptr(out), _stream()), "bitlinear_embed")
     return out
+
+
+KV_INT8, KV_E4M3 = 0, 1
+SAMPLE_MAX_VOCAB = 360448
+
+
+def _kvdt(dtype) -> int:
+    if dtype == torch.int8:
+        return KV_INT8
+    if dtype == torch.float8_e4m3fn:
+        return KV_E4M3
+    raise TypeError("8-bit caches must be int8 or float8_e4m3fn")
+
+
+def _same_device(first: torch.Tensor, *others) -> None:
+    """Every tensor on the current device: the library launches there and takes pointers as they come."""
+    index = torch.cuda.current_device()
+    for t in (first, *others):
+        if t is not None and t.device.index != index:
+            raise ValueError(f"tensors must be on the current device, cuda:{index}; got {t.device}")
+
+
+def _rows(t: torch.Tensor | None, n: int, dtype, name: str) -> None:
+    if t is not None and (_dev(t, dtype, name).dim() != 1 or t.shape[0] != n):
+        raise ValueError(f"{name} must have shape ({n},)")
+
+
+def _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads: int, head_dim: int):
+    """(kv_dtype, n_blocks, block_rows) of an 8-bit cache: codes [n_blocks, n_kv, block_rows, D], scales [n_blocks, n_kv]."""
+    kind = _kvdt(k_cache.dtype)
+    _dev(k_cache, k_cache.dtype, "k_cache"), _dev(v_cache, k_cache.dtype, "v_cache")
+    shape = k_cache.shape
+    if v_cache.shape != shape or len(shape) != 4 or shape[1] != n_kv_heads or shape[3] != head_dim:
+        raise ValueError(f"caches must both be [n_blocks, {n_kv_heads}, block_rows, {head_dim}]")
+    _dev(k_scale, torch.float32, "k_scale"), _dev(v_scale, torch.float32, "v_scale")
+    if k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
+        raise ValueError(f"scales must both be [{shape[0]}, {n_kv_heads}]")
+    return kind, shape[0], shape[2]
+
+
+def bitlinear_block_tables(lengths, new_tokens, tables, free_blocks, n_free, block_rows: int, t_cap: int, lengths_out=None, n_free_out=None):
+    """One step's bookkeeping of a paged cache: lengths, new_tokens int32 [R] (negative: finished), tables int32 [R, max_blocks] and
+    free_blocks int32 [n_blocks] updated in place, n_free int32 [1] -> (lengths_out [R], n_free_out [1], served [R], cu_tokens
+    [R + 1], seq_ids, positions, row_lengths, slots [t_cap]), all int32.  lengths_out / n_free_out may be lengths / n_free."""
+    if tables.dim() != 2 or free_blocks.dim() != 1 or t_cap < 0:
+        raise ValueError("tables must be [R, max_blocks], free_blocks [n_blocks], t_cap not negative")
+    R, max_blocks = tables.shape
+    _dev(tables, torch.int32, "tables"), _dev(free_blocks, torch.int32, "free_blocks")
+    _rows(lengths, R, torch.int32, "lengths"), _rows(new_tokens, R, torch.int32, "new_tokens"), _rows(n_free, 1, torch.int32, "n_free")
+    _rows(lengths_out, R, torch.int32, "lengths_out"), _rows(n_free_out, 1, torch.int32, "n_free_out")
+    _same_device(lengths, new_tokens, tables, free_blocks, n_free, lengths_out, n_free_out)
+    # one buffer for what is returned: four columns of tokens (16-byte aligned), then the requests' rows
+    cap, per = (t_cap + 3) // 4 * 4, (R + 4) // 4 * 4
+    out = torch.empty(4 * cap + 3 * per + 4, dtype=torch.int32, device=lengths.device)
+    columns = [out[i * cap:i * cap + t_cap] for i in range(4)]
+    served, cu = out[4 * cap:4 * cap + R], out[4 * cap + per:4 * cap + per + R + 1]
+    if lengths_out is None:
+        lengths_out = out[4 * cap + 2 * per:4 * cap + 2 * per + R]
+    if n_free_out is None:
+        n_free_out = out[4 * cap + 3 * per:4 * cap + 3 * per + 1]
+    rc = lib().bitlinear_block_tables(_ptr(lengths), _ptr(new_tokens), R, _ptr(tables), max_blocks, _ptr(free_blocks), _ptr(n_free),
+                                      free_blocks.shape[0], block_rows, t_cap, _ptr(lengths_out), _ptr(n_free_out), _ptr(served), _ptr(cu),
+                                      *[_ptr(c) for c in columns], _stream())
+    _check(rc, "bitlinear_block_tables")
+    return (lengths_out, n_free_out, served, cu, *columns)
+
+
+def bitlinear_rope_kv8(q, k, v, positions, slots, rope_table, k_cache, v_cache, k_scale, v_scale, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                       q_out=None):
+    """Rotate q, k (fp32 [T, heads * D]) at `positions` (int32 [T]); q -> bf16 (returned), k / v quantised into the 8-bit pool
+    (codes [n_blocks, n_kv, block_rows, D], scales [n_blocks, n_kv]) at `slots` (int32 [T])."""
+    T = q.shape[0]
+    kind, n_blocks, block_rows = _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads, head_dim)
+    for t, heads, name in ((q, n_q_heads, "q"), (k, n_kv_heads, "k"), (v, n_kv_heads, "v")):
+        if tuple(_dev(t, torch.float32, name).shape) != (T, heads * head_dim):
+            raise ValueError(f"{name} must be [{T}, {heads * head_dim}]")
+    _rows(positions, T, torch.int32, "positions"), _rows(slots, T, torch.int32, "slots"), _dev(rope_table, torch.float32, "rope_table")
+    if rope_table.dim() != 3 or tuple(rope_table.shape[1:]) != (head_dim // 2, 2):
+        raise ValueError(f"rope_table must be [t_max, {head_dim // 2}, 2]")
+    if q_out is None:
+        q_out = torch.empty(T, n_q_heads * head_dim, dtype=torch.bfloat16, device=q.device)
+    elif _dev(q_out, torch.bfloat16, "q_out").shape != q.shape:
+        raise ValueError(f"q_out must be {tuple(q.shape)}")
+    _same_device(q, k, v, positions, slots, rope_table, k_cache, v_cache, k_scale, v_scale, q_out)
+    rc = lib().bitlinear_rope_kv8(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(slots), _ptr(rope_table), T, rope_table.shape[0], n_q_heads,
+                                  n_kv_heads, head_dim, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), kind, n_blocks,
+                                  block_rows, _stream())
+    _check(rc, "bitlinear_rope_kv8")
+    return q_out
+
+
+def bitlinear_attention_kv8_workspace_bytes(n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim))
+
+
+def bitlinear_attention_decode_kv8(q, k_cache, v_cache, k_scale, v_scale, tables, lengths, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                                   seq_ids=None, out=None, ws=None):
+    """q bf16 [M, n_q * D] against the first lengths[m] rows of sequence seq_ids[m] (None: sequence m) of an 8-bit pool, whose blocks
+    `tables` (int32 [n_seq, max_blocks]) names -> bf16 [M, n_q * D]."""
+    M = q.shape[0]
+    kind, n_blocks, block_rows = _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads, head_dim)
+    if tuple(_dev(q, torch.bfloat16, "q").shape) != (M, n_q_heads * head_dim):
+        raise ValueError(f"q must be [{M}, {n_q_heads * head_dim}]")
+    if _dev(tables, torch.int32, "tables").dim() != 2:
+        raise ValueError("tables must be [n_seq, max_blocks]")
+    _rows(lengths, M, torch.int32, "lengths"), _rows(seq_ids, M, torch.int32, "seq_ids")
+    if out is None:
+        out = torch.empty(M, n_q_heads * head_dim, dtype=torch.bfloat16, device=q.device)
+    elif _dev(out, torch.bfloat16, "out").shape != q.shape:
+        raise ValueError(f"out must be {tuple(q.shape)}")
+    if ws is None:
+        ws = _workspace(bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), q.device)
+    _same_device(q, k_cache, v_cache, k_scale, v_scale, tables, lengths, seq_ids, out, _dev(ws, torch.uint8, "ws"))
+    rc = lib().bitlinear_attention_decode_kv8(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(tables), _ptr(lengths),
+                                              _ptr(seq_ids), M, n_q_heads, n_kv_heads, head_dim, kind, n_blocks, block_rows, tables.shape[0],
+                                              tables.shape[1], _ptr(out), _ptr(ws), ws.numel(), _stream())
+    _check(rc, "bitlinear_attention_decode_kv8")
+    return out
+
+
+def bitlinear_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, ids=None, logprobs=None):
+    """One token per row of logits (fp32 or bf16 [M, V], rows may be strided) from the given random numbers u (fp32 [M]) ->
+    (ids int32 [M], logprobs fp32 [M]).  temperature, top_p, min_p fp32 [M], top_k int32 [M], None where not wanted."""
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("logits must be a CUDA tensor [M, V] of float32 or bfloat16")
+    M, V = logits.shape
+    stride = logits.stride(0) if M > 1 else V
+    if (V > 1 and logits.stride(1) != 1) or stride < V:
+        raise ValueError("the rows of logits must be contiguous and must not overlap")
+    _rows(u, M, torch.float32, "u"), _rows(temperature, M, torch.float32, "temperature"), _rows(top_k, M, torch.int32, "top_k")
+    _rows(top_p, M, torch.float32, "top_p"), _rows(min_p, M, torch.float32, "min_p")
+    _rows(ids, M, torch.int32, "ids"), _rows(logprobs, M, torch.float32, "logprobs")
+    if ids is None:
+        ids = torch.empty(M, dtype=torch.int32, device=logits.device)
+    if logprobs is None:
+        logprobs = torch.empty(M, dtype=torch.float32, device=logits.device)
+    _same_device(logits, u, temperature, top_k, top_p, min_p, ids, logprobs)
+    rc = lib().bitlinear_sample(_ptr(logits), F32 if logits.dtype == torch.float32 else BF16, M, V, stride, _ptr(u), _ptr(temperature),
+                                _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(ids), _ptr(logprobs), _stream())
+    _check(rc, "bitlinear_sample")
+    return ids, logprobs
 
 
 def bitlinear_selftest_wait_timeout(limit_us: int = 1000) -> None:

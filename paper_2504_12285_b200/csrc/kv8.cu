@@ -1,0 +1,964 @@
+// A paged key/value cache held in 8 bits with one scale per block of rows and KV head: the append (rotary embedding and
+// quantisation) and grouped-query decode attention over it.
+//
+// Layout: pools [n_blocks][n_kv][block_rows][D] of codes (int8, or e4m3 floats), scales fp32 [n_blocks][n_kv]; a row's value is
+// code * scale.  A (block, head) tile is contiguous, so attention fetches it with one tensor-map copy.
+#include "common.cuh"
+#include "sm100_sync.cuh"
+#include "tensor_map.cuh"
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <mutex>
+
+namespace bitlinear {
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------- append
+
+constexpr int kAppendThreads = 128;
+constexpr double kAmaxFloor = 1e-30;  // below this a block counts as all zero
+
+// The scale a block with this largest magnitude needs.  int8: amax / 127, rounded once.  e4m3: the smallest power of two whose
+// 448-fold is no less than amax - the codes are floating point, so a finer scale would gain nothing, and bringing
+// codes to a larger power of two is exact but for the subnormal ones.
+template <int KIND>
+__device__ __forceinline__ float scale_for(double amax) {
+    amax = fmax(amax, kAmaxFloor);
+    if constexpr (KIND == BITLINEAR_KV_INT8) return (float)__ddiv_rn(amax, 127.0);
+    const int hi = __double2hiint(amax);
+    int k = (hi >> 20) - 1023 - 8;  // amax = f * 2^(k + 8), 448 = 1.75 * 2^8
+    const double f = __hiloint2double((hi & 0x000fffff) | 0x3ff00000, __double2loint(amax));
+    if (f > 1.75) ++k;
+    return __int_as_float(min(k + 127, 254) << 23);
+}
+
+// The code nearest to value / scale, ties to even, decided on the quotient in 64 bits: in 32 the quotient's own rounding
+// moves about one code in a million across the middle between two.  int8: the product with the reciprocal decides
+// except next to the middle, where the division itself does.
+__device__ __forceinline__ uint32_t code_int8(double value, double scale, double inv) {
+    double x = value * inv;
+    double c = rint(x);
+    if (fabs(fabs(x - c) - 0.5) < 1e-6) c = rint(__ddiv_rn(value, scale));
+    return (uint32_t)(int)fmin(fmax(c, -127.0), 127.0) & 0xffu;
+}
+// e4m3: the scale is a power of two, so the quotient is exact; it goes to fp32 with the last bit sticky (round to odd),
+// and the conversion to e4m3 then rounds as if it saw all bits
+__device__ __forceinline__ uint32_t code_e4m3(double quotient) {
+    float f = __double2float_rz(quotient);
+    if ((double)f != quotient) f = __int_as_float(__float_as_int(f) | 1);
+    return (uint32_t)__nv_cvt_float_to_fp8(f, __NV_SATFINITE, __NV_E4M3);
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t code_of(double value, double scale, double inv) {
+    if constexpr (KIND == BITLINEAR_KV_INT8) return code_int8(value, scale, inv);
+    else return code_e4m3(value * inv);
+}
+template <int KIND>
+__device__ __forceinline__ double decoded(uint32_t code) {
+    if constexpr (KIND == BITLINEAR_KV_INT8) return (double)(int)(int8_t)code;
+    const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3);
+    return (double)__half2float(__half(h));
+}
+
+struct AppendArgs {
+    const float* q;
+    const float* k;
+    const float* v;
+    const int* positions;
+    const int* slots;
+    const float2* table;
+    int T, t_max, n_q, n_kv, block_rows, n_blocks;
+    __nv_bfloat16* q_out;
+    uint8_t* k_cache;
+    uint8_t* v_cache;
+    float* k_scale;
+    float* v_scale;
+    int tile;       // tokens per CTA of the key/value part
+    int kv_ctas;    // CTAs of the key/value part; those behind it rotate q
+};
+
+// Key/value part: one CTA per (tile of tokens, KV head, keys or values).  The tokens of one block stand next to each other in a
+// call; the first of such a run leads it: its CTA finds the run's largest magnitude, settles the block's scale
+// (scale = max(old, needed) where the block has rows in front of the run, else what is needed), brings the earlier rows' codes
+// to the new scale if it grew, and writes the run's codes.  So a block's scale has one writer and no atomics.
+// Rotation in fp64: the products of two floats are exact there, and the quantiser sees one rounding.
+template <int D, int KIND>
+__device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int h, int which) {
+    constexpr int TPR = D / 8;  // threads per row: four dims and their rotation partners each
+    constexpr int ROWS = kAppendThreads / TPR;
+    __shared__ double red[kAppendThreads / 32];
+    __shared__ int first_s[kAppendThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int sub = tid / TPR, i4 = 4 * (tid % TPR);
+    const int block = a.slots[m0] / a.block_rows;
+    const float* src = which == 0 ? a.k : a.v;
+    // this thread's eight values of token m; false if the token is not of this run (which then ends)
+    auto values = [&](int m, int pos, double (&x)[8]) {
+        const float* row = src + ((size_t)m * a.n_kv + h) * D;
+        const float4 lo = *reinterpret_cast<const float4*>(row + i4), hi = *reinterpret_cast<const float4*>(row + i4 + D / 2);
+        const float l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
+        if (which == 0) {
+            const float4* cs = reinterpret_cast<const float4*>(a.table + (size_t)pos * (D / 2) + i4);
+            const float4 c0 = cs[0], c1 = cs[1];
+            const float c[4] = {c0.x, c0.z, c1.x, c1.z}, s[4] = {c0.y, c0.w, c1.y, c1.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = __dsub_rn((double)l[e] * (double)c[e], (double)u[e] * (double)s[e]);
+                x[4 + e] = __dadd_rn((double)u[e] * (double)c[e], (double)l[e] * (double)s[e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (double)l[e], x[4 + e] = (double)u[e];
+        }
+    };
+    // pass 1: the run's end, its first row in the block, its largest magnitude
+    int end = m0 + 1;
+    while (end < a.T) {  // 32 tokens at a time, the same in every warp
+        const int s = end + lane < a.T ? a.slots[end + lane] : -1;
+        const unsigned other = __ballot_sync(0xffffffffu, s < 0 || s / a.block_rows != block);
+        if (other) {
+            end += __ffs((int)other) - 1;
+            break;
+        }
+        end += 32;
+    }
+    double amax = 0.0;
+    int first = a.block_rows;
+    for (int m = m0 + sub; m < end; m += ROWS) {
+        const int pos = a.positions[m];
+        if (pos < 0 || pos >= a.t_max) continue;
+        double x[8];
+        values(m, pos, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = fmax(amax, fabs(x[e]));
+        first = min(first, a.slots[m] - block * a.block_rows);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, off));
+        first = min(first, __shfl_xor_sync(0xffffffffu, first, off));
+    }
+    if (lane == 0) red[warp] = amax, first_s[warp] = first;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAppendThreads / 32; ++w) amax = fmax(amax, red[w]), first = min(first, first_s[w]);
+    if (first >= a.block_rows) {  // no token of the run has a place in the table of angles
+        __syncthreads();
+        return;
+    }
+    float* scale = (which == 0 ? a.k_scale : a.v_scale) + (size_t)block * a.n_kv + h;
+    uint8_t* tile = (which == 0 ? a.k_cache : a.v_cache) + ((size_t)block * a.n_kv + h) * a.block_rows * D;
+    const float old = *scale, need = scale_for<KIND>(amax);
+    const float now = first > 0 ? fmaxf(old, need) : need;
+    const double s = (double)now, inv = __ddiv_rn(1.0, s);
+    __syncthreads();  // everyone has read the old scale, and the shared buffers are free
+    if (tid == 0) *scale = now;
+    // pass 2: codes
+    for (int m = m0 + sub; m < end; m += ROWS) {
+        const int pos = a.positions[m];
+        if (pos < 0 || pos >= a.t_max) continue;
+        double x[8];
+        values(m, pos, x);
+        uint32_t w[2] = {0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e >> 2] |= code_of<KIND>(x[e], s, inv) << (8 * (e & 3));
+        uint8_t* dst = tile + (size_t)(a.slots[m] - block * a.block_rows) * D;
+        *reinterpret_cast<uint32_t*>(dst + i4) = w[0];
+        *reinterpret_cast<uint32_t*>(dst + i4 + D / 2) = w[1];
+    }
+    if (first > 0 && now > old) {
+        uint32_t* words = reinterpret_cast<uint32_t*>(tile);
+        for (int i = tid; i < first * (D / 4); i += kAppendThreads) {
+            const uint32_t w = words[i];
+            uint32_t r = 0u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r |= code_of<KIND>(decoded<KIND>((w >> (8 * e)) & 0xffu) * (double)old, s, inv) << (8 * e);
+            words[i] = r;
+        }
+    }
+}
+
+template <int D, int KIND>
+__global__ void __launch_bounds__(kAppendThreads) rope_kv8_kernel(const AppendArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n_slots = a.n_blocks * a.block_rows;
+    if ((int)blockIdx.x < a.kv_ctas) {
+        const int item = blockIdx.x % (2 * a.n_kv), t0 = (int)(blockIdx.x / (2 * a.n_kv)) * a.tile;
+        for (int m = t0; m < min(t0 + a.tile, a.T); ++m) {
+            const int s = a.slots[m], p = m > 0 ? a.slots[m - 1] : -1;
+            if (s < 0 || s >= n_slots) continue;
+            if (p >= 0 && p / a.block_rows == s / a.block_rows) continue;  // not the first of its run
+            append_run<D, KIND>(a, m, item >> 1, item & 1);
+        }
+    } else {
+        // rotated queries, four pairs per thread; the same fp32 operations in the same order as the other append calls
+        constexpr int UNITS = D / 8;
+        const long long n = (long long)a.T * a.n_q * UNITS, step = (long long)(gridDim.x - a.kv_ctas) * kAppendThreads;
+        for (long long u = (long long)(blockIdx.x - a.kv_ctas) * kAppendThreads + threadIdx.x; u < n; u += step) {
+            const long long mh = u / UNITS;
+            const int i4 = 4 * (int)(u - mh * UNITS), m = (int)(mh / a.n_q), pos = a.positions[m];
+            const float* row = a.q + mh * D;
+            uint2 lo2 = make_uint2(0u, 0u), hi2 = lo2;  // a row without a position: zeros
+            if (pos >= 0 && pos < a.t_max) {
+                const float4 lo = *reinterpret_cast<const float4*>(row + i4), hi = *reinterpret_cast<const float4*>(row + i4 + D / 2);
+                const float4* cs = reinterpret_cast<const float4*>(a.table + (size_t)pos * (D / 2) + i4);
+                const float4 c0 = cs[0], c1 = cs[1];
+                const float l[4] = {lo.x, lo.y, lo.z, lo.w}, r[4] = {hi.x, hi.y, hi.z, hi.w};
+                const float c[4] = {c0.x, c0.z, c1.x, c1.z}, s[4] = {c0.y, c0.w, c1.y, c1.w};
+                float ol[4], oh[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ol[e] = __fsub_rn(__fmul_rn(l[e], c[e]), __fmul_rn(r[e], s[e]));
+                    oh[e] = __fadd_rn(__fmul_rn(r[e], c[e]), __fmul_rn(l[e], s[e]));
+                }
+                auto pair = [](float x, float y) {
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+                    return *reinterpret_cast<const uint32_t*>(&b);
+                };
+                lo2 = make_uint2(pair(ol[0], ol[1]), pair(ol[2], ol[3]));
+                hi2 = make_uint2(pair(oh[0], oh[1]), pair(oh[2], oh[3]));
+            }
+            *reinterpret_cast<uint2*>(a.q_out + mh * D + i4) = lo2;
+            *reinterpret_cast<uint2*>(a.q_out + mh * D + i4 + D / 2) = hi2;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- decode attention
+
+constexpr int kUnit = 32;        // cache rows a warp takes at a time
+constexpr int kWarps = 8;        // each with its own ring of units in shared memory
+constexpr int kMaxCtas = 160;    // one CTA per SM; partial results are reserved for this many
+constexpr int kMaxStages = 8;
+
+// One (row, KV head) pair is the work of one softmax.  All units of all pairs, in the order (row, head, unit), are cut into equal
+// runs, one per warp of the grid, so that a batch of any lengths loads every SM alike.  A run covers pairs in whole
+// (finished by the warp) and at most two in part; those meet in shared memory with the neighbouring warps' and,
+// where a pair reaches beyond the CTA, in global memory, where a second launch merges them.
+struct AttnArgs {
+    const __nv_bfloat16* q;
+    const float* k_scale;
+    const float* v_scale;
+    const int* tables;
+    const int* lengths;
+    const int* seq_ids;
+    int M, n_q, n_kv, n_seq, max_blocks, log2_rows, n_blocks;
+    int stages;
+    float scale_log2;  // log2(e) / sqrt(D)
+    __nv_bfloat16* out;
+    float* part;       // [CTA][2][group * D values, then (max, sum) of each head]
+    int2* desc;        // [CTA][2] (pair, last CTA that holds a part of it); pair -1: none
+    int* status;
+};
+
+struct UnitMeta {
+    int m, h;
+    uint32_t rows;   // live rows, one bit each
+    int flags;       // 1: first unit of this run's part of the pair, 2: last
+    float ks[2], vs[2];  // scales of the unit's halves
+    long long begin, end;  // the pair's units
+};
+
+struct PartHead {
+    long long begin, end;  // the pair's units
+    int m, h, used, pad;
+    float m_run[8], l_run[8];
+};
+
+__device__ __forceinline__ int row_len(const AttnArgs& a, int m) {
+    const int seq = a.seq_ids ? a.seq_ids[m] : m;
+    if (seq < 0 || seq >= a.n_seq) return 0;
+    return min(max(a.lengths[m], 0), a.max_blocks << a.log2_rows);
+}
+// units of a (row, head) pair: at least one, so that an empty row has someone to write its zeros
+__device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+
+// The order in which the rows of an eight-row group take the tensor core's row slots.  Any order is right as long as scores and
+// values use the same one; in this one neither read of a swizzled tile meets a bank twice (checked for 64- and 128-byte rows).
+__device__ __forceinline__ int row_of_slot(int i) { return (0x25346170 >> (4 * i)) & 7; }
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix_t16(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Four codes of a word -> two pairs of f16, exactly.  int8: the code plus 128 becomes the low bits of 1024 + x, and
+// 1152 is taken off.  e4m3: the conversion instruction.
+template <int KIND>
+__device__ __forceinline__ void to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if constexpr (KIND == BITLINEAR_KV_INT8) {
+        const uint32_t u = w ^ 0x80808080u;
+        const uint32_t off = 0x64806480u, l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&l), *reinterpret_cast<const __half2*>(&off));
+        const __half2 b = __hsub2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&off));
+        lo = *reinterpret_cast<const uint32_t*>(&a);
+        hi = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+    }
+}
+
+__device__ __forceinline__ void lds128(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void lds64(uint32_t addr, uint32_t (&r)[2]) {
+    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
+}
+
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst),
+        "l"(map), "r"(0), "r"(row), "r"(bar), "l"(policy)
+        : "memory");
+}
+
+// a warp's partial result in shared memory: head, then group * D values
+__host__ __device__ inline size_t part_smem(int group, int D) { return sizeof(PartHead) + (size_t)group * D * sizeof(float); }
+__host__ __device__ inline size_t part_floats(int group, int D) { return (size_t)group * D + 2 * group; }
+
+size_t attn8_smem(int group, int D, int stages) {
+    return 1024 + (size_t)kWarps * stages * (2 * kUnit * D + sizeof(UnitMeta) + 8) + kWarps * part_smem(group, D) + 16;
+}
+
+// first unit of worker w's run
+__device__ __forceinline__ long long run_begin(long long units, int w, int workers) { return units * w / workers; }
+
+template <int D, int KIND>
+__global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                                                      const AttnArgs a) {
+    constexpr int KS = D / 16;     // k-steps of the scores, and 16-dim tiles of the result
+    constexpr int VW = D / 32;     // 32-bit words of a value row per lane
+    constexpr uint32_t kUnitBytes = 2u * kUnit * D;  // keys, then values
+    extern __shared__ uint8_t attn8_raw[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
+    const int group = a.n_q / a.n_kv, stages = a.stages;
+    uint8_t* smem = attn8_raw + ((1024u - (smem_u32(attn8_raw) & 1023u)) & 1023u);
+    const uint32_t ring = smem_u32(smem) + (uint32_t)warp * stages * kUnitBytes;
+    UnitMeta* meta = reinterpret_cast<UnitMeta*>(smem + (size_t)kWarps * stages * kUnitBytes) + warp * stages;
+    uint8_t* parts0 = smem + (size_t)kWarps * stages * (kUnitBytes + sizeof(UnitMeta));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(parts0 + kWarps * part_smem(group, D));
+    const uint32_t full = smem_u32(bars + warp * stages);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kWarps * stages);
+    __shared__ int second_used[kWarps];
+    if (tid == 0) *abort_flag = 0;
+    if (lane == 0) {
+        for (int s = 0; s < stages; ++s) mbar_init(full + 8u * s, 1);
+        mbar_init_fence();
+        reinterpret_cast<PartHead*>(parts0 + warp * part_smem(group, D))->used = 0;
+        second_used[warp] = 0;
+    }
+    if (tid == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __syncthreads();
+
+    // ---- this warp's run of units
+    const int workers = gridDim.x * kWarps, me = blockIdx.x * kWarps + warp;
+    long long total = 0;
+    for (int m = lane; m < a.M; m += 32) total += units_of(row_len(a, m));
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
+    const long long units = total * a.n_kv;
+    const long long u0 = run_begin(units, me, workers), u1 = run_begin(units, me + 1, workers);
+    const int n_units = (int)(u1 - u0);
+    // the pair u0 lies in: row pm (its length and units), head ph, first unit of the pair
+    int pm = 0, ph = 0, p_len = 0, p_units = 1, p_unit = 0;
+    long long p_begin = 0;
+    if (n_units > 0) {
+        long long base = 0;
+        for (int m0 = 0; m0 < a.M; m0 += 32) {
+            const int len = m0 + lane < a.M ? row_len(a, m0 + lane) : 0;
+            const long long n = m0 + lane < a.M ? (long long)units_of(len) * a.n_kv : 0;
+            long long incl = n;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += up;
+            }
+            const unsigned past = __ballot_sync(0xffffffffu, base + incl > u0);
+            if (past) {
+                const int src = __ffs((int)past) - 1;
+                pm = m0 + src;
+                p_len = __shfl_sync(0xffffffffu, len, src);
+                p_units = units_of(p_len);
+                const long long row_begin = base + __shfl_sync(0xffffffffu, incl - n, src);
+                ph = (int)((u0 - row_begin) / p_units);
+                p_begin = row_begin + (long long)ph * p_units;
+                p_unit = (int)(u0 - p_begin);
+                break;
+            }
+            base += __shfl_sync(0xffffffffu, incl, 31);
+        }
+    }
+
+    // ---- producer side: issue unit n of the run into its ring place
+    const uint64_t once = l2_evict_first_policy();
+    const int rows_log2 = a.log2_rows, per_unit = rows_log2 < 5 ? 2 : 1;  // blocks a unit spans
+    int c_base = 0, c_id = -1;    // lane l holds table entry c_base + l of the row, its scales for head ph
+    float c_ks = 0.0f, c_vs = 0.0f;
+    bool c_valid = false;
+    int issued = 0;
+    auto issue = [&]() {
+        const int place = issued % stages;
+        const int b = (p_unit * kUnit) >> rows_log2;
+        if (!c_valid || b < c_base || b + per_unit > c_base + 32) {
+            c_base = b;
+            c_valid = true;
+            const int seq = a.seq_ids ? a.seq_ids[pm] : pm;
+            const int idx = b + lane;
+            c_id = ((long long)idx << rows_log2) < p_len ? a.tables[(size_t)seq * a.max_blocks + idx] : -1;
+            if (c_id < 0 || c_id >= a.n_blocks) c_id = -1;
+            c_ks = c_id >= 0 ? a.k_scale[(size_t)c_id * a.n_kv + ph] : 0.0f;
+            c_vs = c_id >= 0 ? a.v_scale[(size_t)c_id * a.n_kv + ph] : 0.0f;
+        }
+        const int l0 = b - c_base, l1 = l0 + per_unit - 1;
+        const int id0 = __shfl_sync(0xffffffffu, c_id, l0), id1 = __shfl_sync(0xffffffffu, c_id, l1);
+        const float ks0 = __shfl_sync(0xffffffffu, c_ks, l0), ks1 = __shfl_sync(0xffffffffu, c_ks, l1);
+        const float vs0 = __shfl_sync(0xffffffffu, c_vs, l0), vs1 = __shfl_sync(0xffffffffu, c_vs, l1);
+        if (lane == 0) {
+            const int live = min(max(p_len - p_unit * kUnit, 0), kUnit);
+            uint32_t rows = live == 32 ? 0xffffffffu : (1u << live) - 1u;
+            if (id0 < 0) rows &= 0xffff0000u;
+            if (id1 < 0) rows &= 0x0000ffffu;
+            UnitMeta& w = meta[place];
+            w.m = pm;
+            w.h = ph;
+            w.rows = rows;
+            w.flags = (issued == 0 || p_unit == 0 ? 1 : 0) | (issued == n_units - 1 || p_unit == p_units - 1 ? 2 : 0);
+            w.ks[0] = ks0, w.ks[1] = ks1, w.vs[0] = vs0, w.vs[1] = vs1;
+            w.begin = p_begin, w.end = p_begin + p_units;
+            const uint32_t dst = ring + (uint32_t)place * kUnitBytes, bar = full + 8u * place;
+            const uint32_t off = (uint32_t)(p_unit * kUnit) & ((1u << rows_log2) - 1u);
+            const uint32_t copies = per_unit == 1 ? (id0 >= 0 ? 1u : 0u) : (id0 >= 0 ? 1u : 0u) + (id1 >= 0 ? 1u : 0u);
+            mbar_expect_tx(bar, copies * (kUnitBytes / per_unit));  // none: the phase completes at once
+            if (id0 >= 0) {
+                const int row = ((id0 * a.n_kv + ph) << rows_log2) + (int)off;
+                tma_rows(dst, &map_k, row, bar, once);
+                tma_rows(dst + kUnitBytes / 2, &map_v, row, bar, once);
+            }
+            if (per_unit == 2 && id1 >= 0) {
+                const int row = (id1 * a.n_kv + ph) << rows_log2;
+                tma_rows(dst + 16 * D, &map_k, row, bar, once);
+                tma_rows(dst + kUnitBytes / 2 + 16 * D, &map_v, row, bar, once);
+            }
+        }
+        ++issued;
+        if (++p_unit == p_units) {  // on to the next pair
+            p_unit = 0;
+            p_begin += p_units;
+            c_valid = false;
+            if (++ph == a.n_kv) {
+                ph = 0;
+                if (++pm < a.M) {
+                    p_len = row_len(a, pm);
+                    p_units = units_of(p_len);
+                }
+            }
+        }
+    };
+
+    // ---- consumer side
+    uint32_t qb[KS][2];
+    float o[KS][4], m_run[2], l_run[2], f_head[2], v_ref = 1.0f;
+    const int r_lo = row_of_slot(g);
+    int r_v[2] = {row_of_slot(2 * qd), row_of_slot(2 * qd + 1)};
+
+    auto begin_pair = [&](int m, int h) {
+        // The group's queries as the second operand: column g = head g of the group.  The order of the dims over the k-slots is
+        // that in which the key codes arrive: word s of 16-byte chunk qd (+ 4).  Each head is scaled by the power
+        // of two that brings its largest magnitude to 2^8 .. 2^9: bf16 values then fit f16 without loss down to
+        // 2^-22 of the largest, and the scores are scaled back in fp32.
+        const uint4* row = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)h * group + min(g, group - 1)) * D);
+        uint32_t raw[KS][2];
+#pragma unroll
+        for (int hf = 0; hf < D / 64; ++hf) {
+            const uint4 x = row[8 * hf + 2 * qd], y = row[8 * hf + 2 * qd + 1];
+            raw[4 * hf + 0][0] = x.x, raw[4 * hf + 0][1] = x.y, raw[4 * hf + 1][0] = x.z, raw[4 * hf + 1][1] = x.w;
+            raw[4 * hf + 2][0] = y.x, raw[4 * hf + 2][1] = y.y, raw[4 * hf + 3][0] = y.z, raw[4 * hf + 3][1] = y.w;
+        }
+        float amax = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(raw[s][e] << 16)), fabsf(__uint_as_float(raw[s][e] & 0xffff0000u))));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const int be = max(__float_as_int(amax) >> 23, 9);
+        const float up = __int_as_float((262 - be) << 23), down = __int_as_float((be - 8) << 23);  // 2^(135 - be), its inverse
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                qb[s][e] = g < group ? pack_f16(__uint_as_float(raw[s][e] << 16) * up, __uint_as_float(raw[s][e] & 0xffff0000u) * up) : 0u;
+        const float f = down * a.scale_log2;
+        f_head[0] = __shfl_sync(0xffffffffu, f, 8 * qd);
+        f_head[1] = __shfl_sync(0xffffffffu, f, 8 * qd + 4);
+        m_run[0] = m_run[1] = -INFINITY;
+        l_run[0] = l_run[1] = 0.0f;
+        v_ref = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) o[t][0] = o[t][1] = o[t][2] = o[t][3] = 0.0f;
+    };
+
+    auto consume = [&](uint32_t base, const UnitMeta& w) {
+        const uint32_t rows = w.rows;
+        const uint32_t vbase = base + kUnitBytes / 2;
+        if (rows != 0xffffffffu) {  // dead rows may hold any bits, and zero times NaN is NaN: overwrite their values
+            for (int i = lane; i < kUnit * (D / 16); i += 32) {
+                if (!((rows >> (i / (D / 16))) & 1u))
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vbase + 16u * i), "r"(0u) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the ring place is a copy's target again later
+            __syncwarp();
+        }
+        // scores of both halves: S^T (16 rows x 8 heads) = K (16 x D) Q^T
+        float sv[2][4];
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+            float s0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const uint32_t row_lo = base + (uint32_t)(16 * hb + r_lo) * D, row_hi = row_lo + 8 * D;
+#pragma unroll
+            for (int hf = 0; hf < D / 64; ++hf) {
+                const uint32_t c = D == 128 ? (uint32_t)(((qd + 4 * hf) ^ r_lo) << 4) : (uint32_t)((qd ^ ((r_lo >> 1) & 3)) << 4);
+                uint32_t x[4], y[4];
+                lds128(row_lo + c, x);
+                lds128(row_hi + c, y);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    uint32_t f[4];
+                    to_f16<KIND>(x[s], f[0], f[2]);
+                    to_f16<KIND>(y[s], f[1], f[3]);
+                    if (s & 1) mma_f16(s1, f, qb[4 * hf + s][0], qb[4 * hf + s][1]);
+                    else mma_f16(s0, f, qb[4 * hf + s][0], qb[4 * hf + s][1]);
+                }
+            }
+            const float ks = w.ks[hb];
+            const bool live_lo = (rows >> (16 * hb + r_lo)) & 1u, live_hi = (rows >> (16 * hb + 8 + r_lo)) & 1u;
+            sv[hb][0] = live_lo ? (s0[0] + s1[0]) * (ks * f_head[0]) : -INFINITY;  // a dead row may hold anything: selected away
+            sv[hb][1] = live_lo ? (s0[1] + s1[1]) * (ks * f_head[1]) : -INFINITY;
+            sv[hb][2] = live_hi ? (s0[2] + s1[2]) * (ks * f_head[0]) : -INFINITY;
+            sv[hb][3] = live_hi ? (s0[3] + s1[3]) * (ks * f_head[1]) : -INFINITY;
+        }
+        float mx0 = fmaxf(fmaxf(sv[0][0], sv[0][2]), fmaxf(sv[1][0], sv[1][2]));
+        float mx1 = fmaxf(fmaxf(sv[0][1], sv[0][3]), fmaxf(sv[1][1], sv[1][3]));
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+        }
+        // The values' scales ride on the weights: o is held in units of the largest scale met so far.
+        const float vs = fmaxf(w.vs[0], w.vs[1]);
+        if (__any_sync(0xffffffffu, mx0 > m_run[0] || mx1 > m_run[1]) || vs > v_ref) {
+            const float n0 = fmaxf(m_run[0], mx0), n1 = fmaxf(m_run[1], mx1), nv = fmaxf(v_ref, vs);
+            const float fv = nv > 0.0f ? v_ref / nv : 0.0f;
+            const float c0 = n0 == -INFINITY ? 1.0f : exp2f(m_run[0] - n0), c1 = n1 == -INFINITY ? 1.0f : exp2f(m_run[1] - n1);
+            l_run[0] *= c0;
+            l_run[1] *= c1;
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                o[t][0] *= c0 * fv;
+                o[t][1] *= c1 * fv;
+                o[t][2] *= c0 * fv;
+                o[t][3] *= c1 * fv;
+            }
+            m_run[0] = n0;
+            m_run[1] = n1;
+            v_ref = nv;
+        }
+        const float b0 = m_run[0] == -INFINITY ? 0.0f : m_run[0], b1 = m_run[1] == -INFINITY ? 0.0f : m_run[1];
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+            const float p0 = exp2f(sv[hb][0] - b0), p1 = exp2f(sv[hb][1] - b1), p2 = exp2f(sv[hb][2] - b0), p3 = exp2f(sv[hb][3] - b1);
+            l_run[0] += p0 + p2;  // this lane's rows; summed over the lanes at the pair's end
+            l_run[1] += p1 + p3;
+            // Weights as f16, scaled by 2^15 so that the smallest ones keep their bits: an error of 2^-12 of a weight, at random
+            // signs, against the result's own rounding of 2^-9.
+            const float wv = v_ref > 0.0f ? 32768.0f * __fdividef(w.vs[hb], v_ref) : 0.0f;
+            const uint32_t w0 = movmatrix_t16(pack_f16(p0 * wv, p1 * wv)), w1 = movmatrix_t16(pack_f16(p2 * wv, p3 * wv));
+            // O^T (D x 8 heads) += V^T (D x 16 rows) P; lane (g, qd) holds dims 2 VW ... of rows in slots 2qd, 2qd+1 (+8)
+            uint32_t x[4][VW];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = r_v[j & 1];
+                const uint32_t row = vbase + (uint32_t)(16 * hb + 8 * (j >> 1) + r) * D;
+                if constexpr (D == 128) lds128(row + (uint32_t)((g ^ r) << 4), x[j]);
+                else lds64(row + (uint32_t)((((g >> 1) ^ ((r >> 1) & 3)) << 4) + ((g & 1) << 3)), x[j]);
+            }
+#pragma unroll
+            for (int q = 0; q < VW; ++q) {
+                const uint32_t t0 = __byte_perm(x[0][q], x[1][q], 0x5140), t1 = __byte_perm(x[2][q], x[3][q], 0x5140);
+                const uint32_t t2 = __byte_perm(x[0][q], x[1][q], 0x7362), t3 = __byte_perm(x[2][q], x[3][q], 0x7362);
+                uint32_t f[4];
+                to_f16<KIND>(t0, f[0], f[1]);
+                to_f16<KIND>(t1, f[2], f[3]);
+                mma_f16(o[2 * q], f, w0, w1);
+                to_f16<KIND>(t2, f[0], f[1]);
+                to_f16<KIND>(t3, f[2], f[3]);
+                mma_f16(o[2 * q + 1], f, w0, w1);
+            }
+        }
+    };
+
+    // lane (g, qd) holds dims (2 KS) g + 0 .. 2 KS - 1 of heads 2qd, 2qd + 1: o[t][e] is dim 2t, o[t][2 + e] dim 2t + 1
+    auto end_pair = [&](const UnitMeta& w) {
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+            l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
+            l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
+        }
+        const float unscale = v_ref * (1.0f / 32768.0f);
+        const bool whole = w.begin >= u0 && w.end <= u1;
+        if (whole) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int head = 2 * qd + e;
+                if (head < group) {
+                    const float f = l_run[e] > 0.0f ? unscale / l_run[e] : 0.0f;
+                    uint32_t r[KS];
+#pragma unroll
+                    for (int t = 0; t < KS; ++t) {
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(o[t][e] * f, o[t][2 + e] * f);
+                        r[t] = *reinterpret_cast<const uint32_t*>(&b);
+                    }
+                    uint4* dst = reinterpret_cast<uint4*>(a.out + ((size_t)w.m * a.n_q + (size_t)w.h * group + head) * D + 2 * KS * g);
+#pragma unroll
+                    for (int i = 0; i < KS / 4; ++i) dst[i] = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+                }
+            }
+            return;
+        }
+        // a part: the pair began before this run (first place), or goes on behind it (second place: this warp's ring, whose
+        // copies have all landed - a pair that goes on is the run's last)
+        const bool second = w.begin >= u0;
+        uint8_t* at = second ? smem + (size_t)warp * stages * kUnitBytes : parts0 + warp * part_smem(group, D);
+        PartHead* head_p = reinterpret_cast<PartHead*>(at);
+        float* val = reinterpret_cast<float*>(at + sizeof(PartHead));
+        __syncwarp();
+        if (lane == 0) {
+            head_p->begin = w.begin, head_p->end = w.end, head_p->m = w.m, head_p->h = w.h, head_p->used = 1;
+            if (second) second_used[warp] = 1;
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int head = 2 * qd + e;
+            if (head < group) {
+                if (g == 0) head_p->m_run[head] = m_run[e], head_p->l_run[head] = l_run[e];
+#pragma unroll
+                for (int t = 0; t < KS; ++t)
+                    *reinterpret_cast<float2*>(val + head * D + 2 * KS * g + 2 * t) = make_float2(o[t][e] * unscale, o[t][2 + e] * unscale);
+            }
+        }
+    };
+
+    const int ahead = min(stages, n_units);
+    for (int n = 0; n < ahead; ++n) issue();
+    for (int n = 0; n < n_units; ++n) {
+        const int place = n % stages;
+        const bool landed = mbar_wait(full + 8u * place, (uint32_t)(n / stages) & 1u, abort_flag);
+        if (!__all_sync(0xffffffffu, landed)) break;
+        const UnitMeta w = meta[place];
+        if (w.flags & 1) begin_pair(w.m, w.h);
+        consume(ring + (uint32_t)place * kUnitBytes, w);
+        if (w.flags & 2) end_pair(w);
+        __syncwarp();
+        if (issued < n_units) issue();
+    }
+
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) {
+            if (a.status != nullptr) atomicExch(a.status, BITLINEAR_ERR_TIMEOUT);
+            a.desc[2 * blockIdx.x] = a.desc[2 * blockIdx.x + 1] = make_int2(-1, 0);
+        }
+        abort_drain();
+        return;
+    }
+    // ---- merge the warps' parts; parts of one pair stand next to each other in the order (warp, place)
+    const long long c0 = run_begin(units, blockIdx.x * kWarps, workers), c1 = run_begin(units, blockIdx.x * kWarps + kWarps, workers);
+    auto part_at = [&](int i) {
+        const int w = i >> 1;
+        return reinterpret_cast<const PartHead*>((i & 1) ? smem + (size_t)w * stages * kUnitBytes : parts0 + w * part_smem(group, D));
+    };
+    auto part_used = [&](int i) { return (i & 1) ? second_used[i >> 1] != 0 : part_at(i)->used != 0; };
+    int2 desc[2] = {make_int2(-1, 0), make_int2(-1, 0)};
+    for (int i = 0; i < 2 * kWarps;) {
+        if (!part_used(i)) {
+            ++i;
+            continue;
+        }
+        const PartHead* lead = part_at(i);
+        int j = i + 1, members = 1;
+        uint32_t mask = 1u << i;
+        for (; j < 2 * kWarps; ++j) {
+            if (!part_used(j)) continue;
+            if (part_at(j)->begin != lead->begin) break;
+            mask |= 1u << j;
+            ++members;
+        }
+        const bool whole = lead->begin >= c0 && lead->end <= c1;
+        const int slot = lead->begin < c0 ? 0 : 1;
+        float* dst = a.part + ((size_t)blockIdx.x * 2 + slot) * part_floats(group, D);
+        for (int e = tid; e < group * D; e += kWarps * 32) {
+            const int head = e / D;
+            float top = -INFINITY;
+            for (uint32_t mk = mask; mk; mk &= mk - 1) top = fmaxf(top, part_at(__ffs((int)mk) - 1)->m_run[head]);
+            float acc = 0.0f, l = 0.0f;
+            for (uint32_t mk = mask; mk; mk &= mk - 1) {
+                const PartHead* p = part_at(__ffs((int)mk) - 1);
+                const float f = p->m_run[head] == -INFINITY ? 0.0f : exp2f(p->m_run[head] - top);
+                l = fmaf(p->l_run[head], f, l);
+                acc = fmaf(reinterpret_cast<const float*>(p + 1)[e], f, acc);
+            }
+            if (whole) a.out[((size_t)lead->m * a.n_q + (size_t)lead->h * group) * D + e] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
+            else {
+                dst[e] = acc;
+                if (e % D == 0) dst[group * D + 2 * head] = top, dst[group * D + 2 * head + 1] = l;
+            }
+        }
+        if (!whole) {
+            // the CTA that holds the pair's last unit
+            const long long x = lead->end - 1;
+            int w = (int)(x * workers / units);
+            while (run_begin(units, w + 1, workers) <= x) ++w;
+            while (run_begin(units, w, workers) > x) --w;
+            desc[slot] = make_int2(lead->m * a.n_kv + lead->h, w / kWarps);
+        }
+        i = j;
+    }
+    if (tid == 0) a.desc[2 * blockIdx.x] = desc[0], a.desc[2 * blockIdx.x + 1] = desc[1];
+}
+
+// Merges the parts of a pair that several CTAs share: CTA (c, head) does nothing unless a pair begins in attention CTA c and goes
+// on behind it.  Eight warps take the parts in turn, a lane D / 32 dims.
+template <int D>
+__global__ void __launch_bounds__(256) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
+                                                                      __nv_bfloat16* __restrict__ out) {
+    constexpr int CPL = D / 32;
+    __shared__ float red_o[8][D], red_m[8], red_l[8];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int c = blockIdx.x, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int2 own = desc[2 * c + 1];
+    if (own.x < 0) return;
+    const size_t stride = part_floats(group, D);
+    float top = -INFINITY, l = 0.0f, acc[CPL];
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) acc[e] = 0.0f;
+    for (int p = c + warp; p <= own.y; p += 8) {
+        const int slot = p == c ? 1 : 0;
+        if (p != c && desc[2 * p].x != own.x) continue;
+        const float* src = part + ((size_t)p * 2 + slot) * stride;
+        const float pm = src[group * D + 2 * head], pl = src[group * D + 2 * head + 1];
+        float v[CPL];
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) v[e] = src[head * D + lane * CPL + e];
+        if (pm == -INFINITY) continue;
+        const float n = fmaxf(top, pm), f0 = exp2f(top - n), f1 = exp2f(pm - n);
+        l = fmaf(l, f0, pl * f1);
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) acc[e] = fmaf(acc[e], f0, v[e] * f1);
+        top = n;
+    }
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) red_o[warp][lane * CPL + e] = acc[e];
+    if (lane == 0) red_m[warp] = top, red_l[warp] = l;
+    __syncthreads();
+    if (threadIdx.x < D) {
+        float t = red_m[0];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) t = fmaxf(t, red_m[w]);
+        float sum = 0.0f, o = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const float f = red_m[w] == -INFINITY ? 0.0f : exp2f(red_m[w] - t);
+            sum = fmaf(red_l[w], f, sum);
+            o = fmaf(red_o[w][threadIdx.x], f, o);
+        }
+        const int m = own.x / n_kv, h = own.x - m * n_kv;
+        out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(sum > 0.0f ? o / sum : 0.0f);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+
+bool kv8_dims_ok(int n_q, int n_kv, int hd, int kind, int n_blocks, int block_rows) {
+    return n_q > 0 && n_kv > 0 && n_q % n_kv == 0 && n_q / n_kv <= 8 && (hd == 64 || hd == 128) && (kind == BITLINEAR_KV_INT8 || kind == BITLINEAR_KV_E4M3) &&
+           n_blocks > 0 && (block_rows == 16 || block_rows == 32 || block_rows == 64 || block_rows == 128) &&
+           (long long)n_blocks * n_kv * block_rows <= (1ll << 31) - 256;
+}
+
+// rows = every (block, head, row) of the pool, columns = D bytes; a box is min(32, block) whole rows, swizzled by the row's width
+bool make_kv8_map(CUtensorMap* map, const void* pool, long long rows, int hd, int block_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)hd, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)hd};
+    const cuuint32_t box[2] = {(cuuint32_t)hd, (cuuint32_t)std::min(block_rows, kUnit)};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr size_t kAttnMaxSmem = 227 * 1024 - 256;
+
+// opted in once per device and kernel
+template <int D, int KIND>
+bool attn8_opt_in() {
+    static std::mutex mu;
+    static bool done[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
+        cudaGetLastError();
+        return false;
+    }
+    std::lock_guard<std::mutex> lock(mu);
+    if (!done[dev]) {
+        if (cudaFuncSetAttribute(attn_decode_kv8_kernel<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAttnMaxSmem) != cudaSuccess) {
+            cudaGetLastError();
+            return false;
+        }
+        done[dev] = true;
+    }
+    return true;
+}
+
+template <int D, int KIND>
+int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a, int ctas, cudaStream_t st) {
+    if (!attn8_opt_in<D, KIND>()) return BITLINEAR_ERR_CUDA;
+    const int group = a.n_q / a.n_kv;
+    a.stages = kMaxStages;
+    while (a.stages > 1 && attn8_smem(group, D, a.stages) > kAttnMaxSmem) --a.stages;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = attn8_smem(group, D, a.stages);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, attn_decode_kv8_kernel<D, KIND>, map_k, map_v, a) != cudaSuccess) {
+        cudaGetLastError();
+        return BITLINEAR_ERR_CUDA;
+    }
+    cfg.gridDim = dim3((unsigned)ctas, (unsigned)group);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = 0;
+    if (cudaLaunchKernelEx(&cfg, attn_decode_kv8_combine_kernel<D>, (const float*)a.part, (const int2*)a.desc, group, a.n_kv, a.out) != cudaSuccess) {
+        cudaGetLastError();
+        return BITLINEAR_ERR_CUDA;
+    }
+    return BITLINEAR_OK;
+}
+
+}  // namespace
+
+}  // namespace bitlinear
+
+using namespace bitlinear;
+
+extern "C" {
+
+int bitlinear_rope_kv8(const float* q, const float* k, const float* v, const int32_t* positions, const int32_t* slots, const float* rope_table, int T,
+                       int t_max, int n_q_heads, int n_kv_heads, int head_dim, void* q_out_bf16, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                       int kv_dtype, int n_blocks, int block_rows, void* stream) {
+    if (kv_dtype != BITLINEAR_KV_INT8 && kv_dtype != BITLINEAR_KV_E4M3) return BITLINEAR_ERR_DTYPE;
+    if (T < 0 || t_max <= 0 || !kv8_dims_ok(n_q_heads, n_kv_heads, head_dim, kv_dtype, n_blocks, block_rows) || (long long)T * n_q_heads * head_dim > (1ll << 40) ||
+        n_kv_heads > 65535)
+        return BITLINEAR_ERR_SHAPE;
+    if (T == 0) return BITLINEAR_OK;
+    if (!q || !k || !v || !positions || !slots || !rope_table || !q_out_bf16 || !k_cache || !v_cache || !k_scale || !v_scale) return BITLINEAR_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(rope_table) || !aligned16(q_out_bf16) || !aligned16(k_cache) || !aligned16(v_cache))
+        return BITLINEAR_ERR_ALIGN;
+    int sm_count = 0;
+    if (const int rc = device_sm_count(&sm_count)) return rc;
+    AppendArgs a = {q, k, v, positions, slots, reinterpret_cast<const float2*>(rope_table), T, t_max, n_q_heads, n_kv_heads, block_rows, n_blocks,
+                    static_cast<__nv_bfloat16*>(q_out_bf16), static_cast<uint8_t*>(k_cache), static_cast<uint8_t*>(v_cache), k_scale, v_scale, 1, 0};
+    // a CTA per token and head while that fits the GPU a few times over, else per tile of tokens (most of them lead no run)
+    a.tile = (long long)T * 2 * n_kv_heads <= 64ll * sm_count ? 1 : 16;
+    const long long kv_ctas = (long long)((T + a.tile - 1) / a.tile) * 2 * n_kv_heads;
+    const long long q_units = (long long)T * n_q_heads * (head_dim / 8);
+    const long long q_ctas = std::min((q_units + kAppendThreads - 1) / kAppendThreads, 64ll * sm_count);
+    if (kv_ctas + q_ctas > 0x7fffffffll) return BITLINEAR_ERR_SHAPE;
+    a.kv_ctas = (int)kv_ctas;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(kv_ctas + q_ctas));
+    cfg.blockDim = dim3(kAppendThreads);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const bool i8 = kv_dtype == BITLINEAR_KV_INT8;
+    const cudaError_t rc = head_dim == 128 ? (i8 ? cudaLaunchKernelEx(&cfg, rope_kv8_kernel<128, BITLINEAR_KV_INT8>, a)
+                                                 : cudaLaunchKernelEx(&cfg, rope_kv8_kernel<128, BITLINEAR_KV_E4M3>, a))
+                                           : (i8 ? cudaLaunchKernelEx(&cfg, rope_kv8_kernel<64, BITLINEAR_KV_INT8>, a)
+                                                 : cudaLaunchKernelEx(&cfg, rope_kv8_kernel<64, BITLINEAR_KV_E4M3>, a));
+    if (rc != cudaSuccess) {
+        cudaGetLastError();
+        return BITLINEAR_ERR_CUDA;
+    }
+    return BITLINEAR_OK;
+}
+
+size_t bitlinear_attention_kv8_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim) {
+    if (n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 8 || (head_dim != 64 && head_dim != 128)) return 0;
+    return align_up(kMaxCtas * 2 * sizeof(int2), 256) + kMaxCtas * 2 * part_floats(n_q_heads / n_kv_heads, head_dim) * sizeof(float);
+}
+
+int bitlinear_attention_decode_kv8(const void* q_bf16, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                   const int32_t* tables, const int32_t* lengths, const int32_t* seq_ids, int M, int n_q_heads, int n_kv_heads, int head_dim,
+                                   int kv_dtype, int n_blocks, int block_rows, int n_seq, int max_blocks, void* out_bf16, void* ws, size_t ws_bytes,
+                                   void* stream) {
+    if (kv_dtype != BITLINEAR_KV_INT8 && kv_dtype != BITLINEAR_KV_E4M3) return BITLINEAR_ERR_DTYPE;
+    if (M < 0 || M > 65535 || n_seq <= 0 || max_blocks <= 0 || !kv8_dims_ok(n_q_heads, n_kv_heads, head_dim, kv_dtype, n_blocks, block_rows) ||
+        (long long)max_blocks * block_rows > (1ll << 30) || (long long)M * n_kv_heads > 0x7fffffffll || (!seq_ids && n_seq < M))
+        return BITLINEAR_ERR_SHAPE;
+    if (M == 0) return BITLINEAR_OK;
+    if (!q_bf16 || !k_cache || !v_cache || !k_scale || !v_scale || !tables || !lengths || !out_bf16) return BITLINEAR_ERR_NULL;
+    if (!aligned16(q_bf16) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out_bf16)) return BITLINEAR_ERR_ALIGN;
+    if (!ws || !aligned16(ws) || ws_bytes < bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim)) return BITLINEAR_ERR_WORKSPACE;
+    int sm_count = 0;
+    if (const int rc = device_sm_count(&sm_count)) return rc;
+    const long long pool_rows = (long long)n_blocks * n_kv_heads * block_rows;
+    CUtensorMap map_k, map_v;
+    if (!make_kv8_map(&map_k, k_cache, pool_rows, head_dim, block_rows) || !make_kv8_map(&map_v, v_cache, pool_rows, head_dim, block_rows))
+        return BITLINEAR_ERR_CUDA;
+    int log2_rows = 4;
+    while ((1 << log2_rows) < block_rows) ++log2_rows;
+    AttnArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, M, n_q_heads, n_kv_heads, n_seq, max_blocks, log2_rows,
+                  n_blocks, 1, 1.4426950408889634f / sqrtf((float)head_dim), static_cast<__nv_bfloat16*>(out_bf16),
+                  reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align_up(kMaxCtas * 2 * sizeof(int2), 256)), static_cast<int2*>(ws), device_status_word()};
+    const int ctas = std::min(sm_count, kMaxCtas);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (head_dim == 128)
+        return kv_dtype == BITLINEAR_KV_INT8 ? attn8_launch<128, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st)
+                                             : attn8_launch<128, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
+    return kv_dtype == BITLINEAR_KV_INT8 ? attn8_launch<64, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st)
+                                         : attn8_launch<64, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
+}
+
+}  // extern "C"
