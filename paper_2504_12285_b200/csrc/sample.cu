@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kBins = 1024;  // two per thread
+constexpr int kList = 512;   // candidates of a row that one CTA finishes with
 constexpr int kMaxCluster = 8;
 constexpr int kMaxShard = 45056;  // floats of a row that one CTA holds
 constexpr double kUnit44 = 17592186044416.0;  // 2^44
@@ -59,11 +60,13 @@ struct Crossing {
 };
 
 struct Shared {
-    double pow2[64];            // 2^(j / 64)
     float top, low;             // largest logit of the part, smallest finite one
     int first;                  // lowest id of the largest logit in the part
     uint32_t ties;
     unsigned long long total;   // kept mass of the part
+    __align__(16) uint32_t list_key[kList];  // rank 0: the row's candidates in the order of ids, once they are few
+    int list_id[kList];
+    unsigned long long list_mass[kList];
     Crossing cross;
     unsigned long long warp_mass[kThreads / 32];
     uint32_t warp_count[kThreads / 32];
@@ -75,34 +78,47 @@ struct Shared {
 
 struct Row {
     float top;        // largest logit
+    float least;      // logits below weigh less than 2^-48 of the largest and are taken as this
     double top_d;
-    double scale;     // 64 log2(e) / T
+    double scale;     // log2(e) / T
     bool top_inf;
-    const double* pow2;
 };
 
-// exp((l - top) / T), by 2^(n / 64) from the table and the series of exp to its fourth power on what is left (at most ln 2 / 128:
-// the next term is below 2^-44); 0 for -inf
+// exp((l - top) / T) = 2^n * 2^f, n whole, |f| <= 1/2: the second by 1 + f q(f), q of degree 7 interpolating (2^f - 1) / f at the Chebyshev nodes of
+// -1/2 .. 1/2 (within 2^-38 of 2^f, exact at 0).  Returned as the two factors.  Without a table: lookups of 64-bit
+// entries at random cost more of shared memory's time than the longer series costs of the fp64 pipe's.
+__device__ __forceinline__ void weight_factors(const Row& r, float l, double& series, double& power) {
+    constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are n
+    const double d = (double)fmaxf(l, r.least) - r.top_d;
+    const double t = fma(d, r.scale, kRound);
+    const double f = fma(d, r.scale, kRound - t);
+    double q = fma(f, 1.325080551750225e-06, 1.5303700711365693e-05);
+    q = fma(f, q, 0.00015403475186530786);
+    q = fma(f, q, 0.0013333478473685416);
+    q = fma(f, q, 0.00961812913523614);
+    q = fma(f, q, 0.055504109063258665);
+    q = fma(f, q, 0.24022650695888503);
+    q = fma(f, q, 0.6931471805568324);
+    series = fma(f, q, 1.0);
+    power = __hiloint2double((__double2loint(t) + 1023) << 20, 0);
+}
 __device__ __forceinline__ double weight_of(const Row& r, float l) {
     if (r.top_inf) return l == r.top ? 1.0 : 0.0;
-    // fp32 -> fp64 by hand (conversions run at a quarter of the rate of the rest): right but for denormals, which come out
-    // below 2^-126 as well
-    const uint32_t b = __float_as_uint(l);
-    const double d = __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(b << 29)) - r.top_d;
-    double x = d * r.scale;
-    if (!(x > -64.0 * 48) || l == -INFINITY) return 0.0;
-    constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52
-    const double t = x + kRound;
-    const int n = __double2loint(t);
-    x = (x - (t - kRound)) * 0.010830424696249145;  // ln 2 / 64
-    double e = fma(x, 1.0 / 24.0, 1.0 / 6.0);
-    e = fma(x, e, 0.5);
-    e = fma(x, e, 1.0);
-    e = fma(x, e, 1.0) * r.pow2[n & 63];
-    return __hiloint2double(__double2hiint(e) + ((n >> 6) << 20), __double2loint(e));
+    if (l == -INFINITY) return 0.0;
+    double series, power;
+    weight_factors(r, l, series, power);
+    return series * power;
 }
-// in units of 2^-44, rounded to nearest: the bits behind 256
-__device__ __forceinline__ unsigned long long fixed_of(double w) { return (unsigned long long)__double_as_longlong(w + 256.0) & 0xfffffffffffffull; }
+// The weight in units of 2^-44, rounded to nearest, on top of the bits of 256: sums of these are right modulo 2^64 once
+// 256's bits are taken off as often as they were added.
+constexpr unsigned long long kBits256 = 0x4070000000000000ull;
+__device__ __forceinline__ unsigned long long biased_of(const Row& r, float l) {
+    if (r.top_inf) return kBits256 + (l == r.top ? 1ull << 44 : 0ull);
+    double series, power;
+    weight_factors(r, l, series, power);
+    return (unsigned long long)__double_as_longlong(fma(series, power, 256.0));
+}
+__device__ __forceinline__ unsigned long long fixed_of(const Row& r, float l) { return biased_of(r, l) - kBits256; }
 
 template <class T>
 __device__ __forceinline__ float load_logit(const T* p);
@@ -115,33 +131,34 @@ template <class T>
 __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     extern __shared__ __align__(16) uint8_t sample_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(sample_raw);
-    float* vals = reinterpret_cast<float*>(sample_raw + (sizeof(Shared) + 15) / 16 * 16);
+    float* room = reinterpret_cast<float*>(sample_raw + (sizeof(Shared) + 15) / 16 * 16);
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (tid < 64) sh.pow2[tid] = exp2((double)tid / 64.0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long begin = (long long)rank * a.shard;
     const int n = (int)max(0ll, min((long long)a.shard, a.V - begin));
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride + begin;
-    const float temp = a.temperature ? a.temperature[row] : 1.0f;
+    const float temp = a.temperature ? fminf(a.temperature[row], 1e30f) : 1.0f;
     const int k = a.top_k ? a.top_k[row] : 0;
     const float p = a.top_p ? a.top_p[row] : 1.0f;
     const float given_mp = a.min_p ? a.min_p[row] : 0.0f;
     const float u = a.u[row];
 
-    // ---- the part into shared memory; the largest and the smallest finite logit
+    // ---- the part into shared memory; the largest and (where a histogram will want it) the smallest finite logit
+    const bool use_k = k > 0 && k < a.V, use_p = p < 1.0f, want_low = use_k || use_p;
     float top = -INFINITY, low = INFINITY;
     auto take = [&](float l) {
         l = l == l ? l : -INFINITY;  // NaN: never drawn
         top = fmaxf(top, l);
-        low = fminf(low, l > -INFINITY ? l : INFINITY);
+        if (want_low) low = fminf(low, l > -INFINITY ? l : INFINITY);
         return l;
     };
-    constexpr int VEC = 16 / sizeof(T), AHEAD = 4;
+    constexpr int VEC = 16 / sizeof(T), AHEAD = 8;
     const int head = (int)min((long long)n, (long long)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
     const int n_vec = (n - head) / VEC;
+    float* vals = room + ((4 - (head & 3)) & 3);  // what comes 16 bytes at a time goes there 16 bytes at a time
     const uint4* vsrc = reinterpret_cast<const uint4*>(src + head);
     for (int v0 = tid; v0 < n_vec; v0 += AHEAD * kThreads) {
         uint4 x[AHEAD];
@@ -152,9 +169,10 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         for (int j = 0; j < AHEAD; ++j) {
             if (v0 + j * kThreads >= n_vec) break;
             const T* e = reinterpret_cast<const T*>(&x[j]);
-            float* dst = vals + head + (v0 + j * kThreads) * VEC;
+            float4* dst = reinterpret_cast<float4*>(vals + head + (v0 + j * kThreads) * VEC);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) dst[i] = take(load_logit(e + i));
+            for (int i = 0; i < VEC / 4; ++i)
+                dst[i] = make_float4(take(load_logit(e + 4 * i)), take(load_logit(e + 4 * i + 1)), take(load_logit(e + 4 * i + 2)), take(load_logit(e + 4 * i + 3)));
         }
     }
     for (int i = tid; i < head; i += kThreads) vals[i] = take(load_logit(src + i));
@@ -167,10 +185,15 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     if (lane == 0) sh.warp_top[warp] = top, sh.warp_low[warp] = low;
     if (tid == 0) sh.first = 0x7fffffff;
     __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kThreads / 32; ++w) top = fmaxf(top, sh.warp_top[w]), low = fminf(low, sh.warp_low[w]);
-        sh.top = top;
-        sh.low = low;
+    if (warp == 0) {
+        top = sh.warp_top[lane & (kThreads / 32 - 1)];
+        low = sh.warp_low[lane & (kThreads / 32 - 1)];
+#pragma unroll
+        for (int off = kThreads / 64; off > 0; off >>= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            low = fminf(low, __shfl_xor_sync(0xffffffffu, low, off));
+        }
+        if (lane == 0) sh.top = top, sh.low = low;
     }
     cluster.sync();
     {
@@ -205,15 +228,41 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         cluster.sync();  // no CTA leaves while another reads its shared memory
         return;
     }
-    const Row rw = {top, (double)top, 64.0 * 1.4426950408889634074 / (double)temp, top == INFINITY, sh.pow2};
+    const Row rw = {top, fminf(top - 34.0f * temp, float_of(key_of(top) - 1)), (double)top, 1.4426950408889634074 / (double)temp, top == INFINITY};
     const uint32_t top_key = key_of(top);
     const double mp = given_mp > 0.0f ? fmin((double)given_mp, 1.0) : 0.0;  // the largest, of weight 1, always stays
-    const bool use_k = k > 0 && k < a.V, use_p = p < 1.0f;
 
     // kept so far: keys above floor_key, and of those equal to it the ones up to floor_index
     uint32_t floor_key = 0;
     int floor_index = 0x7fffffff;
     auto kept = [&](uint32_t key, int i) { return key > floor_key || (key == floor_key && (int)begin + i <= floor_index); };
+    // f(logit, place) for the kept elements of this thread's run
+    auto each_kept = [&](auto&& f) {
+        constexpr int U = 4;
+        if (floor_key == 0) {
+            int i = i0;
+            for (; i + U <= i1; i += U) {
+                float l[U];
+#pragma unroll
+                for (int j = 0; j < U; ++j) l[j] = vals[i + j];
+#pragma unroll
+                for (int j = 0; j < U; ++j) f(l[j], i + j);
+            }
+            for (; i < i1; ++i) f(vals[i], i);
+        } else {
+            int i = i0;
+            for (; i + U <= i1; i += U) {
+                float l[U];
+#pragma unroll
+                for (int j = 0; j < U; ++j) l[j] = vals[i + j];
+#pragma unroll
+                for (int j = 0; j < U; ++j)
+                    if (kept(key_of(l[j]), i + j)) f(l[j], i + j);
+            }
+            for (; i < i1; ++i)
+                if (kept(key_of(vals[i]), i)) f(vals[i], i);
+        }
+    };
 
     // Two cluster barriers make up a pass: its sums are ready, and everyone has read them.  The second is waited for only where
     // the fields it guards are written again.
@@ -225,6 +274,13 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     auto read_done = [&]() {
         cluster.barrier_arrive();
         pending = true;
+    };
+
+    // the running sum that the drawn token is the first to exceed
+    auto goal_of = [&](unsigned long long all) {
+        const double goal = u > 0.0f ? (double)u * (double)all : 0.0;
+        const unsigned long long at = goal < 9.2e18 ? (unsigned long long)goal : all;  // sum > goal, in whole numbers: > its floor
+        return at >= all ? all - 1 : at;                                               // u = 1: the last token that is kept
     };
 
     // ---- thresholds
@@ -263,21 +319,18 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
             for (int j = 0; j < 3; ++j) reinterpret_cast<uint2*>(sh.mass[j])[tid] = none;
         }
         __syncthreads();
-        for (int i = i0; i < i1; ++i) {
-            const float l = vals[i];
-            const uint32_t key = key_of(l);
-            if (!kept(key, i)) continue;
-            const int b = bin_of(l, key);
-            if (b < 0) continue;
+        each_kept([&](float l, int) {
+            const int b = bin_of(l, key_of(l));
+            if (b < 0) return;
             atomicAdd(&sh.count[b], 1u);
             if (by_mass) {
-                const unsigned long long w = fixed_of(weight_of(rw, l));
+                const unsigned long long w = fixed_of(rw, l);
                 const uint32_t w0 = (uint32_t)w & 0xffffu, w1 = (uint32_t)w >> 16, w2 = (uint32_t)(w >> 32);
                 if (w0) atomicAdd(&sh.mass[0][b], w0);
                 if (w1) atomicAdd(&sh.mass[1][b], w1);
                 if (w2) atomicAdd(&sh.mass[2][b], w2);
             }
-        }
+        });
         cluster.sync();
         uint32_t c[2] = {0, 0};
         unsigned long long m[2] = {0, 0};
@@ -329,10 +382,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     auto cut_ties = [&](uint32_t keep) {
         settle();
         uint32_t mine = 0;
-        for (int i = i0; i < i1; ++i) {
-            const uint32_t key = key_of(vals[i]);
-            mine += key == floor_key && kept(key, i);
-        }
+        each_kept([&](float l, int) { mine += key_of(l) == floor_key; });
         uint32_t incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -350,13 +400,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         for (int r = 0; r < rank; ++r) before += cluster.map_shared_rank(&sh, r)->ties;
         if (before < keep && before + mine >= keep) {
             uint32_t left = keep - before;
-            for (int i = i0; i < i1; ++i) {
-                const uint32_t key = key_of(vals[i]);
-                if (key == floor_key && kept(key, i) && --left == 0) {
-                    sh.cut_index = (int)begin + i;
-                    break;
-                }
-            }
+            each_kept([&](float l, int i) {
+                if (key_of(l) == floor_key && --left == 0) sh.cut_index = (int)begin + i;
+            });
         }
         cluster.sync();
         int cut = -1;
@@ -366,8 +412,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     };
     // Narrows what is kept to the run from the largest down that reaches the target.  The bin that holds the run's end
     // is split until the run takes all of it or it is a single key, whose elements then go by id.
-    auto narrow = [&](bool by_mass, uint32_t want, double target) {
-        Crossing x = find(by_mass, want, target, 0, 0, [&](float l, uint32_t) { return linear_bin(l); });
+    auto narrow = [&](Crossing x, bool by_mass, uint32_t want, double target) {
         uint32_t lo = first_key(x.bin), hi = (x.bin == 0 ? top_key + 1 : first_key(x.bin - 1)) - 1;
         while (x.count > 1 && lo < hi && (by_mass || x.count_above + x.count != want)) {
             const int shift = max(0, 32 - __clz((int)(hi - lo)) - 10);
@@ -378,7 +423,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         }
         uint32_t keep = x.count;
         if (by_mass && x.count > 1) {
-            const double each = (double)fixed_of(weight_of(rw, float_of(lo))), need = ceil((target - (double)x.mass_above) / fmax(each, 1.0));
+            const double each = (double)fixed_of(rw, float_of(lo)), need = ceil((target - (double)x.mass_above) / fmax(each, 1.0));
             keep = need < 1.0 ? 1u : need > (double)x.count ? x.count : (uint32_t)need;
         } else if (!by_mass) {
             keep = want - x.count_above;
@@ -386,15 +431,121 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         if (lo > floor_key) floor_key = lo, floor_index = 0x7fffffff;  // an earlier cut was among another key's ties
         if (keep < x.count) cut_ties(keep);
     };
+    // sum of v over the threads in front of this one, and over all
+    auto scan_mass = [&](unsigned long long v, unsigned long long& all) {
+        unsigned long long incl = v;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += up;
+        }
+        __syncthreads();
+        if (lane == 31) sh.warp_mass[warp] = incl;
+        __syncthreads();
+        unsigned long long before = incl - v;
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const unsigned long long t = sh.warp_mass[w];
+            if (w < warp) before += t;
+            all += t;
+        }
+        return before;
+    };
+    // Few candidates are left, those in the bins up to last_bin: rank 0 takes them all, one per thread in the order of ids, ranks
+    // them by counting, and draws; the other CTAs are done.  want: top_k, or 0; target: top_p's mass, below 0 where it is to be formed from
+    // the top_k here.
+    auto finish = [&](int last_bin, uint32_t want, double target) {
+        settle();
+        uint32_t mine = 0;
+        each_kept([&](float l, int) { mine += linear_bin(l) <= last_bin; });
+        uint32_t incl = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t up = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += up;
+        }
+        __syncthreads();
+        if (lane == 31) sh.warp_count[warp] = incl;
+        __syncthreads();
+        uint32_t at = incl - mine, there = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const uint32_t t = sh.warp_count[w];
+            if (w < warp) at += t;
+            there += t;
+        }
+        if (tid == 0) sh.ties = there;
+        cluster.sync();
+        {
+            uint32_t t[kMaxCluster];
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) t[r] = r < ranks ? cluster.map_shared_rank(&sh, r)->ties : 0;
+            there = 0;
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {
+                if (r < rank) at += t[r];
+                there += t[r];
+            }
+        }
+        Shared* first = cluster.map_shared_rank(&sh, 0);
+        if (mine)
+            each_kept([&](float l, int i) {
+                if (linear_bin(l) <= last_bin) {
+                    first->list_key[at] = key_of(l);
+                    first->list_id[at++] = (int)begin + i;
+                }
+            });
+        cluster.sync();
+        if (rank != 0) return;
+        const int m = (int)there;
+        const bool in = tid < m;
+        const uint32_t key = in ? sh.list_key[tid] : 0;
+        int place = 0;  // how many are larger, or equal with a lower id
+        if (warp * 32 < m) {
+            int j = 0;
+            for (; j < m; ++j) {
+                const uint32_t o = sh.list_key[j];
+                place += o > key || (o == key && j < tid);
+            }
+        }
+        const float l = float_of(key);
+        const double w = in ? weight_of(rw, l) : 0.0;
+        unsigned long long mass = in && (want == 0 || place < (int)want) ? fixed_of(rw, l) : 0, total;
+        bool stays = in && (want == 0 || place < (int)want);
+        if (use_p) {
+            sh.list_mass[tid] = 0;
+            __syncthreads();
+            if (stays) sh.list_mass[place] = mass;
+            __syncthreads();
+            const unsigned long long ahead = scan_mass(sh.list_mass[tid], total);
+            if (target < 0.0) target = fmax((double)p * (double)total, 0.5);
+            __syncthreads();
+            sh.list_mass[tid] = ahead;
+            __syncthreads();
+            if (stays) stays = (double)sh.list_mass[place] < target;
+        }
+        if (w < mp) stays = false;
+        if (!stays) mass = 0;
+        const unsigned long long ahead = scan_mass(mass, total);
+        const unsigned long long goal = goal_of(total);
+        if (ahead <= goal && goal < ahead + mass) {
+            a.ids[row] = sh.list_id[tid];
+            if (a.logprobs) a.logprobs[row] = (float)log(w * kUnit44 / (double)total);
+        }
+    };
     // mass of what is kept and weighs at least `least`, over the cluster; `mine`: this thread's run, `before`: what lies in front of it
     auto kept_mass = [&](double least, unsigned long long& mine, unsigned long long& before) {
         settle();
         mine = 0;
-        for (int i = i0; i < i1; ++i) {
-            const float l = vals[i];
-            if (!kept(key_of(l), i)) continue;
-            const double w = weight_of(rw, l);
-            if (w >= least) mine += fixed_of(w);
+        if (least > 0.0) {
+            each_kept([&](float l, int) {
+                if (weight_of(rw, l) >= least) mine += fixed_of(rw, l);
+            });
+        } else {
+            uint32_t taken = 0;
+            each_kept([&](float l, int) { mine += biased_of(rw, l), ++taken; });
+            mine -= taken * kBits256;
         }
         unsigned long long incl = mine;
 #pragma unroll
@@ -424,15 +575,21 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     };
 
     unsigned long long mine, before;
-    if (use_k) narrow(false, (uint32_t)k, 0.0);
+    auto by_distance = [&](float l, uint32_t) { return linear_bin(l); };
+    if (use_k) {
+        const Crossing x = find(false, (uint32_t)k, 0.0, 0, 0, by_distance);
+        if (x.count_above + x.count <= kList) return finish(x.bin, (uint32_t)k, -1.0);
+        narrow(x, false, (uint32_t)k, 0.0);
+    }
     if (use_p) {
         const unsigned long long all = kept_mass(0.0, mine, before);
-        narrow(true, 0, fmax((double)p * (double)all, 0.5));
+        const double target = fmax((double)p * (double)all, 0.5);
+        const Crossing x = find(true, 0, target, 0, 0, by_distance);
+        if (x.count_above + x.count <= kList) return finish(x.bin, 0, target);
+        narrow(x, true, 0, target);
     }
     const unsigned long long all = kept_mass(mp, mine, before);
-    const double goal = u > 0.0f ? (double)u * (double)all : 0.0;
-    unsigned long long at = goal < 9.2e18 ? (unsigned long long)goal : all;  // running sum > goal, in integers: > its floor
-    if (at >= all) at = all - 1;                                             // u = 1: the last token that is kept
+    const unsigned long long at = goal_of(all);
     // the thread whose run holds it; its warp finds the element
     const unsigned holds = __ballot_sync(0xffffffffu, before <= at && at < before + mine);
     if (holds) {
@@ -445,7 +602,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
             unsigned long long f = 0;
             if (i < j1 && kept(key_of(vals[i]), i)) {
                 w = weight_of(rw, vals[i]);
-                if (w >= mp) f = fixed_of(w);
+                if (w >= mp) f = fixed_of(rw, vals[i]);
             }
             unsigned long long incl = f;
 #pragma unroll
@@ -480,7 +637,7 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!done[dev]) {
-            if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + kMaxShard * sizeof(float))) != cudaSuccess) {
+            if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) != cudaSuccess) {
                 cudaGetLastError();
                 return BITLINEAR_ERR_CUDA;
             }
@@ -496,7 +653,7 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.M * ranks));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = fixed + (size_t)a.shard * sizeof(float);
+    cfg.dynamicSmemBytes = fixed + (size_t)(a.shard + 4) * sizeof(float);
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
