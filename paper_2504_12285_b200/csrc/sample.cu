@@ -26,7 +26,7 @@ namespace bitlinear {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kBins = 1024;  // two per thread
+constexpr int kBins = 1024;
 constexpr int kList = 512;   // candidates of a row that one CTA finishes with
 constexpr int kMaxCluster = 8;
 constexpr int kMaxShard = 45056;  // floats of a row that one CTA holds
@@ -68,6 +68,8 @@ struct Shared {
     int list_id[kList];
     unsigned long long list_mass[kList];
     Crossing cross;
+    uint32_t slice_count;       // what this CTA's share of the merged bins holds
+    unsigned long long slice_mass;
     unsigned long long warp_mass[kThreads / 32];
     uint32_t warp_count[kThreads / 32];
     float warp_top[kThreads / 32], warp_low[kThreads / 32];
@@ -81,7 +83,6 @@ struct Row {
     float least;      // logits below weigh less than 2^-48 of the largest and are taken as this
     double top_d;
     double scale;     // log2(e) / T
-    bool top_inf;
 };
 
 // exp((l - top) / T) = 2^n * 2^f, n whole, |f| <= 1/2: the second by 1 + f q(f), q of degree 7 interpolating (2^f - 1) / f at the Chebyshev nodes of
@@ -103,22 +104,17 @@ __device__ __forceinline__ void weight_factors(const Row& r, float l, double& se
     power = __hiloint2double((__double2loint(t) + 1023) << 20, 0);
 }
 __device__ __forceinline__ double weight_of(const Row& r, float l) {
-    if (r.top_inf) return l == r.top ? 1.0 : 0.0;
-    if (l == -INFINITY) return 0.0;
     double series, power;
     weight_factors(r, l, series, power);
     return series * power;
 }
-// The weight in units of 2^-44, rounded to nearest, on top of the bits of 256: sums of these are right modulo 2^64 once
-// 256's bits are taken off as often as they were added.
+// the weight in units of 2^-44, rounded to nearest: the last bits of its sum with 256
 constexpr unsigned long long kBits256 = 0x4070000000000000ull;
-__device__ __forceinline__ unsigned long long biased_of(const Row& r, float l) {
-    if (r.top_inf) return kBits256 + (l == r.top ? 1ull << 44 : 0ull);
+__device__ __forceinline__ unsigned long long fixed_of(const Row& r, float l) {
     double series, power;
     weight_factors(r, l, series, power);
-    return (unsigned long long)__double_as_longlong(fma(series, power, 256.0));
+    return (unsigned long long)__double_as_longlong(fma(series, power, 256.0)) - kBits256;
 }
-__device__ __forceinline__ unsigned long long fixed_of(const Row& r, float l) { return biased_of(r, l) - kBits256; }
 
 template <class T>
 __device__ __forceinline__ float load_logit(const T* p);
@@ -127,9 +123,11 @@ __device__ __forceinline__ float load_logit<float>(const float* p) { return *p; 
 template <>
 __device__ __forceinline__ float load_logit<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 
-template <class T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
-    extern __shared__ __align__(16) uint8_t sample_raw[];
+// kPerSm = 1 where every CTA has an SM to itself (more registers: more elements' chains side by side), else 2, so that one loads
+// while the other computes
+template <class T, int kPerSm>
+__global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleArgs a) {
+        extern __shared__ __align__(16) uint8_t sample_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(sample_raw);
     float* room = reinterpret_cast<float*>(sample_raw + (sizeof(Shared) + 15) / 16 * 16);
     cg::cluster_group cluster = cg::this_cluster();
@@ -155,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         if (want_low) low = fminf(low, l > -INFINITY ? l : INFINITY);
         return l;
     };
-    constexpr int VEC = 16 / sizeof(T), AHEAD = 8;
+    constexpr int VEC = 16 / sizeof(T), AHEAD = 4;
     const int head = (int)min((long long)n, (long long)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
     const int n_vec = (n - head) / VEC;
     float* vals = room + ((4 - (head & 3)) & 3);  // what comes 16 bytes at a time goes there 16 bytes at a time
@@ -228,7 +226,12 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         cluster.sync();  // no CTA leaves while another reads its shared memory
         return;
     }
-    const Row rw = {top, fminf(top - 34.0f * temp, float_of(key_of(top) - 1)), (double)top, 1.4426950408889634074 / (double)temp, top == INFINITY};
+    if (top == INFINITY) {  // +infinity shares all weight: as if it were 0 and all else -infinity
+        for (int i = i0; i < i1; ++i) vals[i] = vals[i] == INFINITY ? 0.0f : -INFINITY;
+        top = low = 0.0f;
+        __syncthreads();
+    }
+    const Row rw = {top, fminf(top - 34.0f * temp, float_of(key_of(top) - 1)), (double)top, 1.4426950408889634074 / (double)temp};
     const uint32_t top_key = key_of(top);
     const double mp = given_mp > 0.0f ? fmin((double)given_mp, 1.0) : 0.0;  // the largest, of weight 1, always stays
 
@@ -236,34 +239,27 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     uint32_t floor_key = 0;
     int floor_index = 0x7fffffff;
     auto kept = [&](uint32_t key, int i) { return key > floor_key || (key == floor_key && (int)begin + i <= floor_index); };
-    // f(logit, place) for the kept elements of this thread's run
-    auto each_kept = [&](auto&& f) {
-        constexpr int U = 4;
-        if (floor_key == 0) {
-            int i = i0;
-            for (; i + U <= i1; i += U) {
-                float l[U];
+    // f(logit, place, whether it is kept) for the elements of this thread's run; four at a time and without branches, so that
+    // the chains of dependent operations of several elements run side by side
+    auto each = [&](auto&& f) {
+        int i = i0;
+        for (; i + 4 <= i1; i += 4) {
+            const float l[4] = {vals[i], vals[i + 1], vals[i + 2], vals[i + 3]};
+            bool in[4] = {true, true, true, true};
+            if (floor_key != 0) {
 #pragma unroll
-                for (int j = 0; j < U; ++j) l[j] = vals[i + j];
-#pragma unroll
-                for (int j = 0; j < U; ++j) f(l[j], i + j);
+                for (int j = 0; j < 4; ++j) in[j] = kept(key_of(l[j]), i + j);
             }
-            for (; i < i1; ++i) f(vals[i], i);
-        } else {
-            int i = i0;
-            for (; i + U <= i1; i += U) {
-                float l[U];
+            f(l, in, i);
+        }
+        if (i < i1) {
+            float l[4];
+            bool in[4];
 #pragma unroll
-                for (int j = 0; j < U; ++j) l[j] = vals[i + j];
-#pragma unroll
-                for (int j = 0; j < U; ++j)
-                    if (kept(key_of(l[j]), i + j)) f(l[j], i + j);
-            }
-            for (; i < i1; ++i)
-                if (kept(key_of(vals[i]), i)) f(vals[i], i);
+            for (int j = 0; j < 4; ++j) l[j] = vals[min(i + j, i1 - 1)], in[j] = i + j < i1 && kept(key_of(l[j]), i + j);
+            f(l, in, i);
         }
     };
-
     // Two cluster barriers make up a pass: its sums are ready, and everyone has read them.  The second is waited for only where
     // the fields it guards are written again.
     bool pending = false;
@@ -295,16 +291,11 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     auto first_key = [&](int bin) {
         uint32_t lo = kLowKey, hi = top_key + 1;  // the answer lies in lo .. hi; hi: none
         while (lo < hi) {
-            const uint32_t step = (hi - lo) / 32 + 1;
-            const unsigned long long at = (unsigned long long)lo + (unsigned long long)lane * step;
-            const bool good = at >= hi || linear_bin(float_of((uint32_t)at)) <= bin;
-            const unsigned m = __ballot_sync(0xffffffffu, good);
-            if (m == 0) lo = lo + 31 * step + 1;
-            else {
-                const uint32_t f = (uint32_t)__ffs((int)m) - 1;
-                hi = (uint32_t)min((unsigned long long)hi, (unsigned long long)lo + (unsigned long long)f * step);
-                if (f > 0) lo = lo + (f - 1) * step + 1;
-            }
+            const uint32_t step = (hi - lo) / 32 + 1, at = lo + lane * step;  // (keys end at infinity's: no overflow)
+            const unsigned m = __ballot_sync(0xffffffffu, at >= hi || linear_bin(float_of(at)) <= bin);
+            const uint32_t f = m ? (uint32_t)__ffs((int)m) - 1 : 32u;
+            if (f < 32) hi = min(hi, lo + f * step);
+            if (f > 0) lo = lo + (f - 1) * step + 1;
         }
         return hi;
     };
@@ -312,49 +303,62 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     // count (or mass) reaches the target
     auto find = [&](bool by_mass, uint32_t want, double target, uint32_t count0, unsigned long long mass0, auto&& bin_of) {
         settle();
-        const uint2 none = make_uint2(0u, 0u);
-        reinterpret_cast<uint2*>(sh.count)[tid] = none;
-        if (by_mass) {
-#pragma unroll
-            for (int j = 0; j < 3; ++j) reinterpret_cast<uint2*>(sh.mass[j])[tid] = none;
+        for (int b = tid; b < kBins; b += kThreads) {
+            sh.count[b] = 0;
+            if (by_mass) sh.mass[0][b] = sh.mass[1][b] = sh.mass[2][b] = 0;
         }
         __syncthreads();
-        each_kept([&](float l, int) {
-            const int b = bin_of(l, key_of(l));
-            if (b < 0) return;
-            atomicAdd(&sh.count[b], 1u);
-            if (by_mass) {
-                const unsigned long long w = fixed_of(rw, l);
-                const uint32_t w0 = (uint32_t)w & 0xffffu, w1 = (uint32_t)w >> 16, w2 = (uint32_t)(w >> 32);
-                if (w0) atomicAdd(&sh.mass[0][b], w0);
-                if (w1) atomicAdd(&sh.mass[1][b], w1);
-                if (w2) atomicAdd(&sh.mass[2][b], w2);
-            }
-        });
+        if (by_mass) {
+            each([&](const float (&l)[4], const bool (&in)[4], int) {
+                unsigned long long w[4];
+                int b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = fixed_of(rw, l[j]), b[j] = in[j] ? bin_of(l[j], key_of(l[j])) : -1;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (b[j] >= 0) {
+                        const uint32_t w2 = (uint32_t)(w[j] >> 32);
+                        atomicAdd(&sh.count[b[j]], 1u);
+                        atomicAdd(&sh.mass[0][b[j]], (uint32_t)w[j] & 0xffffu);
+                        atomicAdd(&sh.mass[1][b[j]], (uint32_t)w[j] >> 16);
+                        if (w2) atomicAdd(&sh.mass[2][b[j]], w2);
+                    }
+            });
+        } else {
+            each([&](const float (&l)[4], const bool (&in)[4], int) {
+                int b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[j] = in[j] ? bin_of(l[j], key_of(l[j])) : -1;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (b[j] >= 0) atomicAdd(&sh.count[b[j]], 1u);
+            });
+        }
         cluster.sync();
-        uint32_t c[2] = {0, 0};
-        unsigned long long m[2] = {0, 0};
-        {
-            uint2 x[kMaxCluster];
+        // each CTA merges its share of the bins, one per thread
+        const int share = kBins / ranks, bin = rank * share + tid;
+        uint32_t c = 0;
+        unsigned long long m = 0;
+        if (tid < share) {
+            uint32_t x[kMaxCluster];
 #pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r) x[r] = r < ranks ? reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh, r)->count)[tid] : none;
+            for (int r = 0; r < kMaxCluster; ++r) x[r] = r < ranks ? cluster.map_shared_rank(&sh, r)->count[bin] : 0u;
 #pragma unroll
-            for (int r = 0; r < kMaxCluster; ++r) c[0] += x[r].x, c[1] += x[r].y;
+            for (int r = 0; r < kMaxCluster; ++r) c += x[r];
             if (by_mass) {
 #pragma unroll
                 for (int j = 0; j < 3; ++j) {
 #pragma unroll
-                    for (int r = 0; r < kMaxCluster; ++r) x[r] = r < ranks ? reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh, r)->mass[j])[tid] : none;
+                    for (int r = 0; r < kMaxCluster; ++r) x[r] = r < ranks ? cluster.map_shared_rank(&sh, r)->mass[j][bin] : 0u;
+                    unsigned long long t = 0;
 #pragma unroll
-                    for (int r = 0; r < kMaxCluster; ++r) m[0] += (unsigned long long)x[r].x << (16 * j), m[1] += (unsigned long long)x[r].y << (16 * j);
+                    for (int r = 0; r < kMaxCluster; ++r) t += x[r];
+                    m += t << (16 * j);
                 }
             }
         }
-        read_done();
-        const uint32_t cs = c[0] + c[1];
-        const unsigned long long ms = m[0] + m[1];
-        uint32_t ci = cs;
-        unsigned long long mi = ms;
+        uint32_t ci = c;
+        unsigned long long mi = m;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const uint32_t cu = __shfl_up_sync(0xffffffffu, ci, d);
@@ -363,26 +367,39 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         }
         if (lane == 31) sh.warp_count[warp] = ci, sh.warp_mass[warp] = mi;
         __syncthreads();
-        uint32_t ca = count0 + ci - cs;
-        unsigned long long ma = mass0 + mi - ms;
+        uint32_t ca = ci - c, cs = 0;
+        unsigned long long ma = mi - m, ms = 0;
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w)
-            if (w < warp) ca += sh.warp_count[w], ma += sh.warp_mass[w];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const bool here = by_mass ? (double)ma < target && (double)(ma + m[j]) >= target : ca < want && ca + c[j] >= want;
-            if (here && c[j] > 0) sh.cross = {2 * tid + j, ca, c[j], ma};
-            ca += c[j];
-            ma += m[j];
+        for (int w = 0; w < kBins / 2 / 32; ++w) {  // (a share is half the bins at most)
+            if (w * 32 >= share) break;
+            const uint32_t ct = sh.warp_count[w];
+            const unsigned long long mt = sh.warp_mass[w];
+            if (w < warp) ca += ct, ma += mt;
+            cs += ct, ms += mt;
         }
-        __syncthreads();
+        if (tid == 0) sh.slice_count = cs, sh.slice_mass = ms;
+        cluster.sync();
+        ca += count0, ma += mass0;
+#pragma unroll
+        for (int r = 0; r < kMaxCluster - 1; ++r)
+            if (r < rank) {
+                const Shared* o = cluster.map_shared_rank(&sh, r);
+                ca += o->slice_count, ma += o->slice_mass;
+            }
+        const bool here = by_mass ? (double)ma < target && (double)(ma + m) >= target : ca < want && ca + c >= want;
+        if (here && c > 0)
+            for (int r = 0; r < ranks; ++r) cluster.map_shared_rank(&sh, r)->cross = {bin, ca, c, ma};
+        cluster.sync();
         return sh.cross;
     };
     // of the elements equal to floor_key the first `keep` by id stay: the id of the last of them
     auto cut_ties = [&](uint32_t keep) {
         settle();
         uint32_t mine = 0;
-        each_kept([&](float l, int) { mine += key_of(l) == floor_key; });
+        each([&](const float (&l)[4], const bool (&in)[4], int) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine += in[j] && key_of(l[j]) == floor_key;
+        });
         uint32_t incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -400,8 +417,10 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         for (int r = 0; r < rank; ++r) before += cluster.map_shared_rank(&sh, r)->ties;
         if (before < keep && before + mine >= keep) {
             uint32_t left = keep - before;
-            each_kept([&](float l, int i) {
-                if (key_of(l) == floor_key && --left == 0) sh.cut_index = (int)begin + i;
+            each([&](const float (&l)[4], const bool (&in)[4], int i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (in[j] && key_of(l[j]) == floor_key && --left == 0) sh.cut_index = (int)begin + i + j;
             });
         }
         cluster.sync();
@@ -458,7 +477,10 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     auto finish = [&](int last_bin, uint32_t want, double target) {
         settle();
         uint32_t mine = 0;
-        each_kept([&](float l, int) { mine += linear_bin(l) <= last_bin; });
+        each([&](const float (&l)[4], const bool (&in)[4], int) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mine += in[j] && linear_bin(l[j]) <= last_bin;
+        });
         uint32_t incl = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -490,11 +512,13 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
         }
         Shared* first = cluster.map_shared_rank(&sh, 0);
         if (mine)
-            each_kept([&](float l, int i) {
-                if (linear_bin(l) <= last_bin) {
-                    first->list_key[at] = key_of(l);
-                    first->list_id[at++] = (int)begin + i;
-                }
+            each([&](const float (&l)[4], const bool (&in)[4], int i) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (in[j] && linear_bin(l[j]) <= last_bin) {
+                        first->list_key[at] = key_of(l[j]);
+                        first->list_id[at++] = (int)begin + i + j;
+                    }
             });
         cluster.sync();
         if (rank != 0) return;
@@ -538,14 +562,27 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     auto kept_mass = [&](double least, unsigned long long& mine, unsigned long long& before) {
         settle();
         mine = 0;
-        if (least > 0.0) {
-            each_kept([&](float l, int) {
-                if (weight_of(rw, l) >= least) mine += fixed_of(rw, l);
-            });
+        if (floor_key == 0 && least == 0.0) {  // nothing is left out: the loop carries no tests, and 256's bits are taken off at its end
+            int i = i0;
+#pragma unroll 1
+            for (; i + 4 <= i1; i += 4) {
+                const float l[4] = {vals[i], vals[i + 1], vals[i + 2], vals[i + 3]};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mine += fixed_of(rw, l[j]) + kBits256;
+            }
+            for (; i < i1; ++i) mine += fixed_of(rw, vals[i]) + kBits256;
+            mine -= (unsigned long long)(i1 - i0) * kBits256;
         } else {
-            uint32_t taken = 0;
-            each_kept([&](float l, int) { mine += biased_of(rw, l), ++taken; });
-            mine -= taken * kBits256;
+            each([&](const float (&l)[4], const bool (&in)[4], int) {
+                double series[4], power[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) weight_factors(rw, l[j], series[j], power[j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bool stays = in[j] && (least == 0.0 || series[j] * power[j] >= least);
+                    mine += stays ? (unsigned long long)__double_as_longlong(fma(series[j], power[j], 256.0)) - kBits256 : 0ull;
+                }
+            });
         }
         unsigned long long incl = mine;
 #pragma unroll
@@ -624,7 +661,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
     settle();  // no CTA leaves while another reads its shared memory
 }
 
-template <class T>
+template <class T, int kPerSm>
 int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     static std::mutex mu;
     static bool done[64];
@@ -637,13 +674,15 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!done[dev]) {
-            if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) != cudaSuccess) {
+            if (cudaFuncSetAttribute(sample_kernel<T, kPerSm>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) !=
+                cudaSuccess) {
                 cudaGetLastError();
                 return BITLINEAR_ERR_CUDA;
             }
             done[dev] = true;
         }
     }
+    a.per = (a.shard + kThreads - 1) / kThreads | 1;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -657,7 +696,7 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, sample_kernel<T>, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, sample_kernel<T, kPerSm>, a) != cudaSuccess) {
         cudaGetLastError();
         return BITLINEAR_ERR_CUDA;
     }
@@ -679,11 +718,13 @@ extern "C" int bitlinear_sample(const void* logits, int logits_dtype, int M, int
     if (reinterpret_cast<uintptr_t>(logits) % (logits_dtype == BITLINEAR_F32 ? 4 : 2)) return BITLINEAR_ERR_ALIGN;
     int sm_count = 0;
     if (const int rc = device_sm_count(&sm_count)) return rc;
-    int ranks = 1;
+    // CTAs per row: two at least (each merges its share of the bins, one per thread), more for long rows
+    int ranks = 2;
     while (ranks < kMaxCluster && V > 2048 * ranks) ranks *= 2;
     SampleArgs a = {logits, row_stride, M, V, 0, 0, u, temperature, top_k, top_p, min_p, ids, logprobs};
     a.shard = ((V + ranks - 1) / ranks + 7) / 8 * 8;
-    a.per = (a.shard + kThreads - 1) / kThreads | 1;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return logits_dtype == BITLINEAR_F32 ? sample_launch<float>(a, ranks, st) : sample_launch<__nv_bfloat16>(a, ranks, st);
+    const bool alone = (long long)M * ranks <= sm_count;
+    if (logits_dtype == BITLINEAR_F32) return alone ? sample_launch<float, 1>(a, ranks, st) : sample_launch<float, 2>(a, ranks, st);
+    return alone ? sample_launch<__nv_bfloat16, 1>(a, ranks, st) : sample_launch<__nv_bfloat16, 2>(a, ranks, st);
 }
