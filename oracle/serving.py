@@ -136,7 +136,10 @@ def attention8(q, k_codes, v_codes, k_scale, v_scale, table, length, n_q, n_kv, 
         out[h] = (p / p.sum()) @ v[:, g]
         # D products in fp32, each addition off by 2^-23 at most (the tensor cores may cut instead of round), and three roundings
         # of the scaled score
-        worst = max(worst, (D + 4) * 2.0 ** -23 * float((np.abs(k[:, g]) @ np.abs(q[h])).max()) / math.sqrt(D))
+        err = (D + 4) * 2.0 ** -23 * float((np.abs(k[:, g]) @ np.abs(q[h])).max()) / math.sqrt(D)
+        if kind == INT8:  # queries rounded to 1 / 16256 of the head's largest
+            err += (0.5 / 16256 + 2.0 ** -23) * float(np.abs(k[:, g]).sum(-1).max() * np.abs(q[h]).max()) / math.sqrt(D)
+        worst = max(worst, err)
     return out, float(np.abs(v).max()), worst
 
 

@@ -232,7 +232,6 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv8_kernel(const AppendAr
 // ---------------------------------------------------------------------------------------------- decode attention
 
 constexpr int kUnit = 32;        // cache rows a warp takes at a time
-constexpr int kWarps = 8;        // each with its own ring of units in shared memory
 constexpr int kMaxCtas = 160;    // one CTA per SM; partial results are reserved for this many
 constexpr int kMaxStages = 8;
 
@@ -258,10 +257,15 @@ struct AttnArgs {
 
 struct UnitMeta {
     int m, h;
-    uint32_t rows;   // live rows, one bit each
-    int flags;       // 1: first unit of this run's part of the pair, 2: last
+    uint32_t rows;       // live rows, one bit each
+    int flags;           // 1: first unit of this run's part of the pair, 2: last, 4: the pair's last; the unit's number in the pair above
     float ks[2], vs[2];  // scales of the unit's halves
-    long long begin, end;  // the pair's units
+};
+
+// entries of a row's table that a warp looks ahead, with their scales for the head at hand
+struct TableWindow {
+    int id[32];
+    float ks[32], vs[32];
 };
 
 struct PartHead {
@@ -288,6 +292,11 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 __device__ __forceinline__ uint32_t movmatrix_t16(uint32_t a) {
     uint32_t d;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
@@ -296,6 +305,12 @@ __device__ __forceinline__ uint32_t movmatrix_t16(uint32_t a) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+// 2^x to two units in the last place; results below 2^-126 are 0
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // Four codes of a word -> two pairs of f16, exactly.  int8: the code plus 128 becomes the low bits of 1024 + x, and
@@ -332,30 +347,44 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
 __host__ __device__ inline size_t part_smem(int group, int D) { return sizeof(PartHead) + (size_t)group * D * sizeof(float); }
 __host__ __device__ inline size_t part_floats(int group, int D) { return (size_t)group * D + 2 * group; }
 
-size_t attn8_smem(int group, int D, int stages) {
-    return 1024 + (size_t)kWarps * stages * (2 * kUnit * D + sizeof(UnitMeta) + 8) + kWarps * part_smem(group, D) + 16;
+// shared memory: [rings: warp][stage][unit] [unit heads] [table windows] [first parts] [barriers, abort flag, which second parts exist, weights of parts]
+struct AttnSmem {
+    size_t meta, window, parts, bars, total;
+};
+__host__ __device__ inline AttnSmem attn8_smem(int group, int D, int warps, int stages) {
+    AttnSmem s;
+    s.meta = (size_t)warps * stages * 2 * kUnit * D;
+    s.window = s.meta + (size_t)warps * stages * sizeof(UnitMeta);
+    s.parts = s.window + (size_t)warps * sizeof(TableWindow);
+    s.bars = s.parts + warps * part_smem(group, D);
+    s.total = s.bars + (size_t)warps * stages * 8 + 16 + (size_t)warps * 4;
+    return s;
 }
 
 // first unit of worker w's run
 __device__ __forceinline__ long long run_begin(long long units, int w, int workers) { return units * w / workers; }
 
-template <int D, int KIND>
-__global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                                      const AttnArgs a) {
-    constexpr int KS = D / 16;     // k-steps of the scores, and 16-dim tiles of the result
+// NARROW: groups of at most four query heads, which leave half of the tensor core's eight columns free.
+template <int D, int KIND, int WARPS, bool NARROW>
+__global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                                                        const AttnArgs a) {
+    constexpr int KS = D / 16;     // 16-dim tiles of the result
     constexpr int VW = D / 32;     // 32-bit words of a value row per lane
+    constexpr bool INT8 = KIND == BITLINEAR_KV_INT8;
     constexpr uint32_t kUnitBytes = 2u * kUnit * D;  // keys, then values
     extern __shared__ uint8_t attn8_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
     const int group = a.n_q / a.n_kv, stages = a.stages;
     uint8_t* smem = attn8_raw + ((1024u - (smem_u32(attn8_raw) & 1023u)) & 1023u);
+    const AttnSmem lay = attn8_smem(group, D, WARPS, stages);
     const uint32_t ring = smem_u32(smem) + (uint32_t)warp * stages * kUnitBytes;
-    UnitMeta* meta = reinterpret_cast<UnitMeta*>(smem + (size_t)kWarps * stages * kUnitBytes) + warp * stages;
-    uint8_t* parts0 = smem + (size_t)kWarps * stages * (kUnitBytes + sizeof(UnitMeta));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(parts0 + kWarps * part_smem(group, D));
+    UnitMeta* meta = reinterpret_cast<UnitMeta*>(smem + lay.meta) + warp * stages;
+    TableWindow& win = reinterpret_cast<TableWindow*>(smem + lay.window)[warp];
+    uint8_t* parts0 = smem + lay.parts;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + lay.bars);
     const uint32_t full = smem_u32(bars + warp * stages);
-    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kWarps * stages);
-    __shared__ int second_used[kWarps];
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + WARPS * stages);
+    int* second_used = const_cast<int*>(abort_flag) + 4;
     if (tid == 0) *abort_flag = 0;
     if (lane == 0) {
         for (int s = 0; s < stages; ++s) mbar_init(full + 8u * s, 1);
@@ -371,81 +400,92 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __syncthreads();
 
-    // ---- this warp's run of units
-    const int workers = gridDim.x * kWarps, me = blockIdx.x * kWarps + warp;
+    // ---- this warp's run of units.  256 rows' lengths at a time, all loads of a batch in flight at once; up to 256 rows they
+    // are read once.
+    constexpr int BATCH = 8;
+    const int workers = gridDim.x * WARPS, me = blockIdx.x * WARPS + warp;
+    int lens[BATCH];
+    auto load_lens = [&](int m0) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int m = m0 + 32 * i + lane;
+            lens[i] = m < a.M ? row_len(a, m) : -1;
+        }
+    };
     long long total = 0;
-    for (int m = lane; m < a.M; m += 32) total += units_of(row_len(a, m));
+    for (int m0 = 0; m0 < a.M; m0 += 32 * BATCH) {
+        load_lens(m0);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) total += lens[i] >= 0 ? units_of(lens[i]) : 0;
+    }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
     const long long units = total * a.n_kv;
     const long long u0 = run_begin(units, me, workers), u1 = run_begin(units, me + 1, workers);
     const int n_units = (int)(u1 - u0);
     // the pair u0 lies in: row pm (its length and units), head ph, first unit of the pair
-    int pm = 0, ph = 0, p_len = 0, p_units = 1, p_unit = 0;
-    long long p_begin = 0;
+    int pm = -1, ph = 0, p_len = 0, p_units = 1, p_unit = 0;
     if (n_units > 0) {
         long long base = 0;
-        for (int m0 = 0; m0 < a.M; m0 += 32) {
-            const int len = m0 + lane < a.M ? row_len(a, m0 + lane) : 0;
-            const long long n = m0 + lane < a.M ? (long long)units_of(len) * a.n_kv : 0;
-            long long incl = n;
+        for (int m0 = 0; m0 < a.M && pm < 0; m0 += 32 * BATCH) {
+            if (a.M > 32 * BATCH) load_lens(m0);
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const long long up = __shfl_up_sync(0xffffffffu, incl, d);
-                if (lane >= d) incl += up;
+            for (int i = 0; i < BATCH; ++i) {
+                if (pm >= 0 || m0 + 32 * i >= a.M) break;
+                const long long n = lens[i] >= 0 ? (long long)units_of(lens[i]) * a.n_kv : 0;
+                long long incl = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                    if (lane >= d) incl += up;
+                }
+                const unsigned past = __ballot_sync(0xffffffffu, base + incl > u0);
+                if (past) {
+                    const int src = __ffs((int)past) - 1;
+                    pm = m0 + 32 * i + src;
+                    p_len = __shfl_sync(0xffffffffu, lens[i], src);
+                    p_units = units_of(p_len);
+                    const long long row_begin = base + __shfl_sync(0xffffffffu, incl - n, src);
+                    ph = (int)((u0 - row_begin) / p_units);
+                    p_unit = (int)(u0 - row_begin - (long long)ph * p_units);
+                }
+                base += __shfl_sync(0xffffffffu, incl, 31);
             }
-            const unsigned past = __ballot_sync(0xffffffffu, base + incl > u0);
-            if (past) {
-                const int src = __ffs((int)past) - 1;
-                pm = m0 + src;
-                p_len = __shfl_sync(0xffffffffu, len, src);
-                p_units = units_of(p_len);
-                const long long row_begin = base + __shfl_sync(0xffffffffu, incl - n, src);
-                ph = (int)((u0 - row_begin) / p_units);
-                p_begin = row_begin + (long long)ph * p_units;
-                p_unit = (int)(u0 - p_begin);
-                break;
-            }
-            base += __shfl_sync(0xffffffffu, incl, 31);
         }
     }
 
-    // ---- producer side: issue unit n of the run into its ring place
+    // ---- producer side: issue the next unit of the run into its ring place
     const uint64_t once = l2_evict_first_policy();
     const int rows_log2 = a.log2_rows, per_unit = rows_log2 < 5 ? 2 : 1;  // blocks a unit spans
-    int c_base = 0, c_id = -1;    // lane l holds table entry c_base + l of the row, its scales for head ph
-    float c_ks = 0.0f, c_vs = 0.0f;
-    bool c_valid = false;
+    int w_base = 0, w_end = 0;  // the window holds table entries w_base .. w_end - 1 of row pm, head ph
     int issued = 0;
     auto issue = [&]() {
         const int place = issued % stages;
         const int b = (p_unit * kUnit) >> rows_log2;
-        if (!c_valid || b < c_base || b + per_unit > c_base + 32) {
-            c_base = b;
-            c_valid = true;
+        if (b < w_base || b + per_unit > w_end) {
+            w_base = b;
+            w_end = b + 32;
             const int seq = a.seq_ids ? a.seq_ids[pm] : pm;
             const int idx = b + lane;
-            c_id = ((long long)idx << rows_log2) < p_len ? a.tables[(size_t)seq * a.max_blocks + idx] : -1;
-            if (c_id < 0 || c_id >= a.n_blocks) c_id = -1;
-            c_ks = c_id >= 0 ? a.k_scale[(size_t)c_id * a.n_kv + ph] : 0.0f;
-            c_vs = c_id >= 0 ? a.v_scale[(size_t)c_id * a.n_kv + ph] : 0.0f;
+            int id = ((long long)idx << rows_log2) < p_len ? a.tables[(size_t)seq * a.max_blocks + idx] : -1;
+            if (id < 0 || id >= a.n_blocks) id = -1;
+            win.id[lane] = id;
+            win.ks[lane] = id >= 0 ? a.k_scale[(size_t)id * a.n_kv + ph] : 0.0f;
+            win.vs[lane] = id >= 0 ? a.v_scale[(size_t)id * a.n_kv + ph] : 0.0f;
+            __syncwarp();
         }
-        const int l0 = b - c_base, l1 = l0 + per_unit - 1;
-        const int id0 = __shfl_sync(0xffffffffu, c_id, l0), id1 = __shfl_sync(0xffffffffu, c_id, l1);
-        const float ks0 = __shfl_sync(0xffffffffu, c_ks, l0), ks1 = __shfl_sync(0xffffffffu, c_ks, l1);
-        const float vs0 = __shfl_sync(0xffffffffu, c_vs, l0), vs1 = __shfl_sync(0xffffffffu, c_vs, l1);
         if (lane == 0) {
+            const int l0 = b - w_base, l1 = l0 + per_unit - 1;
+            const int id0 = win.id[l0], id1 = win.id[l1];
             const int live = min(max(p_len - p_unit * kUnit, 0), kUnit);
             uint32_t rows = live == 32 ? 0xffffffffu : (1u << live) - 1u;
             if (id0 < 0) rows &= 0xffff0000u;
             if (id1 < 0) rows &= 0x0000ffffu;
             UnitMeta& w = meta[place];
-            w.m = pm;
-            w.h = ph;
-            w.rows = rows;
-            w.flags = (issued == 0 || p_unit == 0 ? 1 : 0) | (issued == n_units - 1 || p_unit == p_units - 1 ? 2 : 0);
-            w.ks[0] = ks0, w.ks[1] = ks1, w.vs[0] = vs0, w.vs[1] = vs1;
-            w.begin = p_begin, w.end = p_begin + p_units;
+            const bool pair_end = p_unit == p_units - 1;
+            const int flags = (issued == 0 || p_unit == 0 ? 1 : 0) | (issued == n_units - 1 || pair_end ? 2 : 0) | (pair_end ? 4 : 0) | (p_unit << 3);
+            *reinterpret_cast<int4*>(&w.m) = make_int4(pm, ph, (int)rows, flags);
+            *reinterpret_cast<float4*>(w.ks) = make_float4(win.ks[l0], win.ks[l1], win.vs[l0], win.vs[l1]);
             const uint32_t dst = ring + (uint32_t)place * kUnitBytes, bar = full + 8u * place;
             const uint32_t off = (uint32_t)(p_unit * kUnit) & ((1u << rows_log2) - 1u);
             const uint32_t copies = per_unit == 1 ? (id0 >= 0 ? 1u : 0u) : (id0 >= 0 ? 1u : 0u) + (id1 >= 0 ? 1u : 0u);
@@ -464,8 +504,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
         ++issued;
         if (++p_unit == p_units) {  // on to the next pair
             p_unit = 0;
-            p_begin += p_units;
-            c_valid = false;
+            w_end = 0;
             if (++ph == a.n_kv) {
                 ph = 0;
                 if (++pm < a.M) {
@@ -474,45 +513,69 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
                 }
             }
         }
+        __syncwarp();  // lane 0 has read the window
     };
 
     // ---- consumer side
-    uint32_t qb[KS][2];
+    // The queries as the tensor core's second operand.  int8 codes go to the integer tensor cores as they are, the queries as two
+    // digits of 7 and 8 bits (15 bits of each head's largest magnitude, where bf16 itself has 8 of each value): sums are exact.  With
+    // at most four heads the digits share the eight columns.  e4m3 codes are converted to f16, the queries too.
+    constexpr int QB = INT8 ? D / 32 : D / 16;  // steps along the dims
+    uint32_t qb[INT8 && !NARROW ? 2 * QB : QB][2];
     float o[KS][4], m_run[2], l_run[2], f_head[2], v_ref = 1.0f;
+    int first_unit = 0;  // the number, in its pair, of the first unit of this run's part
     const int r_lo = row_of_slot(g);
-    int r_v[2] = {row_of_slot(2 * qd), row_of_slot(2 * qd + 1)};
+    const int r_v[2] = {row_of_slot(2 * qd), row_of_slot(2 * qd + 1)};
 
     auto begin_pair = [&](int m, int h) {
-        // The group's queries as the second operand: column g = head g of the group.  The order of the dims over the k-slots is
-        // that in which the key codes arrive: word s of 16-byte chunk qd (+ 4).  Each head is scaled by the power
-        // of two that brings its largest magnitude to 2^8 .. 2^9: bf16 values then fit f16 without loss down to
-        // 2^-22 of the largest, and the scores are scaled back in fp32.
-        const uint4* row = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)h * group + min(g, group - 1)) * D);
-        uint32_t raw[KS][2];
+        // The order of the dims over the k-slots is that in which the key codes arrive: those of 16-byte chunk qd (and qd + 4) of a row.
+        const int head = INT8 && NARROW ? g & 3 : g;
+        const uint4* row = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)h * group + min(head, group - 1)) * D);
+        float x[D / 4];
 #pragma unroll
-        for (int hf = 0; hf < D / 64; ++hf) {
-            const uint4 x = row[8 * hf + 2 * qd], y = row[8 * hf + 2 * qd + 1];
-            raw[4 * hf + 0][0] = x.x, raw[4 * hf + 0][1] = x.y, raw[4 * hf + 1][0] = x.z, raw[4 * hf + 1][1] = x.w;
-            raw[4 * hf + 2][0] = y.x, raw[4 * hf + 2][1] = y.y, raw[4 * hf + 3][0] = y.z, raw[4 * hf + 3][1] = y.w;
+        for (int i = 0; i < D / 32; ++i) {
+            const uint4 t = row[8 * (i >> 1) + 2 * qd + (i & 1)];
+            const uint32_t u[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[8 * i + 2 * j] = __uint_as_float(u[j] << 16);
+                x[8 * i + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+            }
         }
         float amax = 0.0f;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                amax = fmaxf(amax, fmaxf(fabsf(__uint_as_float(raw[s][e] << 16)), fabsf(__uint_as_float(raw[s][e] & 0xffff0000u))));
+        for (int i = 0; i < D / 4; ++i) amax = fmaxf(amax, fabsf(x[i]));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const int be = max(__float_as_int(amax) >> 23, 9);
-        const float up = __int_as_float((262 - be) << 23), down = __int_as_float((be - 8) << 23);  // 2^(135 - be), its inverse
+        float f;
+        if constexpr (INT8) {
+            amax = fmaxf(amax, 1e-30f);
+            const float inv = 16256.0f / amax;  // 127 * 128
+            f = amax * (1.0f / 16256.0f) * a.scale_log2;
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+            for (int i = 0; i < D / 16; ++i) {  // four dims to a word
+                uint32_t hi = 0u, lo = 0u;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                qb[s][e] = g < group ? pack_f16(__uint_as_float(raw[s][e] << 16) * up, __uint_as_float(raw[s][e] & 0xffff0000u) * up) : 0u;
-        const float f = down * a.scale_log2;
-        f_head[0] = __shfl_sync(0xffffffffu, f, 8 * qd);
-        f_head[1] = __shfl_sync(0xffffffffu, f, 8 * qd + 4);
+                for (int j = 0; j < 4; ++j) {
+                    const int v = head < group ? __float2int_rn(x[4 * i + j] * inv) : 0, d = (v + 64) >> 7;
+                    hi |= ((uint32_t)d & 0xffu) << (8 * j);
+                    lo |= ((uint32_t)(v - 128 * d) & 0xffu) << (8 * j);
+                }
+                if constexpr (NARROW) qb[i >> 1][i & 1] = g < 4 ? hi : lo;
+                else qb[i >> 1][i & 1] = hi, qb[QB + (i >> 1)][i & 1] = lo;
+            }
+        } else {
+            // each head is scaled by the power of two that brings its largest magnitude to 2^8 .. 2^9: bf16 values then fit f16
+            // without loss down to 2^-22 of the largest, and the scores are scaled back in fp32
+            const int be = max(__float_as_int(amax) >> 23, 9);
+            const float up = __int_as_float((262 - be) << 23), down = __int_as_float((be - 8) << 23);  // 2^(135 - be), its inverse
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) qb[i >> 1][i & 1] = head < group ? pack_f16(x[2 * i] * up, x[2 * i + 1] * up) : 0u;
+            f = down * a.scale_log2;
+        }
+        const int col = INT8 && NARROW ? 8 * (qd & 1) : 8 * qd;  // lane of column 2 qd (qd & 1: both digits' lanes hold the whole score)
+        f_head[0] = __shfl_sync(0xffffffffu, f, col);
+        f_head[1] = __shfl_sync(0xffffffffu, f, col + 4);
         m_run[0] = m_run[1] = -INFINITY;
         l_run[0] = l_run[1] = 0.0f;
         v_ref = 0.0f;
@@ -535,43 +598,75 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
         float sv[2][4];
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-            float s0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             const uint32_t row_lo = base + (uint32_t)(16 * hb + r_lo) * D, row_hi = row_lo + 8 * D;
+            uint32_t x[D / 64][4], y[D / 64][4];
 #pragma unroll
             for (int hf = 0; hf < D / 64; ++hf) {
                 const uint32_t c = D == 128 ? (uint32_t)(((qd + 4 * hf) ^ r_lo) << 4) : (uint32_t)((qd ^ ((r_lo >> 1) & 3)) << 4);
-                uint32_t x[4], y[4];
-                lds128(row_lo + c, x);
-                lds128(row_hi + c, y);
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    uint32_t f[4];
-                    to_f16<KIND>(x[s], f[0], f[2]);
-                    to_f16<KIND>(y[s], f[1], f[3]);
-                    if (s & 1) mma_f16(s1, f, qb[4 * hf + s][0], qb[4 * hf + s][1]);
-                    else mma_f16(s0, f, qb[4 * hf + s][0], qb[4 * hf + s][1]);
-                }
+                lds128(row_lo + c, x[hf]);
+                lds128(row_hi + c, y[hf]);
             }
-            const float ks = w.ks[hb];
-            const bool live_lo = (rows >> (16 * hb + r_lo)) & 1u, live_hi = (rows >> (16 * hb + 8 + r_lo)) & 1u;
-            sv[hb][0] = live_lo ? (s0[0] + s1[0]) * (ks * f_head[0]) : -INFINITY;  // a dead row may hold anything: selected away
-            sv[hb][1] = live_lo ? (s0[1] + s1[1]) * (ks * f_head[1]) : -INFINITY;
-            sv[hb][2] = live_hi ? (s0[2] + s1[2]) * (ks * f_head[0]) : -INFINITY;
-            sv[hb][3] = live_hi ? (s0[3] + s1[3]) * (ks * f_head[1]) : -INFINITY;
+            float s[4];
+            if constexpr (INT8) {
+                int hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int hf = 0; hf < D / 64; ++hf)
+#pragma unroll
+                    for (int st = 0; st < 2; ++st) {
+                        const int i = 2 * hf + st;
+                        mma_s8(hi, x[hf][2 * st], y[hf][2 * st], x[hf][2 * st + 1], y[hf][2 * st + 1], qb[i][0], qb[i][1]);
+                        if constexpr (!NARROW) mma_s8(lo, x[hf][2 * st], y[hf][2 * st], x[hf][2 * st + 1], y[hf][2 * st + 1], qb[QB + i][0], qb[QB + i][1]);
+                    }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (NARROW) {
+                        const int v = qd < 2 ? hi[e] << 7 : hi[e];  // lanes 0, 1 of four hold the high digits' columns, 2, 3 the low digits'
+                        s[e] = (float)(v + __shfl_xor_sync(0xffffffffu, v, 2));
+                    } else {
+                        s[e] = (float)((hi[e] << 7) + lo[e]);
+                    }
+                }
+            } else {
+                float s0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int hf = 0; hf < D / 64; ++hf)
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {
+                        uint32_t f[4];
+                        to_f16<KIND>(x[hf][st], f[0], f[2]);
+                        to_f16<KIND>(y[hf][st], f[1], f[3]);
+                        if (st & 1) mma_f16(s1, f, qb[4 * hf + st][0], qb[4 * hf + st][1]);
+                        else mma_f16(s0, f, qb[4 * hf + st][0], qb[4 * hf + st][1]);
+                    }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = s0[e] + s1[e];
+            }
+            const float ks0 = w.ks[hb] * f_head[0], ks1 = w.ks[hb] * f_head[1];
+            sv[hb][0] = s[0] * ks0;
+            sv[hb][1] = s[1] * ks1;
+            sv[hb][2] = s[2] * ks0;
+            sv[hb][3] = s[3] * ks1;
+        }
+        if (rows != 0xffffffffu) {  // a dead row may hold anything: selected away
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb) {
+                if (!((rows >> (16 * hb + r_lo)) & 1u)) sv[hb][0] = sv[hb][1] = -INFINITY;
+                if (!((rows >> (16 * hb + 8 + r_lo)) & 1u)) sv[hb][2] = sv[hb][3] = -INFINITY;
+            }
         }
         float mx0 = fmaxf(fmaxf(sv[0][0], sv[0][2]), fmaxf(sv[1][0], sv[1][2]));
         float mx1 = fmaxf(fmaxf(sv[0][1], sv[0][3]), fmaxf(sv[1][1], sv[1][3]));
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) {
-            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
-            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
-        }
         // The values' scales ride on the weights: o is held in units of the largest scale met so far.
         const float vs = fmaxf(w.vs[0], w.vs[1]);
-        if (__any_sync(0xffffffffu, mx0 > m_run[0] || mx1 > m_run[1]) || vs > v_ref) {
+        if (__any_sync(0xffffffffu, mx0 > m_run[0] || mx1 > m_run[1] || vs > v_ref)) {
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) {
+                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
+                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+            }
             const float n0 = fmaxf(m_run[0], mx0), n1 = fmaxf(m_run[1], mx1), nv = fmaxf(v_ref, vs);
             const float fv = nv > 0.0f ? v_ref / nv : 0.0f;
-            const float c0 = n0 == -INFINITY ? 1.0f : exp2f(m_run[0] - n0), c1 = n1 == -INFINITY ? 1.0f : exp2f(m_run[1] - n1);
+            const float c0 = n0 == -INFINITY ? 1.0f : ex2(m_run[0] - n0), c1 = n1 == -INFINITY ? 1.0f : ex2(m_run[1] - n1);
             l_run[0] *= c0;
             l_run[1] *= c1;
 #pragma unroll
@@ -586,16 +681,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
             v_ref = nv;
         }
         const float b0 = m_run[0] == -INFINITY ? 0.0f : m_run[0], b1 = m_run[1] == -INFINITY ? 0.0f : m_run[1];
+        const float per_ref = v_ref > 0.0f ? __fdividef(32768.0f, v_ref) : 0.0f;
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-            const float p0 = exp2f(sv[hb][0] - b0), p1 = exp2f(sv[hb][1] - b1), p2 = exp2f(sv[hb][2] - b0), p3 = exp2f(sv[hb][3] - b1);
-            l_run[0] += p0 + p2;  // this lane's rows; summed over the lanes at the pair's end
-            l_run[1] += p1 + p3;
-            // Weights as f16, scaled by 2^15 so that the smallest ones keep their bits: an error of 2^-12 of a weight, at random
-            // signs, against the result's own rounding of 2^-9.
-            const float wv = v_ref > 0.0f ? 32768.0f * __fdividef(w.vs[hb], v_ref) : 0.0f;
-            const uint32_t w0 = movmatrix_t16(pack_f16(p0 * wv, p1 * wv)), w1 = movmatrix_t16(pack_f16(p2 * wv, p3 * wv));
-            // O^T (D x 8 heads) += V^T (D x 16 rows) P; lane (g, qd) holds dims 2 VW ... of rows in slots 2qd, 2qd+1 (+8)
+            // O^T (D x 8 heads) += V^T (D x 16 rows) P; lane (g, qd) holds dims 2 KS g ... of rows in slots 2qd, 2qd+1 (+8)
             uint32_t x[4][VW];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -604,6 +693,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
                 if constexpr (D == 128) lds128(row + (uint32_t)((g ^ r) << 4), x[j]);
                 else lds64(row + (uint32_t)((((g >> 1) ^ ((r >> 1) & 3)) << 4) + ((g & 1) << 3)), x[j]);
             }
+            const float p0 = ex2(sv[hb][0] - b0), p1 = ex2(sv[hb][1] - b1), p2 = ex2(sv[hb][2] - b0), p3 = ex2(sv[hb][3] - b1);
+            l_run[0] += p0 + p2;  // this lane's rows; summed over the lanes at the pair's end
+            l_run[1] += p1 + p3;
+            // Weights as f16, scaled by 2^15 so that the smallest ones keep their bits: an error of 2^-12 of a weight, at random
+            // signs, against the result's own rounding of 2^-9.
+            const float wv = w.vs[hb] * per_ref;
+            const uint32_t w0 = movmatrix_t16(pack_f16(p0 * wv, p1 * wv)), w1 = movmatrix_t16(pack_f16(p2 * wv, p3 * wv));
 #pragma unroll
             for (int q = 0; q < VW; ++q) {
                 const uint32_t t0 = __byte_perm(x[0][q], x[1][q], 0x5140), t1 = __byte_perm(x[2][q], x[3][q], 0x5140);
@@ -620,15 +716,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
     };
 
     // lane (g, qd) holds dims (2 KS) g + 0 .. 2 KS - 1 of heads 2qd, 2qd + 1: o[t][e] is dim 2t, o[t][2 + e] dim 2t + 1
-    auto end_pair = [&](const UnitMeta& w) {
+    auto end_pair = [&](const UnitMeta& w, long long at_unit) {
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) {
             l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
             l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
         }
         const float unscale = v_ref * (1.0f / 32768.0f);
-        const bool whole = w.begin >= u0 && w.end <= u1;
-        if (whole) {
+        if (first_unit == 0 && (w.flags & 4)) {  // the whole pair
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int head = 2 * qd + e;
@@ -649,13 +744,15 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
         }
         // a part: the pair began before this run (first place), or goes on behind it (second place: this warp's ring, whose
         // copies have all landed - a pair that goes on is the run's last)
-        const bool second = w.begin >= u0;
+        const bool second = first_unit == 0;
         uint8_t* at = second ? smem + (size_t)warp * stages * kUnitBytes : parts0 + warp * part_smem(group, D);
         PartHead* head_p = reinterpret_cast<PartHead*>(at);
         float* val = reinterpret_cast<float*>(at + sizeof(PartHead));
         __syncwarp();
         if (lane == 0) {
-            head_p->begin = w.begin, head_p->end = w.end, head_p->m = w.m, head_p->h = w.h, head_p->used = 1;
+            head_p->begin = at_unit - (w.flags >> 3);
+            head_p->end = head_p->begin + units_of(row_len(a, w.m));
+            head_p->m = w.m, head_p->h = w.h, head_p->used = 1;
             if (second) second_used[warp] = 1;
         }
 #pragma unroll
@@ -677,9 +774,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
         const bool landed = mbar_wait(full + 8u * place, (uint32_t)(n / stages) & 1u, abort_flag);
         if (!__all_sync(0xffffffffu, landed)) break;
         const UnitMeta w = meta[place];
-        if (w.flags & 1) begin_pair(w.m, w.h);
+        if (w.flags & 1) {
+            begin_pair(w.m, w.h);
+            first_unit = w.flags >> 3;
+        }
         consume(ring + (uint32_t)place * kUnitBytes, w);
-        if (w.flags & 2) end_pair(w);
+        if (w.flags & 2) end_pair(w, u0 + n);
         __syncwarp();
         if (issued < n_units) issue();
     }
@@ -694,40 +794,40 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
         return;
     }
     // ---- merge the warps' parts; parts of one pair stand next to each other in the order (warp, place)
-    const long long c0 = run_begin(units, blockIdx.x * kWarps, workers), c1 = run_begin(units, blockIdx.x * kWarps + kWarps, workers);
+    const long long c0 = run_begin(units, blockIdx.x * WARPS, workers), c1 = run_begin(units, blockIdx.x * WARPS + WARPS, workers);
     auto part_at = [&](int i) {
         const int w = i >> 1;
         return reinterpret_cast<const PartHead*>((i & 1) ? smem + (size_t)w * stages * kUnitBytes : parts0 + w * part_smem(group, D));
     };
-    auto part_used = [&](int i) { return (i & 1) ? second_used[i >> 1] != 0 : part_at(i)->used != 0; };
-    int2 desc[2] = {make_int2(-1, 0), make_int2(-1, 0)};
-    for (int i = 0; i < 2 * kWarps;) {
-        if (!part_used(i)) {
-            ++i;
-            continue;
-        }
-        const PartHead* lead = part_at(i);
-        int j = i + 1, members = 1;
-        uint32_t mask = 1u << i;
-        for (; j < 2 * kWarps; ++j) {
-            if (!part_used(j)) continue;
-            if (part_at(j)->begin != lead->begin) break;
-            mask |= 1u << j;
-            ++members;
-        }
+    uint32_t used = 0;  // bit i: part i exists
+    if (lane < 2 * WARPS) used = (lane & 1) ? second_used[lane >> 1] != 0 : part_at(lane)->used != 0;
+    used = __ballot_sync(0xffffffffu, used != 0);
+    int2 desc0 = make_int2(-1, 0), desc1 = desc0;
+    while (used) {
+        const PartHead* lead = part_at(__ffs((int)used) - 1);
+        uint32_t mask = 0;
+        if (lane < 2 * WARPS && ((used >> lane) & 1u)) mask = part_at(lane)->begin == lead->begin;
+        mask = __ballot_sync(0xffffffffu, mask != 0);
+        used &= ~mask;
         const bool whole = lead->begin >= c0 && lead->end <= c1;
         const int slot = lead->begin < c0 ? 0 : 1;
         float* dst = a.part + ((size_t)blockIdx.x * 2 + slot) * part_floats(group, D);
-        for (int e = tid; e < group * D; e += kWarps * 32) {
+        for (int e = tid; e < group * D; e += WARPS * 32) {
             const int head = e / D;
-            float top = -INFINITY;
-            for (uint32_t mk = mask; mk; mk &= mk - 1) top = fmaxf(top, part_at(__ffs((int)mk) - 1)->m_run[head]);
-            float acc = 0.0f, l = 0.0f;
+            // lane i weighs part i (a warp's elements belong to one head)
+            const bool mine = lane < 2 * WARPS && ((mask >> lane) & 1u);
+            const float pm_ = mine ? part_at(lane)->m_run[head] : -INFINITY;
+            float top = pm_;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float f = pm_ == -INFINITY ? 0.0f : ex2(pm_ - top);
+            float l = mine ? part_at(lane)->l_run[head] * f : 0.0f;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
+            float acc = 0.0f;
             for (uint32_t mk = mask; mk; mk &= mk - 1) {
-                const PartHead* p = part_at(__ffs((int)mk) - 1);
-                const float f = p->m_run[head] == -INFINITY ? 0.0f : exp2f(p->m_run[head] - top);
-                l = fmaf(p->l_run[head], f, l);
-                acc = fmaf(reinterpret_cast<const float*>(p + 1)[e], f, acc);
+                const int i = __ffs((int)mk) - 1;
+                acc = fmaf(reinterpret_cast<const float*>(part_at(i) + 1)[e], __shfl_sync(0xffffffffu, f, i), acc);
             }
             if (whole) a.out[((size_t)lead->m * a.n_q + (size_t)lead->h * group) * D + e] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
             else {
@@ -741,11 +841,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attn_decode_kv8_kernel(const _
             int w = (int)(x * workers / units);
             while (run_begin(units, w + 1, workers) <= x) ++w;
             while (run_begin(units, w, workers) > x) --w;
-            desc[slot] = make_int2(lead->m * a.n_kv + lead->h, w / kWarps);
+            (slot == 0 ? desc0 : desc1) = make_int2(lead->m * a.n_kv + lead->h, w / WARPS);
         }
-        i = j;
     }
-    if (tid == 0) a.desc[2 * blockIdx.x] = desc[0], a.desc[2 * blockIdx.x + 1] = desc[1];
+    if (tid == 0) *reinterpret_cast<int4*>(a.desc + 2 * blockIdx.x) = make_int4(desc0.x, desc0.y, desc1.x, desc1.y);
 }
 
 // Merges the parts of a pair that several CTAs share: CTA (c, head) does nothing unless a pair begins in attention CTA c and goes
@@ -820,46 +919,43 @@ bool make_kv8_map(CUtensorMap* map, const void* pool, long long rows, int hd, in
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr size_t kAttnMaxSmem = 227 * 1024 - 256;
+constexpr size_t kAttnMaxSmem = 227 * 1024;
 
-// opted in once per device and kernel
-template <int D, int KIND>
-bool attn8_opt_in() {
+template <int D, int KIND, int WARPS, bool NARROW>
+int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a, int ctas, cudaStream_t st) {
+    // opted in once per device and kernel
     static std::mutex mu;
     static bool done[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) {
         cudaGetLastError();
-        return false;
+        return BITLINEAR_ERR_CUDA;
     }
-    std::lock_guard<std::mutex> lock(mu);
-    if (!done[dev]) {
-        if (cudaFuncSetAttribute(attn_decode_kv8_kernel<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAttnMaxSmem) != cudaSuccess) {
-            cudaGetLastError();
-            return false;
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!done[dev]) {
+            if (cudaFuncSetAttribute(attn_decode_kv8_kernel<D, KIND, WARPS, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kAttnMaxSmem) !=
+                cudaSuccess) {
+                cudaGetLastError();
+                return BITLINEAR_ERR_CUDA;
+            }
+            done[dev] = true;
         }
-        done[dev] = true;
     }
-    return true;
-}
-
-template <int D, int KIND>
-int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a, int ctas, cudaStream_t st) {
-    if (!attn8_opt_in<D, KIND>()) return BITLINEAR_ERR_CUDA;
     const int group = a.n_q / a.n_kv;
     a.stages = kMaxStages;
-    while (a.stages > 1 && attn8_smem(group, D, a.stages) > kAttnMaxSmem) --a.stages;
+    while (a.stages > 1 && 1024 + attn8_smem(group, D, WARPS, a.stages).total > kAttnMaxSmem) --a.stages;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kWarps * 32);
-    cfg.dynamicSmemBytes = attn8_smem(group, D, a.stages);
+    cfg.blockDim = dim3(WARPS * 32);
+    cfg.dynamicSmemBytes = 1024 + attn8_smem(group, D, WARPS, a.stages).total;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, attn_decode_kv8_kernel<D, KIND>, map_k, map_v, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, attn_decode_kv8_kernel<D, KIND, WARPS, NARROW>, map_k, map_v, a) != cudaSuccess) {
         cudaGetLastError();
         return BITLINEAR_ERR_CUDA;
     }
@@ -871,6 +967,14 @@ int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a,
         return BITLINEAR_ERR_CUDA;
     }
     return BITLINEAR_OK;
+}
+
+// Twelve warps with rings of two units each, where the parts of a group of at most four heads leave the room; eight
+// warps otherwise.
+template <int D, int KIND>
+int attn8_dispatch(const CUtensorMap& map_k, const CUtensorMap& map_v, const AttnArgs& a, int ctas, cudaStream_t st) {
+    if (a.n_q / a.n_kv <= 4) return attn8_launch<D, KIND, 12, true>(map_k, map_v, a, ctas, st);
+    return attn8_launch<D, KIND, D == 64 ? 12 : 8, false>(map_k, map_v, a, ctas, st);
 }
 
 }  // namespace
@@ -955,10 +1059,10 @@ int bitlinear_attention_decode_kv8(const void* q_bf16, const void* k_cache, cons
     const int ctas = std::min(sm_count, kMaxCtas);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (head_dim == 128)
-        return kv_dtype == BITLINEAR_KV_INT8 ? attn8_launch<128, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st)
-                                             : attn8_launch<128, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
-    return kv_dtype == BITLINEAR_KV_INT8 ? attn8_launch<64, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st)
-                                         : attn8_launch<64, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
+        return kv_dtype == BITLINEAR_KV_INT8 ? attn8_dispatch<128, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st)
+                                             : attn8_dispatch<128, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
+    return kv_dtype == BITLINEAR_KV_INT8 ? attn8_dispatch<64, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st)
+                                         : attn8_dispatch<64, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
 }
 
 }  // extern "C"
