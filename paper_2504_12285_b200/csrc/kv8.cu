@@ -238,7 +238,9 @@ constexpr int kMaxStages = 8;
 // One (row, KV head) pair is the work of one softmax.  All units of all pairs, in the order (row, head, unit), are cut into equal
 // runs, one per warp of the grid, so that a batch of any lengths loads every SM alike.  A run covers pairs in whole
 // (finished by the warp) and at most two in part; those meet in shared memory with the neighbouring warps' and,
-// where a pair reaches beyond the CTA, in global memory, where a second launch merges them.
+// where a pair reaches beyond the CTA, in global memory, where a second launch merges them.  A pair counts for one place
+// more than it has units: starting and ending it takes a warp about as long as a unit does, and without that place the warps
+// that meet many short sequences finished last (by a sixth of the time of a batch of 97 sequences of 1 to 16,384 rows).
 struct AttnArgs {
     const __nv_bfloat16* q;
     const float* k_scale;
@@ -255,22 +257,18 @@ struct AttnArgs {
     int* status;
 };
 
-struct UnitMeta {
+struct __align__(16) UnitMeta {
     int m, h;
     uint32_t rows;       // live rows, one bit each
-    int flags;           // 1: first unit of this run's part of the pair, 2: last, 4: the pair's last; the unit's number in the pair above
+    int flags;           // 1: first unit of this run's part of the pair, 2: last
     float ks[2], vs[2];  // scales of the unit's halves
+    int unit, units;     // its number in the pair, of how many
+    int at, pad;         // its place in the order of all
 };
 
-// entries of a row's table that a warp looks ahead, with their scales for the head at hand
-struct TableWindow {
-    int id[32];
-    float ks[32], vs[32];
-};
-
-struct PartHead {
-    long long begin, end;  // the pair's units
-    int m, h, used, pad;
+struct __align__(16) PartHead {
+    int begin, end;  // places of the pair's units in the order of all
+    int m, h, used, pad[3];
     float m_run[8], l_run[8];
 };
 
@@ -278,6 +276,9 @@ __device__ __forceinline__ int row_len(const AttnArgs& a, int m) {
     const int seq = a.seq_ids ? a.seq_ids[m] : m;
     if (seq < 0 || seq >= a.n_seq) return 0;
     return min(max(a.lengths[m], 0), a.max_blocks << a.log2_rows);
+}
+__device__ __forceinline__ int clamped_len(const AttnArgs& a, int seq, int len) {
+    return seq < 0 || seq >= a.n_seq ? 0 : min(max(len, 0), a.max_blocks << a.log2_rows);
 }
 // units of a (row, head) pair: at least one, so that an empty row has someone to write its zeros
 __device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
@@ -347,22 +348,35 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
 __host__ __device__ inline size_t part_smem(int group, int D) { return sizeof(PartHead) + (size_t)group * D * sizeof(float); }
 __host__ __device__ inline size_t part_floats(int group, int D) { return (size_t)group * D + 2 * group; }
 
-// shared memory: [rings: warp][stage][unit] [unit heads] [table windows] [first parts] [barriers, abort flag, which second parts exist, weights of parts]
+// shared memory: [rings: warp][stage][unit] [unit heads] [first parts] [barriers] [abort flag] [which second parts exist]
 struct AttnSmem {
-    size_t meta, window, parts, bars, total;
+    size_t meta, parts, bars, total;
 };
 __host__ __device__ inline AttnSmem attn8_smem(int group, int D, int warps, int stages) {
     AttnSmem s;
     s.meta = (size_t)warps * stages * 2 * kUnit * D;
-    s.window = s.meta + (size_t)warps * stages * sizeof(UnitMeta);
-    s.parts = s.window + (size_t)warps * sizeof(TableWindow);
+    s.parts = s.meta + (size_t)warps * stages * sizeof(UnitMeta);
     s.bars = s.parts + warps * part_smem(group, D);
     s.total = s.bars + (size_t)warps * stages * 8 + 16 + (size_t)warps * 4;
     return s;
 }
 
-// first unit of worker w's run
-__device__ __forceinline__ long long run_begin(long long units, int w, int workers) { return units * w / workers; }
+// the places 0 .. total - 1 in equal runs: worker w has begin(w) .. begin(w + 1) - 1
+struct Runs {
+    int each, more;  // the first `more` workers have one place more
+    __device__ __forceinline__ Runs(int total, int workers) : each((int)((unsigned)total / (unsigned)workers)), more(total - each * workers) {}
+    __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int owner(int at) const {
+        const int border = more * (each + 1);
+        return at < border ? (int)((unsigned)at / (unsigned)(each + 1)) : more + (int)((unsigned)(at - border) / (unsigned)each);
+    }
+};
+
+// a word from global memory into shared memory; the barrier is told when it has landed
+__device__ __forceinline__ void copy_word(uint32_t dst, const float* src, uint32_t bar) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
 
 // NARROW: groups of at most four query heads, which leave half of the tensor core's eight columns free.
 template <int D, int KIND, int WARPS, bool NARROW>
@@ -379,7 +393,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     const AttnSmem lay = attn8_smem(group, D, WARPS, stages);
     const uint32_t ring = smem_u32(smem) + (uint32_t)warp * stages * kUnitBytes;
     UnitMeta* meta = reinterpret_cast<UnitMeta*>(smem + lay.meta) + warp * stages;
-    TableWindow& win = reinterpret_cast<TableWindow*>(smem + lay.window)[warp];
     uint8_t* parts0 = smem + lay.parts;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + lay.bars);
     const uint32_t full = smem_u32(bars + warp * stages);
@@ -387,7 +400,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     int* second_used = const_cast<int*>(abort_flag) + 4;
     if (tid == 0) *abort_flag = 0;
     if (lane == 0) {
-        for (int s = 0; s < stages; ++s) mbar_init(full + 8u * s, 1);
+        for (int s = 0; s < stages; ++s) mbar_init(full + 8u * s, 5);  // the copies' announcement and four scales
         mbar_init_fence();
         reinterpret_cast<PartHead*>(parts0 + warp * part_smem(group, D))->used = 0;
         second_used[warp] = 0;
@@ -412,31 +425,30 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             lens[i] = m < a.M ? row_len(a, m) : -1;
         }
     };
-    long long total = 0;
+    int total = 0;
     for (int m0 = 0; m0 < a.M; m0 += 32 * BATCH) {
         load_lens(m0);
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) total += lens[i] >= 0 ? units_of(lens[i]) : 0;
+        for (int i = 0; i < BATCH; ++i) total += lens[i] >= 0 ? units_of(lens[i]) + 1 : 0;
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
-    const long long units = total * a.n_kv;
-    const long long u0 = run_begin(units, me, workers), u1 = run_begin(units, me + 1, workers);
-    const int n_units = (int)(u1 - u0);
-    // the pair u0 lies in: row pm (its length and units), head ph, first unit of the pair
-    int pm = -1, ph = 0, p_len = 0, p_units = 1, p_unit = 0;
-    if (n_units > 0) {
-        long long base = 0;
-        for (int m0 = 0; m0 < a.M && pm < 0; m0 += 32 * BATCH) {
+    const Runs runs(total * a.n_kv, workers);
+    const int u0 = runs.begin(me), u1 = runs.begin(me + 1);
+    // where the run begins: row pm (its length and units), head ph, unit p_unit of the pair, at place `next`
+    int pm = a.M, ph = 0, p_len = 0, p_units = 1, p_unit = 0, next = u0;
+    if (u0 < u1) {
+        int base = 0;
+        for (int m0 = 0; m0 < a.M && pm == a.M; m0 += 32 * BATCH) {
             if (a.M > 32 * BATCH) load_lens(m0);
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-                if (pm >= 0 || m0 + 32 * i >= a.M) break;
-                const long long n = lens[i] >= 0 ? (long long)units_of(lens[i]) * a.n_kv : 0;
-                long long incl = n;
+                if (pm < a.M || m0 + 32 * i >= a.M) break;
+                const int n = lens[i] >= 0 ? (units_of(lens[i]) + 1) * a.n_kv : 0;
+                int incl = n;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
-                    const long long up = __shfl_up_sync(0xffffffffu, incl, d);
+                    const int up = __shfl_up_sync(0xffffffffu, incl, d);
                     if (lane >= d) incl += up;
                 }
                 const unsigned past = __ballot_sync(0xffffffffu, base + incl > u0);
@@ -445,9 +457,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
                     pm = m0 + 32 * i + src;
                     p_len = __shfl_sync(0xffffffffu, lens[i], src);
                     p_units = units_of(p_len);
-                    const long long row_begin = base + __shfl_sync(0xffffffffu, incl - n, src);
-                    ph = (int)((u0 - row_begin) / p_units);
-                    p_unit = (int)(u0 - row_begin - (long long)ph * p_units);
+                    const int in_row = u0 - base - __shfl_sync(0xffffffffu, incl - n, src);
+                    ph = (int)((unsigned)in_row / (unsigned)(p_units + 1));
+                    p_unit = in_row - ph * (p_units + 1) - 1;
+                    if (p_unit < 0) p_unit = 0, ++next;  // the place that stands for the pair's start
                 }
                 base += __shfl_sync(0xffffffffu, incl, 31);
             }
@@ -457,7 +470,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     // ---- producer side: issue the next unit of the run into its ring place
     const uint64_t once = l2_evict_first_policy();
     const int rows_log2 = a.log2_rows, per_unit = rows_log2 < 5 ? 2 : 1;  // blocks a unit spans
-    int w_base = 0, w_end = 0;  // the window holds table entries w_base .. w_end - 1 of row pm, head ph
+    int w_id = -1, w_base = 0, w_end = 0;  // lane l holds entry w_base + l of row pm's table, up to w_end
+    int p_seq = 0, n_seq_raw = 0, n_len_raw = 0;  // the row's sequence; the next row's, fetched while this one is at work
+    auto fetch_next_row = [&]() {
+        if (pm + 1 < a.M) {
+            n_seq_raw = a.seq_ids ? a.seq_ids[pm + 1] : pm + 1;
+            n_len_raw = a.lengths[pm + 1];
+        }
+    };
+    if (next < u1) {
+        p_seq = a.seq_ids ? a.seq_ids[pm] : pm;
+        fetch_next_row();
+    }
     int issued = 0;
     auto issue = [&]() {
         const int place = issued % stages;
@@ -465,31 +489,36 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         if (b < w_base || b + per_unit > w_end) {
             w_base = b;
             w_end = b + 32;
-            const int seq = a.seq_ids ? a.seq_ids[pm] : pm;
             const int idx = b + lane;
-            int id = ((long long)idx << rows_log2) < p_len ? a.tables[(size_t)seq * a.max_blocks + idx] : -1;
-            if (id < 0 || id >= a.n_blocks) id = -1;
-            win.id[lane] = id;
-            win.ks[lane] = id >= 0 ? a.k_scale[(size_t)id * a.n_kv + ph] : 0.0f;
-            win.vs[lane] = id >= 0 ? a.v_scale[(size_t)id * a.n_kv + ph] : 0.0f;
-            __syncwarp();
+            w_id = ((long long)idx << rows_log2) < p_len ? a.tables[(size_t)p_seq * a.max_blocks + idx] : -1;
+            if (w_id >= a.n_blocks) w_id = -1;
+        }
+        const int l0 = b - w_base, l1 = l0 + per_unit - 1;
+        const int id0 = __shfl_sync(0xffffffffu, w_id, l0), id1 = __shfl_sync(0xffffffffu, w_id, l1);
+        const bool pair_end = p_unit == p_units - 1;
+        const int after = next + (pair_end ? 2 : 1);
+        const uint32_t bar = full + 8u * place;
+        UnitMeta& w = meta[place];
+        if (lane < 4) {  // scales: keys of both halves, values of both
+            const int id = lane & 1 ? id1 : id0;
+            const float* src = (lane & 2 ? a.v_scale : a.k_scale) + (size_t)max(id, 0) * a.n_kv + ph;
+            if (id >= 0) copy_word(smem_u32(&w.ks[lane]), src, bar);
+            else {
+                (&w.ks[0])[lane] = 0.0f;
+                mbar_arrive(bar);
+            }
         }
         if (lane == 0) {
-            const int l0 = b - w_base, l1 = l0 + per_unit - 1;
-            const int id0 = win.id[l0], id1 = win.id[l1];
             const int live = min(max(p_len - p_unit * kUnit, 0), kUnit);
             uint32_t rows = live == 32 ? 0xffffffffu : (1u << live) - 1u;
             if (id0 < 0) rows &= 0xffff0000u;
             if (id1 < 0) rows &= 0x0000ffffu;
-            UnitMeta& w = meta[place];
-            const bool pair_end = p_unit == p_units - 1;
-            const int flags = (issued == 0 || p_unit == 0 ? 1 : 0) | (issued == n_units - 1 || pair_end ? 2 : 0) | (pair_end ? 4 : 0) | (p_unit << 3);
-            *reinterpret_cast<int4*>(&w.m) = make_int4(pm, ph, (int)rows, flags);
-            *reinterpret_cast<float4*>(w.ks) = make_float4(win.ks[l0], win.ks[l1], win.vs[l0], win.vs[l1]);
-            const uint32_t dst = ring + (uint32_t)place * kUnitBytes, bar = full + 8u * place;
+            *reinterpret_cast<int4*>(&w.m) = make_int4(pm, ph, (int)rows, (issued == 0 || p_unit == 0 ? 1 : 0) | (pair_end || after >= u1 ? 2 : 0));
+            *reinterpret_cast<int4*>(&w.unit) = make_int4(p_unit, p_units, next, 0);
+            const uint32_t dst = ring + (uint32_t)place * kUnitBytes;
             const uint32_t off = (uint32_t)(p_unit * kUnit) & ((1u << rows_log2) - 1u);
             const uint32_t copies = per_unit == 1 ? (id0 >= 0 ? 1u : 0u) : (id0 >= 0 ? 1u : 0u) + (id1 >= 0 ? 1u : 0u);
-            mbar_expect_tx(bar, copies * (kUnitBytes / per_unit));  // none: the phase completes at once
+            mbar_expect_tx(bar, copies * (kUnitBytes / per_unit));
             if (id0 >= 0) {
                 const int row = ((id0 * a.n_kv + ph) << rows_log2) + (int)off;
                 tma_rows(dst, &map_k, row, bar, once);
@@ -502,18 +531,21 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             }
         }
         ++issued;
-        if (++p_unit == p_units) {  // on to the next pair
+        next = after;
+        ++p_unit;
+        if (pair_end) {  // on to the next pair
             p_unit = 0;
-            w_end = 0;
             if (++ph == a.n_kv) {
                 ph = 0;
-                if (++pm < a.M) {
-                    p_len = row_len(a, pm);
-                    p_units = units_of(p_len);
-                }
+                w_end = 0;
+                ++pm;
+                p_seq = n_seq_raw;
+                p_len = clamped_len(a, n_seq_raw, n_len_raw);
+                p_units = units_of(p_len);
+                if (next < u1) fetch_next_row();
             }
         }
-        __syncwarp();  // lane 0 has read the window
+        __syncwarp();  // the unit's head is written
     };
 
     // ---- consumer side
@@ -523,7 +555,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     constexpr int QB = INT8 ? D / 32 : D / 16;  // steps along the dims
     uint32_t qb[INT8 && !NARROW ? 2 * QB : QB][2];
     float o[KS][4], m_run[2], l_run[2], f_head[2], v_ref = 1.0f;
-    int first_unit = 0;  // the number, in its pair, of the first unit of this run's part
+    int first_unit = 0;          // the number, in its pair, of the first unit of this run's part
     const int r_lo = row_of_slot(g);
     const int r_v[2] = {row_of_slot(2 * qd), row_of_slot(2 * qd + 1)};
 
@@ -716,14 +748,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     };
 
     // lane (g, qd) holds dims (2 KS) g + 0 .. 2 KS - 1 of heads 2qd, 2qd + 1: o[t][e] is dim 2t, o[t][2 + e] dim 2t + 1
-    auto end_pair = [&](const UnitMeta& w, long long at_unit) {
+    auto end_pair = [&](const UnitMeta& w) {
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) {
             l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
             l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
         }
         const float unscale = v_ref * (1.0f / 32768.0f);
-        if (first_unit == 0 && (w.flags & 4)) {  // the whole pair
+        if (first_unit == 0 && w.unit == w.units - 1) {  // the whole pair
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int head = 2 * qd + e;
@@ -750,8 +782,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         float* val = reinterpret_cast<float*>(at + sizeof(PartHead));
         __syncwarp();
         if (lane == 0) {
-            head_p->begin = at_unit - (w.flags >> 3);
-            head_p->end = head_p->begin + units_of(row_len(a, w.m));
+            head_p->begin = w.at - w.unit;
+            head_p->end = w.at - w.unit + w.units;
             head_p->m = w.m, head_p->h = w.h, head_p->used = 1;
             if (second) second_used[warp] = 1;
         }
@@ -767,21 +799,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         }
     };
 
-    const int ahead = min(stages, n_units);
-    for (int n = 0; n < ahead; ++n) issue();
-    for (int n = 0; n < n_units; ++n) {
+    for (int n = 0; n < stages && next < u1; ++n) issue();
+    for (int n = 0; n < issued; ++n) {
         const int place = n % stages;
+        if (meta[place].flags & 1) {  // (the head is this warp's own and needs no waiting: the queries come in beside the copies)
+            begin_pair(meta[place].m, meta[place].h);
+            first_unit = meta[place].unit;
+        }
         const bool landed = mbar_wait(full + 8u * place, (uint32_t)(n / stages) & 1u, abort_flag);
         if (!__all_sync(0xffffffffu, landed)) break;
         const UnitMeta w = meta[place];
-        if (w.flags & 1) {
-            begin_pair(w.m, w.h);
-            first_unit = w.flags >> 3;
-        }
         consume(ring + (uint32_t)place * kUnitBytes, w);
-        if (w.flags & 2) end_pair(w, u0 + n);
+        if (w.flags & 2) end_pair(w);
         __syncwarp();
-        if (issued < n_units) issue();
+        if (next < u1) issue();
     }
 
     __syncthreads();
@@ -794,7 +825,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         return;
     }
     // ---- merge the warps' parts; parts of one pair stand next to each other in the order (warp, place)
-    const long long c0 = run_begin(units, blockIdx.x * WARPS, workers), c1 = run_begin(units, blockIdx.x * WARPS + WARPS, workers);
+    const int c0 = runs.begin(blockIdx.x * WARPS), c1 = runs.begin(blockIdx.x * WARPS + WARPS);
     auto part_at = [&](int i) {
         const int w = i >> 1;
         return reinterpret_cast<const PartHead*>((i & 1) ? smem + (size_t)w * stages * kUnitBytes : parts0 + w * part_smem(group, D));
@@ -812,9 +843,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         const bool whole = lead->begin >= c0 && lead->end <= c1;
         const int slot = lead->begin < c0 ? 0 : 1;
         float* dst = a.part + ((size_t)blockIdx.x * 2 + slot) * part_floats(group, D);
-        for (int e = tid; e < group * D; e += WARPS * 32) {
+        for (int e = 2 * tid; e < group * D; e += WARPS * 64) {
             const int head = e / D;
-            // lane i weighs part i (a warp's elements belong to one head)
+            // lane i weighs part i (the 64 elements of a warp belong to one head)
             const bool mine = lane < 2 * WARPS && ((mask >> lane) & 1u);
             const float pm_ = mine ? part_at(lane)->m_run[head] : -INFINITY;
             float top = pm_;
@@ -824,78 +855,74 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             float l = mine ? part_at(lane)->l_run[head] * f : 0.0f;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
-            float acc = 0.0f;
-            for (uint32_t mk = mask; mk; mk &= mk - 1) {
-                const int i = __ffs((int)mk) - 1;
-                acc = fmaf(reinterpret_cast<const float*>(part_at(i) + 1)[e], __shfl_sync(0xffffffffu, f, i), acc);
+            float2 acc = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 2 * WARPS; ++i) {
+                if (!((mask >> i) & 1u)) continue;
+                const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(part_at(i) + 1) + e);
+                const float w = __shfl_sync(0xffffffffu, f, i);
+                acc.x = fmaf(v.x, w, acc.x);
+                acc.y = fmaf(v.y, w, acc.y);
             }
-            if (whole) a.out[((size_t)lead->m * a.n_q + (size_t)lead->h * group) * D + e] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
-            else {
-                dst[e] = acc;
+            if (whole) {
+                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                *reinterpret_cast<__nv_bfloat162*>(a.out + ((size_t)lead->m * a.n_q + (size_t)lead->h * group) * D + e) = __floats2bfloat162_rn(acc.x * inv, acc.y * inv);
+            } else {
+                *reinterpret_cast<float2*>(dst + e) = acc;
                 if (e % D == 0) dst[group * D + 2 * head] = top, dst[group * D + 2 * head + 1] = l;
             }
         }
-        if (!whole) {
-            // the CTA that holds the pair's last unit
-            const long long x = lead->end - 1;
-            int w = (int)(x * workers / units);
-            while (run_begin(units, w + 1, workers) <= x) ++w;
-            while (run_begin(units, w, workers) > x) --w;
-            (slot == 0 ? desc0 : desc1) = make_int2(lead->m * a.n_kv + lead->h, w / WARPS);
+        if (!whole) {  // and the CTA that holds the pair's last unit
+            const int2 d = make_int2(lead->m * a.n_kv + lead->h, runs.owner(lead->end - 1) / WARPS);
+            if (slot == 0) desc0 = d;
+            else desc1 = d;
         }
     }
     if (tid == 0) *reinterpret_cast<int4*>(a.desc + 2 * blockIdx.x) = make_int4(desc0.x, desc0.y, desc1.x, desc1.y);
 }
 
 // Merges the parts of a pair that several CTAs share: CTA (c, head) does nothing unless a pair begins in attention CTA c and goes
-// on behind it.  Eight warps take the parts in turn, a lane D / 32 dims.
+// on behind it.  A thread per dim; a lane weighs one of 32 parts at a time, in every warp alike.
 template <int D>
-__global__ void __launch_bounds__(256) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
-                                                                      __nv_bfloat16* __restrict__ out) {
-    constexpr int CPL = D / 32;
-    __shared__ float red_o[8][D], red_m[8], red_l[8];
+__global__ void __launch_bounds__(D) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
+                                                                    __nv_bfloat16* __restrict__ out) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int c = blockIdx.x, head = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31;
     const int2 own = desc[2 * c + 1];
     if (own.x < 0) return;
     const size_t stride = part_floats(group, D);
-    float top = -INFINITY, l = 0.0f, acc[CPL];
+    const float* base = part + head * D + threadIdx.x;
+    float top = -INFINITY, l = 0.0f, acc = 0.0f;
+    for (int p0 = c; p0 <= own.y; p0 += 32) {
+        // CTA c's part is its second, the others' their first (a CTA that has no unit at all has none)
+        const int p = p0 + lane;
+        const bool in = p <= own.y && (p == c || desc[2 * min(p, own.y)].x == own.x);
+        const size_t at = (size_t)min(p, own.y) * 2 + (p == c ? 1 : 0);
+        const float2 ml = *reinterpret_cast<const float2*>(part + at * stride + group * D + 2 * head);
+        float v[32];
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) acc[e] = 0.0f;
-    for (int p = c + warp; p <= own.y; p += 8) {
-        const int slot = p == c ? 1 : 0;
-        if (p != c && desc[2 * p].x != own.x) continue;
-        const float* src = part + ((size_t)p * 2 + slot) * stride;
-        const float pm = src[group * D + 2 * head], pl = src[group * D + 2 * head + 1];
-        float v[CPL];
+        for (int i = 0; i < 32; ++i) v[i] = p0 + i <= own.y ? base[((size_t)(p0 + i) * 2 + (p0 + i == c ? 1 : 0)) * stride] : 0.0f;
+        const float pm = in ? ml.x : -INFINITY;
+        float n = pm;
 #pragma unroll
-        for (int e = 0; e < CPL; ++e) v[e] = src[head * D + lane * CPL + e];
-        if (pm == -INFINITY) continue;
-        const float n = fmaxf(top, pm), f0 = exp2f(top - n), f1 = exp2f(pm - n);
-        l = fmaf(l, f0, pl * f1);
+        for (int off = 16; off > 0; off >>= 1) n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, off));
+        n = fmaxf(n, top);
+        const float f0 = top == -INFINITY ? 0.0f : ex2(top - n), f = pm == -INFINITY ? 0.0f : ex2(pm - n);
+        float lt = in ? ml.y * f : 0.0f;
 #pragma unroll
-        for (int e = 0; e < CPL; ++e) acc[e] = fmaf(acc[e], f0, v[e] * f1);
+        for (int off = 16; off > 0; off >>= 1) lt += __shfl_xor_sync(0xffffffffu, lt, off);
+        l = fmaf(l, f0, lt);
+        acc *= f0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const float w = __shfl_sync(0xffffffffu, f, i);
+            acc = w > 0.0f ? fmaf(v[i], w, acc) : acc;  // (a part that does not exist may hold anything)
+        }
         top = n;
     }
-#pragma unroll
-    for (int e = 0; e < CPL; ++e) red_o[warp][lane * CPL + e] = acc[e];
-    if (lane == 0) red_m[warp] = top, red_l[warp] = l;
-    __syncthreads();
-    if (threadIdx.x < D) {
-        float t = red_m[0];
-#pragma unroll
-        for (int w = 1; w < 8; ++w) t = fmaxf(t, red_m[w]);
-        float sum = 0.0f, o = 0.0f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-            const float f = red_m[w] == -INFINITY ? 0.0f : exp2f(red_m[w] - t);
-            sum = fmaf(red_l[w], f, sum);
-            o = fmaf(red_o[w][threadIdx.x], f, o);
-        }
-        const int m = own.x / n_kv, h = own.x - m * n_kv;
-        out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(sum > 0.0f ? o / sum : 0.0f);
-    }
+    const int m = own.x / n_kv, h = own.x - m * n_kv;
+    out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -960,7 +987,7 @@ int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a,
         return BITLINEAR_ERR_CUDA;
     }
     cfg.gridDim = dim3((unsigned)ctas, (unsigned)group);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(D);
     cfg.dynamicSmemBytes = 0;
     if (cudaLaunchKernelEx(&cfg, attn_decode_kv8_combine_kernel<D>, (const float*)a.part, (const int2*)a.desc, group, a.n_kv, a.out) != cudaSuccess) {
         cudaGetLastError();
@@ -1039,7 +1066,8 @@ int bitlinear_attention_decode_kv8(const void* q_bf16, const void* k_cache, cons
                                    void* stream) {
     if (kv_dtype != BITLINEAR_KV_INT8 && kv_dtype != BITLINEAR_KV_E4M3) return BITLINEAR_ERR_DTYPE;
     if (M < 0 || M > 65535 || n_seq <= 0 || max_blocks <= 0 || !kv8_dims_ok(n_q_heads, n_kv_heads, head_dim, kv_dtype, n_blocks, block_rows) ||
-        (long long)max_blocks * block_rows > (1ll << 30) || (long long)M * n_kv_heads > 0x7fffffffll || (!seq_ids && n_seq < M))
+        (long long)max_blocks * block_rows > (1ll << 30) || (!seq_ids && n_seq < M) ||
+        (double)M * n_kv_heads * (((double)max_blocks * block_rows + kUnit - 1) / kUnit + 1) > 2147483000.0)
         return BITLINEAR_ERR_SHAPE;
     if (M == 0) return BITLINEAR_OK;
     if (!q_bf16 || !k_cache || !v_cache || !k_scale || !v_scale || !tables || !lengths || !out_bf16) return BITLINEAR_ERR_NULL;
