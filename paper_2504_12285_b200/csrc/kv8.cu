@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 namespace bitlinear {
 
@@ -894,15 +895,18 @@ __global__ void __launch_bounds__(D) attn_decode_kv8_combine_kernel(const float*
     const size_t stride = part_floats(group, D);
     const float* base = part + head * D + threadIdx.x;
     float top = -INFINITY, l = 0.0f, acc = 0.0f;
-    for (int p0 = c; p0 <= own.y; p0 += 32) {
-        // CTA c's part is its second, the others' their first (a CTA that has no unit at all has none)
-        const int p = p0 + lane;
-        const bool in = p <= own.y && (p == c || desc[2 * min(p, own.y)].x == own.x);
-        const size_t at = (size_t)min(p, own.y) * 2 + (p == c ? 1 : 0);
-        const float2 ml = *reinterpret_cast<const float2*>(part + at * stride + group * D + 2 * head);
-        float v[32];
+    // N parts from p0 on; CTA c's part is its second, the others' their first (a CTA that has no unit at all has none)
+    auto round = [&](auto n_tag, int p0) {
+        constexpr int N = decltype(n_tag)::value;
+        const int p = min(p0 + lane, own.y);
+        const bool in = lane < N && p0 + lane <= own.y && (p == c || desc[2 * p].x == own.x);
+        const float2 ml = *reinterpret_cast<const float2*>(part + ((size_t)p * 2 + (p == c ? 1 : 0)) * stride + group * D + 2 * head);
+        float v[N];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = p0 + i <= own.y ? base[((size_t)(p0 + i) * 2 + (p0 + i == c ? 1 : 0)) * stride] : 0.0f;
+        for (int i = 0; i < N; ++i) {  // (asm: all loads of a round are in flight before the first result is used)
+            const int q = min(p0 + i, own.y);
+            asm volatile("ld.global.f32 %0, [%1];" : "=f"(v[i]) : "l"(base + ((size_t)q * 2 + (q == c ? 1 : 0)) * stride));
+        }
         const float pm = in ? ml.x : -INFINITY;
         float n = pm;
 #pragma unroll
@@ -915,12 +919,15 @@ __global__ void __launch_bounds__(D) attn_decode_kv8_combine_kernel(const float*
         l = fmaf(l, f0, lt);
         acc *= f0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < N; ++i) {
             const float w = __shfl_sync(0xffffffffu, f, i);
             acc = w > 0.0f ? fmaf(v[i], w, acc) : acc;  // (a part that does not exist may hold anything)
         }
         top = n;
-    }
+    };
+    if (own.y - c < 4) round(std::integral_constant<int, 4>{}, c);
+    else
+        for (int p0 = c; p0 <= own.y; p0 += 32) round(std::integral_constant<int, 32>{}, p0);
     const int m = own.x / n_kv, h = own.x - m * n_kv;
     out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
 }
