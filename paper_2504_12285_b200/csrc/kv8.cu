@@ -37,26 +37,51 @@ __device__ __forceinline__ float scale_for(double amax) {
     return __int_as_float(min(k + 127, 254) << 23);
 }
 
-// The code nearest to value / scale, ties to even, decided on the quotient in 64 bits: in 32 the quotient's own rounding
-// moves about one code in a million across the middle between two.  int8: the product with the reciprocal decides
-// except next to the middle, where the division itself does.
-__device__ __forceinline__ uint32_t code_int8(double value, double scale, double inv) {
-    double x = value * inv;
-    double c = rint(x);
-    if (fabs(fabs(x - c) - 0.5) < 1e-6) c = rint(__ddiv_rn(value, scale));
-    return (uint32_t)(int)fmin(fmax(c, -127.0), 127.0) & 0xffu;
-}
+// The code nearest to value / scale, ties to even, decided on the quotient in 64 bits: in 32 the rotation's and the quotient's
+// own roundings move about one code in a million across the middle between two.
 // e4m3: the scale is a power of two, so the quotient is exact; it goes to fp32 with the last bit sticky (round to odd),
-// and the conversion to e4m3 then rounds as if it saw all bits
-__device__ __forceinline__ uint32_t code_e4m3(double quotient) {
-    float f = __double2float_rz(quotient);
-    if ((double)f != quotient) f = __int_as_float(__float_as_int(f) | 1);
+// and the conversion to e4m3 then rounds as if it saw all bits.
+template <int KIND>
+__device__ __forceinline__ uint32_t code_of(double value, double scale) {
+    const double x = __ddiv_rn(value, scale);
+    if constexpr (KIND == BITLINEAR_KV_INT8) return (uint32_t)(int)fmin(fmax(rint(x), -127.0), 127.0) & 0xffu;
+    float f = __double2float_rz(x);
+    if ((double)f != x) f = __int_as_float(__float_as_int(f) | 1);
     return (uint32_t)__nv_cvt_float_to_fp8(f, __NV_SATFINITE, __NV_E4M3);
 }
+// The same from an fp32 value and the reciprocal of the scale; false where they cannot tell: next to the middle between two codes.
+// `off` bounds the error of value * inv.  For keys a rotated pair's components are at most sqrt 2 of the block's largest magnitude
+// before the turn, two products and a sum round by 2^-24 each, and that magnitude is at most 127 (448) steps: 6e-5 (1.6e-4) with the
+// reciprocal's and the product's own rounding.  Values come as they are: 2.3e-5 (none, the scale is a power of two).
 template <int KIND>
-__device__ __forceinline__ uint32_t code_of(double value, double scale, double inv) {
-    if constexpr (KIND == BITLINEAR_KV_INT8) return code_int8(value, scale, inv);
-    else return code_e4m3(value * inv);
+__device__ __forceinline__ float quick_error(bool keys) {
+    return KIND == BITLINEAR_KV_INT8 ? (keys ? 1e-4f : 4e-5f) : (keys ? 2e-4f : 0.0f);
+}
+template <int KIND>
+__device__ __forceinline__ bool quick_code(float value, float inv, float off, uint32_t& code) {
+    const float x = value * inv;
+    if constexpr (KIND == BITLINEAR_KV_INT8) {
+        const float c = rintf(x);
+        code = (uint32_t)(int)fminf(fmaxf(c, -127.0f), 127.0f) & 0xffu;
+        return fabsf(x - c) < 0.5f - off;
+    } else {
+        const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(x - off, x + off), __NV_SATFINITE, __NV_E4M3);
+        code = two & 0xffu;
+        return code == two >> 8 && x == x;
+    }
+}
+// The code of a value in fp64 that quick_code could not tell.  int8: the value against the middle next to it, times the scale (exact),
+// instead of a division.
+template <int KIND>
+__device__ __forceinline__ uint32_t close_code(double value, double scale, float inv) {
+    if constexpr (KIND == BITLINEAR_KV_INT8) {
+        const float low = floorf((float)value * inv - 0.25f);  // x is within 0.1 of a middle: the whole number below it
+        const double gap = value - ((double)low + 0.5) * scale;
+        const int c = (int)low + (gap > 0.0 || (gap == 0.0 && ((int)low & 1)) ? 1 : 0);
+        return (uint32_t)min(max(c, -127), 127) & 0xffu;
+    } else {
+        return code_of<KIND>(value, scale);
+    }
 }
 template <int KIND>
 __device__ __forceinline__ double decoded(uint32_t code) {
@@ -82,43 +107,55 @@ struct AppendArgs {
     int kv_ctas;    // CTAs of the key/value part; those behind it rotate q
 };
 
+// eight values of a row: four dims from i4 on and their rotation partners, with the angles' (cos, sin)
+template <int D>
+struct RowValues {
+    float l[4], u[4], c[4], s[4];
+    __device__ __forceinline__ void load(const float* row, int i4) {
+        const float4 lo = *reinterpret_cast<const float4*>(row + i4), hi = *reinterpret_cast<const float4*>(row + i4 + D / 2);
+        l[0] = lo.x, l[1] = lo.y, l[2] = lo.z, l[3] = lo.w;
+        u[0] = hi.x, u[1] = hi.y, u[2] = hi.z, u[3] = hi.w;
+    }
+    __device__ __forceinline__ void load_angles(const float2* table, int pos, int i4) {
+        const float4* cs = reinterpret_cast<const float4*>(table + (size_t)pos * (D / 2) + i4);
+        const float4 c0 = cs[0], c1 = cs[1];
+        c[0] = c0.x, c[1] = c0.z, c[2] = c1.x, c[3] = c1.z;
+        s[0] = c0.y, s[1] = c0.w, s[2] = c1.y, s[3] = c1.w;
+    }
+    // the fp32 operations of the other append calls, in their order
+    __device__ __forceinline__ void turned(float (&x)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] = __fsub_rn(__fmul_rn(l[e], c[e]), __fmul_rn(u[e], s[e]));
+            x[4 + e] = __fadd_rn(__fmul_rn(u[e], c[e]), __fmul_rn(l[e], s[e]));
+        }
+    }
+    // one of them in fp64, where the products are exact
+    __device__ __forceinline__ double exact(int e) const {
+        const int j = e & 3;
+        return e < 4 ? __dsub_rn((double)l[j] * (double)c[j], (double)u[j] * (double)s[j]) : __dadd_rn((double)u[j] * (double)c[j], (double)l[j] * (double)s[j]);
+    }
+};
+
 // Key/value part: one CTA per (tile of tokens, KV head, keys or values).  The tokens of one block stand next to each other in a
 // call; the first of such a run leads it: its CTA finds the run's largest magnitude, settles the block's scale
 // (scale = max(old, needed) where the block has rows in front of the run, else what is needed), brings the earlier rows' codes
 // to the new scale if it grew, and writes the run's codes.  So a block's scale has one writer and no atomics.
-// Rotation in fp64: the products of two floats are exact there, and the quantiser sees one rounding.
+// The result is that of fp64 arithmetic, the work mostly fp32: only values next to the largest, and next to the middle between two
+// codes, are formed again in fp64 (all of it in fp64 took 3.5 times as long for prompts).
 template <int D, int KIND>
-__device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int h, int which) {
-    constexpr int TPR = D / 8;  // threads per row: four dims and their rotation partners each
-    constexpr int ROWS = kAppendThreads / TPR;
-    __shared__ double red[kAppendThreads / 32];
-    __shared__ int first_s[kAppendThreads / 32];
+__device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int block, int h, int which) {
+    constexpr int TPR = D / 8;  // threads per row
+    constexpr int ROWS = kAppendThreads / TPR, WARPS = kAppendThreads / 32;
+    __shared__ float red[WARPS];
+    __shared__ double red_d[WARPS];
+    __shared__ int first_s[WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int sub = tid / TPR, i4 = 4 * (tid % TPR);
-    const int block = a.slots[m0] / a.block_rows;
-    const float* src = which == 0 ? a.k : a.v;
-    // this thread's eight values of token m; false if the token is not of this run (which then ends)
-    auto values = [&](int m, int pos, double (&x)[8]) {
-        const float* row = src + ((size_t)m * a.n_kv + h) * D;
-        const float4 lo = *reinterpret_cast<const float4*>(row + i4), hi = *reinterpret_cast<const float4*>(row + i4 + D / 2);
-        const float l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w};
-        if (which == 0) {
-            const float4* cs = reinterpret_cast<const float4*>(a.table + (size_t)pos * (D / 2) + i4);
-            const float4 c0 = cs[0], c1 = cs[1];
-            const float c[4] = {c0.x, c0.z, c1.x, c1.z}, s[4] = {c0.y, c0.w, c1.y, c1.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[e] = __dsub_rn((double)l[e] * (double)c[e], (double)u[e] * (double)s[e]);
-                x[4 + e] = __dadd_rn((double)u[e] * (double)c[e], (double)l[e] * (double)s[e]);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = (double)l[e], x[4 + e] = (double)u[e];
-        }
-    };
-    // pass 1: the run's end, its first row in the block, its largest magnitude
+    const float* src = (which == 0 ? a.k : a.v) + (size_t)h * D;
+    const size_t row_stride = (size_t)a.n_kv * D;
     int end = m0 + 1;
-    while (end < a.T) {  // 32 tokens at a time, the same in every warp
+    while (end < a.T) {  // the run's end, 32 tokens at a time, the same in every warp
         const int s = end + lane < a.T ? a.slots[end + lane] : -1;
         const unsigned other = __ballot_sync(0xffffffffu, s < 0 || s / a.block_rows != block);
         if (other) {
@@ -127,58 +164,101 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int h, i
         }
         end += 32;
     }
-    double amax = 0.0;
+    RowValues<D> r;
+    float x[8];
+    auto load = [&](int m, int pos) {
+        r.load(src + (size_t)m * row_stride, i4);
+        if (which == 0) {
+            r.load_angles(a.table, pos, i4);
+            r.turned(x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = r.l[e], x[4 + e] = r.u[e];
+        }
+    };
+    // the largest magnitude, in fp32, and the run's first row in the block
+    float top = 0.0f;
     int first = a.block_rows;
+#pragma unroll 2
     for (int m = m0 + sub; m < end; m += ROWS) {
         const int pos = a.positions[m];
         if (pos < 0 || pos >= a.t_max) continue;
-        double x[8];
-        values(m, pos, x);
+        load(m, pos);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmax(amax, fabs(x[e]));
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
         first = min(first, a.slots[m] - block * a.block_rows);
     }
+    const float own_top = top;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-        amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, off));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
         first = min(first, __shfl_xor_sync(0xffffffffu, first, off));
     }
-    if (lane == 0) red[warp] = amax, first_s[warp] = first;
+    if (lane == 0) red[warp] = top, first_s[warp] = first;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kAppendThreads / 32; ++w) amax = fmax(amax, red[w]), first = min(first, first_s[w]);
+    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, red[w]), first = min(first, first_s[w]);
     if (first >= a.block_rows) {  // no token of the run has a place in the table of angles
         __syncthreads();
         return;
     }
+    double amax = (double)top;
+    if (which == 0) {  // keys: the largest in fp64 is among those within the fp32 errors of the largest in fp32
+        amax = 0.0;
+        const float near = top * (1.0f - 1.0f / 524288.0f);
+        if (own_top >= near) {
+            for (int m = m0 + sub; m < end; m += ROWS) {
+                const int pos = a.positions[m];
+                if (pos < 0 || pos >= a.t_max) continue;
+                load(m, pos);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (fabsf(x[e]) >= near) amax = fmax(amax, fabs(r.exact(e)));
+            }
+        }
+        if (__any_sync(0xffffffffu, own_top >= near)) {
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) amax = fmax(amax, __shfl_xor_sync(0xffffffffu, amax, off));
+        }
+        if (lane == 0) red_d[warp] = amax;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) amax = fmax(amax, red_d[w]);
+    }
     float* scale = (which == 0 ? a.k_scale : a.v_scale) + (size_t)block * a.n_kv + h;
     uint8_t* tile = (which == 0 ? a.k_cache : a.v_cache) + ((size_t)block * a.n_kv + h) * a.block_rows * D;
-    const float old = *scale, need = scale_for<KIND>(amax);
+    const float old = first > 0 ? *scale : 0.0f, need = scale_for<KIND>(amax);
     const float now = first > 0 ? fmaxf(old, need) : need;
-    const double s = (double)now, inv = __ddiv_rn(1.0, s);
+    const double s = (double)now;
+    const float inv = __frcp_rn(now), off = quick_error<KIND>(which == 0);
     __syncthreads();  // everyone has read the old scale, and the shared buffers are free
     if (tid == 0) *scale = now;
-    // pass 2: codes
+#pragma unroll 2
     for (int m = m0 + sub; m < end; m += ROWS) {
         const int pos = a.positions[m];
         if (pos < 0 || pos >= a.t_max) continue;
-        double x[8];
-        values(m, pos, x);
-        uint32_t w[2] = {0u, 0u};
+        load(m, pos);
+        uint32_t code[8], unsure = 0u;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e >> 2] |= code_of<KIND>(x[e], s, inv) << (8 * (e & 3));
+        for (int e = 0; e < 8; ++e)
+            if (!quick_code<KIND>(x[e], inv, off, code[e])) unsure |= 1u << e;
+        if (unsure) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((unsure >> e) & 1u) code[e] = close_code<KIND>(which == 0 ? r.exact(e) : (double)x[e], s, inv);
+        }
         uint8_t* dst = tile + (size_t)(a.slots[m] - block * a.block_rows) * D;
-        *reinterpret_cast<uint32_t*>(dst + i4) = w[0];
-        *reinterpret_cast<uint32_t*>(dst + i4 + D / 2) = w[1];
+        *reinterpret_cast<uint32_t*>(dst + i4) = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+        *reinterpret_cast<uint32_t*>(dst + i4 + D / 2) = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
     }
     if (first > 0 && now > old) {
         uint32_t* words = reinterpret_cast<uint32_t*>(tile);
         for (int i = tid; i < first * (D / 4); i += kAppendThreads) {
             const uint32_t w = words[i];
-            uint32_t r = 0u;
+            uint32_t v = 0u;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r |= code_of<KIND>(decoded<KIND>((w >> (8 * e)) & 0xffu) * (double)old, s, inv) << (8 * e);
-            words[i] = r;
+            for (int e = 0; e < 4; ++e) v |= code_of<KIND>(decoded<KIND>((w >> (8 * e)) & 0xffu) * (double)old, s) << (8 * e);
+            words[i] = v;
         }
     }
 }
@@ -187,45 +267,48 @@ template <int D, int KIND>
 __global__ void __launch_bounds__(kAppendThreads) rope_kv8_kernel(const AppendArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int n_slots = a.n_blocks * a.block_rows;
     if ((int)blockIdx.x < a.kv_ctas) {
+        const int n_slots = a.n_blocks * a.block_rows, lane = threadIdx.x & 31;
         const int item = blockIdx.x % (2 * a.n_kv), t0 = (int)(blockIdx.x / (2 * a.n_kv)) * a.tile;
-        for (int m = t0; m < min(t0 + a.tile, a.T); ++m) {
-            const int s = a.slots[m], p = m > 0 ? a.slots[m - 1] : -1;
-            if (s < 0 || s >= n_slots) continue;
-            if (p >= 0 && p / a.block_rows == s / a.block_rows) continue;  // not the first of its run
-            append_run<D, KIND>(a, m, item >> 1, item & 1);
+        // the blocks of the tile's tokens (at most 31) and of the one in front, one per lane; a token leads a run if its block is another
+        // than that of the token in front
+        const int m = t0 - 1 + lane;
+        const int s = m >= 0 && m < a.T && lane <= a.tile ? a.slots[m] : -1;
+        const int block = s >= 0 && s < n_slots ? s / a.block_rows : -1;
+        const int front = __shfl_up_sync(0xffffffffu, block, 1);
+        unsigned leads = __ballot_sync(0xffffffffu, lane > 0 && block >= 0 && block != front);
+        for (; leads; leads &= leads - 1) {
+            const int at = __ffs((int)leads) - 1;
+            append_run<D, KIND>(a, t0 - 1 + at, __shfl_sync(0xffffffffu, block, at), item >> 1, item & 1);
         }
     } else {
-        // rotated queries, four pairs per thread; the same fp32 operations in the same order as the other append calls
+        // rotated queries, a token at a time; a thread's dims are the same in every head that it meets, so the angles are read once
         constexpr int UNITS = D / 8;
-        const long long n = (long long)a.T * a.n_q * UNITS, step = (long long)(gridDim.x - a.kv_ctas) * kAppendThreads;
-        for (long long u = (long long)(blockIdx.x - a.kv_ctas) * kAppendThreads + threadIdx.x; u < n; u += step) {
-            const long long mh = u / UNITS;
-            const int i4 = 4 * (int)(u - mh * UNITS), m = (int)(mh / a.n_q), pos = a.positions[m];
-            const float* row = a.q + mh * D;
-            uint2 lo2 = make_uint2(0u, 0u), hi2 = lo2;  // a row without a position: zeros
-            if (pos >= 0 && pos < a.t_max) {
-                const float4 lo = *reinterpret_cast<const float4*>(row + i4), hi = *reinterpret_cast<const float4*>(row + i4 + D / 2);
-                const float4* cs = reinterpret_cast<const float4*>(a.table + (size_t)pos * (D / 2) + i4);
-                const float4 c0 = cs[0], c1 = cs[1];
-                const float l[4] = {lo.x, lo.y, lo.z, lo.w}, r[4] = {hi.x, hi.y, hi.z, hi.w};
-                const float c[4] = {c0.x, c0.z, c1.x, c1.z}, s[4] = {c0.y, c0.w, c1.y, c1.w};
-                float ol[4], oh[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    ol[e] = __fsub_rn(__fmul_rn(l[e], c[e]), __fmul_rn(r[e], s[e]));
-                    oh[e] = __fadd_rn(__fmul_rn(r[e], c[e]), __fmul_rn(l[e], s[e]));
+        static_assert(kAppendThreads % UNITS == 0, "a thread keeps its dims from head to head");
+        const int i4 = 4 * (threadIdx.x % UNITS), units = a.n_q * UNITS;
+        for (int m = blockIdx.x - a.kv_ctas; m < a.T; m += gridDim.x - a.kv_ctas) {
+            const int pos = a.positions[m];
+            const bool placed = pos >= 0 && pos < a.t_max;  // a row without a position: zeros
+            RowValues<D> r;
+            if (placed) r.load_angles(a.table, pos, i4);
+#pragma unroll 3
+            for (int u = threadIdx.x; u < units; u += kAppendThreads) {
+                const size_t row = ((size_t)m * a.n_q + u / UNITS) * D;
+                uint2 lo2 = make_uint2(0u, 0u), hi2 = lo2;
+                if (placed) {
+                    float x[8];
+                    r.load(a.q + row, i4);
+                    r.turned(x);
+                    auto pair = [](float p, float q) {
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(p, q);
+                        return *reinterpret_cast<const uint32_t*>(&b);
+                    };
+                    lo2 = make_uint2(pair(x[0], x[1]), pair(x[2], x[3]));
+                    hi2 = make_uint2(pair(x[4], x[5]), pair(x[6], x[7]));
                 }
-                auto pair = [](float x, float y) {
-                    const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
-                    return *reinterpret_cast<const uint32_t*>(&b);
-                };
-                lo2 = make_uint2(pair(ol[0], ol[1]), pair(ol[2], ol[3]));
-                hi2 = make_uint2(pair(oh[0], oh[1]), pair(oh[2], oh[3]));
+                *reinterpret_cast<uint2*>(a.q_out + row + i4) = lo2;
+                *reinterpret_cast<uint2*>(a.q_out + row + i4 + D / 2) = hi2;
             }
-            *reinterpret_cast<uint2*>(a.q_out + mh * D + i4) = lo2;
-            *reinterpret_cast<uint2*>(a.q_out + mh * D + i4 + D / 2) = hi2;
         }
     }
 }
@@ -1037,8 +1120,7 @@ int bitlinear_rope_kv8(const float* q, const float* k, const float* v, const int
     // a CTA per token and head while that fits the GPU a few times over, else per tile of tokens (most of them lead no run)
     a.tile = (long long)T * 2 * n_kv_heads <= 64ll * sm_count ? 1 : 16;
     const long long kv_ctas = (long long)((T + a.tile - 1) / a.tile) * 2 * n_kv_heads;
-    const long long q_units = (long long)T * n_q_heads * (head_dim / 8);
-    const long long q_ctas = std::min((q_units + kAppendThreads - 1) / kAppendThreads, 64ll * sm_count);
+    const long long q_ctas = std::min((long long)T, 16ll * sm_count);
     if (kv_ctas + q_ctas > 0x7fffffffll) return BITLINEAR_ERR_SHAPE;
     a.kv_ctas = (int)kv_ctas;
     cudaLaunchAttribute attr[1];
