@@ -138,7 +138,7 @@ def _ptr(t: torch.Tensor | None) -> int | None:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())  # torch.cuda.current_stream().cuda_stream without its 2 us
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
@@ -637,27 +637,33 @@ def _kvdt(dtype) -> int:
     raise TypeError("8-bit caches must be int8 or float8_e4m3fn")
 
 
-def _same_device(first: torch.Tensor, *others) -> None:
-    """Every tensor on the current device: the library launches there and takes pointers as they come."""
-    index = torch.cuda.current_device()
-    for t in (first, *others):
-        if t is not None and t.device.index != index:
-            raise ValueError(f"tensors must be on the current device, cuda:{index}; got {t.device}")
+def _tensors(*given) -> None:
+    """Each (tensor or None, dtype, name): contiguous, of that type and on the current device, where the library launches - it takes
+    pointers as they come."""
+    index = -1
+    for t, dtype, name in given:
+        if t is None:
+            continue
+        at = t.get_device()
+        if at < 0 or t.dtype != dtype or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous CUDA tensor of {dtype}")
+        if at != index:
+            index = torch._C._cuda_getDevice()
+            if at != index:
+                raise ValueError(f"{name} is on cuda:{at}, the current device is cuda:{index}")
 
 
-def _rows(t: torch.Tensor | None, n: int, dtype, name: str) -> None:
-    if t is not None and (_dev(t, dtype, name).dim() != 1 or t.shape[0] != n):
-        raise ValueError(f"{name} must have shape ({n},)")
+def _shape(t, shape, name: str) -> None:
+    if t is not None and t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
 
 
 def _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads: int, head_dim: int):
     """(kv_dtype, n_blocks, block_rows) of an 8-bit cache: codes [n_blocks, n_kv, block_rows, D], scales [n_blocks, n_kv]."""
     kind = _kvdt(k_cache.dtype)
-    _dev(k_cache, k_cache.dtype, "k_cache"), _dev(v_cache, k_cache.dtype, "v_cache")
     shape = k_cache.shape
-    if v_cache.shape != shape or len(shape) != 4 or shape[1] != n_kv_heads or shape[3] != head_dim:
+    if len(shape) != 4 or shape[1] != n_kv_heads or shape[3] != head_dim or v_cache.shape != shape:
         raise ValueError(f"caches must both be [n_blocks, {n_kv_heads}, block_rows, {head_dim}]")
-    _dev(k_scale, torch.float32, "k_scale"), _dev(v_scale, torch.float32, "v_scale")
     if k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
         raise ValueError(f"scales must both be [{shape[0]}, {n_kv_heads}]")
     return kind, shape[0], shape[2]
@@ -667,27 +673,29 @@ def bitlinear_block_tables(lengths, new_tokens, tables, free_blocks, n_free, blo
     """One step's bookkeeping of a paged cache: lengths, new_tokens int32 [R] (negative: finished), tables int32 [R, max_blocks] and
     free_blocks int32 [n_blocks] updated in place, n_free int32 [1] -> (lengths_out [R], n_free_out [1], served [R], cu_tokens
     [R + 1], seq_ids, positions, row_lengths, slots [t_cap]), all int32.  lengths_out / n_free_out may be lengths / n_free."""
+    i32 = torch.int32
+    _tensors((lengths, i32, "lengths"), (new_tokens, i32, "new_tokens"), (tables, i32, "tables"), (free_blocks, i32, "free_blocks"), (n_free, i32, "n_free"),
+             (lengths_out, i32, "lengths_out"), (n_free_out, i32, "n_free_out"))
     if tables.dim() != 2 or free_blocks.dim() != 1 or t_cap < 0:
         raise ValueError("tables must be [R, max_blocks], free_blocks [n_blocks], t_cap not negative")
     R, max_blocks = tables.shape
-    _dev(tables, torch.int32, "tables"), _dev(free_blocks, torch.int32, "free_blocks")
-    _rows(lengths, R, torch.int32, "lengths"), _rows(new_tokens, R, torch.int32, "new_tokens"), _rows(n_free, 1, torch.int32, "n_free")
-    _rows(lengths_out, R, torch.int32, "lengths_out"), _rows(n_free_out, 1, torch.int32, "n_free_out")
-    _same_device(lengths, new_tokens, tables, free_blocks, n_free, lengths_out, n_free_out)
-    # one buffer for what is returned: four columns of tokens (16-byte aligned), then the requests' rows
-    cap, per = (t_cap + 3) // 4 * 4, (R + 4) // 4 * 4
-    out = torch.empty(4 * cap + 3 * per + 4, dtype=torch.int32, device=lengths.device)
-    columns = [out[i * cap:i * cap + t_cap] for i in range(4)]
-    served, cu = out[4 * cap:4 * cap + R], out[4 * cap + per:4 * cap + per + R + 1]
+    _shape(lengths, (R,), "lengths"), _shape(new_tokens, (R,), "new_tokens"), _shape(n_free, (1,), "n_free")
+    _shape(lengths_out, (R,), "lengths_out"), _shape(n_free_out, (1,), "n_free_out")
+    # one buffer for what is returned: four columns of tokens (each 16-byte aligned), then the requests' rows
+    pad = -t_cap % 4
+    sizes = ([t_cap, pad] if pad else [t_cap]) * 4 + [R, R + 1, R, 1]
+    parts = lengths.new_empty(sum(sizes)).split_with_sizes(sizes)
+    served, cu, own_lengths, own_free = parts[-4:]
+    seq_ids, positions, row_lengths, slots = parts[:8:2] if pad else parts[:4]
     if lengths_out is None:
-        lengths_out = out[4 * cap + 2 * per:4 * cap + 2 * per + R]
+        lengths_out = own_lengths
     if n_free_out is None:
-        n_free_out = out[4 * cap + 3 * per:4 * cap + 3 * per + 1]
-    rc = lib().bitlinear_block_tables(_ptr(lengths), _ptr(new_tokens), R, _ptr(tables), max_blocks, _ptr(free_blocks), _ptr(n_free),
-                                      free_blocks.shape[0], block_rows, t_cap, _ptr(lengths_out), _ptr(n_free_out), _ptr(served), _ptr(cu),
-                                      *[_ptr(c) for c in columns], _stream())
+        n_free_out = own_free
+    rc = lib().bitlinear_block_tables(lengths.data_ptr(), new_tokens.data_ptr(), R, tables.data_ptr(), max_blocks, free_blocks.data_ptr(), n_free.data_ptr(),
+                                      free_blocks.shape[0], block_rows, t_cap, lengths_out.data_ptr(), n_free_out.data_ptr(), served.data_ptr(),
+                                      cu.data_ptr(), seq_ids.data_ptr(), positions.data_ptr(), row_lengths.data_ptr(), slots.data_ptr(), _stream())
     _check(rc, "bitlinear_block_tables")
-    return (lengths_out, n_free_out, served, cu, *columns)
+    return lengths_out, n_free_out, served, cu, seq_ids, positions, row_lengths, slots
 
 
 def bitlinear_rope_kv8(q, k, v, positions, slots, rope_table, k_cache, v_cache, k_scale, v_scale, n_q_heads: int, n_kv_heads: int, head_dim: int,
@@ -696,20 +704,20 @@ def bitlinear_rope_kv8(q, k, v, positions, slots, rope_table, k_cache, v_cache, 
     (codes [n_blocks, n_kv, block_rows, D], scales [n_blocks, n_kv]) at `slots` (int32 [T])."""
     T = q.shape[0]
     kind, n_blocks, block_rows = _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads, head_dim)
-    for t, heads, name in ((q, n_q_heads, "q"), (k, n_kv_heads, "k"), (v, n_kv_heads, "v")):
-        if tuple(_dev(t, torch.float32, name).shape) != (T, heads * head_dim):
-            raise ValueError(f"{name} must be [{T}, {heads * head_dim}]")
-    _rows(positions, T, torch.int32, "positions"), _rows(slots, T, torch.int32, "slots"), _dev(rope_table, torch.float32, "rope_table")
-    if rope_table.dim() != 3 or tuple(rope_table.shape[1:]) != (head_dim // 2, 2):
-        raise ValueError(f"rope_table must be [t_max, {head_dim // 2}, 2]")
+    f32, i32 = torch.float32, torch.int32
     if q_out is None:
         q_out = torch.empty(T, n_q_heads * head_dim, dtype=torch.bfloat16, device=q.device)
-    elif _dev(q_out, torch.bfloat16, "q_out").shape != q.shape:
-        raise ValueError(f"q_out must be {tuple(q.shape)}")
-    _same_device(q, k, v, positions, slots, rope_table, k_cache, v_cache, k_scale, v_scale, q_out)
-    rc = lib().bitlinear_rope_kv8(_ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(slots), _ptr(rope_table), T, rope_table.shape[0], n_q_heads,
-                                  n_kv_heads, head_dim, _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), kind, n_blocks,
-                                  block_rows, _stream())
+    _tensors((q, f32, "q"), (k, f32, "k"), (v, f32, "v"), (positions, i32, "positions"), (slots, i32, "slots"), (rope_table, f32, "rope_table"),
+             (k_cache, k_cache.dtype, "k_cache"), (v_cache, k_cache.dtype, "v_cache"), (k_scale, f32, "k_scale"), (v_scale, f32, "v_scale"),
+             (q_out, torch.bfloat16, "q_out"))
+    kv = (T, n_kv_heads * head_dim)
+    _shape(q, (T, n_q_heads * head_dim), "q"), _shape(k, kv, "k"), _shape(v, kv, "v"), _shape(q_out, q.shape, "q_out")
+    _shape(positions, (T,), "positions"), _shape(slots, (T,), "slots")
+    if rope_table.dim() != 3 or rope_table.shape[1] != head_dim // 2 or rope_table.shape[2] != 2:
+        raise ValueError(f"rope_table must be [t_max, {head_dim // 2}, 2]")
+    rc = lib().bitlinear_rope_kv8(q.data_ptr(), k.data_ptr(), v.data_ptr(), positions.data_ptr(), slots.data_ptr(), rope_table.data_ptr(), T,
+                                  rope_table.shape[0], n_q_heads, n_kv_heads, head_dim, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                                  k_scale.data_ptr(), v_scale.data_ptr(), kind, n_blocks, block_rows, _stream())
     _check(rc, "bitlinear_rope_kv8")
     return q_out
 
@@ -724,21 +732,20 @@ def bitlinear_attention_decode_kv8(q, k_cache, v_cache, k_scale, v_scale, tables
     `tables` (int32 [n_seq, max_blocks]) names -> bf16 [M, n_q * D]."""
     M = q.shape[0]
     kind, n_blocks, block_rows = _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads, head_dim)
-    if tuple(_dev(q, torch.bfloat16, "q").shape) != (M, n_q_heads * head_dim):
-        raise ValueError(f"q must be [{M}, {n_q_heads * head_dim}]")
-    if _dev(tables, torch.int32, "tables").dim() != 2:
-        raise ValueError("tables must be [n_seq, max_blocks]")
-    _rows(lengths, M, torch.int32, "lengths"), _rows(seq_ids, M, torch.int32, "seq_ids")
     if out is None:
-        out = torch.empty(M, n_q_heads * head_dim, dtype=torch.bfloat16, device=q.device)
-    elif _dev(out, torch.bfloat16, "out").shape != q.shape:
-        raise ValueError(f"out must be {tuple(q.shape)}")
+        out = torch.empty_like(q)
     if ws is None:
         ws = _workspace(bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), q.device)
-    _same_device(q, k_cache, v_cache, k_scale, v_scale, tables, lengths, seq_ids, out, _dev(ws, torch.uint8, "ws"))
-    rc = lib().bitlinear_attention_decode_kv8(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(tables), _ptr(lengths),
-                                              _ptr(seq_ids), M, n_q_heads, n_kv_heads, head_dim, kind, n_blocks, block_rows, tables.shape[0],
-                                              tables.shape[1], _ptr(out), _ptr(ws), ws.numel(), _stream())
+    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    _tensors((q, bf16, "q"), (k_cache, k_cache.dtype, "k_cache"), (v_cache, k_cache.dtype, "v_cache"), (k_scale, f32, "k_scale"), (v_scale, f32, "v_scale"),
+             (tables, i32, "tables"), (lengths, i32, "lengths"), (seq_ids, i32, "seq_ids"), (out, bf16, "out"), (ws, torch.uint8, "ws"))
+    _shape(q, (M, n_q_heads * head_dim), "q"), _shape(out, q.shape, "out"), _shape(lengths, (M,), "lengths"), _shape(seq_ids, (M,), "seq_ids")
+    if tables.dim() != 2:
+        raise ValueError("tables must be [n_seq, max_blocks]")
+    n_seq, max_blocks = tables.shape
+    rc = lib().bitlinear_attention_decode_kv8(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), tables.data_ptr(),
+                                              lengths.data_ptr(), _ptr(seq_ids), M, n_q_heads, n_kv_heads, head_dim, kind, n_blocks, block_rows, n_seq,
+                                              max_blocks, out.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
     _check(rc, "bitlinear_attention_decode_kv8")
     return out
 
@@ -752,16 +759,17 @@ def bitlinear_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=
     stride = logits.stride(0) if M > 1 else V
     if (V > 1 and logits.stride(1) != 1) or stride < V:
         raise ValueError("the rows of logits must be contiguous and must not overlap")
-    _rows(u, M, torch.float32, "u"), _rows(temperature, M, torch.float32, "temperature"), _rows(top_k, M, torch.int32, "top_k")
-    _rows(top_p, M, torch.float32, "top_p"), _rows(min_p, M, torch.float32, "min_p")
-    _rows(ids, M, torch.int32, "ids"), _rows(logprobs, M, torch.float32, "logprobs")
+    f32, i32, rows = torch.float32, torch.int32, (M,)
     if ids is None:
-        ids = torch.empty(M, dtype=torch.int32, device=logits.device)
+        ids = torch.empty(M, dtype=i32, device=logits.device)
     if logprobs is None:
-        logprobs = torch.empty(M, dtype=torch.float32, device=logits.device)
-    _same_device(logits, u, temperature, top_k, top_p, min_p, ids, logprobs)
-    rc = lib().bitlinear_sample(_ptr(logits), F32 if logits.dtype == torch.float32 else BF16, M, V, stride, _ptr(u), _ptr(temperature),
-                                _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(ids), _ptr(logprobs), _stream())
+        logprobs = torch.empty(M, dtype=f32, device=logits.device)
+    _tensors((logits[:1, :1], logits.dtype, "logits"), (u, f32, "u"), (temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"),
+             (min_p, f32, "min_p"), (ids, i32, "ids"), (logprobs, f32, "logprobs"))
+    for t, name in ((u, "u"), (temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p"), (ids, "ids"), (logprobs, "logprobs")):
+        _shape(t, rows, name)
+    rc = lib().bitlinear_sample(logits.data_ptr(), F32 if logits.dtype == f32 else BF16, M, V, stride, u.data_ptr(), _ptr(temperature), _ptr(top_k),
+                                _ptr(top_p), _ptr(min_p), ids.data_ptr(), logprobs.data_ptr(), _stream())
     _check(rc, "bitlinear_sample")
     return ids, logprobs
 
