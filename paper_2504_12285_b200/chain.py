@@ -74,6 +74,32 @@ class DecodeChain:
         return self.h_mid
 
 
+def _token_calls(b, layers, rms_eps: float, dev):
+    """Per layer the four batched BitLinear calls (q/k/v, o, gate/up, down) of a decoded token on the buffers of b, each with its
+    workspace: lists of (ProblemBatch, workspace)."""
+    calls = []
+    for li, layer in enumerate(layers):
+        def item(name, x, y, step=None):
+            packed, s_w, gain = layer[name]
+            return (x, gain, packed, s_w, y) if step is None else (x, gain, packed, s_w, y, step)
+        res_in = None if li == 0 else (bl.X_RESIDUAL, b.dn, b.h_in, 0, 0)
+        x_qkv = b.h_in if li == 0 else b.h_mid
+        res_mid = (bl.X_RESIDUAL, b.o, b.h_mid, 0, 0)
+        relu2 = (bl.X_RELU2, b.u, None, 0, 0)
+        groups = [[item("q", x_qkv, b.q, res_in), item("k", x_qkv, b.k, res_in), item("v", x_qkv, b.v, res_in)],
+                  [item("o", b.attn, b.o)],
+                  [item("gate", b.h_in, b.g, res_mid), item("up", b.h_in, b.u, res_mid)],
+                  [item("down", b.g, b.dn, relu2)]]
+        per_layer = []
+        for grp in groups:
+            batch = bl.ProblemBatch(grp, rms_eps)
+            ws = torch.empty(batch.workspace_bytes(), dtype=torch.uint8, device=dev)
+            bl.bitlinear_forward_batch(batch, ws)  # uploads the plan; results are overwritten by step()
+            per_layer.append((batch, ws))
+        calls.append(per_layer)
+    return calls
+
+
 class DecodeStep:
     """One whole decoded token for M sequences: embedding gather, per layer {q/k/v BitLinear, rotary embedding + cache
     append, grouped-query attention over the cache, o BitLinear, gate/up BitLinear, down BitLinear} with the residual
@@ -107,26 +133,7 @@ class DecodeStep:
         self.lengths = torch.ones(M, dtype=torch.int32, device=dev)     # cache rows attended to: positions + 1
         self.attn_ws = torch.empty(bl.bitlinear_attention_workspace_bytes(M, n_q_heads, n_kv_heads, head_dim, t_max),
                                    dtype=torch.uint8, device=dev)
-        self.calls = []
-        for li, layer in enumerate(layers):
-            def item(name, x, y, step=None):
-                packed, s_w, gain = layer[name]
-                return (x, gain, packed, s_w, y) if step is None else (x, gain, packed, s_w, y, step)
-            res_in = None if li == 0 else (bl.X_RESIDUAL, self.dn, self.h_in, 0, 0)
-            x_qkv = self.h_in if li == 0 else self.h_mid
-            res_mid = (bl.X_RESIDUAL, self.o, self.h_mid, 0, 0)
-            relu2 = (bl.X_RELU2, self.u, None, 0, 0)
-            groups = [[item("q", x_qkv, self.q, res_in), item("k", x_qkv, self.k, res_in), item("v", x_qkv, self.v, res_in)],
-                      [item("o", self.attn, self.o)],
-                      [item("gate", self.h_in, self.g, res_mid), item("up", self.h_in, self.u, res_mid)],
-                      [item("down", self.g, self.dn, relu2)]]
-            per_layer = []
-            for grp in groups:
-                batch = bl.ProblemBatch(grp, rms_eps)
-                ws = torch.empty(batch.workspace_bytes(), dtype=torch.uint8, device=dev)
-                bl.bitlinear_forward_batch(batch, ws)  # uploads the plan; results are overwritten by step()
-                per_layer.append((batch, ws))
-            self.calls.append(per_layer)
+        self.calls = _token_calls(self, layers, rms_eps, dev)
         torch.cuda.synchronize(dev)
 
     @property
@@ -177,6 +184,90 @@ class DecodeStep:
         """Replay the recorded step on the current ids_buf / positions / lengths -> logits fp32 [M, V]."""
         self.graph.replay()
         return self.logits
+
+
+class PagedDecodeStep:
+    """Decoded tokens of many requests at once over a paged 8-bit cache: block tables from the requests' lengths, embedding gather, per layer
+    {q/k/v BitLinear, rotary embedding + append, attention, o, gate/up, down}, output head, and the draw of the next tokens.
+
+    A step carries up to `rows` tokens: new_tokens[p] of the request in place p (more than one for a prompt or for drafted tokens, none
+    for an idle place, -1 for one that has finished and gives its blocks back), in the order of the places."""
+
+    def __init__(self, layers, embedding: torch.Tensor, rows: int, places: int, n_blocks: int, block_rows: int, max_blocks: int, hidden: int, ffn: int,
+                 n_q_heads: int, n_kv_heads: int, head_dim: int, kv_dtype=torch.int8, rms_eps: float = 1e-5, rope_base: float = 500000.0,
+                 device="cuda:0"):
+        """layers, embedding: as for DecodeStep; rows at most 16 (the output head's limit); kv_dtype: torch.int8 or torch.float8_e4m3fn."""
+        dev = torch.device(device)
+        self.rows, self.dims, self.block_rows, self.table = rows, (n_q_heads, n_kv_heads, head_dim), block_rows, embedding
+        kv = n_kv_heads * head_dim
+        f32 = dict(dtype=torch.float32, device=dev)
+        bf = dict(dtype=torch.bfloat16, device=dev)
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.rope_table = bl.bitlinear_rope_table(head_dim, max_blocks * block_rows, rope_base, device=dev)
+        self.h_in, self.h_mid = torch.zeros(rows, hidden, **bf), torch.zeros(rows, hidden, **bf)
+        self.q, self.k, self.v = torch.empty(rows, hidden, **f32), torch.empty(rows, kv, **f32), torch.empty(rows, kv, **f32)
+        self.q_rot, self.attn = torch.empty(rows, hidden, **bf), torch.empty(rows, hidden, **bf)
+        self.o = torch.empty(rows, hidden, **f32)
+        self.g, self.u = torch.empty(rows, ffn, **f32), torch.empty(rows, ffn, **f32)
+        self.dn = torch.empty(rows, hidden, **f32)
+        self.logits = torch.empty(rows, embedding.shape[0], **f32)
+        # the cache of every layer, and the bookkeeping that all layers share
+        pool = (n_blocks, n_kv_heads, block_rows, head_dim)
+        self.cache = [(torch.zeros(pool, dtype=torch.uint8, device=dev).view(kv_dtype), torch.zeros(pool, dtype=torch.uint8, device=dev).view(kv_dtype),
+                       torch.zeros(pool[:2], **f32), torch.zeros(pool[:2], **f32)) for _ in layers]
+        self.lengths, self.new_tokens = torch.zeros(places, **i32), torch.zeros(places, **i32)
+        self.tables = torch.full((places, max_blocks), -1, **i32)
+        self.free_blocks, self.n_free = torch.arange(n_blocks, **i32), torch.full((1,), n_blocks, **i32)
+        # how each place draws its tokens: temperature (0: the likeliest), top_k (0: off), top_p (1: off), min_p (0: off)
+        self.temperature, self.top_k = torch.ones(places, **f32), torch.zeros(places, **i32)
+        self.top_p, self.min_p = torch.ones(places, **f32), torch.zeros(places, **f32)
+        self.attn_ws = torch.empty(bl.bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), dtype=torch.uint8, device=dev)
+        self.ids, self.logprobs = torch.zeros(rows, **i32), torch.zeros(rows, **f32)
+        self.calls = _token_calls(self, layers, rms_eps, dev)
+        torch.cuda.synchronize(dev)
+
+    def step(self, token_ids: torch.Tensor, u: torch.Tensor):
+        """token_ids: int32 [rows] (device), the tokens of this step in the order of the places; u: fp32 [rows], a random number for each row.
+        -> (ids int32 [rows], logprobs fp32 [rows]): the token drawn behind each row; the last row of place p is row
+        cu_tokens[p + 1] - 1, and rows from cu_tokens[-1] on mean nothing.  served[p] is 0 where the pool or the rows did not suffice
+        and the place's tokens were left out."""
+        n_q, n_kv, hd = self.dims
+        (_, _, self.served, self.cu_tokens, self.seq_ids, self.positions, self.row_lengths, self.slots) = bl.bitlinear_block_tables(
+            self.lengths, self.new_tokens, self.tables, self.free_blocks, self.n_free, self.block_rows, self.rows, lengths_out=self.lengths,
+            n_free_out=self.n_free)
+        bl.bitlinear_embed(token_ids, self.table, out=self.h_in)
+        for (qkv, o, gu, down), cache in zip(self.calls, self.cache):
+            bl.bitlinear_forward_batch(*qkv, reuse_plan=True)
+            bl.bitlinear_rope_kv8(self.q, self.k, self.v, self.positions, self.slots, self.rope_table, *cache, n_q, n_kv, hd, q_out=self.q_rot)
+            bl.bitlinear_attention_decode_kv8(self.q_rot, *cache, self.tables, self.row_lengths, n_q, n_kv, hd, seq_ids=self.seq_ids, out=self.attn,
+                                              ws=self.attn_ws)
+            for batch, ws in (o, gu, down):
+                bl.bitlinear_forward_batch(batch, ws, reuse_plan=True)
+        bl.bitlinear_glue_residual_add(self.h_mid, self.dn)  # the last layer's residual
+        bl.bitlinear_lm_head(self.h_mid, self.table, out=self.logits)
+        place = self.seq_ids.clamp(min=0)
+        return bl.bitlinear_sample(self.logits, u, *(x.index_select(0, place) for x in (self.temperature, self.top_k, self.top_p, self.min_p)),
+                                   ids=self.ids, logprobs=self.logprobs)
+
+    def capture(self) -> None:
+        """Record the launches of step() once into a CUDA graph; step_graph() replays them on the current contents of new_tokens, token_buf and
+        u_buf.  Call it before the first token: the recording's own run places nothing."""
+        dev = self.h_in.device
+        self.token_buf, self.u_buf = torch.zeros(self.rows, dtype=torch.int32, device=dev), torch.zeros(self.rows, device=dev)
+        self.new_tokens.zero_()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            self.step(self.token_buf, self.u_buf)  # every kernel has run once outside the recording
+            self.graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(self.graph, stream=side):
+                self.step(self.token_buf, self.u_buf)
+        torch.cuda.current_stream().wait_stream(side)
+
+    def step_graph(self):
+        """Replay the recorded step -> (ids, logprobs) as step()."""
+        self.graph.replay()
+        return self.ids, self.logprobs
 
 
 class PersistentChain:

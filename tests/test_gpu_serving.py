@@ -551,6 +551,93 @@ def test_operators_in_a_recorded_graph_and_on_another_stream():
     check_attention(out, q, codes, scales, tables, [max(1, n - 14) for n in lengths], n_q, n_kv, D, kind)
 
 
+def small_layers(n_layers, H, F, kv, seed):
+    layers = []
+    for li in range(n_layers):
+        layer = {}
+        for i, (name, n, k) in enumerate((("q", H, H), ("k", kv, H), ("v", kv, H), ("o", H, H), ("gate", F, H), ("up", F, H), ("down", H, F))):
+            packed, s_w = bl.bitlinear_pack_weights(wl.latent_weights(n, k, seed + 10 * li + i).to(DEV), wl.WEIGHT_EPS)
+            layer[name] = (packed, s_w, wl.gain_random(k, seed + 100 + 10 * li + i).to(DEV))
+        layers.append(layer)
+    return layers
+
+
+def paged_step(kv_dtype, rows=6, places=4, n_blocks=14, layers=2):
+    from paper_2504_12285_b200 import chain as gpu_chain
+
+    H, F, n_q, n_kv, hd, V = 256, 512, 4, 2, 64, 500
+    table = (torch.randn(V, H, generator=torch.Generator().manual_seed(50)) * 0.3).to(torch.bfloat16).to(DEV)
+    return gpu_chain.PagedDecodeStep(small_layers(layers, H, F, n_kv * hd, 8700), table, rows, places, n_blocks, 16, 5, H, F, n_q, n_kv, hd, kv_dtype, wl.RMS_EPS,
+                                     device=DEV), table
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_paged_decode_step_stage_by_stage(kind):
+    """Requests of different lengths through PagedDecodeStep; the serving stages of a step against the oracle applied to the
+    values the GPU fed into them."""
+    st, table = paged_step(DTYPE[kind], layers=1)
+    n_q, n_kv, hd = st.dims
+    gen = torch.Generator().manual_seed(60)
+    st.temperature.copy_(torch.tensor([0.0, 0.7, 1.0, 1.5]))
+    st.top_k.copy_(torch.tensor([0, 20, 0, 5], dtype=torch.int32))
+    st.top_p.copy_(torch.tensor([1.0, 1.0, 0.8, 0.95]))
+    state = [host(t).copy() for t in (st.lengths, st.tables, st.free_blocks)] + [int(st.n_free[0])]
+    pool = [host(t).copy() for t in st.cache[0]]
+    tab = host(st.rope_table)
+    for new in ([5, 1, 0, 0], [1, 1, 4, 0], [1, 1, 1, 1], [-1, 2, 1, 1], [6, 0, 0, 0], [3, 1, 1, 2]):
+        st.new_tokens.copy_(torch.tensor(new, dtype=torch.int32))
+        ids = torch.randint(0, 500, (6,), generator=gen, dtype=torch.int32)
+        u = torch.rand(6, generator=gen)
+        got_ids, logp = st.step(ids.to(DEV), u.to(DEV))
+        torch.cuda.synchronize()
+        assert bl.bitlinear_poll_status() == 0
+        want = sv.block_tables(state[0], new, state[1], state[2], state[3], 16, 6)
+        state = [want["lengths"], want["tables"], want["free_blocks"], want["n_free"]]
+        for name, t in (("lengths", st.lengths), ("tables", st.tables), ("free_blocks", st.free_blocks), ("served", st.served), ("cu_tokens", st.cu_tokens),
+                        ("slots", st.slots), ("positions", st.positions)):
+            assert np.array_equal(host(t), want[name]), name
+        at = np.maximum(want["positions"], 0)
+        sv.append8(sv.rotate(host(st.k).reshape(6, n_kv, hd), at, tab), want["slots"], pool[0], pool[2], kind)
+        sv.append8(host(st.v).reshape(6, n_kv, hd).astype(np.float64), want["slots"], pool[1], pool[3], kind)
+        for got, w in zip(st.cache[0], pool):
+            assert np.array_equal(host(got), w)
+        check_attention(st.attn, st.q_rot.cpu(), pool[:2], pool[2:], want["tables"], want["row_lengths"], n_q, n_kv, hd, kind, seq_ids=want["seq_ids"])
+        logits = host(st.logits)
+        for r in range(want["cu_tokens"][-1]):
+            p = want["seq_ids"][r]
+            token, lp = sv.sample(logits[r], float(u[r]), float(st.temperature[p]), int(st.top_k[p]), float(st.top_p[p]))
+            assert int(got_ids[r]) == token and abs(float(logp[r]) - lp) <= 1e-5 + 2.0 ** -23 * abs(lp)
+
+
+def test_paged_decode_step_recorded():
+    """The recorded step replays a changing batch - prompts, single tokens, a finished request whose blocks go to another - with the bits of
+    the eager calls."""
+    plan = ([5, 1, 0, 0], [1, 1, 4, 0], [1, 1, 1, 1], [-1, 2, 1, 1], [3, 1, 1, 1], [1, 1, 1, 1])
+
+    def run(recorded):
+        st, _ = paged_step(torch.int8)
+        st.temperature.fill_(0.9), st.top_p.fill_(0.9)
+        if recorded:
+            st.capture()
+        gen, outs = torch.Generator().manual_seed(61), []
+        for new in plan:
+            st.new_tokens.copy_(torch.tensor(new, dtype=torch.int32))
+            ids, u = torch.randint(0, 500, (6,), generator=gen, dtype=torch.int32).to(DEV), torch.rand(6, generator=gen).to(DEV)
+            if recorded:
+                st.token_buf.copy_(ids), st.u_buf.copy_(u)
+                got = st.step_graph()
+            else:
+                got = st.step(ids, u)
+            n = int(st.cu_tokens[-1])
+            outs += [got[0][:n].clone(), got[1][:n].clone(), st.logits[:n].clone()]
+        torch.cuda.synchronize()
+        return outs + [t.clone() for c in st.cache for t in (c[0].view(torch.uint8), c[1].view(torch.uint8), c[2], c[3])]
+
+    for a, b in zip(run(False), run(True)):
+        assert torch.equal(a, b)
+    assert bl.bitlinear_poll_status() == 0
+
+
 def test_binding_checks_shapes_types_and_devices():
     pool = pool_to_dev(*make_pool(4, 2, 16, 64, sv.INT8, 1), sv.INT8)
     q, t, n = torch.zeros(2, 256, dtype=torch.bfloat16, device=DEV), torch.zeros(2, 4, dtype=torch.int32, device=DEV), torch.ones(2, dtype=torch.int32, device=DEV)
