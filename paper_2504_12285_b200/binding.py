@@ -638,24 +638,21 @@ def _kvdt(dtype) -> int:
 
 
 def _tensors(*given) -> None:
-    """Each (tensor or None, dtype, name): contiguous, of that type and on the current device, where the library launches - it takes
-    pointers as they come."""
+    """Each (tensor or None, dtype, shape or None, name): contiguous, of that type and shape and on the current device, where the library
+    launches - it takes pointers as they come."""
     index = -1
-    for t, dtype, name in given:
+    for t, dtype, shape, name in given:
         if t is None:
             continue
         at = t.get_device()
         if at < 0 or t.dtype != dtype or not t.is_contiguous():
             raise TypeError(f"{name} must be a contiguous CUDA tensor of {dtype}")
+        if shape is not None and t.shape != shape:
+            raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
         if at != index:
             index = torch._C._cuda_getDevice()
             if at != index:
                 raise ValueError(f"{name} is on cuda:{at}, the current device is cuda:{index}")
-
-
-def _shape(t, shape, name: str) -> None:
-    if t is not None and t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
 
 
 def _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads: int, head_dim: int):
@@ -673,14 +670,12 @@ def bitlinear_block_tables(lengths, new_tokens, tables, free_blocks, n_free, blo
     """One step's bookkeeping of a paged cache: lengths, new_tokens int32 [R] (negative: finished), tables int32 [R, max_blocks] and
     free_blocks int32 [n_blocks] updated in place, n_free int32 [1] -> (lengths_out [R], n_free_out [1], served [R], cu_tokens
     [R + 1], seq_ids, positions, row_lengths, slots [t_cap]), all int32.  lengths_out / n_free_out may be lengths / n_free."""
-    i32 = torch.int32
-    _tensors((lengths, i32, "lengths"), (new_tokens, i32, "new_tokens"), (tables, i32, "tables"), (free_blocks, i32, "free_blocks"), (n_free, i32, "n_free"),
-             (lengths_out, i32, "lengths_out"), (n_free_out, i32, "n_free_out"))
     if tables.dim() != 2 or free_blocks.dim() != 1 or t_cap < 0:
         raise ValueError("tables must be [R, max_blocks], free_blocks [n_blocks], t_cap not negative")
-    R, max_blocks = tables.shape
-    _shape(lengths, (R,), "lengths"), _shape(new_tokens, (R,), "new_tokens"), _shape(n_free, (1,), "n_free")
-    _shape(lengths_out, (R,), "lengths_out"), _shape(n_free_out, (1,), "n_free_out")
+    i32, (R, max_blocks), n_blocks = torch.int32, tables.shape, free_blocks.shape[0]
+    each, one = (R,), (1,)
+    _tensors((lengths, i32, each, "lengths"), (new_tokens, i32, each, "new_tokens"), (tables, i32, None, "tables"), (free_blocks, i32, None, "free_blocks"),
+             (n_free, i32, one, "n_free"), (lengths_out, i32, each, "lengths_out"), (n_free_out, i32, one, "n_free_out"))
     # one buffer for what is returned: four columns of tokens (each 16-byte aligned), then the requests' rows
     pad = -t_cap % 4
     sizes = ([t_cap, pad] if pad else [t_cap]) * 4 + [R, R + 1, R, 1]
@@ -692,7 +687,7 @@ def bitlinear_block_tables(lengths, new_tokens, tables, free_blocks, n_free, blo
     if n_free_out is None:
         n_free_out = own_free
     rc = lib().bitlinear_block_tables(lengths.data_ptr(), new_tokens.data_ptr(), R, tables.data_ptr(), max_blocks, free_blocks.data_ptr(), n_free.data_ptr(),
-                                      free_blocks.shape[0], block_rows, t_cap, lengths_out.data_ptr(), n_free_out.data_ptr(), served.data_ptr(),
+                                      n_blocks, block_rows, t_cap, lengths_out.data_ptr(), n_free_out.data_ptr(), served.data_ptr(),
                                       cu.data_ptr(), seq_ids.data_ptr(), positions.data_ptr(), row_lengths.data_ptr(), slots.data_ptr(), _stream())
     _check(rc, "bitlinear_block_tables")
     return lengths_out, n_free_out, served, cu, seq_ids, positions, row_lengths, slots
@@ -707,12 +702,10 @@ def bitlinear_rope_kv8(q, k, v, positions, slots, rope_table, k_cache, v_cache, 
     f32, i32 = torch.float32, torch.int32
     if q_out is None:
         q_out = torch.empty(T, n_q_heads * head_dim, dtype=torch.bfloat16, device=q.device)
-    _tensors((q, f32, "q"), (k, f32, "k"), (v, f32, "v"), (positions, i32, "positions"), (slots, i32, "slots"), (rope_table, f32, "rope_table"),
-             (k_cache, k_cache.dtype, "k_cache"), (v_cache, k_cache.dtype, "v_cache"), (k_scale, f32, "k_scale"), (v_scale, f32, "v_scale"),
-             (q_out, torch.bfloat16, "q_out"))
-    kv = (T, n_kv_heads * head_dim)
-    _shape(q, (T, n_q_heads * head_dim), "q"), _shape(k, kv, "k"), _shape(v, kv, "v"), _shape(q_out, q.shape, "q_out")
-    _shape(positions, (T,), "positions"), _shape(slots, (T,), "slots")
+    rows, code, kv, pool = (T,), k_cache.dtype, (T, n_kv_heads * head_dim), k_cache.shape
+    _tensors((q, f32, (T, n_q_heads * head_dim), "q"), (k, f32, kv, "k"), (v, f32, kv, "v"), (positions, i32, rows, "positions"), (slots, i32, rows, "slots"),
+             (rope_table, f32, None, "rope_table"), (k_cache, code, None, "k_cache"), (v_cache, code, pool, "v_cache"), (k_scale, f32, None, "k_scale"),
+             (v_scale, f32, None, "v_scale"), (q_out, torch.bfloat16, q.shape, "q_out"))
     if rope_table.dim() != 3 or rope_table.shape[1] != head_dim // 2 or rope_table.shape[2] != 2:
         raise ValueError(f"rope_table must be [t_max, {head_dim // 2}, 2]")
     rc = lib().bitlinear_rope_kv8(q.data_ptr(), k.data_ptr(), v.data_ptr(), positions.data_ptr(), slots.data_ptr(), rope_table.data_ptr(), T,
@@ -736,10 +729,10 @@ def bitlinear_attention_decode_kv8(q, k_cache, v_cache, k_scale, v_scale, tables
         out = torch.empty_like(q)
     if ws is None:
         ws = _workspace(bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), q.device)
-    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
-    _tensors((q, bf16, "q"), (k_cache, k_cache.dtype, "k_cache"), (v_cache, k_cache.dtype, "v_cache"), (k_scale, f32, "k_scale"), (v_scale, f32, "v_scale"),
-             (tables, i32, "tables"), (lengths, i32, "lengths"), (seq_ids, i32, "seq_ids"), (out, bf16, "out"), (ws, torch.uint8, "ws"))
-    _shape(q, (M, n_q_heads * head_dim), "q"), _shape(out, q.shape, "out"), _shape(lengths, (M,), "lengths"), _shape(seq_ids, (M,), "seq_ids")
+    bf16, f32, i32, code, rows = torch.bfloat16, torch.float32, torch.int32, k_cache.dtype, (M,)
+    _tensors((q, bf16, (M, n_q_heads * head_dim), "q"), (k_cache, code, None, "k_cache"), (v_cache, code, None, "v_cache"), (k_scale, f32, None, "k_scale"),
+             (v_scale, f32, None, "v_scale"), (tables, i32, None, "tables"), (lengths, i32, rows, "lengths"), (seq_ids, i32, rows, "seq_ids"),
+             (out, bf16, q.shape, "out"), (ws, torch.uint8, None, "ws"))
     if tables.dim() != 2:
         raise ValueError("tables must be [n_seq, max_blocks]")
     n_seq, max_blocks = tables.shape
@@ -764,10 +757,10 @@ def bitlinear_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=
         ids = torch.empty(M, dtype=i32, device=logits.device)
     if logprobs is None:
         logprobs = torch.empty(M, dtype=f32, device=logits.device)
-    _tensors((logits[:1, :1], logits.dtype, "logits"), (u, f32, "u"), (temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"),
-             (min_p, f32, "min_p"), (ids, i32, "ids"), (logprobs, f32, "logprobs"))
-    for t, name in ((u, "u"), (temperature, "temperature"), (top_k, "top_k"), (top_p, "top_p"), (min_p, "min_p"), (ids, "ids"), (logprobs, "logprobs")):
-        _shape(t, rows, name)
+    if logits.get_device() != u.get_device():
+        raise ValueError("logits and u must be on one device")
+    _tensors((u, f32, rows, "u"), (temperature, f32, rows, "temperature"), (top_k, i32, rows, "top_k"), (top_p, f32, rows, "top_p"),
+             (min_p, f32, rows, "min_p"), (ids, i32, rows, "ids"), (logprobs, f32, rows, "logprobs"))
     rc = lib().bitlinear_sample(logits.data_ptr(), F32 if logits.dtype == f32 else BF16, M, V, stride, u.data_ptr(), _ptr(temperature), _ptr(top_k),
                                 _ptr(top_p), _ptr(min_p), ids.data_ptr(), logprobs.data_ptr(), _stream())
     _check(rc, "bitlinear_sample")
