@@ -25,9 +25,6 @@ namespace bitlinear {
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kBins = 1024;
-constexpr int kList = 512;   // candidates of a row that one CTA finishes with
 constexpr int kMaxCluster = 8;
 constexpr int kMaxShard = 45056;  // floats of a row that one CTA holds
 constexpr double kUnit44 = 17592186044416.0;  // 2^44
@@ -59,14 +56,16 @@ struct Crossing {
     unsigned long long mass_above;
 };
 
-struct Shared {
+// kThreads: of a CTA
+template <int kThreads>
+struct SampleShared {
+    static constexpr int kBins = 2 * kThreads;  // a row has two CTAs at least, and each merges its share of the bins, one per thread
+    static constexpr int kList = kThreads;      // candidates of a row that one CTA finishes with
+    double pow2[16];                            // 2^(j / 16): one entry to a pair of banks
     float top, low;             // largest logit of the part, smallest finite one
     int first;                  // lowest id of the largest logit in the part
     uint32_t ties;
     unsigned long long total;   // kept mass of the part
-    __align__(16) uint32_t list_key[kList];  // rank 0: the row's candidates in the order of ids, once they are few
-    int list_id[kList];
-    unsigned long long list_mass[kList];
     Crossing cross;
     uint32_t slice_count;       // what this CTA's share of the merged bins holds
     unsigned long long slice_mass;
@@ -74,34 +73,43 @@ struct Shared {
     uint32_t warp_count[kThreads / 32];
     float warp_top[kThreads / 32], warp_low[kThreads / 32];
     int cut_index;
-    __align__(16) uint32_t count[kBins];
-    __align__(16) uint32_t mass[3][kBins];  // sums of the weights' low, middle and high 16 bits: shared memory adds 32-bit integers natively
+    union {
+        struct {
+            uint32_t count[kBins];
+            uint32_t mass[3][kBins];  // sums of the weights' low, middle and high 16 bits: shared memory adds 32-bit integers natively
+        };
+        struct {  // rank 0: the row's candidates in the order of ids, once they are few
+            unsigned long long list_mass[kList];
+            uint32_t list_key[kList];
+            int list_id[kList];
+        };
+    };
 };
 
 struct Row {
     float top;        // largest logit
     float least;      // logits below weigh less than 2^-48 of the largest and are taken as this
     double top_d;
-    double scale;     // log2(e) / T
+    double scale;     // 16 log2(e) / T
+    const double* pow2;
 };
 
-// exp((l - top) / T) = 2^n * 2^f, n whole, |f| <= 1/2: the second by 1 + f q(f), q of degree 7 interpolating (2^f - 1) / f at the Chebyshev nodes of
-// -1/2 .. 1/2 (within 2^-38 of 2^f, exact at 0).  Returned as the two factors.  Without a table: lookups of 64-bit
-// entries at random cost more of shared memory's time than the longer series costs of the fp64 pipe's.
+// exp((l - top) / T) = 2^(n / 16) * 2^(f / 16), n whole, |f| <= 1/2: the first from the table, the second by 1 + f q(f), q of degree 3 interpolating
+// (2^(f / 16) - 1) / f at the Chebyshev nodes of -1/2 .. 1/2 (within 2^-37 of 2^(f / 16), exact at 0).  Returned as the two factors.  The table's
+// entries lie in different banks, so lookups do not queue up; without it the series takes four more fp64 operations (42 cycles
+// per 32 weights and scheduler against 35).
 __device__ __forceinline__ void weight_factors(const Row& r, float l, double& series, double& power) {
     constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are n
     const double d = (double)fmaxf(l, r.least) - r.top_d;
     const double t = fma(d, r.scale, kRound);
     const double f = fma(d, r.scale, kRound - t);
-    double q = fma(f, 1.325080551750225e-06, 1.5303700711365693e-05);
-    q = fma(f, q, 0.00015403475186530786);
-    q = fma(f, q, 0.0013333478473685416);
-    q = fma(f, q, 0.00961812913523614);
-    q = fma(f, q, 0.055504109063258665);
-    q = fma(f, q, 0.24022650695888503);
-    q = fma(f, q, 0.6931471805568324);
+    const int n = __double2loint(t);
+    double q = fma(f, 1.4676329855091502e-07, 1.3551125679403628e-05);
+    q = fma(f, q, 0.0009383847927372583);
+    q = fma(f, q, 0.043321698775062194);
     series = fma(f, q, 1.0);
-    power = __hiloint2double((__double2loint(t) + 1023) << 20, 0);
+    const double base = r.pow2[n & 15];
+    power = __hiloint2double(__double2hiint(base) + ((n << 16) & 0xfff00000), __double2loint(base));
 }
 __device__ __forceinline__ double weight_of(const Row& r, float l) {
     double series, power;
@@ -123,10 +131,12 @@ __device__ __forceinline__ float load_logit<float>(const float* p) { return *p; 
 template <>
 __device__ __forceinline__ float load_logit<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 
-// kPerSm = 1 where every CTA has an SM to itself (more registers: more elements' chains side by side), else 2, so that one loads
-// while the other computes
-template <class T, int kPerSm>
-__global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleArgs a) {
+// 512 threads and an SM to itself where every CTA can have one; else 256, of which three CTAs share an SM, so that some load while
+// others compute (192 rows of 128,256 without filters: two CTAs of 512 took 77 us, three of 256 took 64)
+template <class T, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kernel(const SampleArgs a) {
+    using Shared = SampleShared<kThreads>;
+    constexpr int kBins = Shared::kBins, kList = Shared::kList;
         extern __shared__ __align__(16) uint8_t sample_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(sample_raw);
     float* room = reinterpret_cast<float*>(sample_raw + (sizeof(Shared) + 15) / 16 * 16);
@@ -134,6 +144,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid < 16) sh.pow2[tid] = exp2((double)tid / 16.0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long begin = (long long)rank * a.shard;
     const int n = (int)max(0ll, min((long long)a.shard, a.V - begin));
@@ -231,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
         top = low = 0.0f;
         __syncthreads();
     }
-    const Row rw = {top, fminf(top - 34.0f * temp, float_of(key_of(top) - 1)), (double)top, 1.4426950408889634074 / (double)temp};
+    const Row rw = {top, fminf(top - 34.0f * temp, float_of(key_of(top) - 1)), (double)top, 16.0 * 1.4426950408889634074 / (double)temp, sh.pow2};
     const uint32_t top_key = key_of(top);
     const double mp = given_mp > 0.0f ? fmin((double)given_mp, 1.0) : 0.0;  // the largest, of weight 1, always stays
 
@@ -370,7 +381,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
         uint32_t ca = ci - c, cs = 0;
         unsigned long long ma = mi - m, ms = 0;
 #pragma unroll
-        for (int w = 0; w < kBins / 2 / 32; ++w) {  // (a share is half the bins at most)
+        for (int w = 0; w < kThreads / 32; ++w) {
             if (w * 32 >= share) break;
             const uint32_t ct = sh.warp_count[w];
             const unsigned long long mt = sh.warp_mass[w];
@@ -661,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     settle();  // no CTA leaves while another reads its shared memory
 }
 
-template <class T, int kPerSm>
+template <class T, int kThreads>
 int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     static std::mutex mu;
     static bool done[64];
@@ -670,11 +681,11 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
         cudaGetLastError();
         return BITLINEAR_ERR_CUDA;
     }
-    constexpr size_t fixed = (sizeof(Shared) + 15) / 16 * 16;
+    constexpr size_t fixed = (sizeof(SampleShared<kThreads>) + 15) / 16 * 16;
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!done[dev]) {
-            if (cudaFuncSetAttribute(sample_kernel<T, kPerSm>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) !=
+            if (cudaFuncSetAttribute(sample_kernel<T, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) !=
                 cudaSuccess) {
                 cudaGetLastError();
                 return BITLINEAR_ERR_CUDA;
@@ -696,7 +707,7 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, sample_kernel<T, kPerSm>, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads>, a) != cudaSuccess) {
         cudaGetLastError();
         return BITLINEAR_ERR_CUDA;
     }
@@ -725,6 +736,6 @@ extern "C" int bitlinear_sample(const void* logits, int logits_dtype, int M, int
     a.shard = ((V + ranks - 1) / ranks + 7) / 8 * 8;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool alone = (long long)M * ranks <= sm_count;
-    if (logits_dtype == BITLINEAR_F32) return alone ? sample_launch<float, 1>(a, ranks, st) : sample_launch<float, 2>(a, ranks, st);
-    return alone ? sample_launch<__nv_bfloat16, 1>(a, ranks, st) : sample_launch<__nv_bfloat16, 2>(a, ranks, st);
+    if (logits_dtype == BITLINEAR_F32) return alone ? sample_launch<float, 512>(a, ranks, st) : sample_launch<float, 256>(a, ranks, st);
+    return alone ? sample_launch<__nv_bfloat16, 512>(a, ranks, st) : sample_launch<__nv_bfloat16, 256>(a, ranks, st);
 }
