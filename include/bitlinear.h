@@ -562,7 +562,7 @@ int bitlinear_embed(const int32_t* ids, const void* table_bf16, int M, int V, in
  *   A temperature that is not above 0: the largest logit, lowest id first, logprob 0.  A NaN counts as -infinity; rows of -infinity
  *   alone give id -1 and logprob -infinity; +infinity shares all weight.  u outside [0, 1): the nearest inside.
  *   Weights are formed in fp64 (to 2^-37 of themselves) and summed as integers in units of 2^-44 of the largest, so the result does
- *   not depend on the order of a sum.  A temperature above 1e30 counts as 1e30.
+ *   not depend on the order of a sum.  A temperature above 1e29 counts as 1e29.
  *   V <= BITLINEAR_SAMPLE_MAX_VOCAB.  One launch, no workspace.
  */
 #define BITLINEAR_SAMPLE_MAX_VOCAB 360448

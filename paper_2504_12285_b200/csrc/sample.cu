@@ -92,7 +92,13 @@ struct Row {
     double top_d;
     double scale;     // 16 log2(e) / T
     const double* pow2;
+    bool alone;       // nothing but the largest weighs anything: it is +infinity, or the next lower float is 34 temperatures away (or -infinity)
 };
+__device__ __forceinline__ Row relative_to(float top, float temp, const double* pow2) {
+    const float least = top - 34.0f * temp;
+    const bool alone = top == INFINITY || top < -3e38f || float_of(key_of(top) - 1) < least;
+    return {top, least, (double)top, 16.0 * 1.4426950408889634074 / (double)temp, pow2, alone};
+}
 
 // exp((l - top) / T) = 2^(n / 16) * 2^(f / 16), n whole, |f| <= 1/2: the first from the table, the second by 1 + f q(f), q of degree 3 interpolating
 // (2^(f / 16) - 1) / f at the Chebyshev nodes of -1/2 .. 1/2 (within 2^-37 of 2^(f / 16), exact at 0).  Returned as the two factors.  The table's
@@ -124,6 +130,13 @@ __device__ __forceinline__ unsigned long long fixed_of(const Row& r, float l) {
     return (unsigned long long)__double_as_longlong(fma(series, power, 256.0)) - kBits256;
 }
 
+// the running sum that the drawn token is the first to exceed
+__device__ __forceinline__ unsigned long long drawn_at(float u, unsigned long long all) {
+    const double goal = u > 0.0f ? (double)u * (double)all : 0.0;
+    const unsigned long long at = goal < 9.2e18 ? (unsigned long long)goal : all;  // sum > goal, in whole numbers: > its floor
+    return at >= all ? all - 1 : at;                                               // u = 1: the last token that is kept
+}
+
 template <class T>
 __device__ __forceinline__ float load_logit(const T* p);
 template <>
@@ -149,7 +162,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     const long long begin = (long long)rank * a.shard;
     const int n = (int)max(0ll, min((long long)a.shard, a.V - begin));
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride + begin;
-    const float temp = a.temperature ? fminf(a.temperature[row], 1e30f) : 1.0f;
+    const float temp = a.temperature ? fminf(a.temperature[row], 1e29f) : 1.0f;
     const int k = a.top_k ? a.top_k[row] : 0;
     const float p = a.top_p ? a.top_p[row] : 1.0f;
     const float given_mp = a.min_p ? a.min_p[row] : 0.0f;
@@ -237,12 +250,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
         cluster.sync();  // no CTA leaves while another reads its shared memory
         return;
     }
-    if (top == INFINITY) {  // +infinity shares all weight: as if it were 0 and all else -infinity
-        for (int i = i0; i < i1; ++i) vals[i] = vals[i] == INFINITY ? 0.0f : -INFINITY;
+    Row rw = relative_to(top, temp, sh.pow2);
+    if (rw.alone) {  // as if the largest were 0 and all else -infinity, at any temperature
+        for (int i = i0; i < i1; ++i) vals[i] = vals[i] == top ? 0.0f : -INFINITY;
         top = low = 0.0f;
+        rw = relative_to(top, 1.0f, sh.pow2);
         __syncthreads();
     }
-    const Row rw = {top, fminf(top - 34.0f * temp, float_of(key_of(top) - 1)), (double)top, 16.0 * 1.4426950408889634074 / (double)temp, sh.pow2};
     const uint32_t top_key = key_of(top);
     const double mp = given_mp > 0.0f ? fmin((double)given_mp, 1.0) : 0.0;  // the largest, of weight 1, always stays
 
@@ -283,13 +297,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
         pending = true;
     };
 
-    // the running sum that the drawn token is the first to exceed
-    auto goal_of = [&](unsigned long long all) {
-        const double goal = u > 0.0f ? (double)u * (double)all : 0.0;
-        const unsigned long long at = goal < 9.2e18 ? (unsigned long long)goal : all;  // sum > goal, in whole numbers: > its floor
-        return at >= all ? all - 1 : at;                                               // u = 1: the last token that is kept
-    };
-
     // ---- thresholds
     // linear bins of the first histogram: distances from the largest up to where weights vanish or the logits end
     const float span = fminf(top - low, 40.0f * temp);
@@ -312,14 +319,22 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     };
     // one histogram over the part's elements to which bin_of gives a bin, merged over the cluster; the bin in which the running
     // count (or mass) reaches the target
-    auto find = [&](bool by_mass, uint32_t want, double target, uint32_t count0, unsigned long long mass0, auto&& bin_of) {
+    // (sparse: few elements have a bin, so weights are formed for those alone)
+    auto find = [&](bool by_mass, bool sparse, uint32_t want, double target, uint32_t count0, unsigned long long mass0, auto&& bin_of) {
         settle();
         for (int b = tid; b < kBins; b += kThreads) {
             sh.count[b] = 0;
             if (by_mass) sh.mass[0][b] = sh.mass[1][b] = sh.mass[2][b] = 0;
         }
         __syncthreads();
-        if (by_mass) {
+        auto add = [&](int b, unsigned long long w) {
+            const uint32_t w2 = (uint32_t)(w >> 32);
+            atomicAdd(&sh.count[b], 1u);
+            atomicAdd(&sh.mass[0][b], (uint32_t)w & 0xffffu);
+            atomicAdd(&sh.mass[1][b], (uint32_t)w >> 16);
+            if (w2) atomicAdd(&sh.mass[2][b], w2);
+        };
+        if (by_mass && !sparse) {
             each([&](const float (&l)[4], const bool (&in)[4], int) {
                 unsigned long long w[4];
                 int b[4];
@@ -327,13 +342,16 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
                 for (int j = 0; j < 4; ++j) w[j] = fixed_of(rw, l[j]), b[j] = in[j] ? bin_of(l[j], key_of(l[j])) : -1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (b[j] >= 0) {
-                        const uint32_t w2 = (uint32_t)(w[j] >> 32);
-                        atomicAdd(&sh.count[b[j]], 1u);
-                        atomicAdd(&sh.mass[0][b[j]], (uint32_t)w[j] & 0xffffu);
-                        atomicAdd(&sh.mass[1][b[j]], (uint32_t)w[j] >> 16);
-                        if (w2) atomicAdd(&sh.mass[2][b[j]], w2);
-                    }
+                    if (b[j] >= 0) add(b[j], w[j]);
+            });
+        } else if (by_mass) {
+            each([&](const float (&l)[4], const bool (&in)[4], int) {
+                int b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[j] = in[j] ? bin_of(l[j], key_of(l[j])) : -1;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (b[j] >= 0) add(b[j], fixed_of(rw, l[j]));
             });
         } else {
             each([&](const float (&l)[4], const bool (&in)[4], int) {
@@ -447,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
         while (x.count > 1 && lo < hi && (by_mass || x.count_above + x.count != want)) {
             const int shift = max(0, 32 - __clz((int)(hi - lo)) - 10);
             const uint32_t from = hi, to = lo;
-            x = find(by_mass, want, target, x.count_above, x.mass_above, [&](float, uint32_t key) { return key >= to && key <= from ? (int)((from - key) >> shift) : -1; });
+            x = find(by_mass, true, want, target, x.count_above, x.mass_above, [&](float, uint32_t key) { return key >= to && key <= from ? (int)((from - key) >> shift) : -1; });
             hi = from - ((uint32_t)x.bin << shift);
             lo = hi - to >= (1u << shift) ? hi - ((1u << shift) - 1u) : to;
         }
@@ -563,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
         if (w < mp) stays = false;
         if (!stays) mass = 0;
         const unsigned long long ahead = scan_mass(mass, total);
-        const unsigned long long goal = goal_of(total);
+        const unsigned long long goal = drawn_at(u, total);
         if (ahead <= goal && goal < ahead + mass) {
             a.ids[row] = sh.list_id[tid];
             if (a.logprobs) a.logprobs[row] = (float)log(w * kUnit44 / (double)total);
@@ -625,19 +643,19 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     unsigned long long mine, before;
     auto by_distance = [&](float l, uint32_t) { return linear_bin(l); };
     if (use_k) {
-        const Crossing x = find(false, (uint32_t)k, 0.0, 0, 0, by_distance);
+        const Crossing x = find(false, false, (uint32_t)k, 0.0, 0, 0, by_distance);
         if (x.count_above + x.count <= kList) return finish(x.bin, (uint32_t)k, -1.0);
         narrow(x, false, (uint32_t)k, 0.0);
     }
     if (use_p) {
         const unsigned long long all = kept_mass(0.0, mine, before);
         const double target = fmax((double)p * (double)all, 0.5);
-        const Crossing x = find(true, 0, target, 0, 0, by_distance);
+        const Crossing x = find(true, false, 0, target, 0, 0, by_distance);
         if (x.count_above + x.count <= kList) return finish(x.bin, 0, target);
         narrow(x, true, 0, target);
     }
     const unsigned long long all = kept_mass(mp, mine, before);
-    const unsigned long long at = goal_of(all);
+    const unsigned long long at = drawn_at(u, all);
     // the thread whose run holds it; its warp finds the element
     const unsigned holds = __ballot_sync(0xffffffffu, before <= at && at < before + mine);
     if (holds) {
@@ -672,6 +690,243 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     settle();  // no CTA leaves while another reads its shared memory
 }
 
+// The draw without filters: no threshold is wanted, so nothing is kept of a row.  Each warp of a cluster streams a contiguous part, its
+// weights relative to the largest logit it has met (a larger one rescales its sum); the cluster joins the warps' sums, and the
+// warp in whose part the goal lies goes over that part once more.  Bound by the fp64 pipe: 35 cycles per 32 weights and
+// scheduler are 24 us for 192 rows of 128,256.
+constexpr int kPlainThreads = 512, kPlainWarps = kPlainThreads / 32;
+struct PlainShared {
+    double pow2[16];
+    float warp_top[kPlainWarps];
+    unsigned long long warp_mass[kPlainWarps];
+    unsigned long long best[kPlainWarps];  // greedy: key of the largest logit, ~id
+    float top;
+    unsigned long long total, first;
+};
+
+template <class T>
+__global__ void __launch_bounds__(kPlainThreads, 2) sample_plain_kernel(const SampleArgs a) {
+    __shared__ PlainShared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (tid < 16) sh.pow2[tid] = exp2((double)tid / 16.0);
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const float temp = a.temperature ? fminf(a.temperature[row], 1e29f) : 1.0f;
+    const float u = a.u[row];
+    const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride;
+    // the row: elements up to a 16-byte border (worker 0), 16-byte vectors dealt to the workers in equal runs, the rest (the last worker)
+    constexpr int VEC = 16 / sizeof(T), SUB = 16 / VEC;  // a lane takes 16 elements at a time, SUB vectors
+    const int head = min(a.V, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
+    const int n_vec = (a.V - head) / VEC, tail = head + n_vec * VEC;
+    const int workers = ranks * kPlainWarps, me = rank * kPlainWarps + warp;
+    const int v0 = (int)((long long)n_vec * me / workers), v1 = (int)((long long)n_vec * (me + 1) / workers);
+    const uint4* vsrc = reinterpret_cast<const uint4*>(src + head);
+    // f(logits, id of the first, ids between subs, elements of a sub) over this warp's part in the order of ids until it returns true; what does not
+    // exist, and NaN, is -inf
+    auto over_part = [&](auto&& f) {
+        auto single = [&](int from, int to) {  // fewer than 8 elements, one per lane
+            float l[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) l[i] = -INFINITY;
+            if (from + lane < to) l[0] = fmaxf(load_logit(src + from + lane), -INFINITY);
+            return f(l, from + lane, 0, 1);
+        };
+        if (me == 0 && head > 0 && single(0, head)) return;
+        for (int v = v0; v < v1; v += 32 * SUB) {
+            uint4 x[SUB];
+            float l[16];
+#pragma unroll
+            for (int j = 0; j < SUB; ++j)
+                if (v + 32 * j + lane < v1) x[j] = __ldcs(vsrc + v + 32 * j + lane);
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) {
+                const T* e = reinterpret_cast<const T*>(&x[j]);
+                const bool in = v + 32 * j + lane < v1;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) l[j * VEC + i] = in ? fmaxf(load_logit(e + i), -INFINITY) : -INFINITY;
+            }
+            if (f(l, head + (v + lane) * VEC, 32 * VEC, VEC)) return;
+        }
+        if (me == workers - 1 && tail < a.V) single(tail, a.V);
+    };
+    if (!(temp > 0.0f)) {  // greedy: the largest, lowest id first
+        unsigned long long best = 0;
+        over_part([&](const float (&l)[16], int id, int step, int n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (step > 0 || i == 0)
+                    best = max(best, ((unsigned long long)key_of(l[i]) << 32) | (0xffffffffu - (uint32_t)(id + (i / VEC) * step + i % VEC)));
+            return false;
+        });
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, off));
+        if (lane == 0) sh.best[warp] = best;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < kPlainWarps; ++w) best = max(best, sh.best[w]);
+            sh.first = best;
+        }
+        cluster.sync();
+        if (rank == 0 && tid == 0) {
+            for (int r = 0; r < ranks; ++r) best = max(best, cluster.map_shared_rank(&sh, r)->first);
+            const bool none = (uint32_t)(best >> 32) <= kLowKey;
+            a.ids[row] = none ? -1 : (int)(0xffffffffu - (uint32_t)best);
+            if (a.logprobs) a.logprobs[row] = none ? -INFINITY : 0.0f;
+        }
+        cluster.sync();  // no CTA leaves while another reads its shared memory
+        return;
+    }
+    auto fixed_at = [&](const Row& r, float l) { return r.alone ? (l == r.top ? 1ull << 44 : 0ull) : fixed_of(r, l); };
+    Row rw = {-INFINITY, 0.0f, 0.0, 0.0, sh.pow2, false};
+    unsigned long long mass = 0;  // this lane's, in units of 2^-44 of the weight of rw.top
+    over_part([&](const float (&l)[16], int, int, int) {
+        float top = l[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, l[i]);
+        if (__any_sync(0xffffffffu, top > rw.top)) {
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const Row next = relative_to(top, temp, sh.pow2);
+            mass = rw.top <= next.least || next.alone ? 0ull : (unsigned long long)__double2ll_rn((double)mass * weight_of(next, rw.top));
+            rw = next;
+        }
+        if (rw.top == -INFINITY) return false;
+        if (rw.alone) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mass += l[i] == rw.top ? 1ull << 44 : 0ull;
+            return false;
+        }
+        unsigned long long sum = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += fixed_of(rw, l[i]) + kBits256;
+        mass += sum - 16 * kBits256;
+        return false;
+    });
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, off);
+    if (lane == 0) sh.warp_top[warp] = rw.top, sh.warp_mass[warp] = mass;
+    __syncthreads();
+    // the largest of the row, and the warps' sums relative to it; every warp joins them for itself
+    const float w_top = sh.warp_top[lane & (kPlainWarps - 1)];
+    float top = w_top;
+#pragma unroll
+    for (int off = kPlainWarps / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if (tid == 0) sh.top = top;
+    cluster.sync();
+    for (int r = 0; r < ranks; ++r) top = fmaxf(top, cluster.map_shared_rank(&sh, r)->top);
+    if (top == -INFINITY) {  // the same in every CTA of the cluster
+        if (rank == 0 && tid == 0) {
+            a.ids[row] = -1;
+            if (a.logprobs) a.logprobs[row] = -INFINITY;
+        }
+        cluster.sync();
+        return;
+    }
+    const Row rt = relative_to(top, temp, sh.pow2);
+    const double factor = w_top == top ? 1.0 : w_top <= rt.least || rt.alone ? 0.0 : weight_of(rt, w_top);
+    const unsigned long long joined = lane < kPlainWarps ? (unsigned long long)__double2ll_rn((double)sh.warp_mass[lane] * factor) : 0ull;
+    unsigned long long incl = joined;
+#pragma unroll
+    for (int d = 1; d < kPlainWarps; d <<= 1) {
+        const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += up;
+    }
+    if (tid == kPlainWarps - 1) sh.total = incl;
+    cluster.sync();
+    unsigned long long before = 0, all = 0;
+    for (int r = 0; r < ranks; ++r) {
+        const unsigned long long t = cluster.map_shared_rank(&sh, r)->total;
+        if (r < rank) before += t;
+        all += t;
+    }
+    cluster.barrier_arrive();
+    const unsigned long long at = drawn_at(u, all);
+    before += __shfl_sync(0xffffffffu, incl - joined, warp);
+    if (before <= at && at < before + __shfl_sync(0xffffffffu, joined, warp)) {
+        // sums of single weights may differ from the joined ones in the last units: where they end short of the goal, the last
+        // element of any weight is the one, or the largest where each alone rounds to none
+        unsigned long long run = before;
+        int last = -1, big = 0;
+        float last_l = 0.0f, big_l = -INFINITY;
+        over_part([&](const float (&l)[16], int id, int step, int n) {
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) {
+                if (step == 0 && j > 0) break;
+                unsigned long long f[VEC], sum = 0;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    f[i] = i < n ? fixed_at(rt, l[j * VEC + i]) : 0ull;
+                    if (f[i]) last = id + j * step + i, last_l = l[j * VEC + i];
+                    if (i < n && l[j * VEC + i] > big_l) big = id + j * step + i, big_l = l[j * VEC + i];
+                    sum += f[i];
+                }
+                unsigned long long upto = sum;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const unsigned long long up = __shfl_up_sync(0xffffffffu, upto, d);
+                    if (lane >= d) upto += up;
+                }
+                const unsigned past = __ballot_sync(0xffffffffu, run + upto > at);
+                if (past) {
+                    if (lane == __ffs((int)past) - 1) {
+                        unsigned long long s = run + upto - sum;
+                        bool taken = false;
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) {
+                            s += f[i];
+                            if (!taken && s > at) taken = true, last = id + j * step + i, last_l = l[j * VEC + i];
+                        }
+                    } else {
+                        last = -1;
+                    }
+                    return true;
+                }
+                run += __shfl_sync(0xffffffffu, upto, 31);
+            }
+            return false;
+        });
+        if (!__any_sync(0xffffffffu, last >= 0)) {
+            float most_l = big_l;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) most_l = fmaxf(most_l, __shfl_xor_sync(0xffffffffu, most_l, off));
+            if (big_l == most_l) last = big, last_l = big_l;
+        }
+        int most = last;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, off));
+        if (last == most && last >= 0) {
+            a.ids[row] = last;
+            if (a.logprobs) a.logprobs[row] = (float)log((rt.alone ? 1.0 : weight_of(rt, last_l)) * kUnit44 / (double)all);
+        }
+    }
+    cluster.barrier_wait();
+}
+
+int launch_rows(const void* kernel, SampleArgs a, int ranks, int threads, size_t smem, cudaStream_t st) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.M * ranks));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    void* args[1] = {&a};
+    if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) {
+        cudaGetLastError();
+        return BITLINEAR_ERR_CUDA;
+    }
+    return BITLINEAR_OK;
+}
+
 template <class T, int kThreads>
 int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
     static std::mutex mu;
@@ -682,11 +937,11 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
         return BITLINEAR_ERR_CUDA;
     }
     constexpr size_t fixed = (sizeof(SampleShared<kThreads>) + 15) / 16 * 16;
+    const void* kernel = reinterpret_cast<const void*>(sample_kernel<T, kThreads>);
     {
         std::lock_guard<std::mutex> lock(mu);
         if (!done[dev]) {
-            if (cudaFuncSetAttribute(sample_kernel<T, kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) !=
-                cudaSuccess) {
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(fixed + (kMaxShard + 4) * sizeof(float))) != cudaSuccess) {
                 cudaGetLastError();
                 return BITLINEAR_ERR_CUDA;
             }
@@ -694,24 +949,7 @@ int sample_launch(SampleArgs a, int ranks, cudaStream_t st) {
         }
     }
     a.per = (a.shard + kThreads - 1) / kThreads | 1;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)ranks;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.M * ranks));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = fixed + (size_t)(a.shard + 4) * sizeof(float);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads>, a) != cudaSuccess) {
-        cudaGetLastError();
-        return BITLINEAR_ERR_CUDA;
-    }
-    return BITLINEAR_OK;
+    return launch_rows(kernel, a, ranks, kThreads, fixed + (size_t)(a.shard + 4) * sizeof(float), st);
 }
 
 }  // namespace
@@ -735,6 +973,11 @@ extern "C" int bitlinear_sample(const void* logits, int logits_dtype, int M, int
     SampleArgs a = {logits, row_stride, M, V, 0, 0, u, temperature, top_k, top_p, min_p, ids, logprobs};
     a.shard = ((V + ranks - 1) / ranks + 7) / 8 * 8;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!top_k && !top_p && !min_p) {
+        const void* kernel = logits_dtype == BITLINEAR_F32 ? reinterpret_cast<const void*>(sample_plain_kernel<float>)
+                                                           : reinterpret_cast<const void*>(sample_plain_kernel<__nv_bfloat16>);
+        return launch_rows(kernel, a, ranks, kPlainThreads, 0, st);
+    }
     const bool alone = (long long)M * ranks <= sm_count;
     if (logits_dtype == BITLINEAR_F32) return alone ? sample_launch<float, 512>(a, ranks, st) : sample_launch<float, 256>(a, ranks, st);
     return alone ? sample_launch<__nv_bfloat16, 512>(a, ranks, st) : sample_launch<__nv_bfloat16, 256>(a, ranks, st);

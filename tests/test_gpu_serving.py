@@ -452,6 +452,27 @@ def test_sample_masked_rows(filters):
         check_sample(l, rng.random(9), **filters)
 
 
+@pytest.mark.parametrize("filters", [dict(), dict(top_p=0.7), dict(top_k=4), dict(min_p=0.5), dict(temperature=1e35), dict(temperature=1e-12), dict(temperature=1e-12, top_p=0.6),
+                                     dict(temperature=1e-40, top_k=3)])
+def test_sample_rows_at_the_ends_of_the_type(filters):
+    """Rows whose largest logit is the type's lowest (what a mask left of a row) beside -infinity, or the type's largest, or whose parts
+    are all masked but one."""
+    low, high, V = np.finfo(np.float32).min, np.finfo(np.float32).max, 9000
+    rng = np.random.default_rng(21)
+    l = np.full((6, V), -np.inf, np.float32)
+    l[0, rng.random(V) < 0.3] = low
+    l[1, 4444] = low
+    l[2] = low
+    l[2, 5000:5003] = [1.0, 2.0, 1.5]
+    l[3, rng.random(V) < 0.01] = high
+    l[4, 7000:] = rng.standard_normal(2000) - 60.0
+    l[4, 3] = 0.5
+    l[5, ::2] = 0.0
+    with np.errstate(over="ignore"):
+        check_sample(l, rng.random(6), **filters)
+        check_sample(l, np.full(6, 1 - 2.0 ** -24), **filters)
+
+
 def test_sample_random_numbers_at_their_ends():
     rng = np.random.default_rng(14)
     l = np.tile(rng.standard_normal((1, 700)), (6, 1))
