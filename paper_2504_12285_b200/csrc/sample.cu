@@ -144,6 +144,9 @@ __device__ __forceinline__ float load_logit<float>(const float* p) { return *p; 
 template <>
 __device__ __forceinline__ float load_logit<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 
+// 2^(j / 16)
+__device__ const double kPow2Table[16] = {1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
+
 // 512 threads and an SM to itself where every CTA can have one; else 256, of which three CTAs share an SM, so that some load while
 // others compute (192 rows of 128,256 without filters: two CTAs of 512 took 77 us, three of 256 took 64)
 template <class T, int kThreads>
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (tid < 16) sh.pow2[tid] = exp2((double)tid / 16.0);
+    if (tid < 16) sh.pow2[tid] = kPow2Table[tid];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long begin = (long long)rank * a.shard;
     const int n = (int)max(0ll, min((long long)a.shard, a.V - begin));
@@ -692,55 +695,61 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
 
 // The draw without filters: no threshold is wanted, so nothing is kept of a row.  Each warp of a cluster streams a contiguous part, its
 // weights relative to the largest logit it has met (a larger one rescales its sum); the cluster joins the warps' sums, and the
-// warp in whose part the goal lies goes over that part once more.  Bound by the fp64 pipe: 35 cycles per 32 weights and
-// scheduler are 24 us for 192 rows of 128,256.
-constexpr int kPlainThreads = 512, kPlainWarps = kPlainThreads / 32;
+// warp in whose part the goal lies goes over that part once more.  The weights' fp64 operations alone, 35 cycles per 32 weights and
+// scheduler, are 24 us for 192 rows of 128,256; the kernel takes 52 us (the one with filters 64): four CTAs of 256 threads per SM
+// beat two of 512 (63 us), eight elements per lane with the next eight on their way beat sixteen (62 us), and one join by the
+// first warps beat two barriers (80 us).
+constexpr int kPlainThreads = 256, kPlainWarps = kPlainThreads / 32;
+constexpr int kLane = 8;  // elements that a lane takes at a time
 struct PlainShared {
     double pow2[16];
     float warp_top[kPlainWarps];
     unsigned long long warp_mass[kPlainWarps];
     unsigned long long best[kPlainWarps];  // greedy: key of the largest logit, ~id
-    float top;
-    unsigned long long total, first;
+    unsigned long long first;
 };
 
 template <class T>
-__global__ void __launch_bounds__(kPlainThreads, 2) sample_plain_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kPlainThreads, 4) sample_plain_kernel(const SampleArgs a) {
     __shared__ PlainShared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (tid < 16) sh.pow2[tid] = exp2((double)tid / 16.0);
+    if (tid < 16) sh.pow2[tid] = kPow2Table[tid];
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float temp = a.temperature ? fminf(a.temperature[row], 1e29f) : 1.0f;
     const float u = a.u[row];
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride;
     // the row: elements up to a 16-byte border (worker 0), 16-byte vectors dealt to the workers in equal runs, the rest (the last worker)
-    constexpr int VEC = 16 / sizeof(T), SUB = 16 / VEC;  // a lane takes 16 elements at a time, SUB vectors
+    constexpr int VEC = 16 / sizeof(T), SUB = kLane / VEC;  // vectors of a lane's elements
     const int head = min(a.V, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
     const int n_vec = (a.V - head) / VEC, tail = head + n_vec * VEC;
     const int workers = ranks * kPlainWarps, me = rank * kPlainWarps + warp;
-    const int v0 = (int)((long long)n_vec * me / workers), v1 = (int)((long long)n_vec * (me + 1) / workers);
     const uint4* vsrc = reinterpret_cast<const uint4*>(src + head);
-    // f(logits, id of the first, ids between subs, elements of a sub) over this warp's part in the order of ids until it returns true; what does not
+    // f(logits, id of the first, ids between subs, elements of a sub) over worker w's part in the order of ids until it returns true; what does not
     // exist, and NaN, is -inf
-    auto over_part = [&](auto&& f) {
+    auto over_part = [&](int w, auto&& f) {
+        const int v0 = (int)((long long)n_vec * w / workers), v1 = (int)((long long)n_vec * (w + 1) / workers);
         auto single = [&](int from, int to) {  // fewer than 8 elements, one per lane
-            float l[16];
+            float l[kLane];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) l[i] = -INFINITY;
+            for (int i = 0; i < kLane; ++i) l[i] = -INFINITY;
             if (from + lane < to) l[0] = fmaxf(load_logit(src + from + lane), -INFINITY);
             return f(l, from + lane, 0, 1);
         };
-        if (me == 0 && head > 0 && single(0, head)) return;
-        for (int v = v0; v < v1; v += 32 * SUB) {
-            uint4 x[SUB];
-            float l[16];
+        if (w == 0 && head > 0 && single(0, head)) return;
+        uint4 x[SUB], y[SUB];
+        auto fetch = [&](uint4 (&z)[SUB], int v) {
 #pragma unroll
             for (int j = 0; j < SUB; ++j)
-                if (v + 32 * j + lane < v1) x[j] = __ldcs(vsrc + v + 32 * j + lane);
+                if (v + 32 * j + lane < v1) z[j] = __ldcs(vsrc + v + 32 * j + lane);
+        };
+        fetch(x, v0);
+        for (int v = v0; v < v1; v += 32 * SUB) {
+            fetch(y, v + 32 * SUB);  // the next ones come in while these are worked on
+            float l[kLane];
 #pragma unroll
             for (int j = 0; j < SUB; ++j) {
                 const T* e = reinterpret_cast<const T*>(&x[j]);
@@ -749,14 +758,16 @@ __global__ void __launch_bounds__(kPlainThreads, 2) sample_plain_kernel(const Sa
                 for (int i = 0; i < VEC; ++i) l[j * VEC + i] = in ? fmaxf(load_logit(e + i), -INFINITY) : -INFINITY;
             }
             if (f(l, head + (v + lane) * VEC, 32 * VEC, VEC)) return;
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) x[j] = y[j];
         }
-        if (me == workers - 1 && tail < a.V) single(tail, a.V);
+        if (w == workers - 1 && tail < a.V) single(tail, a.V);
     };
     if (!(temp > 0.0f)) {  // greedy: the largest, lowest id first
         unsigned long long best = 0;
-        over_part([&](const float (&l)[16], int id, int step, int n) {
+        over_part(me, [&](const float (&l)[kLane], int id, int step, int n) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < kLane; ++i)
                 if (step > 0 || i == 0)
                     best = max(best, ((unsigned long long)key_of(l[i]) << 32) | (0xffffffffu - (uint32_t)(id + (i / VEC) * step + i % VEC)));
             return false;
@@ -782,10 +793,10 @@ __global__ void __launch_bounds__(kPlainThreads, 2) sample_plain_kernel(const Sa
     auto fixed_at = [&](const Row& r, float l) { return r.alone ? (l == r.top ? 1ull << 44 : 0ull) : fixed_of(r, l); };
     Row rw = {-INFINITY, 0.0f, 0.0, 0.0, sh.pow2, false};
     unsigned long long mass = 0;  // this lane's, in units of 2^-44 of the weight of rw.top
-    over_part([&](const float (&l)[16], int, int, int) {
+    over_part(me, [&](const float (&l)[kLane], int, int, int) {
         float top = l[0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, l[i]);
+        for (int i = 1; i < kLane; ++i) top = fmaxf(top, l[i]);
         if (__any_sync(0xffffffffu, top > rw.top)) {
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -796,62 +807,80 @@ __global__ void __launch_bounds__(kPlainThreads, 2) sample_plain_kernel(const Sa
         if (rw.top == -INFINITY) return false;
         if (rw.alone) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mass += l[i] == rw.top ? 1ull << 44 : 0ull;
+            for (int i = 0; i < kLane; ++i) mass += l[i] == rw.top ? 1ull << 44 : 0ull;
             return false;
         }
         unsigned long long sum = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += fixed_of(rw, l[i]) + kBits256;
-        mass += sum - 16 * kBits256;
+        for (int i = 0; i < kLane; ++i) sum += fixed_of(rw, l[i]) + kBits256;
+        mass += sum - kLane * kBits256;
         return false;
     });
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, off);
     if (lane == 0) sh.warp_top[warp] = rw.top, sh.warp_mass[warp] = mass;
-    __syncthreads();
-    // the largest of the row, and the warps' sums relative to it; every warp joins them for itself
-    const float w_top = sh.warp_top[lane & (kPlainWarps - 1)];
-    float top = w_top;
-#pragma unroll
-    for (int off = kPlainWarps / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    if (tid == 0) sh.top = top;
     cluster.sync();
-    for (int r = 0; r < ranks; ++r) top = fmaxf(top, cluster.map_shared_rank(&sh, r)->top);
-    if (top == -INFINITY) {  // the same in every CTA of the cluster
+    if (warp > 0) {  // the first warp of every CTA joins the sums of all; what it has read it needs no more
+        cluster.barrier_arrive();
+        cluster.barrier_wait();
+        return;
+    }
+    constexpr int EACH = kMaxCluster * kPlainWarps / 32;  // lane l holds the sums of workers EACH l ...
+    float tops[EACH];
+    unsigned long long sums[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int w = EACH * lane + i;
+        const PlainShared* o = cluster.map_shared_rank(&sh, min(w / kPlainWarps, ranks - 1));
+        tops[i] = w < workers ? o->warp_top[w % kPlainWarps] : -INFINITY;
+        sums[i] = w < workers ? o->warp_mass[w % kPlainWarps] : 0ull;
+    }
+    cluster.barrier_arrive();
+    float top = tops[0];
+#pragma unroll
+    for (int i = 1; i < EACH; ++i) top = fmaxf(top, tops[i]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    if (top == -INFINITY) {
         if (rank == 0 && tid == 0) {
             a.ids[row] = -1;
             if (a.logprobs) a.logprobs[row] = -INFINITY;
         }
-        cluster.sync();
+        cluster.barrier_wait();
         return;
     }
     const Row rt = relative_to(top, temp, sh.pow2);
-    const double factor = w_top == top ? 1.0 : w_top <= rt.least || rt.alone ? 0.0 : weight_of(rt, w_top);
-    const unsigned long long joined = lane < kPlainWarps ? (unsigned long long)__double2ll_rn((double)sh.warp_mass[lane] * factor) : 0ull;
+    unsigned long long joined = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const double factor = tops[i] == top ? 1.0 : tops[i] <= rt.least || rt.alone ? 0.0 : weight_of(rt, tops[i]);
+        sums[i] = (unsigned long long)__double2ll_rn((double)sums[i] * factor);
+        joined += sums[i];
+    }
     unsigned long long incl = joined;
 #pragma unroll
-    for (int d = 1; d < kPlainWarps; d <<= 1) {
+    for (int d = 1; d < 32; d <<= 1) {
         const unsigned long long up = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += up;
     }
-    if (tid == kPlainWarps - 1) sh.total = incl;
-    cluster.sync();
-    unsigned long long before = 0, all = 0;
-    for (int r = 0; r < ranks; ++r) {
-        const unsigned long long t = cluster.map_shared_rank(&sh, r)->total;
-        if (r < rank) before += t;
-        all += t;
-    }
-    cluster.barrier_arrive();
+    const unsigned long long all = __shfl_sync(0xffffffffu, incl, 31);
     const unsigned long long at = drawn_at(u, all);
-    before += __shfl_sync(0xffffffffu, incl - joined, warp);
-    if (before <= at && at < before + __shfl_sync(0xffffffffu, joined, warp)) {
+    // the worker in whose part the goal lies, and what lies in front of it
+    const int holder = __ffs((int)__ballot_sync(0xffffffffu, incl > at)) - 1;
+    int owner = EACH * lane;
+    unsigned long long before = incl - joined;
+#pragma unroll
+    for (int i = 0; i < EACH - 1; ++i)
+        if (owner == EACH * lane + i && before + sums[i] <= at) before += sums[i], ++owner;
+    owner = __shfl_sync(0xffffffffu, owner, holder);
+    before = __shfl_sync(0xffffffffu, before, holder);
+    if (owner / kPlainWarps == rank) {
         // sums of single weights may differ from the joined ones in the last units: where they end short of the goal, the last
         // element of any weight is the one, or the largest where each alone rounds to none
         unsigned long long run = before;
         int last = -1, big = 0;
         float last_l = 0.0f, big_l = -INFINITY;
-        over_part([&](const float (&l)[16], int id, int step, int n) {
+        over_part(owner, [&](const float (&l)[kLane], int id, int step, int n) {
 #pragma unroll
             for (int j = 0; j < SUB; ++j) {
                 if (step == 0 && j > 0) break;
