@@ -57,31 +57,49 @@ template <int KIND>
 __device__ __forceinline__ float quick_error(bool keys) {
     return KIND == BITLINEAR_KV_INT8 ? (keys ? 1e-4f : 4e-5f) : (keys ? 2e-4f : 0.0f);
 }
+// Eight codes in two words; false if one of them cannot be told.  int8: adding 1.5 * 2^23 rounds to the nearest whole number, ties to even, and
+// leaves it in the low bits (no value is more than 127 steps: the scale is what the largest needs, or more).  e4m3: both ends of the
+// error are converted, two values to an instruction.
 template <int KIND>
-__device__ __forceinline__ bool quick_code(float value, float inv, float off, uint32_t& code) {
-    const float x = value * inv;
+__device__ __forceinline__ bool quick_codes(const float (&x)[8], float inv, float off, uint32_t (&word)[2]) {
     if constexpr (KIND == BITLINEAR_KV_INT8) {
-        const float c = rintf(x);
-        code = (uint32_t)(int)fminf(fmaxf(c, -127.0f), 127.0f) & 0xffu;
-        return fabsf(x - c) < 0.5f - off;
+        constexpr float kRound = 12582912.0f;
+        float worst = 0.0f;
+        uint32_t t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = fmaf(x[e], inv, kRound);
+            worst = fmaxf(worst, fabsf(fmaf(x[e], inv, kRound - y)));
+            t[e] = __float_as_uint(y);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) word[h] = __byte_perm(__byte_perm(t[4 * h], t[4 * h + 1], 0x0040), __byte_perm(t[4 * h + 2], t[4 * h + 3], 0x0040), 0x5410);
+        return worst < 0.5f - off;
     } else {
-        const uint32_t two = __nv_cvt_float2_to_fp8x2(make_float2(x - off, x + off), __NV_SATFINITE, __NV_E4M3);
-        code = two & 0xffu;
-        return code == two >> 8 && x == x;
+        uint32_t differ = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t low[2], high[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float a = x[4 * h + 2 * j] * inv, b = x[4 * h + 2 * j + 1] * inv;
+                low[j] = __nv_cvt_float2_to_fp8x2(make_float2(a - off, b - off), __NV_SATFINITE, __NV_E4M3);
+                high[j] = __nv_cvt_float2_to_fp8x2(make_float2(a + off, b + off), __NV_SATFINITE, __NV_E4M3);
+            }
+            word[h] = __byte_perm(low[0], low[1], 0x5410);
+            differ |= word[h] ^ __byte_perm(high[0], high[1], 0x5410);
+        }
+        return differ == 0;
     }
 }
-// The code of a value in fp64 that quick_code could not tell.  int8: the value against the middle next to it, times the scale (exact),
-// instead of a division.
+// int8, where some value of a row is next to the middle between two codes: the value in fp64 against the middle nearest to its
+// approximate quotient, times the scale (exact), instead of a division
 template <int KIND>
-__device__ __forceinline__ uint32_t close_code(double value, double scale, float inv) {
-    if constexpr (KIND == BITLINEAR_KV_INT8) {
-        const float low = floorf((float)value * inv - 0.25f);  // x is within 0.1 of a middle: the whole number below it
-        const double gap = value - ((double)low + 0.5) * scale;
-        const int c = (int)low + (gap > 0.0 || (gap == 0.0 && ((int)low & 1)) ? 1 : 0);
-        return (uint32_t)min(max(c, -127), 127) & 0xffu;
-    } else {
-        return code_of<KIND>(value, scale);
-    }
+__device__ __forceinline__ uint32_t close_code(double value, float quotient, double scale) {
+    const float low = floorf(quotient);  // the middle above it is the only one within 0.5
+    const double gap = value - ((double)low + 0.5) * scale;
+    const int c = (int)low + (gap > 0.0 || (gap == 0.0 && ((int)low & 1)) ? 1 : 0);
+    return (uint32_t)min(max(c, -127), 127) & 0xffu;
 }
 template <int KIND>
 __device__ __forceinline__ double decoded(uint32_t code) {
@@ -97,7 +115,7 @@ struct AppendArgs {
     const int* positions;
     const int* slots;
     const float2* table;
-    int T, t_max, n_q, n_kv, block_rows, n_blocks;
+    int T, t_max, n_q, n_kv, log2_rows, n_blocks;
     __nv_bfloat16* q_out;
     uint8_t* k_cache;
     uint8_t* v_cache;
@@ -150,6 +168,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     __shared__ float red[WARPS];
     __shared__ double red_d[WARPS];
     __shared__ int first_s[WARPS];
+    __shared__ float scale_s[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int sub = tid / TPR, i4 = 4 * (tid % TPR);
     const float* src = (which == 0 ? a.k : a.v) + (size_t)h * D;
@@ -157,7 +176,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     int end = m0 + 1;
     while (end < a.T) {  // the run's end, 32 tokens at a time, the same in every warp
         const int s = end + lane < a.T ? a.slots[end + lane] : -1;
-        const unsigned other = __ballot_sync(0xffffffffu, s < 0 || s / a.block_rows != block);
+        const unsigned other = __ballot_sync(0xffffffffu, s < 0 || s >> a.log2_rows != block);
         if (other) {
             end += __ffs((int)other) - 1;
             break;
@@ -178,7 +197,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     };
     // the largest magnitude, in fp32, and the run's first row in the block
     float top = 0.0f;
-    int first = a.block_rows;
+    int first = 1 << a.log2_rows;
 #pragma unroll 2
     for (int m = m0 + sub; m < end; m += ROWS) {
         const int pos = a.positions[m];
@@ -186,7 +205,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
         load(m, pos);
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
-        first = min(first, a.slots[m] - block * a.block_rows);
+        first = min(first, a.slots[m] - (block << a.log2_rows));
     }
     const float own_top = top;
 #pragma unroll
@@ -198,13 +217,12 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) top = fmaxf(top, red[w]), first = min(first, first_s[w]);
-    if (first >= a.block_rows) {  // no token of the run has a place in the table of angles
+    if (first >> a.log2_rows) {  // no token of the run has a place in the table of angles
         __syncthreads();
         return;
     }
-    double amax = (double)top;
     if (which == 0) {  // keys: the largest in fp64 is among those within the fp32 errors of the largest in fp32
-        amax = 0.0;
+        double amax = 0.0;
         const float near = top * (1.0f - 1.0f / 524288.0f);
         if (own_top >= near) {
             for (int m = m0 + sub; m < end; m += ROWS) {
@@ -222,34 +240,42 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
         }
         if (lane == 0) red_d[warp] = amax;
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) amax = fmax(amax, red_d[w]);
     }
-    float* scale = (which == 0 ? a.k_scale : a.v_scale) + (size_t)block * a.n_kv + h;
-    uint8_t* tile = (which == 0 ? a.k_cache : a.v_cache) + ((size_t)block * a.n_kv + h) * a.block_rows * D;
-    const float old = first > 0 ? *scale : 0.0f, need = scale_for<KIND>(amax);
-    const float now = first > 0 ? fmaxf(old, need) : need;
+    uint8_t* tile = (which == 0 ? a.k_cache : a.v_cache) + (((size_t)block * a.n_kv + h) << a.log2_rows) * D;
+    if (tid == 0) {  // the one reader and writer of the scale
+        float* scale = (which == 0 ? a.k_scale : a.v_scale) + (size_t)block * a.n_kv + h;
+        double amax = (double)top;
+        if (which == 0) {
+            amax = red_d[0];
+#pragma unroll
+            for (int w = 1; w < WARPS; ++w) amax = fmax(amax, red_d[w]);
+        }
+        const float need = scale_for<KIND>(amax), old = first > 0 ? *scale : need;
+        const float now = first > 0 ? fmaxf(old, need) : need;
+        *scale = now;
+        scale_s[0] = old, scale_s[1] = now;
+    }
+    __syncthreads();
+    const float old = scale_s[0], now = scale_s[1];
     const double s = (double)now;
     const float inv = __frcp_rn(now), off = quick_error<KIND>(which == 0);
-    __syncthreads();  // everyone has read the old scale, and the shared buffers are free
-    if (tid == 0) *scale = now;
 #pragma unroll 2
     for (int m = m0 + sub; m < end; m += ROWS) {
         const int pos = a.positions[m];
         if (pos < 0 || pos >= a.t_max) continue;
         load(m, pos);
-        uint32_t code[8], unsure = 0u;
+        uint32_t word[2];
+        if (!quick_codes<KIND>(x, inv, off, word)) {
+            word[0] = word[1] = 0u;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (!quick_code<KIND>(x[e], inv, off, code[e])) unsure |= 1u << e;
-        if (unsure) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if ((unsure >> e) & 1u) code[e] = close_code<KIND>(which == 0 ? r.exact(e) : (double)x[e], s, inv);
+            for (int e = 0; e < 8; ++e) {
+                const double value = which == 0 ? r.exact(e) : (double)x[e];
+                word[e >> 2] |= (KIND == BITLINEAR_KV_INT8 ? close_code<KIND>(value, x[e] * inv, s) : code_of<KIND>(value, s)) << (8 * (e & 3));
+            }
         }
-        uint8_t* dst = tile + (size_t)(a.slots[m] - block * a.block_rows) * D;
-        *reinterpret_cast<uint32_t*>(dst + i4) = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-        *reinterpret_cast<uint32_t*>(dst + i4 + D / 2) = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+        uint8_t* dst = tile + (size_t)(a.slots[m] - (block << a.log2_rows)) * D;
+        *reinterpret_cast<uint32_t*>(dst + i4) = word[0];
+        *reinterpret_cast<uint32_t*>(dst + i4 + D / 2) = word[1];
     }
     if (first > 0 && now > old) {
         uint32_t* words = reinterpret_cast<uint32_t*>(tile);
@@ -268,13 +294,13 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv8_kernel(const AppendAr
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if ((int)blockIdx.x < a.kv_ctas) {
-        const int n_slots = a.n_blocks * a.block_rows, lane = threadIdx.x & 31;
+        const int n_slots = a.n_blocks << a.log2_rows, lane = threadIdx.x & 31;
         const int item = blockIdx.x % (2 * a.n_kv), t0 = (int)(blockIdx.x / (2 * a.n_kv)) * a.tile;
         // the blocks of the tile's tokens (at most 31) and of the one in front, one per lane; a token leads a run if its block is another
         // than that of the token in front
         const int m = t0 - 1 + lane;
         const int s = m >= 0 && m < a.T && lane <= a.tile ? a.slots[m] : -1;
-        const int block = s >= 0 && s < n_slots ? s / a.block_rows : -1;
+        const int block = s >= 0 && s < n_slots ? s >> a.log2_rows : -1;
         const int front = __shfl_up_sync(0xffffffffu, block, 1);
         unsigned leads = __ballot_sync(0xffffffffu, lane > 0 && block >= 0 && block != front);
         for (; leads; leads &= leads - 1) {
@@ -286,28 +312,43 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv8_kernel(const AppendAr
         constexpr int UNITS = D / 8;
         static_assert(kAppendThreads % UNITS == 0, "a thread keeps its dims from head to head");
         const int i4 = 4 * (threadIdx.x % UNITS), units = a.n_q * UNITS;
-        for (int m = blockIdx.x - a.kv_ctas; m < a.T; m += gridDim.x - a.kv_ctas) {
-            const int pos = a.positions[m];
+        const int step = gridDim.x - a.kv_ctas;
+        int m = blockIdx.x - a.kv_ctas, pos = m < a.T ? a.positions[m] : -1;
+        for (; m < a.T; m += step) {
             const bool placed = pos >= 0 && pos < a.t_max;  // a row without a position: zeros
             RowValues<D> r;
             if (placed) r.load_angles(a.table, pos, i4);
-#pragma unroll 3
-            for (int u = threadIdx.x; u < units; u += kAppendThreads) {
-                const size_t row = ((size_t)m * a.n_q + u / UNITS) * D;
-                uint2 lo2 = make_uint2(0u, 0u), hi2 = lo2;
-                if (placed) {
-                    float x[8];
-                    r.load(a.q + row, i4);
-                    r.turned(x);
-                    auto pair = [](float p, float q) {
-                        const __nv_bfloat162 b = __floats2bfloat162_rn(p, q);
-                        return *reinterpret_cast<const uint32_t*>(&b);
-                    };
-                    lo2 = make_uint2(pair(x[0], x[1]), pair(x[2], x[3]));
-                    hi2 = make_uint2(pair(x[4], x[5]), pair(x[6], x[7]));
+            if (m + step < a.T) pos = a.positions[m + step];
+            const float* row = a.q + (size_t)m * a.n_q * D + i4;
+            __nv_bfloat16* out = a.q_out + (size_t)m * a.n_q * D + i4;
+            for (int u0 = threadIdx.x; u0 < units; u0 += 3 * kAppendThreads) {
+                float4 lo[3], hi[3];
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    const float* src = row + (size_t)(min(u0 + j * kAppendThreads, units - 1) / UNITS) * D;
+                    lo[j] = __ldcs(reinterpret_cast<const float4*>(src));
+                    hi[j] = __ldcs(reinterpret_cast<const float4*>(src + D / 2));
                 }
-                *reinterpret_cast<uint2*>(a.q_out + row + i4) = lo2;
-                *reinterpret_cast<uint2*>(a.q_out + row + i4 + D / 2) = hi2;
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    const int u = u0 + j * kAppendThreads;
+                    if (u >= units) break;
+                    uint2 lo2 = make_uint2(0u, 0u), hi2 = lo2;
+                    if (placed) {
+                        float x[8];
+                        r.l[0] = lo[j].x, r.l[1] = lo[j].y, r.l[2] = lo[j].z, r.l[3] = lo[j].w;
+                        r.u[0] = hi[j].x, r.u[1] = hi[j].y, r.u[2] = hi[j].z, r.u[3] = hi[j].w;
+                        r.turned(x);
+                        auto pair = [](float p, float q) {
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(p, q);
+                            return *reinterpret_cast<const uint32_t*>(&b);
+                        };
+                        lo2 = make_uint2(pair(x[0], x[1]), pair(x[2], x[3]));
+                        hi2 = make_uint2(pair(x[4], x[5]), pair(x[6], x[7]));
+                    }
+                    *reinterpret_cast<uint2*>(out + (size_t)(u / UNITS) * D) = lo2;
+                    *reinterpret_cast<uint2*>(out + (size_t)(u / UNITS) * D + D / 2) = hi2;
+                }
             }
         }
     }
@@ -1023,6 +1064,8 @@ bool kv8_dims_ok(int n_q, int n_kv, int hd, int kind, int n_blocks, int block_ro
            (long long)n_blocks * n_kv * block_rows <= (1ll << 31) - 256;
 }
 
+int log2_of(int block_rows) { return block_rows == 16 ? 4 : block_rows == 32 ? 5 : block_rows == 64 ? 6 : 7; }
+
 // rows = every (block, head, row) of the pool, columns = D bytes; a box is min(32, block) whole rows, swizzled by the row's width
 bool make_kv8_map(CUtensorMap* map, const void* pool, long long rows, int hd, int block_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
@@ -1115,7 +1158,7 @@ int bitlinear_rope_kv8(const float* q, const float* k, const float* v, const int
         return BITLINEAR_ERR_ALIGN;
     int sm_count = 0;
     if (const int rc = device_sm_count(&sm_count)) return rc;
-    AppendArgs a = {q, k, v, positions, slots, reinterpret_cast<const float2*>(rope_table), T, t_max, n_q_heads, n_kv_heads, block_rows, n_blocks,
+    AppendArgs a = {q, k, v, positions, slots, reinterpret_cast<const float2*>(rope_table), T, t_max, n_q_heads, n_kv_heads, log2_of(block_rows), n_blocks,
                     static_cast<__nv_bfloat16*>(q_out_bf16), static_cast<uint8_t*>(k_cache), static_cast<uint8_t*>(v_cache), k_scale, v_scale, 1, 0};
     // a CTA per token and head while that fits the GPU a few times over, else per tile of tokens (most of them lead no run)
     a.tile = (long long)T * 2 * n_kv_heads <= 64ll * sm_count ? 1 : 16;
@@ -1168,9 +1211,7 @@ int bitlinear_attention_decode_kv8(const void* q_bf16, const void* k_cache, cons
     CUtensorMap map_k, map_v;
     if (!make_kv8_map(&map_k, k_cache, pool_rows, head_dim, block_rows) || !make_kv8_map(&map_v, v_cache, pool_rows, head_dim, block_rows))
         return BITLINEAR_ERR_CUDA;
-    int log2_rows = 4;
-    while ((1 << log2_rows) < block_rows) ++log2_rows;
-    AttnArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, M, n_q_heads, n_kv_heads, n_seq, max_blocks, log2_rows,
+    AttnArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, M, n_q_heads, n_kv_heads, n_seq, max_blocks, log2_of(block_rows),
                   n_blocks, 1, 1.4426950408889634f / sqrtf((float)head_dim), static_cast<__nv_bfloat16*>(out_bf16),
                   reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align_up(kMaxCtas * 2 * sizeof(int2), 256)), static_cast<int2*>(ws), device_status_word()};
     const int ctas = std::min(sm_count, kMaxCtas);
