@@ -59,7 +59,8 @@ struct Crossing {
 // kThreads: of a CTA
 template <int kThreads>
 struct SampleShared {
-    static constexpr int kBins = 2 * kThreads;  // a row has two CTAs at least, and each merges its share of the bins, one per thread
+    static constexpr int kBinBits = kThreads == 512 ? 10 : 9;
+    static constexpr int kBins = 1 << kBinBits;  // two per thread: a row has two CTAs at least, and each merges its share of the bins
     static constexpr int kList = kThreads;      // candidates of a row that one CTA finishes with
     double pow2[16];                            // 2^(j / 16): one entry to a pair of banks
     float top, low;             // largest logit of the part, smallest finite one
@@ -466,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     auto narrow = [&](Crossing x, bool by_mass, uint32_t want, double target) {
         uint32_t lo = first_key(x.bin), hi = (x.bin == 0 ? top_key + 1 : first_key(x.bin - 1)) - 1;
         while (x.count > 1 && lo < hi && (by_mass || x.count_above + x.count != want)) {
-            const int shift = max(0, 32 - __clz((int)(hi - lo)) - 10);
+            const int shift = max(0, 32 - __clz((int)(hi - lo)) - Shared::kBinBits);  // hi - lo < 2^(shift + kBinBits)
             const uint32_t from = hi, to = lo;
             x = find(by_mass, true, want, target, x.count_above, x.mass_above, [&](float, uint32_t key) { return key >= to && key <= from ? (int)((from - key) >> shift) : -1; });
             hi = from - ((uint32_t)x.bin << shift);

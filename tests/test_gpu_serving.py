@@ -85,6 +85,12 @@ def test_block_tables_no_requests_and_bad_state():
     assert host(td).tolist() == [[2, 1, 0, -1]] and int(out[1][0]) == 0
 
 
+def test_block_tables_many_requests():
+    for in_place in (False, True):
+        case = tables_case(20000, 6, 16, 6, shortage=5)
+        check_tables(*case, 16, int(np.maximum(case[1], 0).sum()) - 1000, in_place)
+
+
 def test_block_tables_large_step_is_the_same_every_time():
     case = tables_case(3000, 40, 16, 5, longest=200)
     tokens = int(np.maximum(case[1], 0).sum())
@@ -283,6 +289,25 @@ def test_attention_many_rows_of_all_lengths(kind):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+def test_attention_more_rows_than_a_batch_of_lengths(kind):
+    rng = np.random.default_rng(4)
+    lengths = [int(x) for x in rng.integers(0, 40, 700)]
+    lengths[300] = 900
+    q, codes, scales, tables = attend_case(kind, 2, 1, 64, 16, lengths, 63, slack_blocks=0)
+    out = bl.bitlinear_attention_decode_kv8(q.to(DEV), *pool_to_dev(codes, scales, kind), dev(tables), dev(np.array(lengths, np.int32)), 2, 1, 64)
+    check_attention(out, q, codes, scales, tables, lengths, 2, 1, 64, kind)
+
+
+@pytest.mark.parametrize("kind,D", [(sv.INT8, 64), (sv.E4M3, 128)])
+def test_attention_long_sequence(kind, D):
+    lengths = [150001, 3]
+    q, codes, scales, tables = attend_case(kind, 6, 2, D, 128, lengths, 64)
+    out = bl.bitlinear_attention_decode_kv8(q.to(DEV), *pool_to_dev(codes, scales, kind), dev(tables), dev(np.array(lengths, np.int32)), 6, 2, D)
+    check_attention(out, q, codes, scales, tables, lengths, 6, 2, D, kind)
+    assert bl.bitlinear_poll_status() == 0
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_attention_rows_of_one_sequence_and_missing_ones(kind):
     lengths = [10, 11, 12, 400, 5, -3, 10 ** 6, 77]
     seq = [0, 0, 0, 1, 9, 1, 1, -1]
@@ -424,6 +449,33 @@ def test_sample_types_strides_and_settings_per_row(dtype, strided):
     M, V = 33, 3001
     check_sample(rng.standard_normal((M, V)) * 3, rng.random(M), dtype, strided, temperature=rng.choice([0.0, 0.5, 1.0, 2.0], M), top_k=rng.choice([0, -3, 1, 40, V, V + 9], M),
                  top_p=rng.choice([1.0, 0.9, 0.5, 1.5], M), min_p=rng.choice([0.0, 0.05, 0.3], M))
+
+
+@pytest.mark.parametrize("filters", FILTERS + [dict(top_k=300), dict(top_k=700, top_p=0.8), dict(top_p=0.97, min_p=0.001)])
+@pytest.mark.parametrize("spread", [0.6, 3.0])
+def test_sample_many_rows(filters, spread):
+    """More rows than the GPU takes at a time with a CTA per SM: smaller CTAs that share one."""
+    rng = np.random.default_rng(31)
+    l = rng.standard_normal((41, 17001)) * spread
+    l[3] = np.round(l[3])  # ties
+    l[4, 100:] = -np.inf
+    l[5] = -np.inf
+    check_sample(l, rng.random(41), **filters)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [3, 7, 130, 4097, 50001])
+def test_sample_without_filters_types_and_strides(dtype, V):
+    rng = np.random.default_rng(V)
+    l = rng.standard_normal((9, V)) * 2
+    u = rng.random(9)
+    t = rng.choice([0.0, 0.3, 1.0, 4.0], 9)
+    check_sample(l, u, dtype, True)
+    check_sample(l, u, dtype, True, temperature=t)
+    check_sample(l, u, dtype, False, temperature=t)
+    l[:, : V // 2] -= 200.0  # the parts of most warps weigh nothing
+    check_sample(l, u, dtype, True)
+    check_sample(l, np.full(9, 1 - 2.0 ** -24), dtype, True)
 
 
 @pytest.mark.parametrize("filters", FILTERS)
@@ -657,6 +709,36 @@ def test_paged_decode_step_recorded():
     for a, b in zip(run(False), run(True)):
         assert torch.equal(a, b)
     assert bl.bitlinear_poll_status() == 0
+
+
+def test_calls_on_two_streams_at_once():
+    """Independent calls, each with a workspace of its own, in flight together: the bits of the calls alone."""
+    kind, n_q, n_kv, D = sv.INT8, 20, 5, 128
+    sets = []
+    for i in range(2):
+        lengths = [900 + 50 * i, 17, 2000, 5]
+        q, codes, scales, tables = attend_case(kind, n_q, n_kv, D, 64, lengths, 120 + i)
+        g = torch.Generator(DEV).manual_seed(i)
+        sets.append((q.to(DEV), pool_to_dev(codes, scales, kind), dev(tables), dev(np.array(lengths, np.int32)),
+                     torch.randn(5, 30000, generator=g, device=DEV) * 2, torch.rand(5, generator=g, device=DEV), torch.full((5,), 0.9, device=DEV)))
+    for s in sets:
+        torch.cuda.synchronize()
+
+    def calls(s):
+        return (bl.bitlinear_attention_decode_kv8(s[0], *s[1], s[2], s[3], n_q, n_kv, D), *bl.bitlinear_sample(s[4], s[5], top_p=s[6]), *bl.bitlinear_sample(s[4], s[5]))
+
+    alone = [calls(s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(20):
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                outs.append(calls(s))
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        for a, b in zip(out, alone[i % 2]):
+            assert torch.equal(a, b)
 
 
 def test_binding_checks_shapes_types_and_devices():
