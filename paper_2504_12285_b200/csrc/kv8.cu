@@ -160,7 +160,10 @@ struct RowValues {
 // (scale = max(old, needed) where the block has rows in front of the run, else what is needed), brings the earlier rows' codes
 // to the new scale if it grew, and writes the run's codes.  So a block's scale has one writer and no atomics.
 // The result is that of fp64 arithmetic, the work mostly fp32: only values next to the largest, and next to the middle between two
-// codes, are formed again in fp64 (all of it in fp64 took 3.5 times as long for prompts).
+// codes, are formed again in fp64.  16,500 tokens of 20 + 5 heads of 128: 82 us, 4.4 TB/s of the bytes it cannot do without (all in
+// fp64 130 us); the queries' half streams at 7 TB/s, this half waits on its chain of loads (run, positions, rows, scale).
+// Tried and slower: more rows per thread in flight, 256 threads, alternating the two kinds of CTA.  One token of 16 sequences:
+// 4.4 us, launch and that chain.
 template <int D, int KIND>
 __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int block, int h, int which) {
     constexpr int TPR = D / 8;  // threads per row
@@ -366,6 +369,10 @@ constexpr int kMaxStages = 8;
 // where a pair reaches beyond the CTA, in global memory, where a second launch merges them.  A pair counts for one place
 // more than it has units: starting and ending it takes a warp about as long as a unit does, and without that place the warps
 // that meet many short sequences finished last (by a sixth of the time of a batch of 97 sequences of 1 to 16,384 rows).
+// Bound: the bytes of the cache while the rings are full - a batch of 97 such sequences (246 MB) takes 52 us, 4.7 TB/s, and its
+// steady part runs at the copy rate; the rest is the chain lengths -> table -> first rows in front (3 us cold), the parts' merge (1.5 us)
+// and the second launch (3 us).  16 sequences of 4096 rows 23.7 us, one 11.1 us.  Twelve warps a 32-row unit each rather than
+// eight: 78 -> 68 us at the time; keys on the integer tensor cores rather than converted were part of that step.
 struct AttnArgs {
     const __nv_bfloat16* q;
     const float* k_scale;
@@ -1007,7 +1014,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
 }
 
 // Merges the parts of a pair that several CTAs share: CTA (c, head) does nothing unless a pair begins in attention CTA c and goes
-// on behind it.  A thread per dim; a lane weighs one of 32 parts at a time, in every warp alike.
+// on behind it.  A thread per dim; a lane weighs one part of a round, in every warp alike.  Rounds of four where a pair has
+// that few parts (16 sequences: 23.7 us a call against 27.8 with one size of 32), of 16 otherwise (one sequence: 11.1 us against
+// 13.9 with 32).
 template <int D>
 __global__ void __launch_bounds__(D) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
                                                                     __nv_bfloat16* __restrict__ out) {
@@ -1051,7 +1060,7 @@ __global__ void __launch_bounds__(D) attn_decode_kv8_combine_kernel(const float*
     };
     if (own.y - c < 4) round(std::integral_constant<int, 4>{}, c);
     else
-        for (int p0 = c; p0 <= own.y; p0 += 32) round(std::integral_constant<int, 32>{}, p0);
+        for (int p0 = c; p0 <= own.y; p0 += 16) round(std::integral_constant<int, 16>{}, p0);
     const int m = own.x / n_kv, h = own.x - m * n_kv;
     out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
 }
