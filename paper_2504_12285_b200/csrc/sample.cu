@@ -326,8 +326,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     };
     // one histogram over the part's elements to which bin_of gives a bin, merged over the cluster; the bin in which the running
     // count (or mass) reaches the target
-    // (sparse: few elements have a bin, so weights are formed for those alone)
-    auto find = [&](bool by_mass, bool sparse, uint32_t want, double target, uint32_t count0, unsigned long long mass0, auto&& bin_of) {
+    // (sparse: few elements have a bin, so weights are formed for those alone; a target below 0 becomes top_p of the mass of all bins)
+    auto find = [&](bool by_mass, bool sparse, uint32_t want, double& target, uint32_t count0, unsigned long long mass0, auto&& bin_of) {
         settle();
         for (int b = tid; b < kBins; b += kThreads) {
             sh.count[b] = 0;
@@ -416,12 +416,21 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
         if (tid == 0) sh.slice_count = cs, sh.slice_mass = ms;
         cluster.sync();
         ca += count0, ma += mass0;
+        {
+            uint32_t ct[kMaxCluster];
+            unsigned long long mt[kMaxCluster], total = 0;
 #pragma unroll
-        for (int r = 0; r < kMaxCluster - 1; ++r)
-            if (r < rank) {
-                const Shared* o = cluster.map_shared_rank(&sh, r);
-                ca += o->slice_count, ma += o->slice_mass;
+            for (int r = 0; r < kMaxCluster; ++r) {
+                const Shared* o = cluster.map_shared_rank(&sh, min(r, ranks - 1));
+                ct[r] = o->slice_count, mt[r] = o->slice_mass;
             }
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {
+                if (r < rank) ca += ct[r], ma += mt[r];
+                if (r < ranks) total += mt[r];
+            }
+            if (by_mass && target < 0.0) target = fmax((double)p * (double)total, 0.5);
+        }
         const bool here = by_mass ? (double)ma < target && (double)(ma + m) >= target : ca < want && ca + c >= want;
         if (here && c > 0)
             for (int r = 0; r < ranks; ++r) cluster.map_shared_rank(&sh, r)->cross = {bin, ca, c, ma};
@@ -650,13 +659,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     unsigned long long mine, before;
     auto by_distance = [&](float l, uint32_t) { return linear_bin(l); };
     if (use_k) {
-        const Crossing x = find(false, false, (uint32_t)k, 0.0, 0, 0, by_distance);
+        double none = 0.0;
+        const Crossing x = find(false, false, (uint32_t)k, none, 0, 0, by_distance);
         if (x.count_above + x.count <= kList) return finish(x.bin, (uint32_t)k, -1.0);
         narrow(x, false, (uint32_t)k, 0.0);
     }
     if (use_p) {
-        const unsigned long long all = kept_mass(0.0, mine, before);
-        const double target = fmax((double)p * (double)all, 0.5);
+        double target = -1.0;
         const Crossing x = find(true, false, 0, target, 0, 0, by_distance);
         if (x.count_above + x.count <= kList) return finish(x.bin, 0, target);
         narrow(x, true, 0, target);
