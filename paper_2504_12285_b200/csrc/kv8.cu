@@ -359,7 +359,10 @@ __global__ void __launch_bounds__(kAppendThreads) rope_kv8_kernel(const AppendAr
 
 // ---------------------------------------------------------------------------------------------- decode attention
 
-constexpr int kUnit = 32;        // cache rows a warp takes at a time
+// cache rows a warp takes at a time: 8 KB of codes either way (32 rows of 64 dims, half of that, left the copy rate at 3.4 TB/s: a unit's fixed
+// cost - issuing, softmax statistics - was as long as its arithmetic)
+constexpr int unit_rows(int D) { return D == 64 ? 64 : 32; }
+constexpr int kMinUnit = 32;
 constexpr int kMaxCtas = 160;    // one CTA per SM; partial results are reserved for this many
 constexpr int kMaxStages = 8;
 
@@ -371,7 +374,7 @@ constexpr int kMaxStages = 8;
 // that meet many short sequences finished last (by a sixth of the time of a batch of 97 sequences of 1 to 16,384 rows).
 // Bound: the bytes of the cache while the rings are full - a batch of 97 such sequences (246 MB) takes 52 us, 4.7 TB/s, and its
 // steady part runs at the copy rate; the rest is the chain lengths -> table -> first rows in front (3 us cold), the parts' merge (1.5 us)
-// and the second launch (3 us).  16 sequences of 4096 rows 23.7 us, one 11.1 us.  Twelve warps a 32-row unit each rather than
+// and the second launch (3 us).  16 sequences of 4096 rows 23.7 us, one 11.1 us.  Twelve warps rather than
 // eight: 78 -> 68 us at the time; keys on the integer tensor cores rather than converted were part of that step.
 struct AttnArgs {
     const __nv_bfloat16* q;
@@ -391,11 +394,12 @@ struct AttnArgs {
 
 struct __align__(16) UnitMeta {
     int m, h;
-    uint32_t rows;       // live rows, one bit each
     int flags;           // 1: first unit of this run's part of the pair, 2: last
-    float ks[2], vs[2];  // scales of the unit's halves
-    int unit, units;     // its number in the pair, of how many
-    int at, pad;         // its place in the order of all
+    int unit;            // its number in the pair,
+    int units;           // of how many
+    int at;              // its place in the order of all
+    uint32_t rows[2];    // live rows, one bit each
+    float ks[4], vs[4];  // scales of each sixteen rows
 };
 
 struct __align__(16) PartHead {
@@ -413,7 +417,8 @@ __device__ __forceinline__ int clamped_len(const AttnArgs& a, int seq, int len) 
     return seq < 0 || seq >= a.n_seq ? 0 : min(max(len, 0), a.max_blocks << a.log2_rows);
 }
 // units of a (row, head) pair: at least one, so that an empty row has someone to write its zeros
-__device__ __forceinline__ int units_of(int len) { return max(1, (len + kUnit - 1) / kUnit); }
+template <int UNIT>
+__device__ __forceinline__ int units_of(int len) { return max(1, (len + UNIT - 1) / UNIT); }
 
 // The order in which the rows of an eight-row group take the tensor core's row slots.  Any order is right as long as scores and
 // values use the same one; in this one neither read of a swizzled tile meets a bank twice (checked for 64- and 128-byte rows).
@@ -486,7 +491,7 @@ struct AttnSmem {
 };
 __host__ __device__ inline AttnSmem attn8_smem(int group, int D, int warps, int stages) {
     AttnSmem s;
-    s.meta = (size_t)warps * stages * 2 * kUnit * D;
+    s.meta = (size_t)warps * stages * 2 * (D == 64 ? 64 : 32) * D;
     s.parts = s.meta + (size_t)warps * stages * sizeof(UnitMeta);
     s.bars = s.parts + warps * part_smem(group, D);
     s.total = s.bars + (size_t)warps * stages * 8 + 16 + (size_t)warps * 4;
@@ -517,7 +522,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     constexpr int KS = D / 16;     // 16-dim tiles of the result
     constexpr int VW = D / 32;     // 32-bit words of a value row per lane
     constexpr bool INT8 = KIND == BITLINEAR_KV_INT8;
-    constexpr uint32_t kUnitBytes = 2u * kUnit * D;  // keys, then values
+    constexpr int UNIT = D == 64 ? 64 : 32, PIECES = UNIT / 16;  // the tensor core takes sixteen rows at a time
+    constexpr uint32_t kUnitBytes = 2u * UNIT * D;  // keys, then values
     extern __shared__ uint8_t attn8_raw[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, qd = lane & 3;
     const int group = a.n_q / a.n_kv, stages = a.stages;
@@ -532,7 +538,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     int* second_used = const_cast<int*>(abort_flag) + 4;
     if (tid == 0) *abort_flag = 0;
     if (lane == 0) {
-        for (int s = 0; s < stages; ++s) mbar_init(full + 8u * s, 5);  // the copies' announcement and four scales
+        for (int s = 0; s < stages; ++s) mbar_init(full + 8u * s, 1 + 2 * PIECES);  // the copies' announcement and the scales
         mbar_init_fence();
         reinterpret_cast<PartHead*>(parts0 + warp * part_smem(group, D))->used = 0;
         second_used[warp] = 0;
@@ -561,7 +567,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     for (int m0 = 0; m0 < a.M; m0 += 32 * BATCH) {
         load_lens(m0);
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) total += lens[i] >= 0 ? units_of(lens[i]) + 1 : 0;
+        for (int i = 0; i < BATCH; ++i) total += lens[i] >= 0 ? units_of<UNIT>(lens[i]) + 1 : 0;
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
@@ -576,7 +582,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
                 if (pm < a.M || m0 + 32 * i >= a.M) break;
-                const int n = lens[i] >= 0 ? (units_of(lens[i]) + 1) * a.n_kv : 0;
+                const int n = lens[i] >= 0 ? (units_of<UNIT>(lens[i]) + 1) * a.n_kv : 0;
                 int incl = n;
 #pragma unroll
                 for (int d = 1; d < 32; d <<= 1) {
@@ -588,7 +594,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
                     const int src = __ffs((int)past) - 1;
                     pm = m0 + 32 * i + src;
                     p_len = __shfl_sync(0xffffffffu, lens[i], src);
-                    p_units = units_of(p_len);
+                    p_units = units_of<UNIT>(p_len);
                     const int in_row = u0 - base - __shfl_sync(0xffffffffu, incl - n, src);
                     ph = (int)((unsigned)in_row / (unsigned)(p_units + 1));
                     p_unit = in_row - ph * (p_units + 1) - 1;
@@ -601,7 +607,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
 
     // ---- producer side: issue the next unit of the run into its ring place
     const uint64_t once = l2_evict_first_policy();
-    const int rows_log2 = a.log2_rows, per_unit = rows_log2 < 5 ? 2 : 1;  // blocks a unit spans
+    const int rows_log2 = a.log2_rows, per_unit = max(1, UNIT >> a.log2_rows);  // blocks a unit spans
     int w_id = -1, w_base = 0, w_end = 0;  // lane l holds entry w_base + l of row pm's table, up to w_end
     int p_seq = 0, n_seq_raw = 0, n_len_raw = 0;  // the row's sequence; the next row's, fetched while this one is at work
     auto fetch_next_row = [&]() {
@@ -617,7 +623,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     int issued = 0;
     auto issue = [&]() {
         const int place = issued % stages;
-        const int b = (p_unit * kUnit) >> rows_log2;
+        const int b = (p_unit * UNIT) >> rows_log2;
         if (b < w_base || b + per_unit > w_end) {
             w_base = b;
             w_end = b + 32;
@@ -625,41 +631,46 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             w_id = ((long long)idx << rows_log2) < p_len ? a.tables[(size_t)p_seq * a.max_blocks + idx] : -1;
             if (w_id >= a.n_blocks) w_id = -1;
         }
-        const int l0 = b - w_base, l1 = l0 + per_unit - 1;
-        const int id0 = __shfl_sync(0xffffffffu, w_id, l0), id1 = __shfl_sync(0xffffffffu, w_id, l1);
+        int id[PIECES];  // the block of each sixteen rows
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) id[i] = __shfl_sync(0xffffffffu, w_id, ((p_unit * UNIT + 16 * i) >> rows_log2) - w_base);
         const bool pair_end = p_unit == p_units - 1;
         const int after = next + (pair_end ? 2 : 1);
         const uint32_t bar = full + 8u * place;
         UnitMeta& w = meta[place];
-        if (lane < 4) {  // scales: keys of both halves, values of both
-            const int id = lane & 1 ? id1 : id0;
-            const float* src = (lane & 2 ? a.v_scale : a.k_scale) + (size_t)max(id, 0) * a.n_kv + ph;
-            if (id >= 0) copy_word(smem_u32(&w.ks[lane]), src, bar);
+        if (lane < 2 * PIECES) {  // scales: keys of every piece, then values
+            const int i = lane % PIECES;
+            int block = id[0];
+#pragma unroll
+            for (int j = 1; j < PIECES; ++j) block = i == j ? id[j] : block;
+            float* dst = (lane < PIECES ? w.ks : w.vs) + i;
+            const float* src = (lane < PIECES ? a.k_scale : a.v_scale) + (size_t)max(block, 0) * a.n_kv + ph;
+            if (block >= 0) copy_word(smem_u32(dst), src, bar);
             else {
-                (&w.ks[0])[lane] = 0.0f;
+                *dst = 0.0f;
                 mbar_arrive(bar);
             }
         }
         if (lane == 0) {
-            const int live = min(max(p_len - p_unit * kUnit, 0), kUnit);
-            uint32_t rows = live == 32 ? 0xffffffffu : (1u << live) - 1u;
-            if (id0 < 0) rows &= 0xffff0000u;
-            if (id1 < 0) rows &= 0x0000ffffu;
-            *reinterpret_cast<int4*>(&w.m) = make_int4(pm, ph, (int)rows, (issued == 0 || p_unit == 0 ? 1 : 0) | (pair_end || after >= u1 ? 2 : 0));
-            *reinterpret_cast<int4*>(&w.unit) = make_int4(p_unit, p_units, next, 0);
-            const uint32_t dst = ring + (uint32_t)place * kUnitBytes;
-            const uint32_t off = (uint32_t)(p_unit * kUnit) & ((1u << rows_log2) - 1u);
-            const uint32_t copies = per_unit == 1 ? (id0 >= 0 ? 1u : 0u) : (id0 >= 0 ? 1u : 0u) + (id1 >= 0 ? 1u : 0u);
-            mbar_expect_tx(bar, copies * (kUnitBytes / per_unit));
-            if (id0 >= 0) {
-                const int row = ((id0 * a.n_kv + ph) << rows_log2) + (int)off;
-                tma_rows(dst, &map_k, row, bar, once);
-                tma_rows(dst + kUnitBytes / 2, &map_v, row, bar, once);
+            const int live = min(max(p_len - p_unit * UNIT, 0), UNIT);
+            unsigned long long rows = live == 64 ? ~0ull : (1ull << live) - 1ull;
+            uint32_t there = 0;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                if (id[i] < 0) rows &= ~(0xffffull << (16 * i));
+                else ++there;
             }
-            if (per_unit == 2 && id1 >= 0) {
-                const int row = (id1 * a.n_kv + ph) << rows_log2;
-                tma_rows(dst + 16 * D, &map_k, row, bar, once);
-                tma_rows(dst + kUnitBytes / 2 + 16 * D, &map_v, row, bar, once);
+            *reinterpret_cast<int4*>(&w.m) = make_int4(pm, ph, (issued == 0 || p_unit == 0 ? 1 : 0) | (pair_end || after >= u1 ? 2 : 0), p_unit);
+            *reinterpret_cast<int4*>(&w.units) = make_int4(p_units, next, (int)(uint32_t)rows, (int)(uint32_t)(rows >> 32));
+            const uint32_t dst = ring + (uint32_t)place * kUnitBytes;
+            mbar_expect_tx(bar, there * (kUnitBytes / PIECES));
+            const int off = (p_unit * UNIT) & ((1 << rows_log2) - 1), step = PIECES / per_unit;  // pieces of a copy
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                if (i % step != 0 || id[i] < 0) continue;
+                const int row = ((id[i] * a.n_kv + ph) << rows_log2) + (per_unit == 1 ? off : 0);
+                tma_rows(dst + 16 * i * D, &map_k, row, bar, once);
+                tma_rows(dst + kUnitBytes / 2 + 16 * i * D, &map_v, row, bar, once);
             }
         }
         ++issued;
@@ -673,7 +684,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
                 ++pm;
                 p_seq = n_seq_raw;
                 p_len = clamped_len(a, n_seq_raw, n_len_raw);
-                p_units = units_of(p_len);
+                p_units = units_of<UNIT>(p_len);
                 if (next < u1) fetch_next_row();
             }
         }
@@ -748,20 +759,22 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     };
 
     auto consume = [&](uint32_t base, const UnitMeta& w) {
-        const uint32_t rows = w.rows;
+        const uint32_t rows[2] = {w.rows[0], UNIT == 64 ? w.rows[1] : 0xffffffffu};
+        const bool whole = (rows[0] & rows[1]) == 0xffffffffu;
         const uint32_t vbase = base + kUnitBytes / 2;
-        if (rows != 0xffffffffu) {  // dead rows may hold any bits, and zero times NaN is NaN: overwrite their values
-            for (int i = lane; i < kUnit * (D / 16); i += 32) {
-                if (!((rows >> (i / (D / 16))) & 1u))
+        if (!whole) {  // dead rows may hold any bits, and zero times NaN is NaN: overwrite their values
+            for (int i = lane; i < UNIT * (D / 16); i += 32) {
+                const int row = i / (D / 16);
+                if (!((rows[row >> 5] >> (row & 31)) & 1u))
                     asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vbase + 16u * i), "r"(0u) : "memory");
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the ring place is a copy's target again later
             __syncwarp();
         }
-        // scores of both halves: S^T (16 rows x 8 heads) = K (16 x D) Q^T
-        float sv[2][4];
+        // scores of every piece: S^T (16 rows x 8 heads) = K (16 x D) Q^T
+        float sv[PIECES][4];
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
+        for (int hb = 0; hb < PIECES; ++hb) {
             const uint32_t row_lo = base + (uint32_t)(16 * hb + r_lo) * D, row_hi = row_lo + 8 * D;
             uint32_t x[D / 64][4], y[D / 64][4];
 #pragma unroll
@@ -811,17 +824,24 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             sv[hb][2] = s[2] * ks0;
             sv[hb][3] = s[3] * ks1;
         }
-        if (rows != 0xffffffffu) {  // a dead row may hold anything: selected away
+        if (!whole) {  // a dead row may hold anything: selected away
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb) {
-                if (!((rows >> (16 * hb + r_lo)) & 1u)) sv[hb][0] = sv[hb][1] = -INFINITY;
-                if (!((rows >> (16 * hb + 8 + r_lo)) & 1u)) sv[hb][2] = sv[hb][3] = -INFINITY;
+            for (int hb = 0; hb < PIECES; ++hb) {
+                const uint32_t piece = rows[hb >> 1] >> (16 * (hb & 1));
+                if (!((piece >> r_lo) & 1u)) sv[hb][0] = sv[hb][1] = -INFINITY;
+                if (!((piece >> (8 + r_lo)) & 1u)) sv[hb][2] = sv[hb][3] = -INFINITY;
             }
         }
-        float mx0 = fmaxf(fmaxf(sv[0][0], sv[0][2]), fmaxf(sv[1][0], sv[1][2]));
-        float mx1 = fmaxf(fmaxf(sv[0][1], sv[0][3]), fmaxf(sv[1][1], sv[1][3]));
+        float mx0 = fmaxf(sv[0][0], sv[0][2]), mx1 = fmaxf(sv[0][1], sv[0][3]);
+#pragma unroll
+        for (int hb = 1; hb < PIECES; ++hb) {
+            mx0 = fmaxf(mx0, fmaxf(sv[hb][0], sv[hb][2]));
+            mx1 = fmaxf(mx1, fmaxf(sv[hb][1], sv[hb][3]));
+        }
         // The values' scales ride on the weights: o is held in units of the largest scale met so far.
-        const float vs = fmaxf(w.vs[0], w.vs[1]);
+        float vs = w.vs[0];
+#pragma unroll
+        for (int hb = 1; hb < PIECES; ++hb) vs = fmaxf(vs, w.vs[hb]);
         if (__any_sync(0xffffffffu, mx0 > m_run[0] || mx1 > m_run[1] || vs > v_ref)) {
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) {
@@ -847,7 +867,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         const float b0 = m_run[0] == -INFINITY ? 0.0f : m_run[0], b1 = m_run[1] == -INFINITY ? 0.0f : m_run[1];
         const float per_ref = v_ref > 0.0f ? __fdividef(32768.0f, v_ref) : 0.0f;
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
+        for (int hb = 0; hb < PIECES; ++hb) {
             // O^T (D x 8 heads) += V^T (D x 16 rows) P; lane (g, qd) holds dims 2 KS g ... of rows in slots 2qd, 2qd+1 (+8)
             uint32_t x[4][VW];
 #pragma unroll
@@ -1081,7 +1101,7 @@ bool make_kv8_map(CUtensorMap* map, const void* pool, long long rows, int hd, in
     if (!fn) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)hd, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)hd};
-    const cuuint32_t box[2] = {(cuuint32_t)hd, (cuuint32_t)std::min(block_rows, kUnit)};
+    const cuuint32_t box[2] = {(cuuint32_t)hd, (cuuint32_t)std::min(block_rows, unit_rows(hd))};
     const cuuint32_t estr[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -1208,7 +1228,7 @@ int bitlinear_attention_decode_kv8(const void* q_bf16, const void* k_cache, cons
     if (kv_dtype != BITLINEAR_KV_INT8 && kv_dtype != BITLINEAR_KV_E4M3) return BITLINEAR_ERR_DTYPE;
     if (M < 0 || M > 65535 || n_seq <= 0 || max_blocks <= 0 || !kv8_dims_ok(n_q_heads, n_kv_heads, head_dim, kv_dtype, n_blocks, block_rows) ||
         (long long)max_blocks * block_rows > (1ll << 30) || (!seq_ids && n_seq < M) ||
-        (double)M * n_kv_heads * (((double)max_blocks * block_rows + kUnit - 1) / kUnit + 1) > 2147483000.0)
+        (double)M * n_kv_heads * (((double)max_blocks * block_rows + kMinUnit - 1) / kMinUnit + 1) > 2147483000.0)
         return BITLINEAR_ERR_SHAPE;
     if (M == 0) return BITLINEAR_OK;
     if (!q_bf16 || !k_cache || !v_cache || !k_scale || !v_scale || !tables || !lengths || !out_bf16) return BITLINEAR_ERR_NULL;
