@@ -10,8 +10,8 @@
 // over an order-preserving integer image of the logits within the bin that holds the threshold, until that bin is taken
 // whole or holds equal logits only.
 //
-// One row of 128,256 with every filter takes 17 us: load 2, each pass over the row 2 to 5, each meeting of the cluster 0.7;
-// 16 rows of mixed settings 37 us, those with a wide top-p set the time: four shared-memory additions per element.
+// One row of 128,256 with every filter takes 16 us: load 2, each pass over the row 2 to 5, each meeting of the cluster 0.7;
+// 16 rows of mixed settings 34 us, those with a wide top-p set the time: four shared-memory additions per element.
 //
 // Which token comes out hangs on sums next to a border, so weights are formed in fp64 and summed as integers in units of
 // 2^-44: sums of any order are the same, and no two machines' rounding of a sum decides a token.
