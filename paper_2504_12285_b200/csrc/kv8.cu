@@ -51,11 +51,12 @@ __device__ __forceinline__ uint32_t code_of(double value, double scale) {
 }
 // The same from an fp32 value and the reciprocal of the scale; false where they cannot tell: next to the middle between two codes.
 // `off` bounds the error of value * inv.  For keys a rotated pair's components are at most sqrt 2 of the block's largest magnitude
-// before the turn, two products and a sum round by 2^-24 each, and that magnitude is at most 127 (448) steps: 6e-5 (1.6e-4) with the
-// reciprocal's and the product's own rounding.  Values come as they are: 2.3e-5 (none, the scale is a power of two).
+// before the turn, two products and a sum round by 2^-24 each, and that magnitude is at most 127 (448) steps: 6e-5 (2.1e-4) with the
+// reciprocal's and the product's own rounding.  Values come as they are: 2.3e-5 (5.4e-5, and none where the scale is a power of two, as it
+// is unless something else wrote the block's first rows).
 template <int KIND>
 __device__ __forceinline__ float quick_error(bool keys) {
-    return KIND == BITLINEAR_KV_INT8 ? (keys ? 1e-4f : 4e-5f) : (keys ? 2e-4f : 0.0f);
+    return KIND == BITLINEAR_KV_INT8 ? (keys ? 1e-4f : 4e-5f) : (keys ? 3e-4f : 1e-4f);
 }
 // Eight codes in two words; false if one of them cannot be told.  int8: adding 1.5 * 2^23 rounds to the nearest whole number, ties to even, and
 // leaves it in the low bits (no value is more than 127 steps: the scale is what the largest needs, or more).  e4m3: both ends of the
@@ -64,17 +65,17 @@ template <int KIND>
 __device__ __forceinline__ bool quick_codes(const float (&x)[8], float inv, float off, uint32_t (&word)[2]) {
     if constexpr (KIND == BITLINEAR_KV_INT8) {
         constexpr float kRound = 12582912.0f;
-        float worst = 0.0f;
+        bool sure = true;
         uint32_t t[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float y = fmaf(x[e], inv, kRound);
-            worst = fmaxf(worst, fabsf(fmaf(x[e], inv, kRound - y)));
+            sure = sure && fabsf(fmaf(x[e], inv, kRound - y)) < 0.5f - off;
             t[e] = __float_as_uint(y);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) word[h] = __byte_perm(__byte_perm(t[4 * h], t[4 * h + 1], 0x0040), __byte_perm(t[4 * h + 2], t[4 * h + 3], 0x0040), 0x5410);
-        return worst < 0.5f - off;
+        return sure;
     } else {
         uint32_t differ = 0;
 #pragma unroll
@@ -95,8 +96,8 @@ __device__ __forceinline__ bool quick_codes(const float (&x)[8], float inv, floa
 // int8, where some value of a row is next to the middle between two codes: the value in fp64 against the middle nearest to its
 // approximate quotient, times the scale (exact), instead of a division
 template <int KIND>
-__device__ __forceinline__ uint32_t close_code(double value, float quotient, double scale) {
-    const float low = floorf(quotient);  // the middle above it is the only one within 0.5
+__device__ __forceinline__ uint32_t close_code(double value, float inv, double scale) {
+    const float low = floorf((float)(value * (double)inv));  // the middle above it is the only one within 0.5
     const double gap = value - ((double)low + 0.5) * scale;
     const int c = (int)low + (gap > 0.0 || (gap == 0.0 && ((int)low & 1)) ? 1 : 0);
     return (uint32_t)min(max(c, -127), 127) & 0xffu;
@@ -262,18 +263,19 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     const float old = scale_s[0], now = scale_s[1];
     const double s = (double)now;
     const float inv = __frcp_rn(now), off = quick_error<KIND>(which == 0);
+    const bool overflow = !(top < INFINITY);  // a rotated value beyond fp32
 #pragma unroll 2
     for (int m = m0 + sub; m < end; m += ROWS) {
         const int pos = a.positions[m];
         if (pos < 0 || pos >= a.t_max) continue;
         load(m, pos);
         uint32_t word[2];
-        if (!quick_codes<KIND>(x, inv, off, word)) {
+        if (overflow || !quick_codes<KIND>(x, inv, off, word)) {
             word[0] = word[1] = 0u;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const double value = which == 0 ? r.exact(e) : (double)x[e];
-                word[e >> 2] |= (KIND == BITLINEAR_KV_INT8 ? close_code<KIND>(value, x[e] * inv, s) : code_of<KIND>(value, s)) << (8 * (e & 3));
+                word[e >> 2] |= (KIND == BITLINEAR_KV_INT8 ? close_code<KIND>(value, inv, s) : code_of<KIND>(value, s)) << (8 * (e & 3));
             }
         }
         uint8_t* dst = tile + (size_t)(a.slots[m] - (block << a.log2_rows)) * D;

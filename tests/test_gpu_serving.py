@@ -193,6 +193,28 @@ def test_append_extreme_magnitudes(kind, size):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+def test_append_keeps_any_scale_and_survives_fp32_overflow(kind):
+    """A block whose scale something else wrote (no power of two, far larger than needed), and keys whose rotation leaves fp32."""
+    n_kv, D, rows, T = 2, 64, 16, 24
+    rng = np.random.default_rng(5)
+    k, v = ((rng.standard_normal((T, n_kv * D)) * 3).astype(np.float32) for _ in range(2))
+    k[16:] = np.sign(k[16:]) * np.float32(3.3e38)
+    slots = np.array([16 * (t // 4) + 3 + t % 4 for t in range(T)], np.int32)
+    pos = rng.integers(0, 200, T).astype(np.int32)
+    codes, scales = make_pool(7, n_kv, rows, D, kind, 6)
+    for s in scales:
+        s[:3] = rng.uniform(0.01, 0.7, (3, n_kv)).astype(np.float32)
+    pool = pool_to_dev(codes, scales, kind)
+    table = bl.bitlinear_rope_table(D, 200, device=DEV)
+    bl.bitlinear_rope_kv8(torch.zeros(T, 4 * D, device=DEV), dev(k), dev(v), dev(pos), dev(slots), table, *pool, 4, n_kv, D)
+    with np.errstate(over="ignore"):
+        sv.append8(sv.rotate(k.reshape(T, n_kv, D), pos, host(table)), slots, codes[0], scales[0], kind)
+        sv.append8(v.reshape(T, n_kv, D).astype(np.float64), slots, codes[1], scales[1], kind)
+    for got, want in zip(pool, codes + scales):
+        assert np.array_equal(host(got), want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_append_rounds_the_middle_to_even(kind):
     # values exactly in the middle between two codes: position 0 turns nothing, so they arrive as given
     D, rows = 64, 16
