@@ -1002,21 +1002,31 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             // lane i weighs part i (the 64 elements of a warp belong to one head)
             const bool mine = lane < 2 * WARPS && ((mask >> lane) & 1u);
             const float pm_ = mine ? part_at(lane)->m_run[head] : -INFINITY;
-            float top = pm_;
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float pl = mine ? part_at(lane)->l_run[head] : 0.0f;
+            float top;
+            asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(top) : "f"(pm_));
             const float f = pm_ == -INFINITY ? 0.0f : ex2(pm_ - top);
-            float l = mine ? part_at(lane)->l_run[head] * f : 0.0f;
+            float l = pl * f;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) l += __shfl_xor_sync(0xffffffffu, l, off);
             float2 acc = make_float2(0.0f, 0.0f);
+            for (uint32_t mk = mask; mk;) {  // four parts at a time, their loads side by side
+                float2 v[4];
+                float w[4];
 #pragma unroll
-            for (int i = 0; i < 2 * WARPS; ++i) {
-                if (!((mask >> i) & 1u)) continue;
-                const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(part_at(i) + 1) + e);
-                const float w = __shfl_sync(0xffffffffu, f, i);
-                acc.x = fmaf(v.x, w, acc.x);
-                acc.y = fmaf(v.y, w, acc.y);
+                for (int k = 0; k < 4; ++k) {
+                    const bool on = mk != 0;
+                    const int i = __ffs((int)(on ? mk : mask)) - 1;
+                    mk &= mk - 1;
+                    v[k] = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(part_at(i) + 1) + e);
+                    w[k] = __shfl_sync(0xffffffffu, f, i);
+                    if (!on) w[k] = 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    acc.x = fmaf(v[k].x, w[k], acc.x);
+                    acc.y = fmaf(v[k].y, w[k], acc.y);
+                }
             }
             if (whole) {
                 const float inv = l > 0.0f ? 1.0f / l : 0.0f;
