@@ -1045,16 +1045,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     if (tid == 0) *reinterpret_cast<int4*>(a.desc + 2 * blockIdx.x) = make_int4(desc0.x, desc0.y, desc1.x, desc1.y);
 }
 
-// Merges the parts of a pair that several CTAs share: CTA (c, head) does nothing unless a pair begins in attention CTA c and goes
-// on behind it.  A thread per dim; a lane weighs one part of a round, in every warp alike.  Rounds of four where a pair has
+// Merges the parts of a pair that several CTAs share: CTA c does nothing unless a pair begins in attention CTA c and goes on
+// behind it.  A thread per head and dim (a CTA per head is 0.8 us slower); a lane weighs one part of a round, in every warp alike.  Rounds of four where a pair has
 // that few parts (16 sequences: 23.7 us a call against 27.8 with one size of 32), of 16 otherwise (one sequence: 11.1 us against
 // 13.9 with 32).
 template <int D>
-__global__ void __launch_bounds__(D) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
+__global__ void __launch_bounds__(8 * D) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
                                                                     __nv_bfloat16* __restrict__ out) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int c = blockIdx.x, head = blockIdx.y, lane = threadIdx.x & 31;
+    const int c = blockIdx.x, head = threadIdx.y, lane = threadIdx.x & 31;
     const int2 own = desc[2 * c + 1];
     if (own.x < 0) return;
     const size_t stride = part_floats(group, D);
@@ -1160,8 +1160,8 @@ int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a,
         cudaGetLastError();
         return BITLINEAR_ERR_CUDA;
     }
-    cfg.gridDim = dim3((unsigned)ctas, (unsigned)group);
-    cfg.blockDim = dim3(D);
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(D, (unsigned)group);
     cfg.dynamicSmemBytes = 0;
     if (cudaLaunchKernelEx(&cfg, attn_decode_kv8_combine_kernel<D>, (const float*)a.part, (const int2*)a.desc, group, a.n_kv, a.out) != cudaSuccess) {
         cudaGetLastError();
