@@ -374,9 +374,9 @@ constexpr int kMaxStages = 8;
 // where a pair reaches beyond the CTA, in global memory, where a second launch merges them.  A pair counts for one place
 // more than it has units: starting and ending it takes a warp about as long as a unit does, and without that place the warps
 // that meet many short sequences finished last (by a sixth of the time of a batch of 97 sequences of 1 to 16,384 rows).
-// Bound: the bytes of the cache while the rings are full - a batch of 97 such sequences (246 MB) takes 52 us, 4.7 TB/s, and its
-// steady part runs at the copy rate; the rest is the chain lengths -> table -> first rows in front (3 us cold), the parts' merge (1.5 us)
-// and the second launch (3 us).  16 sequences of 4096 rows 23.7 us, one 11.1 us.  Twelve warps rather than
+// Bound: the bytes of the cache while the rings are full - a batch of 97 such sequences (246 MB) takes 50 us, 4.9 TB/s, and its
+// steady part runs at the copy rate; the rest is the chain lengths -> table -> first rows in front (3 us cold), the parts' merge (1 us)
+// and the second launch (2.5 us).  16 sequences of 4096 rows 22.7 us, one 10.7 us.  Twelve warps rather than
 // eight: 78 -> 68 us at the time; keys on the integer tensor cores rather than converted were part of that step.
 struct AttnArgs {
     const __nv_bfloat16* q;
@@ -1047,8 +1047,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
 
 // Merges the parts of a pair that several CTAs share: CTA c does nothing unless a pair begins in attention CTA c and goes on
 // behind it.  A thread per head and dim (a CTA per head is 0.8 us slower); a lane weighs one part of a round, in every warp alike.  Rounds of four where a pair has
-// that few parts (16 sequences: 23.7 us a call against 27.8 with one size of 32), of 16 otherwise (one sequence: 11.1 us against
-// 13.9 with 32).
+// that few parts (16 sequences: 24 us a call against 28 with one size of 32), of 16 otherwise (one sequence: 11 us against 14
+// with 32).
 template <int D>
 __global__ void __launch_bounds__(8 * D) attn_decode_kv8_combine_kernel(const float* __restrict__ part, const int2* __restrict__ desc, int group, int n_kv,
                                                                     __nv_bfloat16* __restrict__ out) {
