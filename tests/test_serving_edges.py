@@ -1,0 +1,43 @@
+"""Serving entry points: what has to be refused before anything is written, and what the oracle's tolerances can tell apart.
+Needs no GPU."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as sv
+from paper_2504_12285_b200 import binding as bl
+from paper_2504_12285_b200 import chain as gpu_chain
+from test_gpu_serving import attend_case
+
+
+class Recorder:
+    """Stands in for the library: notes the calls and launches nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or 0
+
+
+@pytest.mark.parametrize("out", [torch.zeros(6, 64, dtype=torch.bfloat16), torch.zeros(20, 32, dtype=torch.bfloat16), torch.zeros(20 * 64, dtype=torch.bfloat16),
+                                 torch.zeros(30, 64, dtype=torch.bfloat16), torch.zeros(20, 64)])
+def test_embed_refuses_another_output_than_its_rows(monkeypatch, out):
+    lib = Recorder()
+    monkeypatch.setattr(bl, "lib", lambda: lib)
+    monkeypatch.setattr(bl, "_stream", lambda: 0)
+
+    def typed(t, dtype, name):
+        if t.dtype != dtype:
+            raise TypeError(name)
+        return t
+
+    monkeypatch.setattr(bl, "_dev", typed)
+    ids, table = torch.zeros(20, dtype=torch.int32), torch.zeros(50, 64, dtype=torch.bfloat16)
+    with pytest.raises((TypeError, ValueError)):
+        bl.bitlinear_embed(ids, table, out=out)
+    assert not lib.calls
+    good = torch.zeros(20, 64, dtype=torch.bfloat16)
+    assert bl.bitlinear_embed(ids, table, out=good) is good and lib.calls[0][1][2] == 20
