@@ -197,6 +197,8 @@ class PagedDecodeStep:
                  n_q_heads: int, n_kv_heads: int, head_dim: int, kv_dtype=torch.int8, rms_eps: float = 1e-5, rope_base: float = 500000.0,
                  device="cuda:0"):
         """layers, embedding: as for DecodeStep; rows at most 16 (the output head's limit); kv_dtype: torch.int8 or torch.float8_e4m3fn."""
+        if not 1 <= rows <= 16:
+            raise ValueError(f"rows must be 1 to 16, not {rows}")
         dev = torch.device(device)
         self.rows, self.dims, self.block_rows, self.table = rows, (n_q_heads, n_kv_heads, head_dim), block_rows, embedding
         kv = n_kv_heads * head_dim
@@ -223,7 +225,10 @@ class PagedDecodeStep:
         self.top_p, self.min_p = torch.ones(places, **f32), torch.zeros(places, **f32)
         self.attn_ws = torch.empty(bl.bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), dtype=torch.uint8, device=dev)
         self.ids, self.logprobs = torch.zeros(rows, **i32), torch.zeros(rows, **f32)
-        self.calls = _token_calls(self, layers, rms_eps, dev)
+        with torch.cuda.device(dev):
+            self.calls = _token_calls(self, layers, rms_eps, dev)
+            # a step that places nothing: sizes and types that one of the calls refuses are refused here, before there is a state to spoil
+            self.step(torch.zeros(rows, **i32), torch.zeros(rows, **f32))
         torch.cuda.synchronize(dev)
 
     def step(self, token_ids: torch.Tensor, u: torch.Tensor):
@@ -232,6 +237,14 @@ class PagedDecodeStep:
         cu_tokens[p + 1] - 1, and rows from cu_tokens[-1] on mean nothing.  served[p] is 0 where the pool or the rows did not suffice
         and the place's tokens were left out."""
         n_q, n_kv, hd = self.dims
+        # all that a later call would refuse, before the first one changes the state
+        bl._tensors((token_ids, torch.int32, (self.rows,), "token_ids"), (u, torch.float32, (self.rows,), "u"))
+        for name, dtype in (("temperature", torch.float32), ("top_k", torch.int32), ("top_p", torch.float32), ("min_p", torch.float32)):
+            t = getattr(self, name)
+            if t.dtype != dtype or t.get_device() != u.get_device():
+                raise TypeError(f"{name} must be of {dtype} and on the step's device")
+            if t.dim() != 1 or t.shape[0] < self.new_tokens.shape[0]:
+                raise ValueError(f"{name} must have an entry for each place")
         (_, _, self.served, self.cu_tokens, self.seq_ids, self.positions, self.row_lengths, self.slots) = bl.bitlinear_block_tables(
             self.lengths, self.new_tokens, self.tables, self.free_blocks, self.n_free, self.block_rows, self.rows, lengths_out=self.lengths,
             n_free_out=self.n_free)

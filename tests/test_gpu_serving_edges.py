@@ -16,6 +16,48 @@ pytestmark = pytest.mark.gpu
 
 # ------------------------------------------------------------------------------------------------- the paged step
 
+def state_of(st):
+    return [t.clone() for t in (st.lengths, st.tables, st.free_blocks, st.n_free)] + [x.view(torch.uint8).clone() for c in st.cache for x in c]
+
+
+def test_paged_decode_step_refuses_before_it_changes_anything():
+    st, _ = paged_step(torch.int8)
+    ids, u = torch.zeros(6, dtype=torch.int32, device=DEV), torch.rand(6, device=DEV)
+    st.new_tokens.copy_(torch.tensor([3, 1, 1, 0], dtype=torch.int32))
+    before = state_of(st)
+    wide = torch.zeros(20, dtype=torch.int32, device=DEV)
+    for bad in ((wide, u), (ids[:4], u), (ids.long(), u), (ids.cpu(), u), (ids, u[:4]), (ids, u.double()), (ids, torch.rand(12, device=DEV)[::2])):
+        with pytest.raises((TypeError, ValueError)):
+            st.step(*bad)
+    for name, bad in (("temperature", torch.ones(3, device=DEV)), ("top_k", torch.zeros(4, device=DEV)), ("top_p", torch.ones(4).double().to(DEV)), ("min_p", torch.zeros(4))):
+        good = getattr(st, name)
+        setattr(st, name, bad)
+        with pytest.raises((TypeError, ValueError)):
+            st.step(ids, u)
+        setattr(st, name, good)
+    for a, b in zip(before, state_of(st)):
+        assert torch.equal(a, b)
+    st.step(ids, u)
+    assert st.lengths.tolist() == [3, 1, 1, 0]
+
+
+def test_paged_decode_step_is_not_built_where_a_call_would_refuse():
+    from paper_2504_12285_b200 import chain as gpu_chain
+    from paper_2504_12285_b200 import workloads as wl
+    from test_gpu_serving import small_layers
+
+    H, F, n_q, n_kv, hd = 256, 512, 4, 2, 64
+    layers, table = small_layers(1, H, F, n_kv * hd, 8700), torch.zeros(500, H, dtype=torch.bfloat16, device=DEV)
+
+    def build(block_rows=16, n_q=n_q, kv_dtype=torch.int8, table=table):
+        return gpu_chain.PagedDecodeStep(layers, table, 6, 4, 14, block_rows, 5, H, F, n_q, n_kv, hd, kv_dtype, wl.RMS_EPS, device=DEV)
+
+    for bad in (dict(block_rows=48), dict(n_q=2), dict(kv_dtype=torch.float8_e5m2), dict(table=torch.zeros(bl.SAMPLE_MAX_VOCAB + 1, H, dtype=torch.bfloat16, device=DEV))):
+        with pytest.raises((TypeError, ValueError, bl.BitLinearError)):
+            build(**bad)
+    assert int(build().n_free[0]) == 14
+
+
 def test_decode_step_refuses_other_numbers_of_tokens():
     from paper_2504_12285_b200 import chain as gpu_chain
     from paper_2504_12285_b200 import workloads as wl

@@ -41,3 +41,9 @@ def test_embed_refuses_another_output_than_its_rows(monkeypatch, out):
     assert not lib.calls
     good = torch.zeros(20, 64, dtype=torch.bfloat16)
     assert bl.bitlinear_embed(ids, table, out=good) is good and lib.calls[0][1][2] == 20
+
+
+@pytest.mark.parametrize("rows", [0, -1, 17, 64])
+def test_paged_decode_step_refuses_rows_that_the_output_head_cannot_take(rows):
+    with pytest.raises(ValueError, match="rows"):
+        gpu_chain.PagedDecodeStep([], torch.zeros(50, 64, dtype=torch.bfloat16), rows, 4, 8, 16, 4, 64, 128, 1, 1, 64, device="cpu")
