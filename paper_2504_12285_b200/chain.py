@@ -275,11 +275,14 @@ class PagedDecodeStep:
             self.graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(self.graph, stream=side):
                 self.step(self.token_buf, self.u_buf)
+        # what the recording writes of its rows: an eager step after it puts tensors of its own in their place
+        self.recorded = self.served, self.cu_tokens, self.seq_ids, self.positions, self.row_lengths, self.slots
         torch.cuda.current_stream().wait_stream(side)
 
     def step_graph(self):
-        """Replay the recorded step -> (ids, logprobs) as step()."""
+        """Replay the recorded step -> (ids, logprobs) as step(); served, cu_tokens and the like are this step's afterwards."""
         self.graph.replay()
+        self.served, self.cu_tokens, self.seq_ids, self.positions, self.row_lengths, self.slots = self.recorded
         return self.ids, self.logprobs
 
 

@@ -16,6 +16,28 @@ pytestmark = pytest.mark.gpu
 
 # ------------------------------------------------------------------------------------------------- the paged step
 
+def test_paged_decode_step_eager_and_recorded_in_turn():
+    """What the step says of its rows belongs to the step that ran last, recorded or not."""
+    st, _ = paged_step(torch.int8)
+    st.temperature.fill_(0.9)
+    st.capture()
+    state = [host(t).copy() for t in (st.lengths, st.tables, st.free_blocks)] + [int(st.n_free[0])]
+    gen = torch.Generator().manual_seed(62)
+    for i, new in enumerate(([5, 1, 0, 0], [1, 1, 4, 0], [1, 0, 1, 1], [-1, 2, 1, 1], [6, 0, 0, 0], [3, 1, 1, 2], [1, 1, 1, 1])):
+        st.new_tokens.copy_(torch.tensor(new, dtype=torch.int32))
+        ids, u = torch.randint(0, 500, (6,), generator=gen, dtype=torch.int32).to(DEV), torch.rand(6, generator=gen).to(DEV)
+        if i in (0, 2, 3, 5):
+            st.step(ids, u)
+        else:
+            st.token_buf.copy_(ids), st.u_buf.copy_(u)
+            st.step_graph()
+        want = sv.block_tables(state[0], new, state[1], state[2], state[3], 16, 6)
+        state = [want["lengths"], want["tables"], want["free_blocks"], want["n_free"]]
+        for name in ("lengths", "served", "cu_tokens", "seq_ids", "positions", "row_lengths", "slots"):
+            assert np.array_equal(host(getattr(st, name)), want[name]), (i, name)
+    assert bl.bitlinear_poll_status() == 0
+
+
 def state_of(st):
     return [t.clone() for t in (st.lengths, st.tables, st.free_blocks, st.n_free)] + [x.view(torch.uint8).clone() for c in st.cache for x in c]
 
