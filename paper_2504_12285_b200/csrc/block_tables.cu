@@ -39,15 +39,20 @@ struct TablesArgs {
 struct Ask {
     int len, used, n, need, back, fresh;  // fresh: new_tokens as given
 };
+// blocks that n rows take; n + rows - 1 may pass 32 bits, this does not
+__device__ __forceinline__ int blocks_of(int n, int rows) {
+    const int whole = n / rows;
+    return whole + (whole * rows < n);
+}
 __device__ __forceinline__ Ask ask_of(const TablesArgs& a, int r) {
     const int cap = a.max_blocks * a.block_rows;
     Ask k;
     k.fresh = a.new_tokens[r];
     k.len = min(max(a.lengths[r], 0), cap);
-    k.used = (k.len + a.block_rows - 1) / a.block_rows;
+    k.used = blocks_of(k.len, a.block_rows);
     const bool adds = k.fresh > 0 && k.fresh <= cap - k.len;
     k.n = adds ? k.fresh : 0;
-    k.need = adds ? (k.len + k.n + a.block_rows - 1) / a.block_rows - k.used : 0;
+    k.need = adds ? blocks_of(k.len + k.n, a.block_rows) - k.used : 0;
     k.back = k.fresh < 0 ? k.used : 0;
     return k;
 }
@@ -86,7 +91,7 @@ __global__ void __launch_bounds__(kTablesThreads) block_tables_kernel(const Tabl
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
-    const int per = (a.R + threads - 1) / threads;  // requests per chunk
+    const int per = blocks_of(a.R, threads);  // requests per chunk
     const long long first = (long long)tid * per;
     const int r0 = (int)min(first, (long long)a.R), r1 = (int)min(first + per, (long long)a.R);
     const int n_free = min(max(*a.n_free, 0), a.n_blocks);
@@ -223,7 +228,7 @@ __global__ void __launch_bounds__(kTablesThreads) block_tables_kernel(const Tabl
         }
     }
     // blocks given back go above the old top
-    for (int j = blockIdx.x * threads + tid; j < all.back && (long long)n_free + j < a.n_blocks; j += stride) a.free_blocks[n_free + j] = given_back(j);
+    for (long long j = blockIdx.x * threads + tid; j < all.back && n_free + j < a.n_blocks; j += stride) a.free_blocks[n_free + j] = given_back((int)j);
     if (gridDim.x == 1) __syncthreads();  // lengths may be updated in place: every thread has read them
     // requests: chunk c belongs to CTA c % grid
     if (tid % gridDim.x == blockIdx.x) {
@@ -250,7 +255,8 @@ __global__ void __launch_bounds__(kTablesThreads) block_tables_commit_kernel(con
     if (threadIdx.x == 0) delta = 0;
     __syncthreads();
     int d = 0;
-    for (int r = threadIdx.x; r < a.R; r += blockDim.x) {
+    for (long long i = threadIdx.x; i < a.R; i += blockDim.x) {
+        const int r = (int)i;
         const Ask k = ask_of(a, r);
         const bool ok = a.served[r] != 0;
         d += k.back - (ok ? k.need : 0);
@@ -286,9 +292,9 @@ extern "C" int bitlinear_block_tables(const int32_t* lengths, const int32_t* new
     const TablesArgs a = {lengths, new_tokens, tables, free_blocks, n_free, n_requests, max_blocks, block_rows, n_blocks, t_cap,
                           lengths_out, n_free_out, served, cu_tokens, seq_ids, positions, row_lengths, slots};
     // threads: enough for a request or four tokens each; more than one CTA once the tokens fill one
-    const int wanted = std::max(n_requests, (t_cap + 3) / 4);
+    const int wanted = std::max(n_requests, (int)((t_cap + 3ll) / 4));
     const int threads = wanted <= 128 ? 128 : wanted <= 512 ? 512 : kTablesThreads;
-    const int ctas = std::max(1, std::min(sm_count, (t_cap + 4 * threads - 1) / (4 * threads)));
+    const int ctas = std::max(1, (int)std::min<long long>(sm_count, (t_cap + 4ll * threads - 1) / (4 * threads)));
     const bool in_place = lengths_out == lengths || n_free_out == n_free;
     const int commit = ctas == 1 || !in_place;
     cudaLaunchAttribute attr[1];

@@ -14,6 +14,19 @@ from test_gpu_serving import (DEV, DTYPE, KINDS, attend_case, check_append, chec
 pytestmark = pytest.mark.gpu
 
 
+# ------------------------------------------------------------------------------------------------- block tables
+
+def test_block_tables_of_blocks_as_long_as_the_type():
+    """One block of 2^31 - 1 rows: lengths and blocks are counted without passing 32 bits."""
+    rows = 2 ** 31 - 1
+    for lengths, new in (([5, 0], [3, 0]), ([0, 7], [2, -1]), ([0, 0], [4, 9])):
+        tables = np.full((2, 1), -1, np.int32)
+        used = [i for i, n in enumerate(lengths) if n > 0]
+        for i in used:
+            tables[i] = 0
+        check_tables(np.array(lengths, np.int32), np.array(new, np.int32), tables, np.zeros(1, np.int32), 0 if used else 1, rows, 20)
+
+
 # ------------------------------------------------------------------------------------------------- the paged step
 
 def test_paged_decode_step_eager_and_recorded_in_turn():
