@@ -46,6 +46,12 @@ struct SampleArgs {
     float* logprobs;
 };
 
+// at most 1e29; NaN stays NaN, which is not above 0
+__device__ __forceinline__ float temperature_of(const SampleArgs& a, int row) {
+    const float t = a.temperature ? a.temperature[row] : 1.0f;
+    return t > 1e29f ? 1e29f : t;
+}
+
 // larger float, larger integer; -0 and 0 are equal
 __device__ __forceinline__ uint32_t key_of(float l) {
     const uint32_t b = __float_as_uint(l + 0.0f);
@@ -169,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
     const long long begin = (long long)rank * a.shard;
     const int n = (int)max(0ll, min((long long)a.shard, a.V - begin));
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride + begin;
-    const float temp = a.temperature ? fminf(a.temperature[row], 1e29f) : 1.0f;
+    const float temp = temperature_of(a, row);
     const int k = a.top_k ? a.top_k[row] : 0;
     const float p = a.top_p ? a.top_p[row] : 1.0f;
     const float given_mp = a.min_p ? a.min_p[row] : 0.0f;
@@ -732,7 +738,7 @@ __global__ void __launch_bounds__(kPlainThreads, 4) sample_plain_kernel(const Sa
     if (tid < 16) sh.pow2[tid] = kPow2Table[tid];
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float temp = a.temperature ? fminf(a.temperature[row], 1e29f) : 1.0f;
+    const float temp = temperature_of(a, row);
     const float u = a.u[row];
     const T* src = static_cast<const T*>(a.logits) + (size_t)row * a.stride;
     // the row: elements up to a 16-byte border (worker 0), 16-byte vectors dealt to the workers in equal runs, the rest (the last worker)

@@ -14,6 +14,20 @@ from test_gpu_serving import (DEV, DTYPE, KINDS, attend_case, check_append, chec
 pytestmark = pytest.mark.gpu
 
 
+# ------------------------------------------------------------------------------------------------- sampling
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,V", [(4, 3000), (41, 17001)])
+@pytest.mark.parametrize("filters", [dict(), dict(top_k=40, top_p=0.9, min_p=0.01), dict(top_p=0.95)])
+def test_sample_takes_the_largest_where_the_temperature_is_no_number(dtype, M, V, filters):
+    rng = np.random.default_rng(M)
+    t = rng.uniform(0.5, 2.0, M)
+    t[::2] = np.nan
+    t[1] = -np.inf
+    t[3] = np.inf
+    check_sample(rng.standard_normal((M, V)) * 2, rng.random(M), dtype, temperature=t, **filters)
+
+
 # ------------------------------------------------------------------------------------------------- block tables
 
 def test_block_tables_of_blocks_as_long_as_the_type():
