@@ -719,12 +719,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
                 x[8 * i + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
             }
         }
-        float amax = 0.0f;
+        uint32_t most = 0u;  // the largest magnitude by its bits: infinity and NaN are above all others
 #pragma unroll
-        for (int i = 0; i < D / 4; ++i) amax = fmaxf(amax, fabsf(x[i]));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        float f;
+        for (int i = 0; i < D / 4; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        float amax = __uint_as_float(most), f;
         if constexpr (INT8) {
             amax = fmaxf(amax, 1e-30f);
             const float inv = 16256.0f / amax;  // 127 * 128
@@ -750,6 +750,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             for (int i = 0; i < D / 8; ++i) qb[i >> 1][i & 1] = head < group ? pack_f16(x[2 * i] * up, x[2 * i + 1] * up) : 0u;
             f = down * a.scale_log2;
         }
+        if (most >= 0x7f800000u) f = NAN;  // scores of a head that is not finite
         const int col = INT8 && NARROW ? 8 * (qd & 1) : 8 * qd;  // lane of column 2 qd (qd & 1: both digits' lanes hold the whole score)
         f_head[0] = __shfl_sync(0xffffffffu, f, col);
         f_head[1] = __shfl_sync(0xffffffffu, f, col + 4);
@@ -914,7 +915,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             for (int e = 0; e < 2; ++e) {
                 const int head = 2 * qd + e;
                 if (head < group) {
-                    const float f = l_run[e] > 0.0f ? unscale / l_run[e] : 0.0f;
+                    const float f = l_run[e] == 0.0f ? 0.0f : unscale / l_run[e];  // no row: zeros; a sum that is NaN stays one
                     uint32_t r[KS];
 #pragma unroll
                     for (int t = 0; t < KS; ++t) {
@@ -1029,7 +1030,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
                 }
             }
             if (whole) {
-                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 *reinterpret_cast<__nv_bfloat162*>(a.out + ((size_t)lead->m * a.n_q + (size_t)lead->h * group) * D + e) = __floats2bfloat162_rn(acc.x * inv, acc.y * inv);
             } else {
                 *reinterpret_cast<float2*>(dst + e) = acc;
@@ -1085,8 +1086,8 @@ __global__ void __launch_bounds__(8 * D) attn_decode_kv8_combine_kernel(const fl
         acc *= f0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float w = __shfl_sync(0xffffffffu, f, i);
-            acc = w > 0.0f ? fmaf(v[i], w, acc) : acc;  // (a part that does not exist may hold anything)
+            const float w = __shfl_sync(0xffffffffu, in ? f : -1.0f, i);
+            acc = w < 0.0f ? acc : fmaf(v[i], w, acc);  // (a part that does not exist may hold anything; one that is NaN counts)
         }
         top = n;
     };
@@ -1094,7 +1095,7 @@ __global__ void __launch_bounds__(8 * D) attn_decode_kv8_combine_kernel(const fl
     else
         for (int p0 = c; p0 <= own.y; p0 += 16) round(std::integral_constant<int, 16>{}, p0);
     const int m = own.x / n_kv, h = own.x - m * n_kv;
-    out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(l > 0.0f ? acc / l : 0.0f);
+    out[(((size_t)m * n_kv + h) * group + head) * D + threadIdx.x] = __float2bfloat16_rn(l == 0.0f ? 0.0f : acc / l);
 }
 
 // ---------------------------------------------------------------------------------------------- host side

@@ -28,6 +28,54 @@ def test_sample_takes_the_largest_where_the_temperature_is_no_number(dtype, M, V
     check_sample(rng.standard_normal((M, V)) * 2, rng.random(M), dtype, temperature=t, **filters)
 
 
+# ------------------------------------------------------------------------------------------------- attention
+
+LENGTHS = [1, 40, 20000, 7, 300, 0]  # one CTA's own, several warps', and one that many CTAs share
+
+
+def check_attention_but_nan(out, bad, q, codes, scales, tables, lengths, n_q, n_kv, D, kind):
+    """Rows and heads marked in bad [M, n_q] are NaN in every dim, the others as check_attention wants them."""
+    got = out.float().cpu().numpy().reshape(len(lengths), n_q, D)
+    assert np.isnan(got[bad]).all()
+    ref = out.clone().view(len(lengths), n_q, D)
+    for m, n in enumerate(lengths):
+        for h in np.nonzero(bad[m])[0]:
+            want = sv.attention8(np.nan_to_num(q[m].double().numpy().reshape(n_q, D), nan=0.0, posinf=0.0, neginf=0.0), *codes, *scales, tables[m], n, n_q, n_kv, D, kind)[0][h]
+            ref[m, int(h)] = torch.from_numpy(want).to(ref)
+    clean = torch.where(torch.isfinite(q.float()), q.float(), 0.0).to(torch.bfloat16)
+    check_attention(ref.view(len(lengths), -1), clean, codes, scales, tables, lengths, n_q, n_kv, D, kind)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("n_q,n_kv,D", [(4, 1, 128), (8, 1, 64), (4, 2, 64)])
+def test_attention_of_a_query_that_is_not_finite_is_nan(kind, value, n_q, n_kv, D):
+    q, codes, scales, tables = attend_case(kind, n_q, n_kv, D, 64, LENGTHS, 131)
+    bad = np.zeros((len(LENGTHS), n_q), bool)
+    for m in range(len(LENGTHS)):
+        h = (m + 1) % n_q
+        q[m, h * D + 5] = value
+        bad[m, h] = LENGTHS[m] > 0  # a row without a length gives zeros whatever its query
+    out = bl.bitlinear_attention_decode_kv8(q.to(DEV), *pool_to_dev(codes, scales, kind), dev(tables), dev(np.array(LENGTHS, np.int32)), n_q, n_kv, D)
+    assert not out[-1].any()
+    check_attention_but_nan(out, bad, q, codes, scales, tables, LENGTHS, n_q, n_kv, D, kind)
+    assert bl.bitlinear_poll_status() == 0
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("pool", ["keys", "values"])
+@pytest.mark.parametrize("at", [0, 100, 312])  # the first block, one in the middle, the last of 20,000 rows
+def test_attention_over_a_block_whose_scale_is_no_number_is_nan(kind, pool, at):
+    n_q, n_kv, D = 4, 2, 64
+    q, codes, scales, tables = attend_case(kind, n_q, n_kv, D, 64, LENGTHS, 132)
+    broken = [s.copy() for s in scales]
+    broken[0 if pool == "keys" else 1][tables[2, at], 1] = np.nan
+    bad = np.zeros((len(LENGTHS), n_q), bool)
+    bad[2, 2:] = True
+    out = bl.bitlinear_attention_decode_kv8(q.to(DEV), *pool_to_dev(codes, broken, kind), dev(tables), dev(np.array(LENGTHS, np.int32)), n_q, n_kv, D)
+    check_attention_but_nan(out, bad, q, codes, scales, tables, LENGTHS, n_q, n_kv, D, kind)
+
+
 # ------------------------------------------------------------------------------------------------- block tables
 
 def test_block_tables_of_blocks_as_long_as_the_type():
