@@ -538,6 +538,7 @@ int bitlinear_embed(const int32_t* ids, const void* table_bf16, int M, int V, in
  *     scale = need if the first new row is the block's row 0, else max(old scale, need);
  *     new rows : code = value / scale rounded to the nearest code, ties to even;
  *     the rows of the block in front of the new ones, if the scale grew: code = code * old scale / scale, rounded the same way.
+ *   A value that is not finite makes the scale NaN (and the new rows' codes 0), and it stays NaN until the block's row 0 is written again.
  *   So a block's scale depends on nothing but its own rows, whatever an earlier owner left there, and rows behind the new ones
  *   keep their bits.
  *

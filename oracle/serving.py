@@ -79,6 +79,8 @@ def encode(x: np.ndarray, kind: int) -> np.ndarray:
 
 
 def scale_for(amax: float, kind: int) -> np.float32:
+    if not math.isfinite(amax):
+        return np.float32(np.nan)
     a = max(float(amax), 1e-30)
     if kind == INT8:
         return np.float32(a / 127.0)
@@ -109,10 +111,10 @@ def append8(values, slots, codes, scale, kind):
         for h in range(codes.shape[1]):
             need = scale_for(np.abs(values[mine, h]).max(), kind)
             old = scale[b, h]
-            new = need if first == 0 else max(old, need)
+            new = need if first == 0 else np.maximum(old, need)  # NaN if either is
             if first > 0 and new > old:
                 codes[b, h, :first] = encode(decode(codes[b, h, :first], kind) * float(old) / float(new), kind)
-            codes[b, h, off] = encode(values[mine, h] / float(new), kind)
+            codes[b, h, off] = 0 if np.isnan(new) else encode(values[mine, h] / float(new), kind)
             scale[b, h] = new
 
 

@@ -109,6 +109,13 @@ __device__ __forceinline__ double decoded(uint32_t code) {
     return (double)__half2float(__half(h));
 }
 
+// the larger; NaN if either is
+__device__ __forceinline__ float max_nan(float x, float y) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(x), "f"(y));
+    return m;
+}
+
 struct AppendArgs {
     const float* q;
     const float* k;
@@ -199,7 +206,7 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
             for (int e = 0; e < 4; ++e) x[e] = r.l[e], x[4 + e] = r.u[e];
         }
     };
-    // the largest magnitude, in fp32, and the run's first row in the block
+    // the largest magnitude, in fp32 (NaN if a value is), and the run's first row in the block
     float top = 0.0f;
     int first = 1 << a.log2_rows;
 #pragma unroll 2
@@ -208,19 +215,19 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
         if (pos < 0 || pos >= a.t_max) continue;
         load(m, pos);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+        for (int e = 0; e < 8; ++e) top = max_nan(top, fabsf(x[e]));
         first = min(first, a.slots[m] - (block << a.log2_rows));
     }
     const float own_top = top;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, off));
         first = min(first, __shfl_xor_sync(0xffffffffu, first, off));
     }
     if (lane == 0) red[warp] = top, first_s[warp] = first;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, red[w]), first = min(first, first_s[w]);
+    for (int w = 0; w < WARPS; ++w) top = max_nan(top, red[w]), first = min(first, first_s[w]);
     if (first >> a.log2_rows) {  // no token of the run has a place in the table of angles
         __syncthreads();
         return;
@@ -249,13 +256,14 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     if (tid == 0) {  // the one reader and writer of the scale
         float* scale = (which == 0 ? a.k_scale : a.v_scale) + (size_t)block * a.n_kv + h;
         double amax = (double)top;
-        if (which == 0) {
+        if (which == 0 && top == top) {
             amax = red_d[0];
 #pragma unroll
             for (int w = 1; w < WARPS; ++w) amax = fmax(amax, red_d[w]);
         }
-        const float need = scale_for<KIND>(amax), old = first > 0 ? *scale : need;
-        const float now = first > 0 ? fmaxf(old, need) : need;
+        // a value that is not finite leaves the block without a scale until its first row is written again: what reads it gets NaN
+        const float need = amax < (double)INFINITY ? scale_for<KIND>(amax) : NAN, old = first > 0 ? *scale : need;
+        const float now = first > 0 ? max_nan(old, need) : need;
         *scale = now;
         scale_s[0] = old, scale_s[1] = now;
     }
@@ -264,16 +272,17 @@ __device__ __forceinline__ void append_run(const AppendArgs& a, int m0, int bloc
     const double s = (double)now;
     const float inv = __frcp_rn(now), off = quick_error<KIND>(which == 0);
     const bool overflow = !(top < INFINITY);  // a rotated value beyond fp32
+    const bool broken = now != now;
 #pragma unroll 2
     for (int m = m0 + sub; m < end; m += ROWS) {
         const int pos = a.positions[m];
         if (pos < 0 || pos >= a.t_max) continue;
         load(m, pos);
         uint32_t word[2];
-        if (overflow || !quick_codes<KIND>(x, inv, off, word)) {
+        if (broken || overflow || !quick_codes<KIND>(x, inv, off, word)) {
             word[0] = word[1] = 0u;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8 && !broken; ++e) {
                 const double value = which == 0 ? r.exact(e) : (double)x[e];
                 word[e >> 2] |= (KIND == BITLINEAR_KV_INT8 ? close_code<KIND>(value, inv, s) : code_of<KIND>(value, s)) << (8 * (e & 3));
             }

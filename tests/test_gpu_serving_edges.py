@@ -76,6 +76,48 @@ def test_attention_over_a_block_whose_scale_is_no_number_is_nan(kind, pool, at):
     check_attention_but_nan(out, bad, q, codes, scales, tables, LENGTHS, n_q, n_kv, D, kind)
 
 
+# ------------------------------------------------------------------------------------------------- append
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_append_of_values_that_are_not_finite(kind, D, value):
+    """The scale of the block and head that gets one is NaN until the block's first row is written again; nothing else is touched."""
+    n_kv, rows, T = 2, 16, 40
+    rng = np.random.default_rng(6)
+    k, v = ((rng.standard_normal((T, n_kv * D)) * 2).astype(np.float32) for _ in range(2))
+    slots = np.arange(5, 5 + T, dtype=np.int32)
+    k[13, 3] = value      # block 1, head 0
+    v[30, D + 9] = value  # block 2, head 1
+    codes, scales = make_pool(5, n_kv, rows, D, kind, 7)
+    scales[1][0, 0] = np.nan  # block 0 goes on behind rows whose scale is no number
+    pool = pool_to_dev(codes, scales, kind)
+    table = bl.bitlinear_rope_table(D, 64, device=DEV)
+    tab = host(table)
+
+    def append(k, v, slots):
+        T = len(slots)
+        pos = slots.astype(np.int32)
+        bl.bitlinear_rope_kv8(torch.zeros(T, 4 * D, device=DEV), dev(k), dev(v), dev(pos), dev(slots), table, *pool, 4, n_kv, D)
+        with np.errstate(invalid="ignore"):
+            sv.append8(sv.rotate(k.reshape(T, n_kv, D), pos, tab), slots, codes[0], scales[0], kind)
+            sv.append8(v.reshape(T, n_kv, D).astype(np.float64), slots, codes[1], scales[1], kind)
+        for got, want in zip(pool[2:], scales):
+            assert np.array_equal(host(got), want, equal_nan=True)
+        for got, want, s in zip(pool[:2], codes, scales):
+            fine = ~np.isnan(s)
+            assert np.array_equal(host(got)[fine], want[fine])
+            assert np.array_equal(host(got)[~fine], want[~fine])
+
+    append(k, v, slots)
+    nan = [np.argwhere(np.isnan(s)).tolist() for s in scales]
+    assert nan == [[[1, 0]], [[0, 0], [2, 1]]]
+    append(np.ones((1, n_kv * D), np.float32), np.ones((1, n_kv * D), np.float32), np.array([45], np.int32))  # block 2 again: still no number
+    assert np.isnan(host(pool[3])[2, 1])
+    append(np.ones((3, n_kv * D), np.float32), np.ones((3, n_kv * D), np.float32), np.array([0, 16, 32], np.int32))
+    assert not np.isnan(host(pool[2])).any() and not np.isnan(host(pool[3])).any()
+
+
 # ------------------------------------------------------------------------------------------------- block tables
 
 def test_block_tables_of_blocks_as_long_as_the_type():

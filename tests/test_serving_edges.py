@@ -47,3 +47,19 @@ def test_embed_refuses_another_output_than_its_rows(monkeypatch, out):
 def test_paged_decode_step_refuses_rows_that_the_output_head_cannot_take(rows):
     with pytest.raises(ValueError, match="rows"):
         gpu_chain.PagedDecodeStep([], torch.zeros(50, 64, dtype=torch.bfloat16), rows, 4, 8, 16, 4, 64, 128, 1, 1, 64, device="cpu")
+
+
+# ------------------------------------------------------------------------------------------------- attention's tolerance
+
+def test_oracle_keeps_what_is_not_a_number_in_sight():
+    for kind in (sv.INT8, sv.E4M3):
+        for bad in (math.nan, math.inf, -math.inf):
+            codes, scale = np.full((2, 1, 16, 64), 5, np.uint8), np.full((2, 1), 0.5, np.float32)
+            values = np.ones((2, 1, 64))
+            values[1, 0, 3] = bad
+            sv.append8(values, [4, 20], codes, scale, kind)
+            assert scale[0, 0] == 0.5 and np.isnan(scale[1, 0]) and (codes[0, 0, :4] == 5).all()
+            sv.append8(np.ones((1, 1, 64)), [21], codes, scale, kind)
+            assert np.isnan(scale[1, 0])  # a finite row does not hide it
+            sv.append8(np.ones((1, 1, 64)), [16], codes, scale, kind)
+            assert scale[1, 0] == sv.scale_for(1.0, kind)  # the block's next owner does not see it
