@@ -547,6 +547,8 @@ int bitlinear_embed(const int32_t* ids, const void* table_bf16, int M, int V, in
  *   whose length is <= 0 or whose sequence lies outside 0 .. n_seq-1 gives zeros; lengths past the table count as its end; rows
  *   of a block id outside 0 .. n_blocks-1 are left out.  Codes and scales of rows past a length are never used, whatever
  *   they hold.  A query head with an element that is not finite, or one that meets a scale that is NaN, gives NaN, however many rows it has.  Scores, softmax and sums in fp32; the weights enter the tensor cores as f16.
+ *   Over an int8 pool each head's queries are rounded to units of 1 / 4,161,536 of its largest magnitude (at least 1e-30), and their
+ *   products with the codes are summed exactly.
  *   D = 64 or 128, n_q / n_kv <= 8, block_rows 16, 32, 64 or 128, n_blocks * n_kv * block_rows < 2^31 - 256,
  *   max_blocks * block_rows <= 2^30, M * n_kv * (max_blocks * block_rows / 32 + 2) < 2^31, M <= 65535; pools, q, out 16-byte aligned.  ws (device, 16-byte aligned) at least
  *   bitlinear_attention_kv8_workspace_bytes(...) bytes (0 for unsupported sizes); contents need not survive, calls that

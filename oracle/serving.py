@@ -136,11 +136,14 @@ def attention8(q, k_codes, v_codes, k_scale, v_scale, table, length, n_q, n_kv, 
         s = k[:, g] @ q[h] / math.sqrt(D)
         p = np.exp(s - s.max())
         out[h] = (p / p.sum()) @ v[:, g]
-        # D products in fp32, each addition off by 2^-23 at most (the tensor cores may cut instead of round), and three roundings
-        # of the scaled score
-        err = (D + 4) * 2.0 ** -23 * float((np.abs(k[:, g]) @ np.abs(q[h])).max()) / math.sqrt(D)
-        if kind == INT8:  # queries rounded to 1 / 16256 of the head's largest
-            err += (0.5 / 16256 + 2.0 ** -23) * float(np.abs(k[:, g]).sum(-1).max() * np.abs(q[h]).max()) / math.sqrt(D)
+        if kind == INT8:
+            # queries in units of 1 / (16256 * 256) of the head's largest: half a unit by rounding, half by the two fp32 roundings (2^-24 each)
+            # of a quotient of at most 2^22 units.  Sums are whole numbers; ten fp32 roundings of the score and of what scales it
+            err = float(np.abs(k[:, g]).sum(-1).max() * np.abs(q[h]).max()) / (16256 * 256) / math.sqrt(D) + 10 * 2.0 ** -24 * float(np.abs(s).max())
+        else:
+            # D products in fp32, each addition off by 2^-23 at most (the tensor cores may cut instead of round), and three roundings
+            # of the scaled score
+            err = (D + 4) * 2.0 ** -23 * float((np.abs(k[:, g]) @ np.abs(q[h])).max()) / math.sqrt(D)
         worst = max(worst, err)
     return out, float(np.abs(v).max()), worst
 

@@ -383,9 +383,9 @@ constexpr int kMaxStages = 8;
 // where a pair reaches beyond the CTA, in global memory, where a second launch merges them.  A pair counts for one place
 // more than it has units: starting and ending it takes a warp about as long as a unit does, and without that place the warps
 // that meet many short sequences finished last (by a sixth of the time of a batch of 97 sequences of 1 to 16,384 rows).
-// Bound: the bytes of the cache while the rings are full - a batch of 97 such sequences (246 MB) takes 50 us, 4.9 TB/s, and its
+// Bound: the bytes of the cache while the rings are full - a batch of 97 such sequences (246 MB) takes 51.5 us, 4.8 TB/s, and its
 // steady part runs at the copy rate; the rest is the chain lengths -> table -> first rows in front (3 us cold), the parts' merge (1 us)
-// and the second launch (2.5 us).  16 sequences of 4096 rows 22.7 us, one 10.7 us.  Twelve warps rather than
+// and the second launch (2.5 us).  16 sequences of 4096 rows (e4m3) 22.8 us, one (int8) 11.1 us.  Twelve warps rather than
 // eight: 78 -> 68 us at the time; keys on the integer tensor cores rather than converted were part of that step.
 struct AttnArgs {
     const __nv_bfloat16* q;
@@ -703,11 +703,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
     };
 
     // ---- consumer side
-    // The queries as the tensor core's second operand.  int8 codes go to the integer tensor cores as they are, the queries as two
-    // digits of 7 and 8 bits (15 bits of each head's largest magnitude, where bf16 itself has 8 of each value): sums are exact.  With
-    // at most four heads the digits share the eight columns.  e4m3 codes are converted to f16, the queries too.
+    // The queries as the tensor core's second operand.  int8 codes go to the integer tensor cores as they are, the queries as three
+    // digits of 8, 7 and 8 bits, 23 bits of each head's largest magnitude, and sums are exact.  Two digits, 15 bits, left the small channels
+    // beside a large one too few: one of 200 times the others moved results by more than their rounding to bf16.  The third costs
+    // 4 to 7 % of a long batch (97 ragged sequences 49.5 -> 51.5 us, 64 x 6000 rows of 28 / 4 heads 76.6 -> 82.1).  With at most four heads the
+    // first two digits share the eight columns.  e4m3 codes are converted to f16, the queries too.
     constexpr int QB = INT8 ? D / 32 : D / 16;  // steps along the dims
-    uint32_t qb[INT8 && !NARROW ? 2 * QB : QB][2];
+    constexpr int MID = NARROW ? 0 : QB, LOW = MID + QB;  // where the second and third digits lie
+    constexpr float kQueryUnits = 127.0f * 128.0f * 256.0f;
+    uint32_t qb[INT8 ? LOW + QB : QB][2];
     float o[KS][4], m_run[2], l_run[2], f_head[2], v_ref = 1.0f;
     int first_unit = 0;          // the number, in its pair, of the first unit of this run's part
     const int r_lo = row_of_slot(g);
@@ -736,19 +740,21 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
         float amax = __uint_as_float(most), f;
         if constexpr (INT8) {
             amax = fmaxf(amax, 1e-30f);
-            const float inv = 16256.0f / amax;  // 127 * 128
-            f = amax * (1.0f / 16256.0f) * a.scale_log2;
+            const float inv = kQueryUnits / amax;
+            f = amax * (1.0f / kQueryUnits) * a.scale_log2;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {  // four dims to a word
-                uint32_t hi = 0u, lo = 0u;
+                uint32_t hi = 0u, mid = 0u, lo = 0u;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int v = head < group ? __float2int_rn(x[4 * i + j] * inv) : 0, d = (v + 64) >> 7;
+                for (int j = 0; j < 4; ++j) {  // v = 32768 d + 256 (w - 128 d) + (v - 256 w), each digit the nearest: -127 .. 127, -64 .. 63, -128 .. 127
+                    const int v = head < group ? __float2int_rn(x[4 * i + j] * inv) : 0, w = (v + 128) >> 8, d = (w + 64) >> 7;
                     hi |= ((uint32_t)d & 0xffu) << (8 * j);
-                    lo |= ((uint32_t)(v - 128 * d) & 0xffu) << (8 * j);
+                    mid |= ((uint32_t)(w - 128 * d) & 0xffu) << (8 * j);
+                    lo |= ((uint32_t)(v - 256 * w) & 0xffu) << (8 * j);
                 }
-                if constexpr (NARROW) qb[i >> 1][i & 1] = g < 4 ? hi : lo;
-                else qb[i >> 1][i & 1] = hi, qb[QB + (i >> 1)][i & 1] = lo;
+                if constexpr (NARROW) qb[i >> 1][i & 1] = g < 4 ? hi : mid;
+                else qb[i >> 1][i & 1] = hi, qb[MID + (i >> 1)][i & 1] = mid;
+                qb[LOW + (i >> 1)][i & 1] = lo;  // (NARROW: in both halves of the columns)
             }
         } else {
             // each head is scaled by the power of two that brings its largest magnitude to 2^8 .. 2^9: bf16 values then fit f16
@@ -797,23 +803,26 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             }
             float s[4];
             if constexpr (INT8) {
-                int hi[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
+                int hi[4] = {0, 0, 0, 0}, mid[4] = {0, 0, 0, 0}, lo[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int hf = 0; hf < D / 64; ++hf)
 #pragma unroll
                     for (int st = 0; st < 2; ++st) {
                         const int i = 2 * hf + st;
                         mma_s8(hi, x[hf][2 * st], y[hf][2 * st], x[hf][2 * st + 1], y[hf][2 * st + 1], qb[i][0], qb[i][1]);
-                        if constexpr (!NARROW) mma_s8(lo, x[hf][2 * st], y[hf][2 * st], x[hf][2 * st + 1], y[hf][2 * st + 1], qb[QB + i][0], qb[QB + i][1]);
+                        if constexpr (!NARROW) mma_s8(mid, x[hf][2 * st], y[hf][2 * st], x[hf][2 * st + 1], y[hf][2 * st + 1], qb[MID + i][0], qb[MID + i][1]);
+                        mma_s8(lo, x[hf][2 * st], y[hf][2 * st], x[hf][2 * st + 1], y[hf][2 * st + 1], qb[LOW + i][0], qb[LOW + i][1]);
                     }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 4; ++e) {  // the upper digits' sum stays below 2^28, the last one's below 2^21
+                    int v;
                     if constexpr (NARROW) {
-                        const int v = qd < 2 ? hi[e] << 7 : hi[e];  // lanes 0, 1 of four hold the high digits' columns, 2, 3 the low digits'
-                        s[e] = (float)(v + __shfl_xor_sync(0xffffffffu, v, 2));
+                        v = qd < 2 ? hi[e] << 7 : hi[e];  // lanes 0, 1 of four hold the first digits' columns, 2, 3 the second digits'
+                        v += __shfl_xor_sync(0xffffffffu, v, 2);
                     } else {
-                        s[e] = (float)((hi[e] << 7) + lo[e]);
+                        v = (hi[e] << 7) + mid[e];
                     }
+                    s[e] = fmaf((float)v, 256.0f, (float)lo[e]);
                 }
             } else {
                 float s0[4] = {0.0f, 0.0f, 0.0f, 0.0f}, s1[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1181,7 +1190,7 @@ int attn8_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, AttnArgs a,
 }
 
 // Twelve warps with rings of two units each, where the parts of a group of at most four heads (or heads of 64) leave the room; eleven
-// otherwise (64 x 6000 rows, 28 / 4 heads of 128: 79 us for int8, 73 for e4m3; with ten or eight warps 84 to 86 and 79).
+// otherwise (64 x 6000 rows, 28 / 4 heads of 128, two digits then: 79 us for int8, 73 for e4m3; with ten or eight warps 84 to 86 and 79).
 template <int D, int KIND>
 int attn8_dispatch(const CUtensorMap& map_k, const CUtensorMap& map_v, const AttnArgs& a, int ctas, cudaStream_t st) {
     if (a.n_q / a.n_kv <= 4) return attn8_launch<D, KIND, 12, true>(map_k, map_v, a, ctas, st);

@@ -10,6 +10,7 @@ from oracle import serving as sv
 from paper_2504_12285_b200 import binding as bl
 from test_gpu_serving import (DEV, DTYPE, KINDS, attend_case, check_append, check_attention, check_sample, check_tables, dev, host, make_pool, paged_step,
                               pool_to_dev)
+from test_serving_edges import outlier_case
 
 pytestmark = pytest.mark.gpu
 
@@ -74,6 +75,15 @@ def test_attention_over_a_block_whose_scale_is_no_number_is_nan(kind, pool, at):
     bad[2, 2:] = True
     out = bl.bitlinear_attention_decode_kv8(q.to(DEV), *pool_to_dev(codes, broken, kind), dev(tables), dev(np.array(LENGTHS, np.int32)), n_q, n_kv, D)
     check_attention_but_nan(out, bad, q, codes, scales, tables, LENGTHS, n_q, n_kv, D, kind)
+
+
+@pytest.mark.parametrize("size", [4000.0, 200.0])
+@pytest.mark.parametrize("n_q,n_kv,D", [(4, 2, 64), (20, 5, 128), (8, 1, 128), (7, 1, 64)])
+def test_attention_of_queries_with_one_large_channel(size, n_q, n_kv, D):
+    lengths = [300, 40, 17, 5000, 1]
+    q, codes, scales, tables = outlier_case(n_q, n_kv, D, 16, lengths, 8, size)
+    out = bl.bitlinear_attention_decode_kv8(q.to(DEV), *pool_to_dev(codes, scales, sv.INT8), dev(tables), dev(np.array(lengths, np.int32)), n_q, n_kv, D)
+    check_attention(out, q, codes, scales, tables, lengths, n_q, n_kv, D, sv.INT8)
 
 
 # ------------------------------------------------------------------------------------------------- append
