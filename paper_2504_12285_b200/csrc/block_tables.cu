@@ -39,11 +39,8 @@ struct TablesArgs {
 struct Ask {
     int len, used, n, need, back, fresh;  // fresh: new_tokens as given
 };
-// blocks that n rows take; n + rows - 1 may pass 32 bits, this does not
-__device__ __forceinline__ int blocks_of(int n, int rows) {
-    const int whole = n / rows;
-    return whole + (whole * rows < n);
-}
+// blocks that n rows take; n + rows - 1 may pass 2^31, not 2^32
+__device__ __forceinline__ int blocks_of(int n, int rows) { return (int)(((unsigned)n + (unsigned)rows - 1u) / (unsigned)rows); }
 __device__ __forceinline__ Ask ask_of(const TablesArgs& a, int r) {
     const int cap = a.max_blocks * a.block_rows;
     Ask k;
