@@ -621,8 +621,8 @@ def bitlinear_embed(ids, table, out=None):
     M, (V, K) = ids.shape[0], table.shape
     if out is None:
         out = torch.empty(M, K, dtype=torch.bfloat16, device=table.device)
-    elif _dev(out, torch.bfloat16, "out").shape != (M, K):  # the library writes M rows of K wherever out points
-        raise ValueError(f"out must be {(M, K)}, not {tuple(out.shape)}")
+    elif _dev(out, torch.bfloat16, "out").shape[-1] != K or out.numel() < M * K:  # the library writes M rows of K wherever out points
+        raise ValueError(f"out must have {M} rows of {K} or more, not {tuple(out.shape)}")
     _check(lib().bitlinear_embed(_ptr(ids), _ptr(table), M, V, K, _ptr(out), _stream()), "bitlinear_embed")
     return out
 

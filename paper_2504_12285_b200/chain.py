@@ -149,6 +149,8 @@ class DecodeStep:
 
     def step(self, ids: torch.Tensor) -> torch.Tensor:
         """ids: int32 [M] (device) -> logits fp32 [M, V]; appends this token's keys and values to every layer's cache."""
+        if ids.shape[0] != self.M:  # with fewer the rows behind them would go on from an earlier token
+            raise ValueError(f"ids must be [{self.M}], not {tuple(ids.shape)}")
         n_q, n_kv, hd = self.dims
         bl.bitlinear_embed(ids, self.table, out=self.h_in)
         for li, (qkv, o, gu, down) in enumerate(self.calls):
