@@ -128,6 +128,44 @@ def test_append_of_values_that_are_not_finite(kind, D, value):
     assert not np.isnan(host(pool[2])).any() and not np.isnan(host(pool[3])).any()
 
 
+def runs_in_blocks(runs, rows, rng):
+    """Slots and positions of runs (first row, number of rows) of sequences over shuffled blocks, and the number of blocks."""
+    used = [-(-(s + n) // rows) for s, n in runs]
+    ids = rng.permutation(sum(used) + 2)
+    slots, pos, b = [], [], 0
+    for (s, n), u in zip(runs, used):
+        p = np.arange(s, s + n)
+        slots += list(ids[b + p // rows] * rows + p % rows)
+        pos += list(p)
+        b += u
+    return np.array(slots, np.int64), np.array(pos, np.int64), sum(used) + 2
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,rows,shape", [(64, 16, "short"), (128, 16, "short"), (64, 128, "long"), (128, 32, "long"), (128, 64, "mixed"), (64, 32, "mixed")])
+def test_append_of_prompts(kind, D, rows, shape):
+    """More tokens than a CTA each would take (T * 2 * n_kv > 64 SMs' worth) and than one pass of the queries' CTAs: tiles with
+    several runs, runs that cross tiles, a last tile in part, tokens without a place inside a tile."""
+    rng = np.random.default_rng([D, rows])
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    n_kv = 2
+    least = max(16 * sms, 64 * sms // (2 * n_kv)) + 100
+    runs = []
+    while sum(n for _, n in runs) <= least:
+        runs.append((int(rng.integers(0, 2 * rows)), int({"short": rng.integers(1, 6), "long": rng.integers(200, 700), "mixed": rng.choice([1, 2, 3, 17, 90])}[shape])))
+    slots, pos, n_blocks = runs_in_blocks(runs, rows, rng)
+    T = len(slots)
+    if T % 16 == 0:
+        slots, pos, T = slots[:-1], pos[:-1], T - 1
+    assert T > 16 * sms and T * 2 * n_kv > 64 * sms and T % 16
+    # a run's last tokens have no place: padding, a slot past the pool, a position past the table
+    ends = np.cumsum([n for _, n in runs])[:-1] - 1
+    for i, e in enumerate(ends[3::7]):
+        slots[e] = (-1, n_blocks * rows + 5, slots[e])[i % 3]
+        pos[e] = (-1, pos[e], 5000)[i % 3]
+    check_append(kind, 4, n_kv, D, rows, slots, pos, 23, n_blocks=n_blocks, t_max=1024)
+
+
 # ------------------------------------------------------------------------------------------------- block tables
 
 def test_block_tables_of_blocks_as_long_as_the_type():
