@@ -226,7 +226,7 @@ class PagedDecodeStep:
         self.temperature, self.top_k = torch.ones(places, **f32), torch.zeros(places, **i32)
         self.top_p, self.min_p = torch.ones(places, **f32), torch.zeros(places, **f32)
         self.attn_ws = torch.empty(bl.bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), dtype=torch.uint8, device=dev)
-        self.ids, self.logprobs = torch.zeros(rows, **i32), torch.zeros(rows, **f32)
+        self.ids, self.logprobs, self.row_numbers = torch.zeros(rows, **i32), torch.zeros(rows, **f32), torch.arange(rows, device=dev)
         with torch.cuda.device(dev):
             self.calls = _token_calls(self, layers, rms_eps, dev)
             # a step that places nothing: sizes and types that one of the calls refuses are refused here, before there is a state to spoil
@@ -234,10 +234,11 @@ class PagedDecodeStep:
         torch.cuda.synchronize(dev)
 
     def step(self, token_ids: torch.Tensor, u: torch.Tensor):
-        """token_ids: int32 [rows] (device), the tokens of this step in the order of the places; u: fp32 [rows], a random number for each row.
+        """token_ids: int32 [rows] (device), the tokens that the places bring in this step, in the order of the places (those of a place that is
+        left out among them: a place whose tokens end beyond the rows is left out); u: fp32 [rows], a random number for each row.
         -> (ids int32 [rows], logprobs fp32 [rows]): the token drawn behind each row; the last row of place p is row
-        cu_tokens[p + 1] - 1, and rows from cu_tokens[-1] on mean nothing.  served[p] is 0 where the pool or the rows did not suffice
-        and the place's tokens were left out."""
+        cu_tokens[p + 1] - 1, and rows from cu_tokens[-1] on mean nothing.  served[p] is 0 where the pool, the rows or the place's table did
+        not suffice and the place's tokens were left out."""
         n_q, n_kv, hd = self.dims
         # all that a later call would refuse, before the first one changes the state
         bl._tensors((token_ids, torch.int32, (self.rows,), "token_ids"), (u, torch.float32, (self.rows,), "u"))
@@ -247,10 +248,17 @@ class PagedDecodeStep:
                 raise TypeError(f"{name} must be of {dtype} and on the step's device")
             if t.dim() != 1 or t.shape[0] < self.new_tokens.shape[0]:
                 raise ValueError(f"{name} must have an entry for each place")
+        # a place that outgrows its table is left out and those behind it are not: each place keeps its tokens, and one whose tokens are not
+        # all among token_ids asks for more than any table holds
+        brought = self.new_tokens.clamp(min=0)
+        ends = brought.cumsum(0)
+        new_tokens = self.new_tokens.masked_fill((ends > self.rows).logical_and_(brought > 0), 2 ** 31 - 1)
         (_, _, self.served, self.cu_tokens, self.seq_ids, self.positions, self.row_lengths, self.slots) = bl.bitlinear_block_tables(
-            self.lengths, self.new_tokens, self.tables, self.free_blocks, self.n_free, self.block_rows, self.rows, lengths_out=self.lengths,
+            self.lengths, new_tokens, self.tables, self.free_blocks, self.n_free, self.block_rows, self.rows, lengths_out=self.lengths,
             n_free_out=self.n_free)
-        bl.bitlinear_embed(token_ids, self.table, out=self.h_in)
+        place = self.seq_ids.clamp(min=0)
+        ahead = ends.sub_(brought).sub_(self.cu_tokens[:-1])  # tokens in front of a place that have no row
+        bl.bitlinear_embed(token_ids.index_select(0, ahead.index_select(0, place).add_(self.row_numbers)), self.table, out=self.h_in)
         for (qkv, o, gu, down), cache in zip(self.calls, self.cache):
             bl.bitlinear_forward_batch(*qkv, reuse_plan=True)
             bl.bitlinear_rope_kv8(self.q, self.k, self.v, self.positions, self.slots, self.rope_table, *cache, n_q, n_kv, hd, q_out=self.q_rot)
@@ -260,7 +268,6 @@ class PagedDecodeStep:
                 bl.bitlinear_forward_batch(batch, ws, reuse_plan=True)
         bl.bitlinear_glue_residual_add(self.h_mid, self.dn)  # the last layer's residual
         bl.bitlinear_lm_head(self.h_mid, self.table, out=self.logits)
-        place = self.seq_ids.clamp(min=0)
         return bl.bitlinear_sample(self.logits, u, *(x.index_select(0, place) for x in (self.temperature, self.top_k, self.top_p, self.min_p)),
                                    ids=self.ids, logprobs=self.logprobs)
 

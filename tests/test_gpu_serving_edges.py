@@ -256,3 +256,38 @@ def test_decode_step_refuses_other_numbers_of_tokens():
         with pytest.raises(ValueError):
             st.step(torch.zeros(n, dtype=torch.int32, device=DEV))
     assert st.step(torch.zeros(2, dtype=torch.int32, device=DEV)).shape == (2, 500)
+
+
+@pytest.mark.parametrize("recorded", [False, True])
+def test_paged_decode_step_keeps_tokens_with_their_places(recorded):
+    """A place that outgrows its table is left out and does not hold up the others: the places behind it still get their own tokens, those that
+    lie beyond the step's rows none."""
+    def run(new, tokens):
+        st, _ = paged_step(torch.int8)
+        if recorded:
+            st.capture()
+        # place 1 has 79 of the 80 rows that its table can name, the others start
+        st.tables[1] = torch.arange(9, 14, dtype=torch.int32, device=DEV)
+        st.lengths[1] = 79
+        st.n_free.fill_(9)
+        outs = []
+        for n, t in zip(new, tokens):
+            st.new_tokens.copy_(torch.tensor(n, dtype=torch.int32))
+            ids, u = torch.tensor((t + [0] * 6)[:6], dtype=torch.int32, device=DEV), torch.full((6,), 0.4, device=DEV)
+            if recorded:
+                st.token_buf.copy_(ids), st.u_buf.copy_(u)
+                got = st.step_graph()
+            else:
+                got = st.step(ids, u)
+            n = int(st.cu_tokens[-1])
+            outs += [got[0][:n].clone(), got[1][:n].clone(), st.logits[:n].clone(), st.served.clone(), st.lengths.clone()]
+        return outs
+
+    got = run(([1, 3, 1, 1], [1, 2 ** 31 - 1, 1, 0], [0, 2, 2, 2], [1, 1, 1, 1]), ([11, 21, 22, 23, 31, 41], [12, 24, 25, 26, 27, 28], [29, 29, 32, 33, 42, 43], [13, 20, 34, 44]))
+    want = run(([1, 0, 1, 1], [1, 0, 0, 0], [0, 0, 2, 2], [1, 1, 1, 1]), ([11, 31, 41], [12], [32, 33, 42, 43], [13, 20, 34, 44]))
+    served = ([1, 0, 1, 1], [1, 0, 0, 1], [1, 0, 1, 1], [1, 1, 1, 1])
+    for i, s in enumerate(served):
+        assert got[5 * i + 3].tolist() == s
+    for i, (a, b) in enumerate(zip(got, want)):
+        if i % 5 != 3:
+            assert torch.equal(a, b), i
