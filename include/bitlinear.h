@@ -564,9 +564,11 @@ int bitlinear_embed(const int32_t* ids, const void* table_bf16, int M, int V, in
  *     logprobs[m] = log of the kept share of that token (nullable).
  *   A temperature that is not above 0: the largest logit, lowest id first, logprob 0.  A NaN counts as -infinity; rows of -infinity
  *   alone give id -1 and logprob -infinity; +infinity shares all weight.  u outside [0, 1): the nearest inside.
- *   Weights are formed in fp64 (to 2^-37 of themselves) and summed as integers in units of 2^-44 of the largest, so the result does
- *   not depend on the order of a sum.  A temperature above 1e29 counts as 1e29.
- *   V <= BITLINEAR_SAMPLE_MAX_VOCAB.  One launch, no workspace.
+ *   Weights are formed in fp64 (to 2^-37 of themselves).  With a filter (top_k, top_p or min_p given, whatever its values) they are summed as
+ *   integers in units of 2^-44 of the largest, so the result does not depend on the order of a sum.  Without one, parts of a row are summed
+ *   in units of their own largest and then joined: totals are good to 2^-31 and depend in their last bits on how the row is aligned and
+ *   typed, so next to a border between two tokens the same logits elsewhere, or with filters that are all off, may draw the other one.
+ *   A temperature above 1e29 counts as 1e29.  V <= BITLINEAR_SAMPLE_MAX_VOCAB, M <= 2^24.  One launch, no workspace.
  */
 #define BITLINEAR_SAMPLE_MAX_VOCAB 360448
 int bitlinear_block_tables(const int32_t* lengths, const int32_t* new_tokens, int n_requests, int32_t* tables, int max_blocks,

@@ -5,7 +5,7 @@
 // needs is the k-th from the top.  Every CTA forms the three sums over all requests itself (a few kilobytes from L2),
 // which costs less than a second launch or a grid barrier; then it fills its share of the token arrays, four tokens per
 // thread and 16 bytes per store.  A small step is one CTA and bound by its chain of dependent loads (16 requests: 5.7 us,
-// launch included), a large one by the same chain and the bytes it writes (4096 requests, a million slots: 12.9 us, 1.4 TB/s).
+// launch included), a large one by the same chain and the bytes it writes (4096 requests, a million slots: 12.6 us, 1.4 TB/s).
 //
 // Nothing is read that another CTA writes: new table entries lie behind the ones that are looked up, blocks given back are
 // stored above the old top of the stack and taken from the tables where this step hands them out again, and lengths

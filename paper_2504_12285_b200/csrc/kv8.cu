@@ -169,7 +169,8 @@ struct RowValues {
 // to the new scale if it grew, and writes the run's codes.  So a block's scale has one writer and no atomics.
 // The result is that of fp64 arithmetic, the work mostly fp32: only values next to the largest, and next to the middle between two
 // codes, are formed again in fp64.  16,500 tokens of 20 + 5 heads of 128: 82 us, 4.4 TB/s of the bytes it cannot do without (all in
-// fp64 130 us); the queries' half streams at 7 TB/s, this half waits on its chain of loads (run, positions, rows, scale).
+// fp64 130 us); the queries' half alone takes 34 us (part of what it writes is still in L2 then), this half waits on its chain of
+// loads (run, positions, rows, scale).
 // Tried and slower: more rows per thread in flight, 256 threads, alternating the two kinds of CTA.  One token of 16 sequences:
 // 4.4 us, launch and that chain.
 template <int D, int KIND>
@@ -901,8 +902,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
             const float p0 = ex2(sv[hb][0] - b0), p1 = ex2(sv[hb][1] - b1), p2 = ex2(sv[hb][2] - b0), p3 = ex2(sv[hb][3] - b1);
             l_run[0] += p0 + p2;  // this lane's rows; summed over the lanes at the pair's end
             l_run[1] += p1 + p3;
-            // Weights as f16, scaled by 2^15 so that the smallest ones keep their bits: an error of 2^-12 of a weight, at random
-            // signs, against the result's own rounding of 2^-9.
+            // Weights as f16, scaled by 2^15 so that the smallest ones keep their bits: an error of up to 2^-11 of a weight (rows of equal
+            // weights err alike, so it does not average out), an eighth of the result's own rounding to bf16, up to 2^-8.  The sum
+            // that divides the result takes them unrounded.
             const float wv = w.vs[hb] * per_ref;
             const uint32_t w0 = movmatrix_t16(pack_f16(p0 * wv, p1 * wv)), w1 = movmatrix_t16(pack_f16(p2 * wv, p3 * wv));
 #pragma unroll
@@ -1126,7 +1128,7 @@ bool kv8_dims_ok(int n_q, int n_kv, int hd, int kind, int n_blocks, int block_ro
 
 int log2_of(int block_rows) { return block_rows == 16 ? 4 : block_rows == 32 ? 5 : block_rows == 64 ? 6 : 7; }
 
-// rows = every (block, head, row) of the pool, columns = D bytes; a box is min(32, block) whole rows, swizzled by the row's width
+// rows = every (block, head, row) of the pool, columns = D bytes; a box is a unit's rows, or a block's where that is fewer, swizzled by the row's width
 bool make_kv8_map(CUtensorMap* map, const void* pool, long long rows, int hd, int block_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;

@@ -14,7 +14,8 @@
 // 16 rows of mixed settings 34 us, those with a wide top-p set the time: four shared-memory additions per element.
 //
 // Which token comes out hangs on sums next to a border, so weights are formed in fp64 and summed as integers in units of
-// 2^-44: sums of any order are the same, and no two machines' rounding of a sum decides a token.
+// 2^-44 of the largest: sums of any order are the same, and no two machines' rounding of a sum decides a token.  The kernel without filters
+// meets the largest on its way and holds to this within a part of a row only (see there).
 #include "common.cuh"
 
 #include <cooperative_groups.h>
@@ -713,7 +714,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : 3) sample_kern
 }
 
 // The draw without filters: no threshold is wanted, so nothing is kept of a row.  Each warp of a cluster streams a contiguous part, its
-// weights relative to the largest logit it has met (a larger one rescales its sum); the cluster joins the warps' sums, and the
+// weights relative to the largest logit it has met (a larger one rescales its sum, at most 24 times at the largest vocabulary, each by a
+// factor good to 2^-37: a total is good to 2^-31 and depends in its last bits on where the parts begin); the cluster joins the warps' sums, and the
 // warp in whose part the goal lies goes over that part once more.  The weights' fp64 operations alone, 35 cycles per 32 weights and
 // scheduler, are 24 us for 192 rows of 128,256; the kernel takes 52 us (the one with filters 64): four CTAs of 256 threads per SM
 // beat two of 512 (63 us), eight elements per lane with the next eight on their way beat sixteen (62 us), and one join by the
