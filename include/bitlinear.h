@@ -587,6 +587,45 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
                      const int32_t* top_k, const float* top_p, const float* min_p, int32_t* ids, float* logprobs, void* stream);
 
 /*
+ * Answers that are sampled in groups, and learned from.  (No counterpart in the paper's text, which names preference optimisation as the
+ * last step of training, Section 3, without formulas; the definitions are stated here.)
+ *
+ * Logits are [T][V] fp32 or bf16 (logits_dtype), row t the distribution of token targets[t] (int32, device), rows row_stride elements
+ * apart, their base aligned to an element.  A target outside 0 .. V-1 (a prompt's token, padding) counts for nothing: its row is not read, its log probability is 0
+ * and its row of the gradient is zeros.  Logits of -infinity have no weight; a row that holds a NaN or +infinity, or nothing above -infinity, gives NaN.
+ * Gradients dlogits have the logits' type, rows d_stride elements apart; they may be the logits themselves (with the same stride) and must not
+ * overlap them otherwise.  V <= BITLINEAR_SAMPLE_MAX_VOCAB, T <= 2^24.
+ *
+ * bitlinear_token_logprobs: logprobs[t] = l[targets[t]] - max l - log(sum exp(l - max l)); stats [T][2] receives (max l, the sum), 8-byte aligned.
+ *   One launch; exponentials to 2^-22, sums in fp32 over at most V / 256 terms a thread, joined in a fixed order.
+ * bitlinear_token_logprobs_backward: dlogits[t][v] = grad[t] * ((v == targets[t]) - exp(l_v - max) / sum) from those stats; grad [T] fp32, the slope of any
+ *   loss with logprobs.  A row whose grad is 0 gets zeros and is not read.
+ * bitlinear_policy_loss: with r = exp(logp - old_logprobs[t]), A = advantages[t],
+ *     token_loss[t] = weights[t] * ( -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1) ),  d = ref_logprobs[t] - logp,
+ *   loss [1] their sum (fp64, fixed order), dlogits (nullable) its gradient; logits are read once.  weights NULL: 1; ref_logprobs may be NULL where kl_coef is 0.  A token
+ *   of weight 0 adds no loss and no gradient, whatever else stands in its place.  clip_low, clip_high >= 0.
+ * bitlinear_preference_loss: rows cu_tokens[i] .. cu_tokens[i+1]-1 (int32 [2 * pairs + 1], device) belong to answer i; answer 2j is preferred to answer 2j + 1.  With s_i
+ *   the sum of answer i's log probabilities (fp64, fixed order) and ref_logprobs [2 * pairs] the same sums of the reference model,
+ *     delta_j     = beta ((s_2j - ref_2j) - (s_2j+1 - ref_2j+1))
+ *     pair_loss_j = -(1 - label_smoothing) log sigma(delta_j) - label_smoothing log sigma(-delta_j);      loss [1] = their mean,
+ *   seq_logprobs [2 * pairs] = s, dlogits (nullable) the gradient of loss.  Offsets are clamped to 0 .. T and must not decrease; rows of no answer
+ *   get a gradient of zeros.  ws (device, 16-byte aligned) at least bitlinear_preference_loss_workspace_bytes(T) bytes.
+ */
+int bitlinear_token_logprobs(const void* logits, int logits_dtype, int T, int V, long long row_stride, const int32_t* targets, float* logprobs,
+                             float* stats, void* stream);
+int bitlinear_token_logprobs_backward(const void* logits, int logits_dtype, int T, int V, long long row_stride, const int32_t* targets,
+                                      const float* stats, const float* grad, void* dlogits, long long d_stride, void* stream);
+int bitlinear_policy_loss(const void* logits, int logits_dtype, int T, int V, long long row_stride, const int32_t* targets,
+                          const float* old_logprobs, const float* advantages, const float* weights, const float* ref_logprobs, float clip_low,
+                          float clip_high, float kl_coef, float* loss, float* token_loss, float* logprobs, void* dlogits, long long d_stride,
+                          void* stream);
+size_t bitlinear_preference_loss_workspace_bytes(int T);
+int bitlinear_preference_loss(const void* logits, int logits_dtype, int T, int V, long long row_stride, const int32_t* targets,
+                              const int32_t* cu_tokens, int pairs, const float* ref_logprobs, float beta, float label_smoothing, float* loss,
+                              float* pair_loss, float* seq_logprobs, float* logprobs, void* dlogits, long long d_stride, void* ws, size_t ws_bytes,
+                              void* stream);
+
+/*
  * Self-test of the bounded device-side waits (no counterpart in the paper: every kernel of this library waits on
  * barriers - for copies, for other warps, for other CTAs - and every such wait has a time limit, 2 s in production).
  * Launches one small CTA that waits, with a limit of limit_us microseconds (1 .. 100000), on a barrier nobody arrives

@@ -67,6 +67,13 @@ _SIGNATURES = {
     "bitlinear_attention_kv8_workspace_bytes": (_c_size_t, [_c_int, _c_int, _c_int]),
     "bitlinear_attention_decode_kv8": (_c_int, [_c_void_p] * 8 + [_c_int] * 9 + [_c_void_p, _c_void_p, _c_size_t, _c_void_p]),
     "bitlinear_sample": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 8),
+    "bitlinear_token_logprobs": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 4),
+    "bitlinear_token_logprobs_backward": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 4 + [ctypes.c_longlong, _c_void_p]),
+    "bitlinear_policy_loss": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 5 + [_c_float] * 3 + [_c_void_p] * 4 +
+                              [ctypes.c_longlong, _c_void_p]),
+    "bitlinear_preference_loss_workspace_bytes": (_c_size_t, [_c_int]),
+    "bitlinear_preference_loss": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 2 + [_c_int, _c_void_p] + [_c_float] * 2 +
+                                  [_c_void_p] * 5 + [ctypes.c_longlong, _c_void_p, _c_size_t, _c_void_p]),
     "bitlinear_poll_status": (_c_int, [_c_void_p]),
     "bitlinear_probe_int8_mma_rate": (_c_int, [_c_int, ctypes.POINTER(ctypes.c_double), _c_void_p]),
     "bitlinear_selftest_wait_timeout": (_c_int, [ctypes.c_uint, _c_void_p]),
@@ -767,6 +774,106 @@ def bitlinear_sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=
                                 _ptr(top_p), _ptr(min_p), ids.data_ptr(), logprobs.data_ptr(), _stream())
     _check(rc, "bitlinear_sample")
     return ids, logprobs
+
+
+def _logits(logits, name: str = "logits"):
+    """(dtype code, rows, columns, elements from a row to the next) of a matrix whose rows may be strided."""
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name} must be a CUDA tensor [T, V] of float32 or bfloat16")
+    T, V = logits.shape
+    stride = logits.stride(0) if T > 1 else V
+    if (V > 1 and logits.stride(1) != 1) or stride < V:
+        raise ValueError(f"the rows of {name} must be contiguous and must not overlap")
+    return F32 if logits.dtype == torch.float32 else BF16, T, V, stride
+
+
+def _dlogits(dlogits, logits):
+    """(the tensor for the logits' gradient - a new one for True, none for False -, elements from a row to the next)"""
+    if dlogits is None or dlogits is False:
+        return None, 0
+    if dlogits is True:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != logits.device:
+        raise ValueError("the gradient must have the type, shape and device of logits")
+    return dlogits, _logits(dlogits, "the gradient")[3]
+
+
+def bitlinear_token_logprobs(logits, targets, logprobs=None, stats=None):
+    """logits fp32 or bf16 [T, V] (rows may be strided), targets int32 [T] -> (log probability of each target fp32 [T], 0 for one outside the
+    vocabulary; statistics fp32 [T, 2] for the backward pass)."""
+    dtype, T, V, stride = _logits(logits)
+    new = dict(dtype=torch.float32, device=logits.device)
+    logprobs = torch.empty(T, **new) if logprobs is None else logprobs
+    stats = torch.empty(T, 2, **new) if stats is None else stats
+    if logits.get_device() != targets.get_device():
+        raise ValueError("logits and targets must be on one device")
+    _tensors((targets, torch.int32, (T,), "targets"), (logprobs, torch.float32, (T,), "logprobs"), (stats, torch.float32, (T, 2), "stats"))
+    rc = lib().bitlinear_token_logprobs(logits.data_ptr(), dtype, T, V, stride, targets.data_ptr(), logprobs.data_ptr(), stats.data_ptr(), _stream())
+    _check(rc, "bitlinear_token_logprobs")
+    return logprobs, stats
+
+
+def bitlinear_token_logprobs_backward(logits, targets, stats, grad, dlogits=None):
+    """The gradient of the logits for the slopes grad (fp32 [T]) of a loss with the log probabilities; dlogits: where it goes (logits itself, to save memory),
+    None: a new tensor."""
+    dtype, T, V, stride = _logits(logits)
+    dlogits, d_stride = _dlogits(True if dlogits is None else dlogits, logits)
+    if logits.get_device() != targets.get_device():
+        raise ValueError("logits and targets must be on one device")
+    _tensors((targets, torch.int32, (T,), "targets"), (stats, torch.float32, (T, 2), "stats"), (grad, torch.float32, (T,), "grad"))
+    rc = lib().bitlinear_token_logprobs_backward(logits.data_ptr(), dtype, T, V, stride, targets.data_ptr(), stats.data_ptr(), grad.data_ptr(), dlogits.data_ptr(),
+                                                 d_stride, _stream())
+    _check(rc, "bitlinear_token_logprobs_backward")
+    return dlogits
+
+
+def bitlinear_policy_loss(logits, targets, old_logprobs, advantages, weights=None, clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                          ref_logprobs=None, grad=False):
+    """Clipped policy loss with a KL term against a reference over the tokens targets (int32 [T]) of logits [T, V]; old_logprobs, advantages, weights,
+    ref_logprobs fp32 [T].  grad: False, True (a new tensor) or the tensor the gradient goes to (logits itself, to save memory)
+    -> (loss [1], token_loss [T], logprobs [T], dlogits [T, V] or None)."""
+    dtype, T, V, stride = _logits(logits)
+    dlogits, d_stride = _dlogits(grad, logits)
+    f32, rows = torch.float32, (T,)
+    loss, token_loss, logprobs = torch.empty(2 * T + 1, dtype=f32, device=logits.device).split_with_sizes((1, T, T))
+    if logits.get_device() != targets.get_device():
+        raise ValueError("logits and targets must be on one device")
+    if kl_coef != 0 and ref_logprobs is None:
+        raise ValueError("a KL term needs ref_logprobs")
+    _tensors((targets, torch.int32, rows, "targets"), (old_logprobs, f32, rows, "old_logprobs"), (advantages, f32, rows, "advantages"), (weights, f32, rows, "weights"),
+             (ref_logprobs, f32, rows, "ref_logprobs"))
+    rc = lib().bitlinear_policy_loss(logits.data_ptr(), dtype, T, V, stride, targets.data_ptr(), old_logprobs.data_ptr(), advantages.data_ptr(), _ptr(weights),
+                                     _ptr(ref_logprobs), clip_low, clip_high, kl_coef, loss.data_ptr(), token_loss.data_ptr(), logprobs.data_ptr(), _ptr(dlogits),
+                                     d_stride, _stream())
+    _check(rc, "bitlinear_policy_loss")
+    return loss, token_loss, logprobs, dlogits
+
+
+def bitlinear_preference_loss_workspace_bytes(T: int) -> int:
+    return int(lib().bitlinear_preference_loss_workspace_bytes(T))
+
+
+def bitlinear_preference_loss(logits, targets, cu_tokens, ref_logprobs, beta: float = 0.1, label_smoothing: float = 0.0, grad=False, ws=None):
+    """Loss over pairs of answers: rows cu_tokens[i] .. cu_tokens[i + 1] - 1 (int32 [2 * pairs + 1]) of logits [T, V] are answer i, answer 2j is
+    preferred to answer 2j + 1; ref_logprobs fp32 [2 * pairs], the answers' log probabilities under the reference.  grad as for bitlinear_policy_loss
+    -> (loss [1], pair_loss [pairs], seq_logprobs [2 * pairs], logprobs [T], dlogits [T, V] or None)."""
+    dtype, T, V, stride = _logits(logits)
+    dlogits, d_stride = _dlogits(grad, logits)
+    n = ref_logprobs.shape[0] if ref_logprobs.dim() == 1 else 0
+    if n == 0 or n % 2:
+        raise ValueError("ref_logprobs must be [2 * pairs]")
+    f32 = torch.float32
+    loss, pair_loss, seq_logprobs, logprobs = torch.empty(1 + n // 2 + n + T, dtype=f32, device=logits.device).split_with_sizes((1, n // 2, n, T))
+    if ws is None:
+        ws = _workspace(bitlinear_preference_loss_workspace_bytes(T), logits.device)
+    if logits.get_device() != targets.get_device():
+        raise ValueError("logits and targets must be on one device")
+    _tensors((targets, torch.int32, (T,), "targets"), (cu_tokens, torch.int32, (n + 1,), "cu_tokens"), (ref_logprobs, f32, None, "ref_logprobs"), (ws, torch.uint8, None, "ws"))
+    rc = lib().bitlinear_preference_loss(logits.data_ptr(), dtype, T, V, stride, targets.data_ptr(), cu_tokens.data_ptr(), n // 2, ref_logprobs.data_ptr(), beta,
+                                         label_smoothing, loss.data_ptr(), pair_loss.data_ptr(), seq_logprobs.data_ptr(), logprobs.data_ptr(), _ptr(dlogits), d_stride,
+                                         ws.data_ptr(), ws.numel(), _stream())
+    _check(rc, "bitlinear_preference_loss")
+    return loss, pair_loss, seq_logprobs, logprobs, dlogits
 
 
 def bitlinear_selftest_wait_timeout(limit_us: int = 1000) -> None:
