@@ -610,7 +610,25 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
  *     pair_loss_j = -(1 - label_smoothing) log sigma(delta_j) - label_smoothing log sigma(-delta_j);      loss [1] = their mean,
  *   seq_logprobs [2 * pairs] = s, dlogits (nullable) the gradient of loss.  Offsets are clamped to 0 .. T and must not decrease; rows of no answer
  *   get a gradient of zeros.  ws (device, 16-byte aligned) at least bitlinear_preference_loss_workspace_bytes(T) bytes.
+ *
+ * bitlinear_attention_shared_kv8: bitlinear_attention_decode_kv8 for rows that share cache rows, which are then read and multiplied once for all of them.
+ *   Rows group_starts[g] .. group_starts[g+1]-1 (int32 [n_groups + 1], device, not decreasing; clamped to 0 .. M) are group g, and its rows' first
+ *   shared_rows[g] cache rows (int32 [n_groups], device) are the same rows of the pool: their sequences' tables agree there (not checked; they are read by the table
+ *   of the group's first row that has a length).  Answers to one prompt, each a sequence of its own, share the prompt's blocks; the tokens of a
+ *   prompt's chunk are rows of one sequence with lengths position + 1, and share all of it.  A row uses none but the cache rows in front of its own length, shared
+ *   or not; shared_rows need not be a multiple of anything, and may be longer than some rows of the group.  Rows of no group share nothing.
+ *   Definition, types, limits, status word and what becomes of rows without a length as for bitlinear_attention_decode_kv8, with these exceptions:
+ *   queries are scaled by a power of two per head and enter the tensor cores as f16, exactly down to 2^-22 of the head's largest magnitude, and products
+ *   are summed in fp32 over either kind of pool; scales must not be negative; a NaN among the e4m3 codes of a value that one row of a group uses may show in the others.
+ *   M * n_kv * (max_blocks * block_rows / 128 + 3) < 2^30, n_groups <= 65535.  ws (device, 16-byte aligned) at least
+ *   bitlinear_attention_shared_kv8_workspace_bytes(...) bytes (0 for unsupported sizes; it grows with M and n_groups); contents need not survive, calls that share one must not overlap.
+ *   Three launches.
  */
+size_t bitlinear_attention_shared_kv8_workspace_bytes(int M, int n_groups, int n_q_heads, int n_kv_heads, int head_dim);
+int bitlinear_attention_shared_kv8(const void* q_bf16, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                                   const int32_t* tables, const int32_t* lengths, const int32_t* seq_ids, const int32_t* group_starts,
+                                   const int32_t* shared_rows, int M, int n_groups, int n_q_heads, int n_kv_heads, int head_dim, int kv_dtype,
+                                   int n_blocks, int block_rows, int n_seq, int max_blocks, void* out_bf16, void* ws, size_t ws_bytes, void* stream);
 int bitlinear_token_logprobs(const void* logits, int logits_dtype, int T, int V, long long row_stride, const int32_t* targets, float* logprobs,
                              float* stats, void* stream);
 int bitlinear_token_logprobs_backward(const void* logits, int logits_dtype, int T, int V, long long row_stride, const int32_t* targets,

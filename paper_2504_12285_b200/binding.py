@@ -67,6 +67,8 @@ _SIGNATURES = {
     "bitlinear_attention_kv8_workspace_bytes": (_c_size_t, [_c_int, _c_int, _c_int]),
     "bitlinear_attention_decode_kv8": (_c_int, [_c_void_p] * 8 + [_c_int] * 9 + [_c_void_p, _c_void_p, _c_size_t, _c_void_p]),
     "bitlinear_sample": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 8),
+    "bitlinear_attention_shared_kv8_workspace_bytes": (_c_size_t, [_c_int] * 5),
+    "bitlinear_attention_shared_kv8": (_c_int, [_c_void_p] * 10 + [_c_int] * 10 + [_c_void_p, _c_void_p, _c_size_t, _c_void_p]),
     "bitlinear_token_logprobs": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 4),
     "bitlinear_token_logprobs_backward": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 4 + [ctypes.c_longlong, _c_void_p]),
     "bitlinear_policy_loss": (_c_int, [_c_void_p, _c_int, _c_int, _c_int, ctypes.c_longlong] + [_c_void_p] * 5 + [_c_float] * 3 + [_c_void_p] * 4 +
@@ -749,6 +751,35 @@ def bitlinear_attention_decode_kv8(q, k_cache, v_cache, k_scale, v_scale, tables
                                               lengths.data_ptr(), _ptr(seq_ids), M, n_q_heads, n_kv_heads, head_dim, kind, n_blocks, block_rows, n_seq,
                                               max_blocks, out.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
     _check(rc, "bitlinear_attention_decode_kv8")
+    return out
+
+
+def bitlinear_attention_shared_kv8_workspace_bytes(M: int, n_groups: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().bitlinear_attention_shared_kv8_workspace_bytes(M, n_groups, n_q_heads, n_kv_heads, head_dim))
+
+
+def bitlinear_attention_shared_kv8(q, k_cache, v_cache, k_scale, v_scale, tables, lengths, group_starts, shared_rows, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                                   seq_ids=None, out=None, ws=None):
+    """bitlinear_attention_decode_kv8 where rows group_starts[g] .. group_starts[g + 1] - 1 (int32 [G + 1]) share their first shared_rows[g] (int32 [G]) rows of
+    the cache: answers to one prompt, or the tokens of a prompt's chunk -> bf16 [M, n_q * D]."""
+    M = q.shape[0]
+    kind, n_blocks, block_rows = _pool(k_cache, v_cache, k_scale, v_scale, n_kv_heads, head_dim)
+    G = shared_rows.shape[0] if shared_rows.dim() == 1 else -1
+    if tables.dim() != 2 or G < 0:
+        raise ValueError("tables must be [n_seq, max_blocks], shared_rows [G]")
+    if out is None:
+        out = torch.empty_like(q)
+    if ws is None:
+        ws = _workspace(bitlinear_attention_shared_kv8_workspace_bytes(M, G, n_q_heads, n_kv_heads, head_dim), q.device)
+    bf16, f32, i32, code, rows = torch.bfloat16, torch.float32, torch.int32, k_cache.dtype, (M,)
+    _tensors((q, bf16, (M, n_q_heads * head_dim), "q"), (k_cache, code, None, "k_cache"), (v_cache, code, None, "v_cache"), (k_scale, f32, None, "k_scale"),
+             (v_scale, f32, None, "v_scale"), (tables, i32, None, "tables"), (lengths, i32, rows, "lengths"), (seq_ids, i32, rows, "seq_ids"),
+             (group_starts, i32, (G + 1,), "group_starts"), (shared_rows, i32, None, "shared_rows"), (out, bf16, q.shape, "out"), (ws, torch.uint8, None, "ws"))
+    n_seq, max_blocks = tables.shape
+    rc = lib().bitlinear_attention_shared_kv8(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), tables.data_ptr(),
+                                              lengths.data_ptr(), _ptr(seq_ids), group_starts.data_ptr(), shared_rows.data_ptr(), M, G, n_q_heads, n_kv_heads, head_dim, kind,
+                                              n_blocks, block_rows, n_seq, max_blocks, out.data_ptr(), ws.data_ptr(), ws.numel(), _stream())
+    _check(rc, "bitlinear_attention_shared_kv8")
     return out
 
 

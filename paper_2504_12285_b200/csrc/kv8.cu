@@ -4,6 +4,7 @@
 // Layout: pools [n_blocks][n_kv][block_rows][D] of codes (int8, or e4m3 floats), scales fp32 [n_blocks][n_kv]; a row's value is
 // code * scale.  A (block, head) tile is contiguous, so attention fetches it with one tensor-map copy.
 #include "common.cuh"
+#include "kv8.cuh"
 #include "sm100_sync.cuh"
 #include "tensor_map.cuh"
 
@@ -452,36 +453,6 @@ __device__ __forceinline__ uint32_t movmatrix_t16(uint32_t a) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-}
-// 2^x to two units in the last place; results below 2^-126 are 0
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// Four codes of a word -> two pairs of f16, exactly.  int8: the code plus 128 becomes the low bits of 1024 + x, and
-// 1152 is taken off.  e4m3: the conversion instruction.
-template <int KIND>
-__device__ __forceinline__ void to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-    if constexpr (KIND == BITLINEAR_KV_INT8) {
-        const uint32_t u = w ^ 0x80808080u;
-        const uint32_t off = 0x64806480u, l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
-        const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&l), *reinterpret_cast<const __half2*>(&off));
-        const __half2 b = __hsub2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&off));
-        lo = *reinterpret_cast<const uint32_t*>(&a);
-        hi = *reinterpret_cast<const uint32_t*>(&b);
-    } else {
-        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
-    }
-}
-
-__device__ __forceinline__ void lds128(uint32_t addr, uint32_t (&r)[4]) {
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
 __device__ __forceinline__ void lds64(uint32_t addr, uint32_t (&r)[2]) {
     asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
 }
@@ -832,8 +803,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
 #pragma unroll
                     for (int st = 0; st < 4; ++st) {
                         uint32_t f[4];
-                        to_f16<KIND>(x[hf][st], f[0], f[2]);
-                        to_f16<KIND>(y[hf][st], f[1], f[3]);
+                        codes_to_f16<KIND>(x[hf][st], f[0], f[2]);
+                        codes_to_f16<KIND>(y[hf][st], f[1], f[3]);
                         if (st & 1) mma_f16(s1, f, qb[4 * hf + st][0], qb[4 * hf + st][1]);
                         else mma_f16(s0, f, qb[4 * hf + st][0], qb[4 * hf + st][1]);
                     }
@@ -912,11 +883,11 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_decode_kv8_kernel(const __
                 const uint32_t t0 = __byte_perm(x[0][q], x[1][q], 0x5140), t1 = __byte_perm(x[2][q], x[3][q], 0x5140);
                 const uint32_t t2 = __byte_perm(x[0][q], x[1][q], 0x7362), t3 = __byte_perm(x[2][q], x[3][q], 0x7362);
                 uint32_t f[4];
-                to_f16<KIND>(t0, f[0], f[1]);
-                to_f16<KIND>(t1, f[2], f[3]);
+                codes_to_f16<KIND>(t0, f[0], f[1]);
+                codes_to_f16<KIND>(t1, f[2], f[3]);
                 mma_f16(o[2 * q], f, w0, w1);
-                to_f16<KIND>(t2, f[0], f[1]);
-                to_f16<KIND>(t3, f[2], f[3]);
+                codes_to_f16<KIND>(t2, f[0], f[1]);
+                codes_to_f16<KIND>(t3, f[2], f[3]);
                 mma_f16(o[2 * q + 1], f, w0, w1);
             }
         }
@@ -1119,14 +1090,6 @@ __global__ void __launch_bounds__(8 * D) attn_decode_kv8_combine_kernel(const fl
 }
 
 // ---------------------------------------------------------------------------------------------- host side
-
-bool kv8_dims_ok(int n_q, int n_kv, int hd, int kind, int n_blocks, int block_rows) {
-    return n_q > 0 && n_kv > 0 && n_q % n_kv == 0 && n_q / n_kv <= 8 && (hd == 64 || hd == 128) && (kind == BITLINEAR_KV_INT8 || kind == BITLINEAR_KV_E4M3) &&
-           n_blocks > 0 && (block_rows == 16 || block_rows == 32 || block_rows == 64 || block_rows == 128) &&
-           (long long)n_blocks * n_kv * block_rows <= (1ll << 31) - 256;
-}
-
-int log2_of(int block_rows) { return block_rows == 16 ? 4 : block_rows == 32 ? 5 : block_rows == 64 ? 6 : 7; }
 
 // rows = every (block, head, row) of the pool, columns = D bytes; a box is a unit's rows, or a block's where that is fewer, swizzled by the row's width
 bool make_kv8_map(CUtensorMap* map, const void* pool, long long rows, int hd, int block_rows) {

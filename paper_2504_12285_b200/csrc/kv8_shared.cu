@@ -1,0 +1,1083 @@
+// Attention of many rows over an 8-bit paged cache where groups of rows share their first cache rows: answers to one prompt, or the tokens of a
+// prompt's chunk, each of which sees those in front of it.  A group's shared rows are read and multiplied once for all of its rows.
+//
+//   out[m] = sum_t exp(s_t - max s) v_t / sum_t exp(s_t - max s),  s_t = q[m] . k_t / sqrt(D),  over the rows 0 .. lengths[m] - 1
+//
+// The query rows of a group and KV head - a row of the call is n_q / n_kv of them - are the 128 rows of a tensor-core tile, 128 cache rows the other side:
+// S = Q K^T and O += P V by tcgen05.mma (f16 operands, fp32 accumulators in tensor memory).  Codes arrive by tensor-map copies and become f16 in shared
+// memory, which is exact; their scales go onto the scores and the softmax weights in fp32.  Queries are f16 times a power of two per row, exact too.
+//
+// A CTA runs two streams of such tiles, each with a Q tile, a score tile, an accumulator and four softmax warps of its own, so that one stream's
+// softmax runs beside the other's products.  Where a group has more than 128 query rows, the streams take two tiles of them over the same
+// cache rows (which are then converted once); else they take different cache rows.  What a row does not share is work of the same kind, with the few
+// query rows of that row alone.  All of it is cut into equal runs, one per CTA, whatever the lengths; parts of a row meet in a last launch.
+//
+//   warp 0      copies: block tables -> tensor-map copies of code tiles, and the work list that the other warps follow
+//   warp 1      one thread issues the products
+//   warps 4-11  softmax, one thread per query row; four warps per stream
+//   warps 12-15 codes -> f16
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "common.cuh"
+#include "kv8.cuh"
+#include "sm100_sync.cuh"
+#include "tensor_map.cuh"
+
+namespace bitlinear {
+
+namespace {
+
+constexpr int kTile = 128;         // query rows and cache rows of a product
+constexpr int kPlanThreads = 1024;
+constexpr int kThreads = 512;
+constexpr int kSharedCtas = 160;   // parts are reserved for this many
+constexpr int kDescs = 4;
+constexpr float kWeightScale = 128.0f;  // weights of up to 2^8 (the maximum is followed lazily) stay below f16's largest
+
+// Workspace.  A part: fp32 values of its query rows, then (max, sum) of each.
+struct SharedLayout {
+    size_t rows, pairs, cum_pairs, cum_rows, starts, firsts, totals, parts_w, parts_s, total;
+    int max_pairs;
+};
+struct SharedArgs {
+    const __nv_bfloat16* q;
+    const float* k_scale;
+    const float* v_scale;
+    const int* tables;
+    const int* lengths;
+    const int* seq_ids;
+    const int* group_starts;
+    const int* shared_rows;
+    int M, n_groups, n_q, n_kv, group, n_seq, max_blocks, log2_rows, n_blocks;
+    float scale_log2;  // log2(e) / sqrt(D)
+    __nv_bfloat16* out;
+    int4* rows;       // of each row: cache rows it shares, its length, its group's first pair (-1: none), that group's first query row
+    int4* pairs;      // of each pair of query tiles: its first query row, query rows, sequence, cache rows
+    int* cum_pairs;   // units of the pairs in front, all heads
+    int* cum_rows;    // tiles of the rows' own parts in front, all heads
+    int* starts;      // group_starts, in range and not decreasing
+    int* firsts;      // of each group: its first row with something in the cache
+    int* totals;      // pairs, units of pairs, tiles of rows
+    float* parts_w;
+    float* parts_s;
+    int max_pairs;
+    int* status;
+};
+
+__host__ __device__ inline size_t part_floats(int rows, int D) { return (size_t)rows * D + ((2 * rows + 3) & ~3); }  // (a multiple of sixteen bytes)
+
+// the places 0 .. total - 1 in equal runs: worker w has begin(w) .. begin(w + 1) - 1
+struct EqualRuns {
+    int each, more;
+    __device__ __forceinline__ EqualRuns(int total, int workers) : each((int)((unsigned)total / (unsigned)workers)), more(total - each * workers) {}
+    __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int owner(int at) const {
+        const int border = more * (each + 1);
+        return at < border ? (int)((unsigned)at / (unsigned)(each + 1)) : more + (int)((unsigned)(at - border) / (unsigned)each);
+    }
+};
+// A CTA's share: units of pairs (two places each: a step of both streams), then tiles of rows (one place), the first half of them the first stream's.
+struct Share {
+    int w0, w1, s0, s1;
+    __device__ __forceinline__ Share(const EqualRuns& runs, int units, int cta) {
+        const int p0 = runs.begin(cta), p1 = runs.begin(cta + 1), border = 2 * units;
+        w0 = min((p0 + 1) >> 1, units), w1 = min((p1 + 1) >> 1, units);
+        s0 = max(p0 - border, 0), s1 = max(p1 - border, 0);
+    }
+    __device__ __forceinline__ int middle() const { return s0 + ((s1 - s0 + 1) >> 1); }
+};
+
+// ---------------------------------------------------------------------------------------------- plan
+
+__device__ __forceinline__ int block_exclusive_scan(int x, int* warp_sums, int& total) {  // of kPlanThreads numbers
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int incl = x;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += up;
+    }
+    __syncthreads();
+    if (lane == 31) warp_sums[warp] = incl;
+    __syncthreads();
+    int w = warp_sums[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, w, d);
+        if (lane >= d) w += up;
+    }
+    total = __shfl_sync(0xffffffffu, w, 31);
+    const int before = __shfl_sync(0xffffffffu, w, max(warp - 1, 0));
+    return incl - x + (warp > 0 ? before : 0);
+}
+__device__ __forceinline__ int block_max_scan(int x, int* warp_sums) {  // inclusive, of numbers that are not negative
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x = max(x, up);
+    }
+    __syncthreads();
+    if (lane == 31) warp_sums[warp] = x;
+    __syncthreads();
+    int w = warp_sums[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, w, d);
+        if (lane >= d) w = max(w, up);
+    }
+    const int before = __shfl_sync(0xffffffffu, w, max(warp - 1, 0));
+    return warp > 0 ? max(x, before) : x;
+}
+
+// One CTA: which rows share what, the pairs of query tiles, and how many units lie in front of each pair and row.
+__global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedArgs a) {
+    __shared__ int warp_sums[32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int tid = threadIdx.x, cap = a.max_blocks << a.log2_rows;
+    // the groups' borders
+    int carry = 0;
+    for (int g0 = 0; g0 <= a.n_groups; g0 += kPlanThreads) {
+        const int g = g0 + tid;
+        const int x = g <= a.n_groups ? min(max(a.group_starts[g], 0), a.M) : 0;
+        const int y = max(block_max_scan(x, warp_sums), carry);
+        if (g <= a.n_groups) a.starts[g] = y;
+        __syncthreads();
+        carry = a.starts[min(g0 + kPlanThreads - 1, a.n_groups)];
+    }
+    __syncthreads();
+    // the groups' pairs; a row on its own shares nothing.  pairs[].z holds the group for now, pairs[].w the most that the pair's rows share
+    int n_pairs = 0;
+    for (int g0 = 0; g0 < a.n_groups; g0 += kPlanThreads) {
+        const int g = g0 + tid;
+        int n = 0, first = 0, query_rows = 0;
+        if (g < a.n_groups) {
+            first = a.starts[g];
+            const int rows = a.starts[g + 1] - first;
+            query_rows = rows * a.group;
+            if (rows > 1 && a.shared_rows[g] > 0) n = (query_rows + 2 * kTile - 1) / (2 * kTile);
+        }
+        int total;
+        const int at = n_pairs + block_exclusive_scan(n, warp_sums, total);
+        for (int i = 0; i < n; ++i) a.pairs[at + i] = make_int4(first * a.group + i * 2 * kTile, min(2 * kTile, query_rows - i * 2 * kTile), g, 0);
+        if (g < a.n_groups) {
+            a.cum_pairs[g] = n > 0 ? at : -1;  // (for the rows below; overwritten after that)
+            a.firsts[g] = a.M;
+        }
+        n_pairs += total;
+    }
+    __syncthreads();
+    int tiles_before = 0;
+    for (int m0 = 0; m0 < a.M; m0 += kPlanThreads) {
+        const int m = m0 + tid;
+        int tiles = 0;
+        if (m < a.M) {
+            const int seq = a.seq_ids ? a.seq_ids[m] : m;
+            const int len = seq < 0 || seq >= a.n_seq ? 0 : min(max(a.lengths[m], 0), cap);
+            // the last group that begins at or before the row, if the row is not behind its end
+            int lo = 0, hi = a.n_groups;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (a.starts[mid] <= m) lo = mid;
+                else hi = mid - 1;
+            }
+            int4 info = make_int4(0, len, -1, 0);
+            if (lo < a.n_groups && a.starts[lo] <= m && a.cum_pairs[lo] >= 0) {
+                const int flat0 = a.starts[lo] * a.group;
+                info = make_int4(min(len, a.shared_rows[lo]), len, a.cum_pairs[lo], flat0);
+                if (len > 0) {
+                    const int p0 = info.z + (m * a.group - flat0) / (2 * kTile), p1 = info.z + (m * a.group + a.group - 1 - flat0) / (2 * kTile);
+                    for (int p = p0; p <= p1; ++p) atomicMax(&a.pairs[p].w, info.x);
+                    if (a.firsts[lo] > m) atomicMin(&a.firsts[lo], m);
+                }
+            }
+            a.rows[m] = info;
+            if (len > info.x) tiles = (len - ((info.x >> a.log2_rows) << a.log2_rows) + kTile - 1) / kTile * a.n_kv;
+        }
+        int total;
+        const int at = tiles_before + block_exclusive_scan(tiles, warp_sums, total);
+        if (m < a.M) a.cum_rows[m] = at;
+        tiles_before += total;
+    }
+    __syncthreads();
+    int units_before = 0;
+    for (int p0 = 0; p0 < n_pairs; p0 += kPlanThreads) {
+        const int p = p0 + tid;
+        int units = 0;
+        if (p < n_pairs) {
+            int4 info = a.pairs[p];
+            const int span = info.y > kTile ? kTile : 2 * kTile;  // a unit: one tile of cache rows for two query tiles, or two for one
+            units = (info.w + span - 1) / span * a.n_kv;
+            const int first = a.firsts[info.z];
+            info.z = first < a.M ? (a.seq_ids ? a.seq_ids[first] : first) : 0;  // (no row has anything in the cache: no units)
+            a.pairs[p] = info;
+        }
+        int total;
+        const int at = units_before + block_exclusive_scan(units, warp_sums, total);
+        if (p < n_pairs) a.cum_pairs[p] = at;
+        units_before += total;
+    }
+    if (tid == 0) {
+        a.cum_pairs[n_pairs] = units_before;
+        a.cum_rows[a.M] = tiles_before;
+        a.totals[0] = n_pairs, a.totals[1] = units_before, a.totals[2] = tiles_before;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- tensor-core pieces
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Operand tiles: rows of 128 bytes (64 f16), 128-byte swizzle, groups of eight rows 1024 bytes apart; the second 64 columns follow 128 rows later.
+// Read along the rows (queries and keys: the product's sum runs over dims) the leading offset has no meaning; read across them (values: the sum runs over cache
+// rows) it leads from 64 dims to the next 64.
+constexpr uint32_t kHalfTile = kTile * 128;
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(leading >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// D fp32, A and B f16; B read across its rows where `across`
+__host__ __device__ constexpr uint32_t instruction(int n, bool across) {
+    return (1u << 4) | (across ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+}
+
+#define TM32(r) \
+    "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), \
+        "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),     \
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+// lane l of the warp: 32 columns of its row
+__device__ __forceinline__ void tm_load(uint32_t at, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : TM32(r)
+        : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tm_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]),
+        "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]),
+        "r"(v[29]), "r"(v[30]), "r"(v[31])
+        : "memory");
+}
+__device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void code_rows(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(bar)
+                 : "memory");
+}
+
+// ---------------------------------------------------------------------------------------------- main kernel
+
+// One stream's half of a step.
+struct Side {
+    int live, first, last;  // is there one; does its softmax begin, end with it
+    int own;                // 0: a tile of a pair; 1: of what a row has for itself
+    int row0, rows;         // query rows
+    int head;
+    int base;               // first cache row
+    int cache_rows;         // of the tile, those that any query row uses
+    int lost;               // bit i: cache rows 16 i .. 16 i + 15 belong to no block
+    int part, pad;          // where the result goes
+};
+struct __align__(16) Desc {
+    Side side[2];
+    float ks[2][8], vs[2][8];  // scales of each sixteen rows
+    int end, common, pad[2];   // no more steps; both streams use the first one's cache rows
+};
+
+template <int D>
+struct SharedSmem {
+    static constexpr int kOperands = D == 128 ? 3 : 4;  // tiles of f16
+    static constexpr int kStages = D == 128 ? 4 : 8;    // tiles of codes
+    static constexpr uint32_t kOperandBytes = kTile * D * 2, kCodeBytes = kTile * D;
+    static constexpr uint32_t q = 0, operands = 2 * kOperandBytes, codes = operands + kOperands * kOperandBytes, descs = codes + kStages * kCodeBytes;
+    static constexpr uint32_t bars = descs + kDescs * sizeof(Desc);
+    // barriers
+    static constexpr int code_full = 0, code_empty = code_full + kStages, op_full = code_empty + kStages, op_empty = op_full + kOperands, desc_full = op_empty + kOperands,
+                         desc_empty = desc_full + kDescs, q_full = desc_empty + kDescs, s_full = q_full + 2, p_full = s_full + 2, o_full = p_full + 2, n_bars = o_full + 2;
+    static constexpr uint32_t total = bars + n_bars * 8 + 16;
+};
+
+template <int D, int KIND>
+__global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const SharedArgs a) {
+    using L = SharedSmem<D>;
+    extern __shared__ uint8_t shared_raw[];
+    uint8_t* smem = shared_raw + ((1024u - (smem_u32(shared_raw) & 1023u)) & 1023u);
+    const uint32_t base_s = smem_u32(smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+    Desc* descs = reinterpret_cast<Desc*>(smem + L::descs);
+    auto bar = [&](int i) { return base_s + L::bars + 8u * (uint32_t)i; };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::bars + L::n_bars * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    if (tid == 0) {
+        *abort_flag = 0;
+        for (int i = 0; i < L::kStages; ++i) mbar_init(bar(L::code_full + i), 1), mbar_init(bar(L::code_empty + i), 4);
+        for (int i = 0; i < L::kOperands; ++i) mbar_init(bar(L::op_full + i), 4), mbar_init(bar(L::op_empty + i), 1);
+        for (int i = 0; i < kDescs; ++i) mbar_init(bar(L::desc_full + i), 1 + 32), mbar_init(bar(L::desc_empty + i), 1 + 4 + 8);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(L::q_full + s), 4);
+            mbar_init(bar(L::s_full + s), 1);
+            mbar_init(bar(L::p_full + s), 4);
+            mbar_init(bar(L::o_full + s), 1);
+        }
+        mbar_init_fence();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    auto tm_s = [&](int s) { return tmem + (uint32_t)(s * kTile); };            // scores, then weights, of a stream
+    auto tm_o = [&](int s) { return tmem + (uint32_t)(2 * kTile + s * D); };  // its accumulator
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // All roles walk the steps in the same order of products: S of step 0 (both streams), then for every step and stream O, and S of the step behind.
+    // Operand tiles are made and used in that order.
+    if (warp == 0) {
+        // ------------------------------------------------------------------ copies and the work list
+        const int units = a.totals[1], tiles = a.totals[2];
+        const EqualRuns runs(2 * units + tiles, gridDim.x);
+        const Share share(runs, units, cta);
+        // the entry of cum[0 .. n] (not decreasing) that holds `at`: the last one that is not above it
+        auto find = [&](const int* cum, int n, int at) {
+            int lo = 0, hi = n;  // cum[lo] <= at < cum[hi]
+            while (hi - lo > 1) {
+                const int step = max(1, (hi - lo) / 32), probe = min(lo + step * (lane + 1), hi);
+                const unsigned above = __ballot_sync(0xffffffffu, probe >= hi || cum[probe] > at);
+                const int i = __ffs((int)above) - 1;  // (lane 31 may probe below hi)
+                if (i < 0) lo = lo + 32 * step;
+                else {
+                    const int l = lo;
+                    lo = l + step * i;
+                    hi = min(l + step * (i + 1), hi);
+                }
+            }
+            return lo;
+        };
+        // units of pairs
+        int wu = share.w0, pair = 0, w_head = 0, w_unit = 0, w_units = 1;
+        int4 pair_info = make_int4(0, 0, 0, 0);
+        if (wu < share.w1) {
+            pair = find(a.cum_pairs, a.totals[0], wu);
+            const int c = a.cum_pairs[pair];
+            w_units = (a.cum_pairs[pair + 1] - c) / a.n_kv;
+            w_head = (wu - c) / w_units;
+            w_unit = wu - c - w_head * w_units;
+            pair_info = a.pairs[pair];
+        }
+        // tiles of rows, of each stream
+        int su[2] = {share.s0, share.middle()}, s_end[2] = {share.middle(), share.s1}, m[2] = {0, 0}, s_head[2] = {0, 0}, s_tile[2] = {0, 0}, s_tiles[2] = {1, 1};
+        int4 row_info[2] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (su[s] < s_end[s]) {
+                m[s] = find(a.cum_rows, a.M, su[s]);
+                const int c = a.cum_rows[m[s]];
+                s_tiles[s] = (a.cum_rows[m[s] + 1] - c) / a.n_kv;
+                s_head[s] = (su[s] - c) / s_tiles[s];
+                s_tile[s] = su[s] - c - s_head[s] * s_tiles[s];
+                row_info[s] = a.rows[m[s]];
+            }
+        const int per_tile = kTile >> a.log2_rows;  // blocks
+        struct Tiles {  // of a step: lane l has block l of each stream's tile
+            int id[2], head[2];
+            bool there[2];
+        };
+        int made = 0;  // code tiles so far
+        bool ok = true;
+        // publishes step p; false at the end
+        auto publish = [&](int p, Tiles& now) {
+            const int slot = p % kDescs;
+            if (p >= kDescs && !mbar_wait(bar(L::desc_empty + slot), (uint32_t)(p / kDescs - 1) & 1u, abort_flag)) ok = false;
+            if (!(ok = __all_sync(0xffffffffu, ok))) return false;
+            Desc& d = descs[slot];
+            const bool pairs_left = wu < share.w1;
+            const bool end = !pairs_left && su[0] >= s_end[0] && su[1] >= s_end[1];
+            const bool common = pairs_left && pair_info.y > kTile;
+            Side side[2] = {};
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                Side& x = side[s];
+                if (pairs_left) {
+                    const int tile = common ? w_unit : 2 * w_unit + s, rows = pair_info.w;
+                    x.live = tile * kTile < rows;
+                    x.own = 0;
+                    x.first = wu == share.w0 || w_unit == 0;
+                    x.last = wu == share.w1 - 1 || (tile + (common ? 1 : 2)) * kTile >= rows;
+                    x.row0 = pair_info.x + (common ? s * kTile : 0);
+                    x.rows = common ? (s ? pair_info.y - kTile : kTile) : pair_info.y;
+                    x.head = w_head;
+                    x.base = tile * kTile;
+                    x.cache_rows = min(rows - x.base, kTile);
+                    x.part = (pair * a.n_kv + w_head + cta) * 2 + s;
+                } else if (su[s] < s_end[s]) {
+                    x.live = 1;
+                    x.own = 1;
+                    x.first = s_tile[s] == 0 || su[s] == (s ? share.middle() : share.s0);
+                    x.last = s_tile[s] == s_tiles[s] - 1 || su[s] == s_end[s] - 1;
+                    x.row0 = m[s] * a.group;
+                    x.rows = a.group;
+                    x.head = s_head[s];
+                    x.base = ((row_info[s].x >> a.log2_rows) << a.log2_rows) + s_tile[s] * kTile;
+                    x.cache_rows = min(row_info[s].y - x.base, kTile);
+                    x.part = m[s] * a.n_kv + s_head[s] + 2 * cta + s;
+                }
+                // the blocks of the tile
+                const bool loads = x.live && !(common && s == 1);
+                int id = -1;
+                if (loads) {
+                    const int b = (x.base >> a.log2_rows) + lane;
+                    const int seq = pairs_left ? pair_info.z : a.seq_ids ? a.seq_ids[m[s]] : m[s];
+                    if (lane < per_tile && (lane << a.log2_rows) < x.cache_rows) id = a.tables[(size_t)seq * a.max_blocks + b];
+                    if (id >= a.n_blocks) id = -1;
+                }
+                now.id[s] = id;
+                now.head[s] = x.head;
+                now.there[s] = loads;
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int from = common ? 0 : s;
+                int lost = 0;
+                if (side[s].live) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int id = __shfl_sync(0xffffffffu, from ? now.id[1] : now.id[0], (16 * i) >> a.log2_rows);
+                        if (id < 0) lost |= 1 << i;
+                    }
+                }
+                side[s].lost = lost;
+            }
+            // scales: lane 16 s + 8 v + i brings that of cache rows 16 i .. of stream s, of keys or values
+            {
+                const int s = lane >> 4, v = (lane >> 3) & 1, i = lane & 7;
+                const int id0 = __shfl_sync(0xffffffffu, now.id[0], (16 * i) >> a.log2_rows), id1 = __shfl_sync(0xffffffffu, now.id[1], (16 * i) >> a.log2_rows);
+                const int id = s && !common ? id1 : id0;
+                const int head = s && !common ? now.head[1] : now.head[0];
+                const uint32_t to = smem_u32(v ? &d.vs[s][i] : &d.ks[s][i]);
+                if (id >= 0) {
+                    const float* src = (v ? a.v_scale : a.k_scale) + (size_t)id * a.n_kv + head;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar(L::desc_full + slot)) : "memory");
+                } else {
+                    (v ? d.vs : d.ks)[s][i] = 0.0f;
+                    mbar_arrive(bar(L::desc_full + slot));
+                }
+            }
+            if (lane == 0) {
+                d.side[0] = side[0];
+                d.side[1] = side[1];
+                d.end = end;
+                d.common = common;
+                mbar_arrive(bar(L::desc_full + slot));
+            }
+            __syncwarp();
+            // on to the next step
+            if (pairs_left) {
+                ++wu;
+                if (++w_unit == w_units && wu < share.w1) {
+                    w_unit = 0;
+                    if (++w_head == a.n_kv) {
+                        w_head = 0;
+                        do ++pair;
+                        while (a.cum_pairs[pair + 1] == a.cum_pairs[pair]);
+                        w_units = (a.cum_pairs[pair + 1] - a.cum_pairs[pair]) / a.n_kv;
+                        pair_info = a.pairs[pair];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    if (su[s] < s_end[s]) {
+                        ++su[s];
+                        if (++s_tile[s] == s_tiles[s] && su[s] < s_end[s]) {
+                            s_tile[s] = 0;
+                            if (++s_head[s] == a.n_kv) {
+                                s_head[s] = 0;
+                                do ++m[s];
+                                while (a.cum_rows[m[s] + 1] == a.cum_rows[m[s]]);
+                                s_tiles[s] = (a.cum_rows[m[s] + 1] - a.cum_rows[m[s]]) / a.n_kv;
+                                row_info[s] = a.rows[m[s]];
+                            }
+                        }
+                    }
+            }
+            return !end;
+        };
+        auto load = [&](const Tiles& now, int s, const CUtensorMap* map) {
+            if (!ok || !now.there[s]) return;
+            const int place = made % L::kStages;
+            if (made >= L::kStages && !mbar_wait(bar(L::code_empty + place), (uint32_t)(made / L::kStages - 1) & 1u, abort_flag)) ok = false;
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            ++made;
+            const unsigned present = __ballot_sync(0xffffffffu, now.id[s] >= 0);
+            const uint32_t full = bar(L::code_full + place), block_bytes = (uint32_t)D << a.log2_rows;
+            if (lane == 0) mbar_expect_tx(full, (uint32_t)__popc(present) * block_bytes);
+            __syncwarp();
+            if (now.id[s] >= 0)
+                code_rows(base_s + L::codes + (uint32_t)place * L::kCodeBytes + (uint32_t)lane * block_bytes, map, (now.id[s] * a.n_kv + now.head[s]) << a.log2_rows, full);
+        };
+        Tiles now, next;
+        if (publish(0, now)) {
+            load(now, 0, &map_k);
+            load(now, 1, &map_k);
+            for (int p = 0; ok; ++p) {
+                load(now, 0, &map_v);
+                if (!ok) break;
+                const bool more = publish(p + 1, next);
+                if (!ok) break;
+                if (more) load(next, 0, &map_k);
+                load(now, 1, &map_v);
+                if (!more) break;
+                load(next, 1, &map_k);
+                now = next;
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ products
+        if (lane == 0) {
+            constexpr uint32_t kScores = instruction(kTile, false), kValues = instruction(D, true);
+            int taken = 0, key_at[2] = {0, 0}, value_at[2] = {0, 0};  // operand tile of each stream's product under way
+            uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+            bool ok = true;
+            auto take = [&](int& at) {
+                at = taken % L::kOperands;
+                ok = ok && mbar_wait(bar(L::op_full + at), (uint32_t)(taken / L::kOperands) & 1u, abort_flag);
+                ++taken;
+            };
+            auto scores = [&](int p, int s) {
+                const Desc& d = descs[p % kDescs];
+                if (!ok || !d.side[s].live) return;
+                const bool own_tile = !(d.common && s == 1);
+                if (own_tile) take(key_at[s]);
+                else key_at[s] = key_at[0];
+                if (d.side[s].first) {
+                    ok = ok && mbar_wait(bar(L::q_full + s), q_phase[s], abort_flag);
+                    q_phase[s] ^= 1u;
+                }
+                if (!ok) return;
+                tc_fence_after();
+                const uint32_t qa = base_s + L::q + (uint32_t)s * L::kOperandBytes, ka = base_s + L::operands + (uint32_t)key_at[s] * L::kOperandBytes;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = (uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u;
+                    mma_ss(tm_s(s), operand(qa + off, 16), operand(ka + off, 16), kScores, k > 0);
+                }
+                tc_commit(bar(L::s_full + s));
+                if (!d.common || s == 1) tc_commit(bar(L::op_empty + key_at[s]));
+            };
+            auto values = [&](int p, int s) {
+                const Desc& d = descs[p % kDescs];
+                if (!ok || !d.side[s].live) return;
+                if (!(d.common && s == 1)) take(value_at[s]);
+                else value_at[s] = value_at[0];
+                ok = ok && mbar_wait(bar(L::p_full + s), p_phase[s], abort_flag);
+                p_phase[s] ^= 1u;
+                if (!ok) return;
+                tc_fence_after();
+                const uint32_t va = base_s + L::operands + (uint32_t)value_at[s] * L::kOperandBytes;
+                const bool fresh = d.side[s].first;
+#pragma unroll
+                for (int k = 0; k < kTile / 16; ++k) mma_ts(tm_o(s), tm_s(s) + 8 * k, operand(va + 2048u * k, kHalfTile), kValues, !(fresh && k == 0));
+                if (!d.common || s == 1) tc_commit(bar(L::op_empty + value_at[s]));
+                if (d.side[s].last) tc_commit(bar(L::o_full + s));
+            };
+            auto arrived = [&](int p) { return ok = ok && mbar_wait(bar(L::desc_full + p % kDescs), (uint32_t)(p / kDescs) & 1u, abort_flag); };
+            if (arrived(0) && !descs[0].end) {
+                scores(0, 0);
+                scores(0, 1);
+                for (int p = 0; ok; ++p) {
+                    values(p, 0);
+                    if (!arrived(p + 1)) break;
+                    const bool more = !descs[(p + 1) % kDescs].end;
+                    if (more) scores(p + 1, 0);
+                    values(p, 1);
+                    mbar_arrive(bar(L::desc_empty + p % kDescs));
+                    if (!more) break;
+                    scores(p + 1, 1);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 12) {
+        // ------------------------------------------------------------------ codes -> f16
+        const int t = tid - 12 * 32;
+        int made = 0;
+        bool ok = true;
+        auto convert = [&](int p, int s, bool value) {
+            const Desc& d = descs[p % kDescs];
+            const Side& x = d.side[s];
+            if (!ok || !x.live || (d.common && s == 1)) return;
+            const int from = made % L::kStages, to = made % L::kOperands;
+            ok = mbar_wait(bar(L::code_full + from), (uint32_t)(made / L::kStages) & 1u, abort_flag);
+            if (ok && made >= L::kOperands) ok = mbar_wait(bar(L::op_empty + to), (uint32_t)(made / L::kOperands - 1) & 1u, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            ++made;
+            const uint32_t src = base_s + L::codes + (uint32_t)from * L::kCodeBytes, dst = base_s + L::operands + (uint32_t)to * L::kOperandBytes;
+            const int cache_rows = x.cache_rows, lost = x.lost;
+            const bool whole = !value || (cache_rows == kTile && lost == 0);
+            constexpr int CHUNKS = D / 16;  // of sixteen codes, in a row
+            // Eight neighbouring lanes read eight different sixteen-byte columns of the banks, and write eight: four chunks of a row, the other four of its
+            // neighbour (which the swizzle moves by one sixteen-byte unit).
+#pragma unroll 4
+            for (int i = t; i < kTile * CHUNKS; i += 128) {
+                const int c = i % CHUNKS;
+                const int r = D == 128 ? (i / CHUNKS) ^ (c >> 2) : i / CHUNKS;
+                const uint32_t in = src + (uint32_t)(r * D) + (uint32_t)((D == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4);
+                uint32_t w[4], h[8];
+                lds128(in, w);
+                if (!whole && (r >= cache_rows || ((lost >> (r >> 4)) & 1))) w[0] = w[1] = w[2] = w[3] = 0u;  // rows of no one may hold NaN, and zero times NaN is NaN
+#pragma unroll
+                for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
+                const uint32_t line = dst + (uint32_t)(c >> 2) * kHalfTile + (uint32_t)r * 128u;
+                const uint32_t u = (uint32_t)(2 * (c & 3));
+                sts128(line + ((u ^ (uint32_t)(r & 7)) << 4), h[0], h[1], h[2], h[3]);
+                sts128(line + (((u + 1) ^ (uint32_t)(r & 7)) << 4), h[4], h[5], h[6], h[7]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(L::op_full + to));
+                mbar_arrive(bar(L::code_empty + from));
+            }
+        };
+        auto arrived = [&](int p) {
+            const bool landed = mbar_wait(bar(L::desc_full + p % kDescs), (uint32_t)(p / kDescs) & 1u, abort_flag);
+            return ok = __all_sync(0xffffffffu, ok && landed);
+        };
+        if (arrived(0) && !descs[0].end) {
+            convert(0, 0, false);
+            convert(0, 1, false);
+            for (int p = 0; ok; ++p) {
+                convert(p, 0, true);
+                if (!arrived(p + 1)) break;
+                const bool more = !descs[(p + 1) % kDescs].end;
+                if (more) convert(p + 1, 0, false);
+                convert(p, 1, true);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
+                if (!more) break;
+                convert(p + 1, 1, false);
+            }
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ softmax
+        const int s = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
+        const uint32_t ts = tm_s(s) + lane_at, to = tm_o(s) + lane_at;
+        float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+        int lower = 0, upper = 0;
+        uint32_t s_phase = 0, o_phase = 0;
+        for (int p = 0;; ++p) {
+            const int slot = p % kDescs;
+            if (!__all_sync(0xffffffffu, mbar_wait(bar(L::desc_full + slot), (uint32_t)(p / kDescs) & 1u, abort_flag))) break;
+            const Desc& d = descs[slot];
+            if (d.end) break;
+            const Side x = d.side[s];
+            if (!x.live) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
+                continue;
+            }
+            const bool mine = r < x.rows, any = quad * 32 < x.rows;
+            if (x.first) {
+                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+                if (mine) {
+                    const int flat = x.row0 + r, m = flat / a.group, j = flat - m * a.group;
+                    const int4 info = a.rows[m];
+                    lower = x.own ? info.x : 0;
+                    upper = x.own ? info.y : info.x;
+                    const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D);
+                    uint4 v[D / 8];
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) v[i] = __ldg(src + i);
+                    uint32_t most = 0u;  // the largest magnitude by its bits: infinity and NaN are above all others
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) most = max(most, max((u[e] << 16) & 0x7fffffffu, u[e] & 0x7fff0000u));
+                    }
+                    // the power of two that brings the largest magnitude to 2^8 .. 2^9: bf16 values then fit f16 without loss down to 2^-22 of it
+                    const int be = max((int)(most >> 23), 9);
+                    const float up = __int_as_float((262 - be) << 23), down = __int_as_float((be - 8) << 23);
+                    const uint32_t line = base_s + L::q + (uint32_t)s * L::kOperandBytes + (uint32_t)r * 128u;
+#pragma unroll
+                    for (int i = 0; i < D / 8; ++i) {
+                        const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                        uint32_t h[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * up, __uint_as_float(u[e] & 0xffff0000u) * up);
+                        sts128(line + (uint32_t)(i >> 3) * kHalfTile + (uint32_t)(((i & 7) ^ (r & 7)) << 4), h[0], h[1], h[2], h[3]);
+                    }
+                    f = most >= 0x7f800000u ? NAN : down * a.scale_log2;  // a row that is not finite gives NaN
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::q_full + s));
+            }
+            if (!__all_sync(0xffffffffu, mbar_wait(bar(L::s_full + s), s_phase, abort_flag))) break;
+            s_phase ^= 1u;
+            tc_fence_after();
+            if (any) {
+                // what this row uses of the tile
+                const int lo = max(lower - x.base, 0), hi = min(upper - x.base, kTile);
+                const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && x.lost == 0));
+                float ks[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ks[i] = d.ks[s][i] * f;
+                uint32_t used[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int l = max(lo - 32 * c, 0), h = min(max(hi - 32 * c, 0), 32);
+                    uint32_t w = h > l ? (uint32_t)((1ull << h) - (1ull << l)) : 0u;
+                    if ((x.lost >> (2 * c)) & 1) w &= 0xffff0000u;
+                    if ((x.lost >> (2 * c + 1)) & 1) w &= 0x0000ffffu;
+                    used[c] = w;
+                }
+                // the largest score
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32];
+                    tm_load(ts + 32 * c, v);
+                    tm_load_wait();
+                    if (all_used) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float t = __uint_as_float(v[16 * i]);
+#pragma unroll
+                            for (int e = 1; e < 16; ++e) t = fmaxf(t, __uint_as_float(v[16 * i + e]));
+                            top = fmaxf(top, t * ks[2 * c + i]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if ((used[c] >> e) & 1u) top = fmaxf(top, __uint_as_float(v[e]) * ks[2 * c + (e >> 4)]);
+                    }
+                }
+                float vs = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (all_used || ((used[i >> 1] >> (16 * (i & 1))) & 0xffffu)) vs = fmaxf(vs, d.vs[s][i]);
+                // The maximum is followed only where it grows by more than 2^8: weights stay within f16, and the accumulator is rarely scaled.
+                const bool grows = top > m_run + 8.0f || (m_run == -INFINITY && top > -INFINITY), wider = vs > v_ref;
+                if (__any_sync(0xffffffffu, grows || wider)) {
+                    const float n = grows ? top : m_run, nv = fmaxf(v_ref, vs);
+                    const float c = m_run == -INFINITY ? 0.0f : ex2(m_run - n), fo = nv > 0.0f ? c * (v_ref / nv) : c;
+                    l_run *= grows ? c : 1.0f;
+                    if (!x.first) {
+                        const float fs = m_run == -INFINITY ? 0.0f : fo;  // (nothing there yet: zeros)
+#pragma unroll
+                        for (int i = 0; i < D / 32; ++i) {
+                            uint32_t v[32];
+                            tm_load(to + 32 * i, v);
+                            tm_load_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fs);
+                            tm_store32(to + 32 * i, v);
+                        }
+                    }
+                    m_run = n;
+                    v_ref = nv;
+                }
+                const float b = m_run == -INFINITY ? 0.0f : m_run;
+                const float per_ref = v_ref > 0.0f ? __fdividef(kWeightScale, v_ref) : 0.0f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32], w[16];
+                    tm_load(ts + 32 * c, v);
+                    tm_load_wait();
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float wv = d.vs[s][2 * c + i] * per_ref, k = ks[2 * c + i];
+#pragma unroll
+                        for (int e = 0; e < 16; e += 2) {
+                            const int at = 16 * i + e;
+                            float p0 = ex2(fmaf(__uint_as_float(v[at]), k, -b)), p1 = ex2(fmaf(__uint_as_float(v[at + 1]), k, -b));
+                            float w0 = p0 * wv, w1 = p1 * wv;
+                            if (!all_used) {
+                                if (!((used[c] >> at) & 1u)) p0 = w0 = 0.0f;
+                                if (!((used[c] >> (at + 1)) & 1u)) p1 = w1 = 0.0f;
+                            }
+                            sum += p0 + p1;  // unrounded; weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost
+                            w[at / 2] = pack_f16(w0, w1);
+                        }
+                    }
+                    l_run += sum;
+                    tm_store16(ts + 16 * c, w);  // over scores that have been read
+                }
+                tm_store_wait();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(L::p_full + s));
+                mbar_arrive(bar(L::desc_empty + slot));
+            }
+            if (x.last) {
+                if (!__all_sync(0xffffffffu, mbar_wait(bar(L::o_full + s), o_phase, abort_flag))) break;
+                o_phase ^= 1u;
+                tc_fence_after();
+                if (any) {
+                    const int rows = x.own ? a.group : kTile;
+                    float* part = (x.own ? a.parts_s : a.parts_w) + (size_t)x.part * part_floats(rows, D);
+                    const float unscale = v_ref * (1.0f / kWeightScale);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        uint32_t v[32];
+                        tm_load(to + 32 * i, v);
+                        tm_load_wait();
+                        if (mine)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<float4*>(part + (size_t)r * D + 32 * i + e) =
+                                    make_float4(__uint_as_float(v[e]) * unscale, __uint_as_float(v[e + 1]) * unscale, __uint_as_float(v[e + 2]) * unscale,
+                                                __uint_as_float(v[e + 3]) * unscale);
+                    }
+                    if (mine) *reinterpret_cast<float2*>(part + (size_t)rows * D + 2 * r) = make_float2(m_run, l_run);
+                    tc_fence_before();
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        abort_drain();
+        if (tid == 0 && a.status != nullptr) atomicExch(a.status, BITLINEAR_ERR_TIMEOUT);
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- the parts of a row
+
+// A CTA per row and KV head, a thread for four dims of a query head.
+template <int D>
+__global__ void shared_combine_kernel(const SharedArgs a, int ctas) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int m = blockIdx.x, h = blockIdx.y, j = (int)threadIdx.x / (D / 4), dim = 4 * ((int)threadIdx.x % (D / 4));
+    const int units = a.totals[1], tiles = a.totals[2];
+    const EqualRuns runs(2 * units + tiles, ctas);
+    const int4 row = a.rows[m];
+    float top = -INFINITY, l = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](const float* part, int rows, int r) {
+        const float2 ml = *reinterpret_cast<const float2*>(part + (size_t)rows * D + 2 * r);
+        const float4 v = *reinterpret_cast<const float4*>(part + (size_t)r * D + dim);
+        const float n = fmaxf(top, ml.x);
+        const float f0 = top == -INFINITY ? 0.0f : ex2(top - n), f1 = ml.x == -INFINITY ? (ml.y == ml.y ? 0.0f : NAN) : ex2(ml.x - n);
+        l = l * f0 + ml.y * f1;
+        acc.x = acc.x * f0 + v.x * f1, acc.y = acc.y * f0 + v.y * f1, acc.z = acc.z * f0 + v.z * f1, acc.w = acc.w * f0 + v.w * f1;
+        top = n;
+    };
+    if (row.z >= 0 && row.x > 0) {
+        const int in_group = m * a.group + j - row.w, pair = row.z + in_group / (2 * kTile), r = in_group % (2 * kTile);
+        const int4 info = a.pairs[pair];
+        const bool two = info.y > kTile;
+        const int n = (a.cum_pairs[pair + 1] - a.cum_pairs[pair]) / a.n_kv, u0 = a.cum_pairs[pair] + h * n;
+        const int c1 = runs.owner(2 * (u0 + n - 1));
+        for (int c = runs.owner(2 * u0); c <= c1; ++c) {
+            const Share share(runs, units, c);
+            if (share.w0 >= share.w1) continue;  // (a CTA with one place may have the second half of a unit's)
+            const float* part = a.parts_w + (size_t)(pair * a.n_kv + h + c) * 2 * part_floats(kTile, D);
+            if (two) {
+                add(part + (r >= kTile ? part_floats(kTile, D) : 0), kTile, r % kTile);
+            } else {
+                add(part, kTile, r);
+                const int from = max(share.w0 - u0, 0);
+                if ((2 * from + 1) * kTile < info.w) add(part + part_floats(kTile, D), kTile, r);  // else the second stream had no tile
+            }
+        }
+    }
+    if (row.y > row.x) {
+        const int n = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv, t0 = a.cum_rows[m] + h * n;
+        auto worker = [&](int t) {
+            const int c = runs.owner(2 * units + t);
+            return 2 * c + (t >= Share(runs, units, c).middle() ? 1 : 0);
+        };
+        const int w1 = worker(t0 + n - 1);
+        for (int w = worker(t0); w <= w1; ++w) {
+            // (the second stream of a CTA with one tile has none)
+            const Share share(runs, units, w >> 1);
+            if (((w & 1) ? share.s1 - share.middle() : share.middle() - share.s0) > 0) add(a.parts_s + (size_t)(m * a.n_kv + h + w) * part_floats(a.group, D), a.group, j);
+        }
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no row: zeros; a sum that is NaN stays one
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+    *reinterpret_cast<uint2*>(a.out + ((size_t)m * a.n_q + (size_t)h * a.group + j) * D + dim) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+
+SharedLayout shared_layout(int M, int n_groups, int n_q, int n_kv, int D) {
+    SharedLayout l;
+    const int group = n_q / n_kv;
+    l.max_pairs = (int)((long long)M * group / (2 * kTile)) + std::min(n_groups, M / 2);  // groups of one row have none
+    size_t at = 0;
+    auto room = [&](size_t bytes) {
+        const size_t here = at;
+        at = align_up(at + bytes, 256);
+        return here;
+    };
+    l.rows = room((size_t)M * sizeof(int4));
+    l.pairs = room((size_t)l.max_pairs * sizeof(int4));
+    l.cum_pairs = room(((size_t)std::max(l.max_pairs, n_groups) + 1) * sizeof(int));
+    l.cum_rows = room(((size_t)M + 1) * sizeof(int));
+    l.starts = room(((size_t)n_groups + 1) * sizeof(int));
+    l.firsts = room(((size_t)n_groups + 1) * sizeof(int));
+    l.totals = room(3 * sizeof(int));
+    l.parts_w = room(l.max_pairs == 0 ? 0 : ((size_t)l.max_pairs * n_kv + kSharedCtas) * 2 * part_floats(kTile, D) * sizeof(float));
+    l.parts_s = room(((size_t)M * n_kv + 2 * kSharedCtas) * part_floats(group, D) * sizeof(float));
+    l.total = at;
+    return l;
+}
+
+bool shared_sizes_ok(int M, int n_groups, int n_q, int n_kv, int hd) {
+    return M >= 0 && M <= 65535 && n_groups >= 0 && n_groups <= 65535 && n_q > 0 && n_kv > 0 && n_q % n_kv == 0 && n_q / n_kv <= 8 && (hd == 64 || hd == 128) && n_kv <= 65535;
+}
+
+// rows = every (block, head, row) of the pool, columns = D bytes; a box is a block's rows, swizzled by the row's width
+bool make_block_map(CUtensorMap* map, const void* pool, long long rows, int hd, int block_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)hd, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)hd};
+    const cuuint32_t box[2] = {(cuuint32_t)hd, (cuuint32_t)block_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              hd == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int finish(cudaError_t rc) {
+    if (rc == cudaSuccess) return BITLINEAR_OK;
+    cudaGetLastError();
+    return BITLINEAR_ERR_CUDA;
+}
+
+template <int D, int KIND>
+int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const SharedArgs& a, int ctas, cudaStream_t st) {
+    constexpr uint32_t kBytes = 1024 + SharedSmem<D>::total;
+    static_assert(kBytes <= 227 * 1024, "shared memory");
+    static std::mutex mu;
+    static bool done[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return finish(cudaErrorInvalidDevice);
+    {
+        std::lock_guard<std::mutex> lock(mu);
+        if (!done[dev]) {
+            if (cudaFuncSetAttribute(shared_attention_kernel<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes) != cudaSuccess) return finish(cudaErrorUnknown);
+            done[dev] = true;
+        }
+    }
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(1);
+    cfg.blockDim = dim3(kPlanThreads);
+    if (const int rc = finish(cudaLaunchKernelEx(&cfg, shared_plan_kernel, a))) return rc;
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kBytes;
+    if (const int rc = finish(cudaLaunchKernelEx(&cfg, shared_attention_kernel<D, KIND>, map_k, map_v, a))) return rc;
+    cfg.gridDim = dim3((unsigned)a.M, (unsigned)a.n_kv);
+    cfg.blockDim = dim3((unsigned)(a.group * D / 4));
+    cfg.dynamicSmemBytes = 0;
+    return finish(cudaLaunchKernelEx(&cfg, shared_combine_kernel<D>, a, ctas));
+}
+
+}  // namespace
+
+}  // namespace bitlinear
+
+using namespace bitlinear;
+
+extern "C" {
+
+size_t bitlinear_attention_shared_kv8_workspace_bytes(int M, int n_groups, int n_q_heads, int n_kv_heads, int head_dim) {
+    return shared_sizes_ok(M, n_groups, n_q_heads, n_kv_heads, head_dim) ? shared_layout(M, n_groups, n_q_heads, n_kv_heads, head_dim).total : 0;
+}
+
+int bitlinear_attention_shared_kv8(const void* q_bf16, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, const int32_t* tables,
+                                   const int32_t* lengths, const int32_t* seq_ids, const int32_t* group_starts, const int32_t* shared_rows, int M, int n_groups, int n_q_heads,
+                                   int n_kv_heads, int head_dim, int kv_dtype, int n_blocks, int block_rows, int n_seq, int max_blocks, void* out_bf16, void* ws, size_t ws_bytes,
+                                   void* stream) {
+    if (kv_dtype != BITLINEAR_KV_INT8 && kv_dtype != BITLINEAR_KV_E4M3) return BITLINEAR_ERR_DTYPE;
+    if (!shared_sizes_ok(M, n_groups, n_q_heads, n_kv_heads, head_dim) || n_seq <= 0 || max_blocks <= 0 ||
+        !kv8_dims_ok(n_q_heads, n_kv_heads, head_dim, kv_dtype, n_blocks, block_rows) || (long long)max_blocks * block_rows > (1ll << 30) || (!seq_ids && n_seq < M) ||
+        (double)M * n_kv_heads * (((double)max_blocks * block_rows + block_rows) / kTile + 2) * 2 > 2147483000.0)
+        return BITLINEAR_ERR_SHAPE;
+    if (M == 0) return BITLINEAR_OK;
+    if (!q_bf16 || !k_cache || !v_cache || !k_scale || !v_scale || !tables || !lengths || !group_starts || (n_groups > 0 && !shared_rows) || !out_bf16) return BITLINEAR_ERR_NULL;
+    if (!aligned16(q_bf16) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out_bf16)) return BITLINEAR_ERR_ALIGN;
+    const SharedLayout l = shared_layout(M, n_groups, n_q_heads, n_kv_heads, head_dim);
+    if (!ws || !aligned16(ws) || ws_bytes < l.total) return BITLINEAR_ERR_WORKSPACE;
+    int sm_count = 0;
+    if (const int rc = device_sm_count(&sm_count)) return rc;
+    const long long pool_rows = (long long)n_blocks * n_kv_heads * block_rows;
+    CUtensorMap map_k, map_v;
+    if (!make_block_map(&map_k, k_cache, pool_rows, head_dim, block_rows) || !make_block_map(&map_v, v_cache, pool_rows, head_dim, block_rows)) return BITLINEAR_ERR_CUDA;
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    SharedArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, group_starts, shared_rows, M, n_groups, n_q_heads, n_kv_heads,
+                    n_q_heads / n_kv_heads, n_seq, max_blocks, log2_of(block_rows), n_blocks, 1.4426950408889634f / sqrtf((float)head_dim), static_cast<__nv_bfloat16*>(out_bf16),
+                    reinterpret_cast<int4*>(w + l.rows), reinterpret_cast<int4*>(w + l.pairs), reinterpret_cast<int*>(w + l.cum_pairs), reinterpret_cast<int*>(w + l.cum_rows),
+                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.firsts), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
+                    l.max_pairs, device_status_word()};
+    const int ctas = std::min(sm_count, kSharedCtas);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (head_dim == 128)
+        return kv_dtype == BITLINEAR_KV_INT8 ? shared_launch<128, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st) : shared_launch<128, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
+    return kv_dtype == BITLINEAR_KV_INT8 ? shared_launch<64, BITLINEAR_KV_INT8>(map_k, map_v, a, ctas, st) : shared_launch<64, BITLINEAR_KV_E4M3>(map_k, map_v, a, ctas, st);
+}
+
+}  // extern "C"
