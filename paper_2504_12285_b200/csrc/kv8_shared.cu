@@ -292,6 +292,26 @@ __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16])
 }
 __device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// two fp32 operations an instruction
+__device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}" : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
 __device__ __forceinline__ void code_rows(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(bar)
                  : "memory");
@@ -658,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             constexpr int CHUNKS = D / 16;  // of sixteen codes, in a row
             // Eight neighbouring lanes read eight different sixteen-byte columns of the banks, and write eight: four chunks of a row, the other four of its
             // neighbour (which the swizzle moves by one sixteen-byte unit).
-#pragma unroll 4
+#pragma unroll 2
             for (int i = t; i < kTile * CHUNKS; i += 128) {
                 const int c = i % CHUNKS;
                 const int r = D == 128 ? (i / CHUNKS) ^ (c >> 2) : i / CHUNKS;
@@ -762,58 +782,62 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 // what this row uses of the tile
                 const int lo = max(lower - x.base, 0), hi = min(upper - x.base, kTile);
                 const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && x.lost == 0));
-                float ks[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ks[i] = d.ks[s][i] * f;
-                uint32_t used[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                auto used = [&](int c) {  // of columns 32 c .. 32 c + 31
                     const int l = max(lo - 32 * c, 0), h = min(max(hi - 32 * c, 0), 32);
                     uint32_t w = h > l ? (uint32_t)((1ull << h) - (1ull << l)) : 0u;
                     if ((x.lost >> (2 * c)) & 1) w &= 0xffff0000u;
                     if ((x.lost >> (2 * c + 1)) & 1) w &= 0x0000ffffu;
-                    used[c] = w;
-                }
-                // the largest score
-                float top = -INFINITY;
+                    return w;
+                };
+                // The loops over 32 columns stay loops: with all of them unrolled, the roles' code did not fit the instruction caches, and a warp waited for
+                // instructions longer than for anything else (444 us for 2173 rows of two chunks, 0.3 instructions a cycle).
+                float top = -INFINITY, vs = 0.0f;  // the largest score, the largest scale of values
+                if (all_used) {
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tm_load(ts + 32 * c, v);
+                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), w = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
+                        tm_load_wait();
+                        float t0 = __uint_as_float(v[0]), t1 = __uint_as_float(v[16]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tm_load(ts + 32 * c, v);
-                    tm_load_wait();
-                    if (all_used) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float t = __uint_as_float(v[16 * i]);
-#pragma unroll
-                            for (int e = 1; e < 16; ++e) t = fmaxf(t, __uint_as_float(v[16 * i + e]));
-                            top = fmaxf(top, t * ks[2 * c + i]);
+                        for (int e = 1; e < 16; ++e) {
+                            t0 = fmaxf(t0, __uint_as_float(v[e]));
+                            t1 = fmaxf(t1, __uint_as_float(v[16 + e]));
                         }
-                    } else {
+                        top = fmaxf(top, fmaxf(t0 * (k.x * f), t1 * (k.y * f)));
+                        vs = fmaxf(vs, fmaxf(w.x, w.y));
+                    }
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tm_load(ts + 32 * c, v);
+                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), w = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
+                        const uint32_t live = used(c);
+                        tm_load_wait();
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if ((used[c] >> e) & 1u) top = fmaxf(top, __uint_as_float(v[e]) * ks[2 * c + (e >> 4)]);
+                            if ((live >> e) & 1u) top = fmaxf(top, __uint_as_float(v[e]) * ((e < 16 ? k.x : k.y) * f));
+                        if (live & 0x0000ffffu) vs = fmaxf(vs, w.x);
+                        if (live & 0xffff0000u) vs = fmaxf(vs, w.y);
                     }
                 }
-                float vs = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (all_used || ((used[i >> 1] >> (16 * (i & 1))) & 0xffffu)) vs = fmaxf(vs, d.vs[s][i]);
                 // The maximum is followed only where it grows by more than 2^8: weights stay within f16, and the accumulator is rarely scaled.
                 const bool grows = top > m_run + 8.0f || (m_run == -INFINITY && top > -INFINITY), wider = vs > v_ref;
                 if (__any_sync(0xffffffffu, grows || wider)) {
                     const float n = grows ? top : m_run, nv = fmaxf(v_ref, vs);
-                    const float c = m_run == -INFINITY ? 0.0f : ex2(m_run - n), fo = nv > 0.0f ? c * (v_ref / nv) : c;
-                    l_run *= grows ? c : 1.0f;
+                    const float c = m_run == -INFINITY ? 0.0f : ex2(m_run - n);  // (nothing there yet: zeros)
+                    const float fo = nv > 0.0f ? c * (v_ref / nv) : c;
+                    l_run *= c;
                     if (!x.first) {
-                        const float fs = m_run == -INFINITY ? 0.0f : fo;  // (nothing there yet: zeros)
-#pragma unroll
+#pragma unroll 1
                         for (int i = 0; i < D / 32; ++i) {
                             uint32_t v[32];
                             tm_load(to + 32 * i, v);
                             tm_load_wait();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fs);
+                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fo);
                             tm_store32(to + 32 * i, v);
                         }
                     }
@@ -822,30 +846,49 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 }
                 const float b = m_run == -INFINITY ? 0.0f : m_run;
                 const float per_ref = v_ref > 0.0f ? __fdividef(kWeightScale, v_ref) : 0.0f;
+                // Weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost; their sum takes them unrounded.
+                // They go over scores that have been read.
+                if (all_used) {
+                    float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32], w[16];
+                        tm_load(ts + 32 * c, v);
+                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), r2 = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
+                        tm_load_wait();
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32], w[16];
-                    tm_load(ts + 32 * c, v);
-                    tm_load_wait();
-                    float sum = 0.0f;
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 kk = splat((i ? k.y : k.x) * f), ww = splat((i ? r2.y : r2.x) * per_ref), bb = splat(-b);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float wv = d.vs[s][2 * c + i] * per_ref, k = ks[2 * c + i];
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const int at = 16 * i + e;
-                            float p0 = ex2(fmaf(__uint_as_float(v[at]), k, -b)), p1 = ex2(fmaf(__uint_as_float(v[at + 1]), k, -b));
-                            float w0 = p0 * wv, w1 = p1 * wv;
-                            if (!all_used) {
-                                if (!((used[c] >> at) & 1u)) p0 = w0 = 0.0f;
-                                if (!((used[c] >> (at + 1)) & 1u)) p1 = w1 = 0.0f;
+                            for (int e = 0; e < 16; e += 2) {
+                                float2 t = fma2(make_float2(__uint_as_float(v[16 * i + e]), __uint_as_float(v[16 * i + e + 1])), kk, bb);
+                                t.x = ex2(t.x), t.y = ex2(t.y);
+                                sum = add2(sum, t);
+                                t = mul2(t, ww);
+                                w[8 * i + e / 2] = pack_f16(t.x, t.y);
                             }
-                            sum += p0 + p1;  // unrounded; weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost
-                            w[at / 2] = pack_f16(w0, w1);
                         }
+                        tm_store16(ts + 16 * c, w);
                     }
-                    l_run += sum;
-                    tm_store16(ts + 16 * c, w);  // over scores that have been read
+                    l_run += sum.x + sum.y;
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32], w[16];
+                        tm_load(ts + 32 * c, v);
+                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), r2 = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
+                        const uint32_t live = used(c);
+                        tm_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float kk = (e < 16 ? k.x : k.y) * f, ww = (e < 16 ? r2.x : r2.y) * per_ref;
+                            const float p0 = (live >> e) & 1u ? ex2(fmaf(__uint_as_float(v[e]), kk, -b)) : 0.0f;
+                            const float p1 = (live >> (e + 1)) & 1u ? ex2(fmaf(__uint_as_float(v[e + 1]), kk, -b)) : 0.0f;
+                            l_run += p0 + p1;
+                            w[e / 2] = pack_f16((live >> e) & 1u ? p0 * ww : 0.0f, (live >> (e + 1)) & 1u ? p1 * ww : 0.0f);
+                        }
+                        tm_store16(ts + 16 * c, w);
+                    }
                 }
                 tm_store_wait();
             }
