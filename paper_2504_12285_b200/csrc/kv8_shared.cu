@@ -13,7 +13,7 @@
 // query rows of that row alone.  All of it is cut into equal runs, one per CTA, whatever the lengths; parts of a row meet in a last launch.
 //
 //   warp 0      copies: block tables -> tensor-map copies of code tiles, and the work list that the other warps follow
-//   warp 1      one thread issues the products
+//   warps 1, 2  one thread of each issues a stream's products
 //   warps 4-11  softmax, one thread per query row; four warps per stream
 //   warps 12-15 codes -> f16
 #include <cuda.h>
@@ -363,8 +363,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
     if (tid == 0) {
         *abort_flag = 0;
         for (int i = 0; i < L::kStages; ++i) mbar_init(bar(L::code_full + i), 1), mbar_init(bar(L::code_empty + i), 4);
-        for (int i = 0; i < L::kOperands; ++i) mbar_init(bar(L::op_full + i), 4), mbar_init(bar(L::op_empty + i), 1);
-        for (int i = 0; i < kDescs; ++i) mbar_init(bar(L::desc_full + i), 1 + 32), mbar_init(bar(L::desc_empty + i), 1 + 4 + 8);
+        for (int i = 0; i < L::kOperands; ++i) mbar_init(bar(L::op_full + i), 4), mbar_init(bar(L::op_empty + i), 2);
+        for (int i = 0; i < kDescs; ++i) mbar_init(bar(L::desc_full + i), 1 + 32), mbar_init(bar(L::desc_empty + i), 2 + 4 + 8);
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar(L::q_full + s), 4);
             mbar_init(bar(L::s_full + s), 1);
@@ -575,88 +575,91 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             if (now.id[s] >= 0)
                 code_rows(base_s + L::codes + (uint32_t)place * L::kCodeBytes + (uint32_t)lane * block_bytes, map, (now.id[s] * a.n_kv + now.head[s]) << a.log2_rows, full);
         };
-        Tiles now, next;
-        if (publish(0, now)) {
-            load(now, 0, &map_k);
-            load(now, 1, &map_k);
-            for (int p = 0; ok; ++p) {
-                load(now, 0, &map_v);
-                if (!ok) break;
-                const bool more = publish(p + 1, next);
-                if (!ok) break;
-                if (more) load(next, 0, &map_k);
-                load(now, 1, &map_v);
-                if (!more) break;
-                load(next, 1, &map_k);
-                now = next;
-            }
+        Tiles now = {{-1, -1}, {0, 0}, {false, false}}, next;
+        for (int p = -1; ok; ++p) {
+            load(now, 0, &map_v);
+            if (!ok) break;
+            const bool more = publish(p + 1, next);
+            if (!ok) break;
+            if (more) load(next, 0, &map_k);
+            load(now, 1, &map_v);
+            if (!more) break;
+            load(next, 1, &map_k);
+            now = next;
         }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------------ products
-        if (lane == 0) {
-            constexpr uint32_t kScores = instruction(kTile, false), kValues = instruction(D, true);
-            int taken = 0, key_at[2] = {0, 0}, value_at[2] = {0, 0};  // operand tile of each stream's product under way
-            uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-            bool ok = true;
-            auto take = [&](int& at) {
-                at = taken % L::kOperands;
-                ok = ok && mbar_wait(bar(L::op_full + at), (uint32_t)(taken / L::kOperands) & 1u, abort_flag);
-                ++taken;
-            };
-            auto scores = [&](int p, int s) {
-                const Desc& d = descs[p % kDescs];
-                if (!ok || !d.side[s].live) return;
-                const bool own_tile = !(d.common && s == 1);
-                if (own_tile) take(key_at[s]);
-                else key_at[s] = key_at[0];
-                if (d.side[s].first) {
-                    ok = ok && mbar_wait(bar(L::q_full + s), q_phase[s], abort_flag);
-                    q_phase[s] ^= 1u;
+    } else if (warp <= 2) {
+        // ------------------------------------------------------------------ products, a warp for each stream: one thread starts a product every 55 cycles at most
+        const int s = warp - 1;
+        constexpr uint32_t kScores = instruction(kTile, false), kValues = instruction(D, true);
+        const uint64_t q_tile = operand(base_s + L::q + (uint32_t)s * L::kOperandBytes, 16);
+        uint32_t q_phase = 0, p_phase = 0;
+        int made = 0, key = 0, value = 0;  // operand tiles so far; those of the products under way
+        bool ok = true;
+        auto landed = [&](int bar_at, uint32_t parity) { return ok = __all_sync(0xffffffffu, mbar_wait(bar(bar_at), parity, abort_flag)); };
+        auto filled = [&](int tile) { return landed(L::op_full + tile % L::kOperands, (uint32_t)(tile / L::kOperands) & 1u); };
+        for (int p = -1; ok; ++p) {
+            bool more = false;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {  // values of step p, scores of the next, of either stream
+                const bool values = !(i & 1);
+                const int q = values ? p : p + 1, t = i >> 1;
+                const Desc& d = descs[q & (kDescs - 1)];
+                if (i == 1) {
+                    if (!landed(L::desc_full + q % kDescs, (uint32_t)(q / kDescs) & 1u)) break;
+                    more = !d.end;
                 }
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t qa = base_s + L::q + (uint32_t)s * L::kOperandBytes, ka = base_s + L::operands + (uint32_t)key_at[s] * L::kOperandBytes;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u;
-                    mma_ss(tm_s(s), operand(qa + off, 16), operand(ka + off, 16), kScores, k > 0);
+                if (values ? p < 0 : !more) continue;
+                if (!d.side[t].live) continue;
+                const bool common = d.common;
+                if (!(common && t == 1)) {
+                    if (values) value = made;
+                    else key = made;
+                    ++made;
                 }
-                tc_commit(bar(L::s_full + s));
-                if (!d.common || s == 1) tc_commit(bar(L::op_empty + key_at[s]));
-            };
-            auto values = [&](int p, int s) {
-                const Desc& d = descs[p % kDescs];
-                if (!ok || !d.side[s].live) return;
-                if (!(d.common && s == 1)) take(value_at[s]);
-                else value_at[s] = value_at[0];
-                ok = ok && mbar_wait(bar(L::p_full + s), p_phase[s], abort_flag);
-                p_phase[s] ^= 1u;
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t va = base_s + L::operands + (uint32_t)value_at[s] * L::kOperandBytes;
+                const int tile = values ? value : key;
+                if (t != s) {  // the other stream's: a tile is free when both warps have passed it
+                    if (common) continue;
+                    if (!filled(tile)) break;
+                    if (lane == 0) mbar_arrive(bar(L::op_empty + tile % L::kOperands));
+                    continue;
+                }
+                if (!filled(tile)) break;
+                const uint32_t at = base_s + L::operands + (uint32_t)(tile % L::kOperands) * L::kOperandBytes;
                 const bool fresh = d.side[s].first;
+                if (!values) {
+                    if (fresh) {
+                        if (!landed(L::q_full + s, q_phase)) break;
+                        q_phase ^= 1u;
+                    }
+                    tc_fence_after();
+                    if (lane == 0) {
+                        const uint64_t k_tile = operand(at, 16);
 #pragma unroll
-                for (int k = 0; k < kTile / 16; ++k) mma_ts(tm_o(s), tm_s(s) + 8 * k, operand(va + 2048u * k, kHalfTile), kValues, !(fresh && k == 0));
-                if (!d.common || s == 1) tc_commit(bar(L::op_empty + value_at[s]));
-                if (d.side[s].last) tc_commit(bar(L::o_full + s));
-            };
-            auto arrived = [&](int p) { return ok = ok && mbar_wait(bar(L::desc_full + p % kDescs), (uint32_t)(p / kDescs) & 1u, abort_flag); };
-            if (arrived(0) && !descs[0].end) {
-                scores(0, 0);
-                scores(0, 1);
-                for (int p = 0; ok; ++p) {
-                    values(p, 0);
-                    if (!arrived(p + 1)) break;
-                    const bool more = !descs[(p + 1) % kDescs].end;
-                    if (more) scores(p + 1, 0);
-                    values(p, 1);
-                    mbar_arrive(bar(L::desc_empty + p % kDescs));
-                    if (!more) break;
-                    scores(p + 1, 1);
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
+                            mma_ss(tm_s(s), q_tile + off, k_tile + off, kScores, k > 0);
+                        }
+                        tc_commit(bar(L::s_full + s));
+                        tc_commit(bar(L::op_empty + tile % L::kOperands));
+                    }
+                } else {
+                    if (!landed(L::p_full + s, p_phase)) break;
+                    p_phase ^= 1u;
+                    tc_fence_after();
+                    if (lane == 0) {
+                        const uint64_t v_tile = operand(at, kHalfTile);
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k) mma_ts(tm_o(s), tm_s(s) + 8 * k, v_tile + 128u * k, kValues, !(fresh && k == 0));
+                        if (d.side[s].last) tc_commit(bar(L::o_full + s));
+                        tc_commit(bar(L::op_empty + tile % L::kOperands));
+                    }
                 }
+                __syncwarp();
             }
+            if (p >= 0 && lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
+            __syncwarp();
+            if (!more) break;
         }
-        __syncwarp();
     } else if (warp >= 12) {
         // ------------------------------------------------------------------ codes -> f16
         const int t = tid - 12 * 32;
@@ -678,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             constexpr int CHUNKS = D / 16;  // of sixteen codes, in a row
             // Eight neighbouring lanes read eight different sixteen-byte columns of the banks, and write eight: four chunks of a row, the other four of its
             // neighbour (which the swizzle moves by one sixteen-byte unit).
-#pragma unroll 2
+#pragma unroll 4
             for (int i = t; i < kTile * CHUNKS; i += 128) {
                 const int c = i % CHUNKS;
                 const int r = D == 128 ? (i / CHUNKS) ^ (c >> 2) : i / CHUNKS;
@@ -700,24 +703,20 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 mbar_arrive(bar(L::code_empty + from));
             }
         };
-        auto arrived = [&](int p) {
-            const bool landed = mbar_wait(bar(L::desc_full + p % kDescs), (uint32_t)(p / kDescs) & 1u, abort_flag);
-            return ok = __all_sync(0xffffffffu, ok && landed);
-        };
-        if (arrived(0) && !descs[0].end) {
-            convert(0, 0, false);
-            convert(0, 1, false);
-            for (int p = 0; ok; ++p) {
-                convert(p, 0, true);
-                if (!arrived(p + 1)) break;
-                const bool more = !descs[(p + 1) % kDescs].end;
-                if (more) convert(p + 1, 0, false);
-                convert(p, 1, true);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
-                if (!more) break;
-                convert(p + 1, 1, false);
+        for (int p = -1; ok; ++p) {
+            bool more = false;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {  // values of step p, keys of the next, for either stream
+                if (i == 1) {
+                    const bool landed = mbar_wait(bar(L::desc_full + (p + 1) % kDescs), (uint32_t)((p + 1) / kDescs) & 1u, abort_flag);
+                    if (!(ok = __all_sync(0xffffffffu, ok && landed))) break;
+                    more = !descs[(p + 1) % kDescs].end;
+                }
+                if (i & 1 ? more : p >= 0) convert(i & 1 ? p + 1 : p, i >> 1, !(i & 1));
             }
+            __syncwarp();
+            if (p >= 0 && lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
+            if (!more) break;
         }
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ softmax
