@@ -233,6 +233,11 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -345,7 +350,7 @@ struct SharedSmem {
     static constexpr uint32_t bars = descs + kDescs * sizeof(Desc);
     // barriers
     static constexpr int code_full = 0, code_empty = code_full + kStages, op_full = code_empty + kStages, op_empty = op_full + kOperands, desc_full = op_empty + kOperands,
-                         desc_empty = desc_full + kDescs, q_full = desc_empty + kDescs, s_full = q_full + 2, p_full = s_full + 2, o_full = p_full + 2, n_bars = o_full + 2;
+                         desc_empty = desc_full + kDescs, q_full = desc_empty + kDescs, s_full = q_full + 2, p_full = s_full + 2, o_full = p_full + 2, turn = o_full + 2, n_bars = turn + 2;
     static constexpr uint32_t total = bars + n_bars * 8 + 16;
 };
 
@@ -370,6 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             mbar_init(bar(L::s_full + s), 1);
             mbar_init(bar(L::p_full + s), 4);
             mbar_init(bar(L::o_full + s), 1);
+            mbar_init(bar(L::turn + s), 1);
         }
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
@@ -589,10 +595,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         }
     } else if (warp <= 2) {
         // ------------------------------------------------------------------ products, a warp for each stream: one thread starts a product every 55 cycles at most
-        const int s = warp - 1;
+        // (What the instructions take is made the same for all lanes first: they want it in uniform registers.)
+        const int s = __shfl_sync(0xffffffffu, warp - 1, 0);
+        const uint32_t scores_at = __shfl_sync(0xffffffffu, tm_s(s), 0), sums_at = __shfl_sync(0xffffffffu, tm_o(s), 0);
+        const uint32_t s_full = __shfl_sync(0xffffffffu, bar(L::s_full + s), 0), o_full = __shfl_sync(0xffffffffu, bar(L::o_full + s), 0);
         constexpr uint32_t kScores = instruction(kTile, false), kValues = instruction(D, true);
-        const uint64_t q_tile = operand(base_s + L::q + (uint32_t)s * L::kOperandBytes, 16);
-        uint32_t q_phase = 0, p_phase = 0;
+        const uint64_t q_tile = operand(__shfl_sync(0xffffffffu, base_s + L::q + (uint32_t)s * L::kOperandBytes, 0), 16);
+        uint32_t q_phase = 0, p_phase = 0, turn_phase = s == 0 ? 1u : 0u;  // (the first turn is the first stream's)
         int made = 0, key = 0, value = 0;  // operand tiles so far; those of the products under way
         bool ok = true;
         auto landed = [&](int bar_at, uint32_t parity) { return ok = __all_sync(0xffffffffu, mbar_wait(bar(bar_at), parity, abort_flag)); };
@@ -608,51 +617,62 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     if (!landed(L::desc_full + q % kDescs, (uint32_t)(q / kDescs) & 1u)) break;
                     more = !d.end;
                 }
-                if (values ? p < 0 : !more) continue;
-                if (!d.side[t].live) continue;
-                const bool common = d.common;
-                if (!(common && t == 1)) {
+                const bool there = values ? p >= 0 : more, live = there && d.side[t].live, common = there && d.common;
+                if (live && !(common && t == 1)) {
                     if (values) value = made;
                     else key = made;
                     ++made;
                 }
                 const int tile = values ? value : key;
                 if (t != s) {  // the other stream's: a tile is free when both warps have passed it
-                    if (common) continue;
-                    if (!filled(tile)) break;
-                    if (lane == 0) mbar_arrive(bar(L::op_empty + tile % L::kOperands));
+                    if (live && !common) {
+                        if (!filled(tile)) break;
+                        if (lane == 0) mbar_arrive(bar(L::op_empty + tile % L::kOperands));
+                    }
                     continue;
                 }
-                if (!filled(tile)) break;
-                const uint32_t at = base_s + L::operands + (uint32_t)(tile % L::kOperands) * L::kOperandBytes;
-                const bool fresh = d.side[s].first;
-                if (!values) {
-                    if (fresh) {
-                        if (!landed(L::q_full + s, q_phase)) break;
-                        q_phase ^= 1u;
+                if (live && !filled(tile)) break;
+                const uint32_t at = __shfl_sync(0xffffffffu, base_s + L::operands + (uint32_t)(tile % L::kOperands) * L::kOperandBytes, 0);
+                const uint32_t done = __shfl_sync(0xffffffffu, bar(L::op_empty + tile % L::kOperands), 0);
+                const int flags = __shfl_sync(0xffffffffu, live ? d.side[s].first | d.side[s].last << 1 : 0, 0);
+                const bool one = elect_one();
+                if (values) {
+                    if (live) {
+                        if (!landed(L::p_full + s, p_phase)) break;
+                        p_phase ^= 1u;
                     }
-                    tc_fence_after();
-                    if (lane == 0) {
-                        const uint64_t k_tile = operand(at, 16);
+                    // The streams take turns at the tensor cores, so that one's softmax runs beside the other's products; without, both did the same at a time.
+                    if (!landed(L::turn + s, turn_phase)) break;
+                    turn_phase ^= 1u;
+                    if (live) {
+                        tc_fence_after();
+                        if (one) {
+                            const uint64_t v_tile = operand(at, kHalfTile);
+                            const bool fresh = flags & 1;
 #pragma unroll
-                        for (int k = 0; k < D / 16; ++k) {
-                            const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
-                            mma_ss(tm_s(s), q_tile + off, k_tile + off, kScores, k > 0);
+                            for (int k = 0; k < kTile / 16; ++k) mma_ts(sums_at, scores_at + 8 * k, v_tile + 128u * k, kValues, !(fresh && k == 0));
+                            if (flags & 2) tc_commit(o_full);
+                            tc_commit(done);
                         }
-                        tc_commit(bar(L::s_full + s));
-                        tc_commit(bar(L::op_empty + tile % L::kOperands));
                     }
                 } else {
-                    if (!landed(L::p_full + s, p_phase)) break;
-                    p_phase ^= 1u;
-                    tc_fence_after();
-                    if (lane == 0) {
-                        const uint64_t v_tile = operand(at, kHalfTile);
+                    if (live) {
+                        if (flags & 1) {
+                            if (!landed(L::q_full + s, q_phase)) break;
+                            q_phase ^= 1u;
+                        }
+                        if (one) {
+                            const uint64_t k_tile = operand(at, 16);
 #pragma unroll
-                        for (int k = 0; k < kTile / 16; ++k) mma_ts(tm_o(s), tm_s(s) + 8 * k, v_tile + 128u * k, kValues, !(fresh && k == 0));
-                        if (d.side[s].last) tc_commit(bar(L::o_full + s));
-                        tc_commit(bar(L::op_empty + tile % L::kOperands));
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
+                                mma_ss(scores_at, q_tile + off, k_tile + off, kScores, k > 0);
+                            }
+                            tc_commit(s_full);
+                            tc_commit(done);
+                        }
                     }
+                    if (lane == 0) mbar_arrive(bar(L::turn + 1 - s));
                 }
                 __syncwarp();
             }
@@ -663,6 +683,11 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
     } else if (warp >= 12) {
         // ------------------------------------------------------------------ codes -> f16
         const int t = tid - 12 * 32;
+        // A thread takes sixteen codes of every 16th (32nd) row, always of the same columns.  Eight neighbouring lanes read eight different sixteen-byte columns
+        // of the banks and write eight: four pieces of a row, the other four of its neighbour (which the swizzle moves by one sixteen-byte unit).
+        const int chunk = t % (D / 16), row = D == 128 ? (t / 8) ^ (chunk >> 2) : t / 4;
+        const uint32_t in_at = (uint32_t)(row * D) + (uint32_t)((D == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4);
+        const uint32_t out_at = (uint32_t)(chunk >> 2) * kHalfTile + (uint32_t)row * 128u + (uint32_t)(((2 * (chunk & 3)) ^ (row & 7)) << 4);
         int made = 0;
         bool ok = true;
         auto convert = [&](int p, int s, bool value) {
@@ -678,23 +703,30 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             const uint32_t src = base_s + L::codes + (uint32_t)from * L::kCodeBytes, dst = base_s + L::operands + (uint32_t)to * L::kOperandBytes;
             const int cache_rows = x.cache_rows, lost = x.lost;
             const bool whole = !value || (cache_rows == kTile && lost == 0);
-            constexpr int CHUNKS = D / 16;  // of sixteen codes, in a row
-            // Eight neighbouring lanes read eight different sixteen-byte columns of the banks, and write eight: four chunks of a row, the other four of its
-            // neighbour (which the swizzle moves by one sixteen-byte unit).
+            const uint32_t in = src + in_at, out0 = dst + out_at, out1 = dst + (out_at ^ 16u);
+            constexpr int STEP = 128 * 16 / D;  // rows from a thread's piece to its next
+            if (whole) {
 #pragma unroll 4
-            for (int i = t; i < kTile * CHUNKS; i += 128) {
-                const int c = i % CHUNKS;
-                const int r = D == 128 ? (i / CHUNKS) ^ (c >> 2) : i / CHUNKS;
-                const uint32_t in = src + (uint32_t)(r * D) + (uint32_t)((D == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4);
-                uint32_t w[4], h[8];
-                lds128(in, w);
-                if (!whole && (r >= cache_rows || ((lost >> (r >> 4)) & 1))) w[0] = w[1] = w[2] = w[3] = 0u;  // rows of no one may hold NaN, and zero times NaN is NaN
+                for (int i = 0; i < D / 16; ++i) {
+                    uint32_t w[4], h[8];
+                    lds128(in + i * STEP * D, w);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
-                const uint32_t line = dst + (uint32_t)(c >> 2) * kHalfTile + (uint32_t)r * 128u;
-                const uint32_t u = (uint32_t)(2 * (c & 3));
-                sts128(line + ((u ^ (uint32_t)(r & 7)) << 4), h[0], h[1], h[2], h[3]);
-                sts128(line + (((u + 1) ^ (uint32_t)(r & 7)) << 4), h[4], h[5], h[6], h[7]);
+                    for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
+                    sts128(out0 + i * STEP * 128, h[0], h[1], h[2], h[3]);
+                    sts128(out1 + i * STEP * 128, h[4], h[5], h[6], h[7]);
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < D / 16; ++i) {
+                    uint32_t w[4], h[8];
+                    const int r = row + i * STEP;
+                    lds128(in + i * STEP * D, w);
+                    if (r >= cache_rows || ((lost >> (r >> 4)) & 1)) w[0] = w[1] = w[2] = w[3] = 0u;  // rows of no one may hold NaN, and zero times NaN is NaN
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
+                    sts128(out0 + i * STEP * 128, h[0], h[1], h[2], h[3]);
+                    sts128(out1 + i * STEP * 128, h[4], h[5], h[6], h[7]);
+                }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
