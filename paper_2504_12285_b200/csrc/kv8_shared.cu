@@ -33,6 +33,7 @@ namespace {
 
 constexpr int kTile = 128;         // query rows and cache rows of a product
 constexpr int kPlanThreads = 1024;
+constexpr int kFewGroups = 1024;
 constexpr int kThreads = 512;
 constexpr int kSharedCtas = 160;   // parts are reserved for this many
 constexpr int kDescs = 4;
@@ -40,7 +41,7 @@ constexpr float kWeightScale = 128.0f;  // weights of up to 2^8 (the maximum is 
 
 // Workspace.  A part: fp32 values of its query rows, then (max, sum) of each.
 struct SharedLayout {
-    size_t rows, pairs, cum_pairs, cum_rows, starts, firsts, totals, parts_w, parts_s, total;
+    size_t rows, pairs, cum_pairs, cum_rows, starts, firsts, pair_rows, totals, parts_w, parts_s, total;
     int max_pairs;
 };
 struct SharedArgs {
@@ -61,6 +62,7 @@ struct SharedArgs {
     int* cum_rows;    // tiles of the rows' own parts in front, all heads
     int* starts;      // group_starts, in range and not decreasing
     int* firsts;      // of each group: its first row with something in the cache
+    int* pair_rows;   // of each pair: cache rows
     int* totals;      // pairs, units of pairs, tiles of rows
     float* parts_w;
     float* parts_s;
@@ -137,37 +139,47 @@ __device__ __forceinline__ int block_max_scan(int x, int* warp_sums) {  // inclu
 // One CTA: which rows share what, the pairs of query tiles, and how many units lie in front of each pair and row.
 __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedArgs a) {
     __shared__ int warp_sums[32];
+    __shared__ int few[3][kFewGroups + 1];
+    __shared__ int few_pairs[kFewGroups];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, cap = a.max_blocks << a.log2_rows;
+    // what the phases hand on lies in shared memory where it fits: a phase costs a microsecond less than by way of L2
+    int* const starts = a.n_groups <= kFewGroups ? few[0] : a.starts;
+    int* const firsts = a.n_groups <= kFewGroups ? few[1] : a.firsts;
+    int* const first_pairs = a.n_groups <= kFewGroups ? few[2] : a.cum_pairs;  // (overwritten later)
+    int* const pair_rows = a.max_pairs <= kFewGroups ? few_pairs : a.pair_rows;
     // the groups' borders
     int carry = 0;
     for (int g0 = 0; g0 <= a.n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
         const int x = g <= a.n_groups ? min(max(a.group_starts[g], 0), a.M) : 0;
         const int y = max(block_max_scan(x, warp_sums), carry);
-        if (g <= a.n_groups) a.starts[g] = y;
+        if (g <= a.n_groups) starts[g] = y;
         __syncthreads();
-        carry = a.starts[min(g0 + kPlanThreads - 1, a.n_groups)];
+        carry = starts[min(g0 + kPlanThreads - 1, a.n_groups)];
     }
     __syncthreads();
-    // the groups' pairs; a row on its own shares nothing.  pairs[].z holds the group for now, pairs[].w the most that the pair's rows share
+    // the groups' pairs; a row on its own shares nothing.  pairs[].z holds the group for now; pair_rows: the most that a pair's rows share
     int n_pairs = 0;
     for (int g0 = 0; g0 < a.n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
         int n = 0, first = 0, query_rows = 0;
         if (g < a.n_groups) {
-            first = a.starts[g];
-            const int rows = a.starts[g + 1] - first;
+            first = starts[g];
+            const int rows = starts[g + 1] - first;
             query_rows = rows * a.group;
             if (rows > 1 && a.shared_rows[g] > 0) n = (query_rows + 2 * kTile - 1) / (2 * kTile);
         }
         int total;
         const int at = n_pairs + block_exclusive_scan(n, warp_sums, total);
-        for (int i = 0; i < n; ++i) a.pairs[at + i] = make_int4(first * a.group + i * 2 * kTile, min(2 * kTile, query_rows - i * 2 * kTile), g, 0);
+        for (int i = 0; i < n; ++i) {
+            a.pairs[at + i] = make_int4(first * a.group + i * 2 * kTile, min(2 * kTile, query_rows - i * 2 * kTile), g, 0);
+            pair_rows[at + i] = 0;
+        }
         if (g < a.n_groups) {
-            a.cum_pairs[g] = n > 0 ? at : -1;  // (for the rows below; overwritten after that)
-            a.firsts[g] = a.M;
+            first_pairs[g] = n > 0 ? at : -1;
+            firsts[g] = a.M;
         }
         n_pairs += total;
     }
@@ -183,17 +195,18 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
             int lo = 0, hi = a.n_groups;
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
-                if (a.starts[mid] <= m) lo = mid;
+                if (starts[mid] <= m) lo = mid;
                 else hi = mid - 1;
             }
             int4 info = make_int4(0, len, -1, 0);
-            if (lo < a.n_groups && a.starts[lo] <= m && a.cum_pairs[lo] >= 0) {
-                const int flat0 = a.starts[lo] * a.group;
-                info = make_int4(min(len, a.shared_rows[lo]), len, a.cum_pairs[lo], flat0);
+            if (lo < a.n_groups && starts[lo] <= m && first_pairs[lo] >= 0) {
+                const int flat0 = starts[lo] * a.group;
+                info = make_int4(min(len, a.shared_rows[lo]), len, first_pairs[lo], flat0);
                 if (len > 0) {
                     const int p0 = info.z + (m * a.group - flat0) / (2 * kTile), p1 = info.z + (m * a.group + a.group - 1 - flat0) / (2 * kTile);
-                    for (int p = p0; p <= p1; ++p) atomicMax(&a.pairs[p].w, info.x);
-                    if (a.firsts[lo] > m) atomicMin(&a.firsts[lo], m);
+                    for (int p = p0; p <= p1; ++p)
+                        if (pair_rows[p] < info.x) atomicMax(&pair_rows[p], info.x);
+                    if (firsts[lo] > m) atomicMin(&firsts[lo], m);
                 }
             }
             a.rows[m] = info;
@@ -211,9 +224,10 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
         int units = 0;
         if (p < n_pairs) {
             int4 info = a.pairs[p];
+            info.w = pair_rows[p];
             const int span = info.y > kTile ? kTile : 2 * kTile;  // a unit: one tile of cache rows for two query tiles, or two for one
             units = (info.w + span - 1) / span * a.n_kv;
-            const int first = a.firsts[info.z];
+            const int first = firsts[info.z];
             info.z = first < a.M ? (a.seq_ids ? a.seq_ids[first] : first) : 0;  // (no row has anything in the cache: no units)
             a.pairs[p] = info;
         }
@@ -325,19 +339,19 @@ __device__ __forceinline__ void code_rows(uint32_t dst, const CUtensorMap* map, 
 // ---------------------------------------------------------------------------------------------- main kernel
 
 // One stream's half of a step.
+constexpr int kLive = 1, kFirst = 2, kLast = 4, kOwn = 8;  // there is one; its softmax begins, ends with it; a tile of what a row has for itself (else of a pair)
 struct Side {
-    int live, first, last;  // is there one; does its softmax begin, end with it
-    int own;                // 0: a tile of a pair; 1: of what a row has for itself
+    int flags;
     int row0, rows;         // query rows
     int head;
     int base;               // first cache row
     int cache_rows;         // of the tile, those that any query row uses
     int lost;               // bit i: cache rows 16 i .. 16 i + 15 belong to no block
-    int part, pad;          // where the result goes
+    int part;               // where the result goes
 };
 struct __align__(16) Desc {
-    Side side[2];
     float ks[2][8], vs[2][8];  // scales of each sixteen rows
+    Side side[2];
     int end, common, pad[2];   // no more steps; both streams use the first one's cache rows
 };
 
@@ -346,20 +360,24 @@ struct SharedSmem {
     static constexpr int kOperands = D == 128 ? 3 : 4;  // tiles of f16
     static constexpr int kStages = D == 128 ? 4 : 8;    // tiles of codes
     static constexpr uint32_t kOperandBytes = kTile * D * 2, kCodeBytes = kTile * D;
-    static constexpr uint32_t q = 0, operands = 2 * kOperandBytes, codes = operands + kOperands * kOperandBytes, descs = codes + kStages * kCodeBytes;
-    static constexpr uint32_t bars = descs + kDescs * sizeof(Desc);
+    // what is small lies in front of the tiles
+    static constexpr uint32_t descs = 0, bars = descs + kDescs * sizeof(Desc);
     // barriers
     static constexpr int code_full = 0, code_empty = code_full + kStages, op_full = code_empty + kStages, op_empty = op_full + kOperands, desc_full = op_empty + kOperands,
                          desc_empty = desc_full + kDescs, q_full = desc_empty + kDescs, s_full = q_full + 2, p_full = s_full + 2, o_full = p_full + 2, turn = o_full + 2, n_bars = turn + 2;
-    static constexpr uint32_t total = bars + n_bars * 8 + 16;
+    static constexpr uint32_t small = bars + n_bars * 8 + 8, q = (small + 1023) / 1024 * 1024, operands = q + 2 * kOperandBytes, codes = operands + kOperands * kOperandBytes;
+    static constexpr uint32_t total = codes + kStages * kCodeBytes;
 };
 
 template <int D, int KIND>
 __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const SharedArgs a) {
     using L = SharedSmem<D>;
-    extern __shared__ uint8_t shared_raw[];
-    uint8_t* smem = shared_raw + ((1024u - (smem_u32(shared_raw) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) uint8_t smem[];  // (the tiles' swizzle wants borders of 1024; there is no other shared memory in front)
     const uint32_t base_s = smem_u32(smem);
+    if (base_s & 1023u) {  // (never so far: copies to other borders would fault)
+        if (threadIdx.x == 0 && a.status != nullptr) atomicExch(a.status, BITLINEAR_ERR_CUDA);
+        return;
+    }
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     Desc* descs = reinterpret_cast<Desc*>(smem + L::descs);
     auto bar = [&](int i) { return base_s + L::bars + 8u * (uint32_t)i; };
@@ -393,6 +411,14 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
     auto tm_o = [&](int s) { return tmem + (uint32_t)(2 * kTile + s * D); };  // its accumulator
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // A wait that runs out raises the abort flag and lets its warp go on; every role looks at the flag once a step (a vote after each wait cost the products a
+    // hundred cycles apiece).  Until then it works on what is there: nothing leaves its bounds.
+    auto wait = [&](int i, uint32_t parity) {
+        if (!mbar_try_wait(bar(i), parity)) mbar_wait(bar(i), parity, abort_flag);
+        __syncwarp();
+    };
+    auto aborted = [&] { return __any_sync(0xffffffffu, *abort_flag != 0); };
 
     // All roles walk the steps in the same order of products: S of step 0 (both streams), then for every step and stream O, and S of the step behind.
     // Operand tiles are made and used in that order.
@@ -447,12 +473,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             bool there[2];
         };
         int made = 0;  // code tiles so far
-        bool ok = true;
         // publishes step p; false at the end
         auto publish = [&](int p, Tiles& now) {
             const int slot = p % kDescs;
-            if (p >= kDescs && !mbar_wait(bar(L::desc_empty + slot), (uint32_t)(p / kDescs - 1) & 1u, abort_flag)) ok = false;
-            if (!(ok = __all_sync(0xffffffffu, ok))) return false;
+            if (p >= kDescs) wait(L::desc_empty + slot, (uint32_t)(p / kDescs - 1) & 1u);
             Desc& d = descs[slot];
             const bool pairs_left = wu < share.w1;
             const bool end = !pairs_left && su[0] >= s_end[0] && su[1] >= s_end[1];
@@ -463,10 +487,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 Side& x = side[s];
                 if (pairs_left) {
                     const int tile = common ? w_unit : 2 * w_unit + s, rows = pair_info.w;
-                    x.live = tile * kTile < rows;
-                    x.own = 0;
-                    x.first = wu == share.w0 || w_unit == 0;
-                    x.last = wu == share.w1 - 1 || (tile + (common ? 1 : 2)) * kTile >= rows;
+                    const bool first = wu == share.w0 || w_unit == 0, last = wu == share.w1 - 1 || (tile + (common ? 1 : 2)) * kTile >= rows;
+                    x.flags = tile * kTile < rows ? kLive | (first ? kFirst : 0) | (last ? kLast : 0) : 0;
                     x.row0 = pair_info.x + (common ? s * kTile : 0);
                     x.rows = common ? (s ? pair_info.y - kTile : kTile) : pair_info.y;
                     x.head = w_head;
@@ -474,10 +496,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     x.cache_rows = min(rows - x.base, kTile);
                     x.part = (pair * a.n_kv + w_head + cta) * 2 + s;
                 } else if (su[s] < s_end[s]) {
-                    x.live = 1;
-                    x.own = 1;
-                    x.first = s_tile[s] == 0 || su[s] == (s ? share.middle() : share.s0);
-                    x.last = s_tile[s] == s_tiles[s] - 1 || su[s] == s_end[s] - 1;
+                    const bool first = s_tile[s] == 0 || su[s] == (s ? share.middle() : share.s0), last = s_tile[s] == s_tiles[s] - 1 || su[s] == s_end[s] - 1;
+                    x.flags = kLive | kOwn | (first ? kFirst : 0) | (last ? kLast : 0);
                     x.row0 = m[s] * a.group;
                     x.rows = a.group;
                     x.head = s_head[s];
@@ -485,8 +505,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     x.cache_rows = min(row_info[s].y - x.base, kTile);
                     x.part = m[s] * a.n_kv + s_head[s] + 2 * cta + s;
                 }
+                const bool live = x.flags & kLive;
                 // the blocks of the tile
-                const bool loads = x.live && !(common && s == 1);
+                const bool loads = live && !(common && s == 1);
                 int id = -1;
                 if (loads) {
                     const int b = (x.base >> a.log2_rows) + lane;
@@ -502,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             for (int s = 0; s < 2; ++s) {
                 const int from = common ? 0 : s;
                 int lost = 0;
-                if (side[s].live) {
+                if (side[s].flags & kLive) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int id = __shfl_sync(0xffffffffu, from ? now.id[1] : now.id[0], (16 * i) >> a.log2_rows);
@@ -568,11 +589,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             return !end;
         };
         auto load = [&](const Tiles& now, int s, const CUtensorMap* map) {
-            if (!ok || !now.there[s]) return;
+            if (!now.there[s]) return;
             const int place = made % L::kStages;
-            if (made >= L::kStages && !mbar_wait(bar(L::code_empty + place), (uint32_t)(made / L::kStages - 1) & 1u, abort_flag)) ok = false;
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) return;
+            if (made >= L::kStages) wait(L::code_empty + place, (uint32_t)(made / L::kStages - 1) & 1u);
             ++made;
             const unsigned present = __ballot_sync(0xffffffffu, now.id[s] >= 0);
             const uint32_t full = bar(L::code_full + place), block_bytes = (uint32_t)D << a.log2_rows;
@@ -582,11 +601,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 code_rows(base_s + L::codes + (uint32_t)place * L::kCodeBytes + (uint32_t)lane * block_bytes, map, (now.id[s] * a.n_kv + now.head[s]) << a.log2_rows, full);
         };
         Tiles now = {{-1, -1}, {0, 0}, {false, false}}, next;
-        for (int p = -1; ok; ++p) {
+        for (int p = -1; !aborted(); ++p) {
             load(now, 0, &map_v);
-            if (!ok) break;
             const bool more = publish(p + 1, next);
-            if (!ok) break;
             if (more) load(next, 0, &map_k);
             load(now, 1, &map_v);
             if (!more) break;
@@ -602,83 +619,82 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         constexpr uint32_t kScores = instruction(kTile, false), kValues = instruction(D, true);
         const uint64_t q_tile = operand(__shfl_sync(0xffffffffu, base_s + L::q + (uint32_t)s * L::kOperandBytes, 0), 16);
         uint32_t q_phase = 0, p_phase = 0, turn_phase = s == 0 ? 1u : 0u;  // (the first turn is the first stream's)
-        int made = 0, key = 0, value = 0;  // operand tiles so far; those of the products under way
-        bool ok = true;
-        auto landed = [&](int bar_at, uint32_t parity) { return ok = __all_sync(0xffffffffu, mbar_wait(bar(bar_at), parity, abort_flag)); };
-        auto filled = [&](int tile) { return landed(L::op_full + tile % L::kOperands, (uint32_t)(tile / L::kOperands) & 1u); };
-        for (int p = -1; ok; ++p) {
-            bool more = false;
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {  // values of step p, scores of the next, of either stream
-                const bool values = !(i & 1);
-                const int q = values ? p : p + 1, t = i >> 1;
-                const Desc& d = descs[q & (kDescs - 1)];
-                if (i == 1) {
-                    if (!landed(L::desc_full + q % kDescs, (uint32_t)(q / kDescs) & 1u)) break;
-                    more = !d.end;
-                }
-                const bool there = values ? p >= 0 : more, live = there && d.side[t].live, common = there && d.common;
-                if (live && !(common && t == 1)) {
-                    if (values) value = made;
-                    else key = made;
-                    ++made;
-                }
-                const int tile = values ? value : key;
-                if (t != s) {  // the other stream's: a tile is free when both warps have passed it
-                    if (live && !common) {
-                        if (!filled(tile)) break;
-                        if (lane == 0) mbar_arrive(bar(L::op_empty + tile % L::kOperands));
-                    }
-                    continue;
-                }
-                if (live && !filled(tile)) break;
-                const uint32_t at = __shfl_sync(0xffffffffu, base_s + L::operands + (uint32_t)(tile % L::kOperands) * L::kOperandBytes, 0);
-                const uint32_t done = __shfl_sync(0xffffffffu, bar(L::op_empty + tile % L::kOperands), 0);
-                const int flags = __shfl_sync(0xffffffffu, live ? d.side[s].first | d.side[s].last << 1 : 0, 0);
-                const bool one = elect_one();
-                if (values) {
-                    if (live) {
-                        if (!landed(L::p_full + s, p_phase)) break;
-                        p_phase ^= 1u;
-                    }
-                    // The streams take turns at the tensor cores, so that one's softmax runs beside the other's products; without, both did the same at a time.
-                    if (!landed(L::turn + s, turn_phase)) break;
-                    turn_phase ^= 1u;
-                    if (live) {
-                        tc_fence_after();
-                        if (one) {
-                            const uint64_t v_tile = operand(at, kHalfTile);
-                            const bool fresh = flags & 1;
-#pragma unroll
-                            for (int k = 0; k < kTile / 16; ++k) mma_ts(sums_at, scores_at + 8 * k, v_tile + 128u * k, kValues, !(fresh && k == 0));
-                            if (flags & 2) tc_commit(o_full);
-                            tc_commit(done);
-                        }
-                    }
-                } else {
-                    if (live) {
-                        if (flags & 1) {
-                            if (!landed(L::q_full + s, q_phase)) break;
-                            q_phase ^= 1u;
-                        }
-                        if (one) {
-                            const uint64_t k_tile = operand(at, 16);
-#pragma unroll
-                            for (int k = 0; k < D / 16; ++k) {
-                                const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
-                                mma_ss(scores_at, q_tile + off, k_tile + off, kScores, k > 0);
-                            }
-                            tc_commit(s_full);
-                            tc_commit(done);
-                        }
-                    }
-                    if (lane == 0) mbar_arrive(bar(L::turn + 1 - s));
-                }
-                __syncwarp();
+        int made = 0;                            // operand tiles so far, of both streams
+        int now = 0, other_now = 0;              // flags of step p, this stream's and the other's
+        bool common_now = false;
+        auto filled = [&](int tile) { wait(L::op_full + tile % L::kOperands, (uint32_t)(tile / L::kOperands) & 1u); };
+        // the other stream's tile: one is free when both warps have passed it
+        auto pass = [&](int tile) {
+            filled(tile);
+            if (lane == 0) mbar_arrive(bar(L::op_empty + tile % L::kOperands));
+        };
+        // Step p's values, then the scores of the next, of this stream.  All that the second needs is looked up before the first's weights are waited for.
+        for (int p = -1; !aborted(); ++p) {
+            const int slot = (p + 1) % kDescs;
+            wait(L::desc_full + slot, (uint32_t)((p + 1) / kDescs) & 1u);
+            const Desc& d = descs[slot];
+            const bool more = !d.end, common = d.common;
+            const int next = __shfl_sync(0xffffffffu, d.side[s].flags, 0), other = __shfl_sync(0xffffffffu, d.side[1 - s].flags, 0);
+            // tiles in the order of all products: values of the first stream, its next scores, the second's values, its next scores
+            const bool v0 = (s ? other_now : now) & kLive, k0 = (s ? other : next) & kLive, v1 = ((s ? now : other_now) & kLive) && !common_now, k1 = ((s ? next : other) & kLive) && !common;
+            const int tile_v0 = made, tile_k0 = tile_v0 + v0, tile_v1 = tile_k0 + k0, tile_k1 = tile_v1 + v1;
+            made = tile_k1 + k1;
+            const int value = s && !common_now ? tile_v1 : tile_v0, key = s && !common ? tile_k1 : tile_k0;
+            if (s == 1) {
+                if (v0 && !common_now) pass(tile_v0);
+                if (k0 && !common) pass(tile_k0);
             }
-            if (p >= 0 && lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
+            const bool has_value = now & kLive, has_key = next & kLive;
+            const uint32_t tiles_at = base_s + L::operands;
+            const uint32_t v_at = __shfl_sync(0xffffffffu, tiles_at + (uint32_t)(value % L::kOperands) * L::kOperandBytes, 0);
+            const uint32_t k_at = __shfl_sync(0xffffffffu, tiles_at + (uint32_t)(key % L::kOperands) * L::kOperandBytes, 0);
+            const uint32_t v_done = __shfl_sync(0xffffffffu, bar(L::op_empty + value % L::kOperands), 0), k_done = __shfl_sync(0xffffffffu, bar(L::op_empty + key % L::kOperands), 0);
+            const bool one = elect_one();
+            if (has_value) {
+                filled(value);
+                wait(L::p_full + s, p_phase);
+                p_phase ^= 1u;
+            }
+            const bool key_there = has_key && __all_sync(0xffffffffu, mbar_try_wait(bar(L::op_full + key % L::kOperands), (uint32_t)(key / L::kOperands) & 1u));
+            // The streams take turns at the tensor cores, so that one's softmax runs beside the other's products; without, both did the same at a time.
+            wait(L::turn + s, turn_phase);
+            turn_phase ^= 1u;
+            tc_fence_after();
+            if (has_value && one) {
+                const uint64_t v_tile = operand(v_at, kHalfTile);
+#pragma unroll
+                for (int k = 0; k < kTile / 16; ++k) mma_ts(sums_at, scores_at + 8 * k, v_tile + 128u * k, kValues, !((now & kFirst) && k == 0));
+                if (now & kLast) tc_commit(o_full);
+                tc_commit(v_done);
+            }
+            if (has_key) {
+                if (!key_there) filled(key);
+                if (next & kFirst) {
+                    wait(L::q_full + s, q_phase);
+                    q_phase ^= 1u;
+                }
+                if (one) {
+                    const uint64_t k_tile = operand(k_at, 16);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
+                        mma_ss(scores_at, q_tile + off, k_tile + off, kScores, k > 0);
+                    }
+                    tc_commit(s_full);
+                    tc_commit(k_done);
+                }
+            }
+            if (lane == 0) {
+                mbar_arrive(bar(L::turn + 1 - s));
+                if (p >= 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
+            }
             __syncwarp();
             if (!more) break;
+            if (s == 0) {
+                if (v1) pass(tile_v1);
+                if (k1) pass(tile_k1);
+            }
+            now = next, other_now = other, common_now = common;
         }
     } else if (warp >= 12) {
         // ------------------------------------------------------------------ codes -> f16
@@ -689,16 +705,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         const uint32_t in_at = (uint32_t)(row * D) + (uint32_t)((D == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4);
         const uint32_t out_at = (uint32_t)(chunk >> 2) * kHalfTile + (uint32_t)row * 128u + (uint32_t)(((2 * (chunk & 3)) ^ (row & 7)) << 4);
         int made = 0;
-        bool ok = true;
         auto convert = [&](int p, int s, bool value) {
             const Desc& d = descs[p % kDescs];
             const Side& x = d.side[s];
-            if (!ok || !x.live || (d.common && s == 1)) return;
+            if (!(x.flags & kLive) || (d.common && s == 1)) return;
             const int from = made % L::kStages, to = made % L::kOperands;
-            ok = mbar_wait(bar(L::code_full + from), (uint32_t)(made / L::kStages) & 1u, abort_flag);
-            if (ok && made >= L::kOperands) ok = mbar_wait(bar(L::op_empty + to), (uint32_t)(made / L::kOperands - 1) & 1u, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) return;
+            wait(L::code_full + from, (uint32_t)(made / L::kStages) & 1u);
+            if (made >= L::kOperands) wait(L::op_empty + to, (uint32_t)(made / L::kOperands - 1) & 1u);
             ++made;
             const uint32_t src = base_s + L::codes + (uint32_t)from * L::kCodeBytes, dst = base_s + L::operands + (uint32_t)to * L::kOperandBytes;
             const int cache_rows = x.cache_rows, lost = x.lost;
@@ -735,13 +748,12 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 mbar_arrive(bar(L::code_empty + from));
             }
         };
-        for (int p = -1; ok; ++p) {
+        for (int p = -1; !aborted(); ++p) {
             bool more = false;
 #pragma unroll 1
             for (int i = 0; i < 4; ++i) {  // values of step p, keys of the next, for either stream
                 if (i == 1) {
-                    const bool landed = mbar_wait(bar(L::desc_full + (p + 1) % kDescs), (uint32_t)((p + 1) / kDescs) & 1u, abort_flag);
-                    if (!(ok = __all_sync(0xffffffffu, ok && landed))) break;
+                    wait(L::desc_full + (p + 1) % kDescs, (uint32_t)((p + 1) / kDescs) & 1u);
                     more = !descs[(p + 1) % kDescs].end;
                 }
                 if (i & 1 ? more : p >= 0) convert(i & 1 ? p + 1 : p, i >> 1, !(i & 1));
@@ -758,25 +770,25 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
         int lower = 0, upper = 0;
         uint32_t s_phase = 0, o_phase = 0;
-        for (int p = 0;; ++p) {
+        for (int p = 0; !aborted(); ++p) {
             const int slot = p % kDescs;
-            if (!__all_sync(0xffffffffu, mbar_wait(bar(L::desc_full + slot), (uint32_t)(p / kDescs) & 1u, abort_flag))) break;
+            wait(L::desc_full + slot, (uint32_t)(p / kDescs) & 1u);
             const Desc& d = descs[slot];
             if (d.end) break;
             const Side x = d.side[s];
-            if (!x.live) {
+            if (!(x.flags & kLive)) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
                 continue;
             }
             const bool mine = r < x.rows, any = quad * 32 < x.rows;
-            if (x.first) {
+            if (x.flags & kFirst) {
                 m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
                 if (mine) {
                     const int flat = x.row0 + r, m = flat / a.group, j = flat - m * a.group;
                     const int4 info = a.rows[m];
-                    lower = x.own ? info.x : 0;
-                    upper = x.own ? info.y : info.x;
+                    lower = x.flags & kOwn ? info.x : 0;
+                    upper = x.flags & kOwn ? info.y : info.x;
                     const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D);
                     uint4 v[D / 8];
 #pragma unroll
@@ -806,38 +818,44 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(L::q_full + s));
             }
-            if (!__all_sync(0xffffffffu, mbar_wait(bar(L::s_full + s), s_phase, abort_flag))) break;
+            // what this row uses of the tile
+            const int lo = max(lower - x.base, 0), hi = min(upper - x.base, kTile);
+            const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && x.lost == 0));
+            auto used = [&](int c) {  // of columns 32 c .. 32 c + 31
+                const int l = max(lo - 32 * c, 0), h = min(max(hi - 32 * c, 0), 32);
+                uint32_t w = h > l ? (uint32_t)((1ull << h) - (1ull << l)) : 0u;
+                if ((x.lost >> (2 * c)) & 1) w &= 0xffff0000u;
+                if ((x.lost >> (2 * c + 1)) & 1) w &= 0x0000ffffu;
+                return w;
+            };
+            float vs = 0.0f;  // the largest scale of values that the row uses
+            if (all_used) {
+                const float4 w0 = *reinterpret_cast<const float4*>(&d.vs[s][0]), w1 = *reinterpret_cast<const float4*>(&d.vs[s][4]);
+                vs = fmaxf(fmaxf(fmaxf(w0.x, w0.y), fmaxf(w0.z, w0.w)), fmaxf(fmaxf(w1.x, w1.y), fmaxf(w1.z, fmaxf(w1.w, 0.0f))));
+            }
+            wait(L::s_full + s, s_phase);
             s_phase ^= 1u;
             tc_fence_after();
             if (any) {
-                // what this row uses of the tile
-                const int lo = max(lower - x.base, 0), hi = min(upper - x.base, kTile);
-                const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && x.lost == 0));
-                auto used = [&](int c) {  // of columns 32 c .. 32 c + 31
-                    const int l = max(lo - 32 * c, 0), h = min(max(hi - 32 * c, 0), 32);
-                    uint32_t w = h > l ? (uint32_t)((1ull << h) - (1ull << l)) : 0u;
-                    if ((x.lost >> (2 * c)) & 1) w &= 0xffff0000u;
-                    if ((x.lost >> (2 * c + 1)) & 1) w &= 0x0000ffffu;
-                    return w;
-                };
-                // The loops over 32 columns stay loops: with all of them unrolled, the roles' code did not fit the instruction caches, and a warp waited for
+                // The loops over columns stay loops: with all of them unrolled, the roles' code did not fit the instruction caches, and a warp waited for
                 // instructions longer than for anything else (444 us for 2173 rows of two chunks, 0.3 instructions a cycle).
-                float top = -INFINITY, vs = 0.0f;  // the largest score, the largest scale of values
+                float top = -INFINITY;  // the largest score
                 if (all_used) {
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32];
-                        tm_load(ts + 32 * c, v);
-                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), w = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
+                    for (int c = 0; c < 4; c += 2) {
+                        uint32_t v[2][32];
+                        tm_load(ts + 32 * c, v[0]);
+                        tm_load(ts + 32 * c + 32, v[1]);
+                        const float4 k = *reinterpret_cast<const float4*>(&d.ks[s][2 * c]);
                         tm_load_wait();
-                        float t0 = __uint_as_float(v[0]), t1 = __uint_as_float(v[16]);
+                        float t[4];
 #pragma unroll
-                        for (int e = 1; e < 16; ++e) {
-                            t0 = fmaxf(t0, __uint_as_float(v[e]));
-                            t1 = fmaxf(t1, __uint_as_float(v[16 + e]));
-                        }
-                        top = fmaxf(top, fmaxf(t0 * (k.x * f), t1 * (k.y * f)));
-                        vs = fmaxf(vs, fmaxf(w.x, w.y));
+                        for (int i = 0; i < 4; ++i) t[i] = __uint_as_float(v[i >> 1][16 * (i & 1)]);
+#pragma unroll
+                        for (int e = 1; e < 16; ++e)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) t[i] = fmaxf(t[i], __uint_as_float(v[i >> 1][16 * (i & 1) + e]));
+                        top = fmaxf(top, fmaxf(fmaxf(t[0] * (k.x * f), t[1] * (k.y * f)), fmaxf(t[2] * (k.z * f), t[3] * (k.w * f))));
                     }
                 } else {
 #pragma unroll 1
@@ -861,7 +879,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     const float c = m_run == -INFINITY ? 0.0f : ex2(m_run - n);  // (nothing there yet: zeros)
                     const float fo = nv > 0.0f ? c * (v_ref / nv) : c;
                     l_run *= c;
-                    if (!x.first) {
+                    if (!(x.flags & kFirst)) {
 #pragma unroll 1
                         for (int i = 0; i < D / 32; ++i) {
                             uint32_t v[32];
@@ -881,6 +899,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 // They go over scores that have been read.
                 if (all_used) {
                     float2 sum = make_float2(0.0f, 0.0f);
+                    const float2 bb = splat(-b);
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c) {
                         uint32_t v[32], w[16];
@@ -889,7 +908,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                         tm_load_wait();
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const float2 kk = splat((i ? k.y : k.x) * f), ww = splat((i ? r2.y : r2.x) * per_ref), bb = splat(-b);
+                            const float2 kk = splat((i ? k.y : k.x) * f), ww = splat((i ? r2.y : r2.x) * per_ref);
 #pragma unroll
                             for (int e = 0; e < 16; e += 2) {
                                 float2 t = fma2(make_float2(__uint_as_float(v[16 * i + e]), __uint_as_float(v[16 * i + e + 1])), kk, bb);
@@ -929,15 +948,15 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 mbar_arrive(bar(L::p_full + s));
                 mbar_arrive(bar(L::desc_empty + slot));
             }
-            if (x.last) {
-                if (!__all_sync(0xffffffffu, mbar_wait(bar(L::o_full + s), o_phase, abort_flag))) break;
+            if (x.flags & kLast) {
+                wait(L::o_full + s, o_phase);
                 o_phase ^= 1u;
                 tc_fence_after();
                 if (any) {
-                    const int rows = x.own ? a.group : kTile;
-                    float* part = (x.own ? a.parts_s : a.parts_w) + (size_t)x.part * part_floats(rows, D);
+                    const int rows = x.flags & kOwn ? a.group : kTile;
+                    float* part = (x.flags & kOwn ? a.parts_s : a.parts_w) + (size_t)x.part * part_floats(rows, D);
                     const float unscale = v_ref * (1.0f / kWeightScale);
-#pragma unroll
+#pragma unroll 1
                     for (int i = 0; i < D / 32; ++i) {
                         uint32_t v[32];
                         tm_load(to + 32 * i, v);
@@ -970,44 +989,82 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 
 // ---------------------------------------------------------------------------------------------- the parts of a row
 
-// A CTA per row and KV head, a thread for four dims of a query head.
-template <int D>
-__global__ void shared_combine_kernel(const SharedArgs a, int ctas) {
+// A query head's parts, by WARPS warps: warp w takes parts w, w + WARPS, ... of each of the two kinds.  Lane l first finds the l-th of a round's parts and weighs it;
+// then all lanes add up the rounds' values, a few dims each, eight parts' loads in flight.
+template <int D, int WARPS>
+__global__ void __launch_bounds__(128) shared_combine_kernel(const SharedArgs a, int ctas) {
+    constexpr int DIMS = D / 32;
+    __shared__ float2 joined[4];
+    __shared__ float values[4][D];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int m = blockIdx.x, h = blockIdx.y, j = (int)threadIdx.x / (D / 4), dim = 4 * ((int)threadIdx.x % (D / 4));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int item = (int)blockIdx.x * (4 / WARPS) + warp / WARPS, m = item / a.n_q, head = item - m * a.n_q, h = head / a.group, j = head - h * a.group, w = warp % WARPS;
+    const bool there = m < a.M;
     const int units = a.totals[1], tiles = a.totals[2];
     const EqualRuns runs(2 * units + tiles, ctas);
-    const int4 row = a.rows[m];
-    float top = -INFINITY, l = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    auto add = [&](const float* part, int rows, int r) {
-        const float2 ml = *reinterpret_cast<const float2*>(part + (size_t)rows * D + 2 * r);
-        const float4 v = *reinterpret_cast<const float4*>(part + (size_t)r * D + dim);
-        const float n = fmaxf(top, ml.x);
-        const float f0 = top == -INFINITY ? 0.0f : ex2(top - n), f1 = ml.x == -INFINITY ? (ml.y == ml.y ? 0.0f : NAN) : ex2(ml.x - n);
-        l = l * f0 + ml.y * f1;
-        acc.x = acc.x * f0 + v.x * f1, acc.y = acc.y * f0 + v.y * f1, acc.z = acc.z * f0 + v.z * f1, acc.w = acc.w * f0 + v.w * f1;
-        top = n;
+    const int4 row = there ? a.rows[m] : make_int4(0, 0, -1, 0);
+    float top = -INFINITY, l = 0.0f, acc[DIMS] = {};
+    // parts first .. last (a lane finds its own by `find`: nullptr where it is none; its query rows, and which of them)
+    auto gather = [&](int n, auto find) {
+        for (int i0 = 32 * w; i0 < n; i0 += 32 * WARPS) {
+            const float* part = nullptr;
+            int rows = 0, r = 0;
+            if (i0 + lane < n) part = find(i0 + lane, rows, r);
+            float2 ml = make_float2(-INFINITY, 0.0f);
+            if (part) ml = *reinterpret_cast<const float2*>(part + (size_t)rows * D + 2 * r);
+            const float* mine = part ? part + (size_t)r * D : nullptr;
+            float most = ml.x;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+            const float now = fmaxf(top, most), f0 = top == -INFINITY ? 0.0f : ex2(top - now);
+            // (a part whose scores are all NaN has a sum that is NaN and no maximum)
+            const float f = ml.x == -INFINITY ? (ml.y == ml.y ? 0.0f : NAN) : ex2(ml.x - now);
+            float sum = ml.y * f;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            l = l * f0 + sum;
+            top = now;
+#pragma unroll
+            for (int e = 0; e < DIMS; ++e) acc[e] *= f0;
+            unsigned have = __ballot_sync(0xffffffffu, mine != nullptr && !(f == 0.0f));
+            while (have) {
+                float v[8][DIMS], g[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int src = have ? __ffs((int)have) - 1 : 0;
+                    const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)mine, src));
+                    g[k] = have ? __shfl_sync(0xffffffffu, f, src) : 0.0f;
+                    if (have) {
+                        if constexpr (DIMS == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(p + 4 * lane);
+                        else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(p + 2 * lane);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < DIMS; ++e) v[k][e] = 0.0f;
+                    }
+                    have &= have - 1;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int e = 0; e < DIMS; ++e) acc[e] = fmaf(v[k][e], g[k], acc[e]);
+            }
+        }
     };
     if (row.z >= 0 && row.x > 0) {
-        const int in_group = m * a.group + j - row.w, pair = row.z + in_group / (2 * kTile), r = in_group % (2 * kTile);
+        const int in_group = m * a.group + j - row.w, pair = row.z + in_group / (2 * kTile), r0 = in_group % (2 * kTile);
         const int4 info = a.pairs[pair];
         const bool two = info.y > kTile;
         const int n = (a.cum_pairs[pair + 1] - a.cum_pairs[pair]) / a.n_kv, u0 = a.cum_pairs[pair] + h * n;
-        const int c1 = runs.owner(2 * (u0 + n - 1));
-        for (int c = runs.owner(2 * u0); c <= c1; ++c) {
+        const int c0 = runs.owner(2 * u0), c1 = runs.owner(2 * (u0 + n - 1));
+        gather((c1 - c0 + 1) * (two ? 1 : 2), [&](int i, int& rows, int& r) -> const float* {
+            const int c = c0 + (two ? i : i >> 1), s = two ? r0 / kTile : i & 1;
+            rows = kTile, r = r0 % kTile;
             const Share share(runs, units, c);
-            if (share.w0 >= share.w1) continue;  // (a CTA with one place may have the second half of a unit's)
-            const float* part = a.parts_w + (size_t)(pair * a.n_kv + h + c) * 2 * part_floats(kTile, D);
-            if (two) {
-                add(part + (r >= kTile ? part_floats(kTile, D) : 0), kTile, r % kTile);
-            } else {
-                add(part, kTile, r);
-                const int from = max(share.w0 - u0, 0);
-                if ((2 * from + 1) * kTile < info.w) add(part + part_floats(kTile, D), kTile, r);  // else the second stream had no tile
-            }
-        }
+            if (share.w0 >= share.w1) return nullptr;                                                      // (a CTA with one place may have the second half of a unit's)
+            if (!two && s == 1 && (2 * max(share.w0 - u0, 0) + 1) * kTile >= info.w) return nullptr;  // the second stream had no tile
+            return a.parts_w + ((size_t)(pair * a.n_kv + h + c) * 2 + s) * part_floats(kTile, D);
+        });
     }
     if (row.y > row.x) {
         const int n = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv, t0 = a.cum_rows[m] + h * n;
@@ -1015,17 +1072,48 @@ __global__ void shared_combine_kernel(const SharedArgs a, int ctas) {
             const int c = runs.owner(2 * units + t);
             return 2 * c + (t >= Share(runs, units, c).middle() ? 1 : 0);
         };
-        const int w1 = worker(t0 + n - 1);
-        for (int w = worker(t0); w <= w1; ++w) {
-            // (the second stream of a CTA with one tile has none)
-            const Share share(runs, units, w >> 1);
-            if (((w & 1) ? share.s1 - share.middle() : share.middle() - share.s0) > 0) add(a.parts_s + (size_t)(m * a.n_kv + h + w) * part_floats(a.group, D), a.group, j);
+        const int first = worker(t0), last = worker(t0 + n - 1);
+        gather(last - first + 1, [&](int i, int& rows, int& r) -> const float* {
+            const int k = first + i;
+            rows = a.group, r = j;
+            const Share share(runs, units, k >> 1);
+            if (((k & 1) ? share.s1 - share.middle() : share.middle() - share.s0) <= 0) return nullptr;  // (the second stream of a CTA with one tile)
+            return a.parts_s + (size_t)(m * a.n_kv + h + k) * part_floats(a.group, D);
+        });
+    }
+    if constexpr (WARPS > 1) {
+        if (lane == 0) joined[warp] = make_float2(top, l);
+#pragma unroll
+        for (int e = 0; e < DIMS; ++e) values[warp][DIMS * lane + e] = acc[e];
+        __syncthreads();
+        if (w != 0) return;
+        float most = top;
+#pragma unroll
+        for (int k = 1; k < WARPS; ++k) most = fmaxf(most, joined[warp + k].x);
+        const float f0 = top == -INFINITY ? (l == l ? 0.0f : NAN) : ex2(top - most);
+        l *= f0;
+#pragma unroll
+        for (int e = 0; e < DIMS; ++e) acc[e] *= f0;
+#pragma unroll
+        for (int k = 1; k < WARPS; ++k) {
+            const float2 o = joined[warp + k];
+            const float f = o.x == -INFINITY ? (o.y == o.y ? 0.0f : NAN) : ex2(o.x - most);
+            l = fmaf(o.y, f, l);
+#pragma unroll
+            for (int e = 0; e < DIMS; ++e) acc[e] = fmaf(values[warp + k][DIMS * lane + e], f, acc[e]);
         }
     }
+    if (!there) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no row: zeros; a sum that is NaN stays one
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-    *reinterpret_cast<uint2*>(a.out + ((size_t)m * a.n_q + (size_t)h * a.group + j) * D + dim) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    uint32_t out[DIMS / 2];
+#pragma unroll
+    for (int e = 0; e < DIMS; e += 2) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(acc[e] * inv, acc[e + 1] * inv);
+        out[e / 2] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    __nv_bfloat16* dst = a.out + (size_t)item * D + DIMS * lane;
+    if constexpr (DIMS == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = out[0];
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -1046,6 +1134,7 @@ SharedLayout shared_layout(int M, int n_groups, int n_q, int n_kv, int D) {
     l.cum_rows = room(((size_t)M + 1) * sizeof(int));
     l.starts = room(((size_t)n_groups + 1) * sizeof(int));
     l.firsts = room(((size_t)n_groups + 1) * sizeof(int));
+    l.pair_rows = room((size_t)l.max_pairs * sizeof(int));
     l.totals = room(3 * sizeof(int));
     l.parts_w = room(l.max_pairs == 0 ? 0 : ((size_t)l.max_pairs * n_kv + kSharedCtas) * 2 * part_floats(kTile, D) * sizeof(float));
     l.parts_s = room(((size_t)M * n_kv + 2 * kSharedCtas) * part_floats(group, D) * sizeof(float));
@@ -1054,7 +1143,7 @@ SharedLayout shared_layout(int M, int n_groups, int n_q, int n_kv, int D) {
 }
 
 bool shared_sizes_ok(int M, int n_groups, int n_q, int n_kv, int hd) {
-    return M >= 0 && M <= 65535 && n_groups >= 0 && n_groups <= 65535 && n_q > 0 && n_kv > 0 && n_q % n_kv == 0 && n_q / n_kv <= 8 && (hd == 64 || hd == 128) && n_kv <= 65535;
+    return M >= 0 && M <= 65535 && n_groups >= 0 && n_groups <= 65535 && n_q > 0 && n_kv > 0 && n_q % n_kv == 0 && n_q / n_kv <= 8 && (hd == 64 || hd == 128) && n_kv <= 65535 && (long long)M * n_q < (1ll << 30);
 }
 
 // rows = every (block, head, row) of the pool, columns = D bytes; a box is a block's rows, swizzled by the row's width
@@ -1077,7 +1166,7 @@ int finish(cudaError_t rc) {
 
 template <int D, int KIND>
 int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const SharedArgs& a, int ctas, cudaStream_t st) {
-    constexpr uint32_t kBytes = 1024 + SharedSmem<D>::total;
+    constexpr uint32_t kBytes = SharedSmem<D>::total;
     static_assert(kBytes <= 227 * 1024, "shared memory");
     static std::mutex mu;
     static bool done[64];
@@ -1104,10 +1193,13 @@ int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const Shar
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kBytes;
     if (const int rc = finish(cudaLaunchKernelEx(&cfg, shared_attention_kernel<D, KIND>, map_k, map_v, a))) return rc;
-    cfg.gridDim = dim3((unsigned)a.M, (unsigned)a.n_kv);
-    cfg.blockDim = dim3((unsigned)(a.group * D / 4));
+    // a warp per query head where there are enough of them, else four
+    const long long heads = (long long)a.M * a.n_q;
+    const bool many = heads >= 32ll * ctas;
+    cfg.gridDim = dim3((unsigned)(many ? (heads + 3) / 4 : heads));
+    cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;
-    return finish(cudaLaunchKernelEx(&cfg, shared_combine_kernel<D>, a, ctas));
+    return finish(many ? cudaLaunchKernelEx(&cfg, shared_combine_kernel<D, 1>, a, ctas) : cudaLaunchKernelEx(&cfg, shared_combine_kernel<D, 4>, a, ctas));
 }
 
 }  // namespace
@@ -1145,7 +1237,7 @@ int bitlinear_attention_shared_kv8(const void* q_bf16, const void* k_cache, cons
     SharedArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, group_starts, shared_rows, M, n_groups, n_q_heads, n_kv_heads,
                     n_q_heads / n_kv_heads, n_seq, max_blocks, log2_of(block_rows), n_blocks, 1.4426950408889634f / sqrtf((float)head_dim), static_cast<__nv_bfloat16*>(out_bf16),
                     reinterpret_cast<int4*>(w + l.rows), reinterpret_cast<int4*>(w + l.pairs), reinterpret_cast<int*>(w + l.cum_pairs), reinterpret_cast<int*>(w + l.cum_rows),
-                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.firsts), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
+                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.firsts), reinterpret_cast<int*>(w + l.pair_rows), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
                     l.max_pairs, device_status_word()};
     const int ctas = std::min(sm_count, kSharedCtas);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
