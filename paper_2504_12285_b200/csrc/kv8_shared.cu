@@ -7,15 +7,17 @@
 // S = Q K^T and O += P V by tcgen05.mma (f16 operands, fp32 accumulators in tensor memory).  Codes arrive by tensor-map copies and become f16 in shared
 // memory, which is exact; their scales go onto the scores and the softmax weights in fp32.  Queries are f16 times a power of two per row, exact too.
 //
-// A CTA runs two streams of such tiles, each with a Q tile, a score tile, an accumulator and four softmax warps of its own, so that one stream's
-// softmax runs beside the other's products.  Where a group has more than 128 query rows, the streams take two tiles of them over the same
+// A CTA runs two streams of such tiles, each with a Q tile, a score tile, an accumulator and four softmax warps of its own.  A stream works in half steps of 64
+// cache rows: while the softmax is at one half's scores, the products of the other half - its weights with the values, then the next step's scores in their
+// place - run, so neither waits for the other.  Where a group has more than 128 query rows, the streams take two tiles of them over the same
 // cache rows (which are then converted once); else they take different cache rows.  What a row does not share is work of the same kind, with the few
 // query rows of that row alone.  All of it is cut into equal runs, one per CTA, whatever the lengths; parts of a row meet in a last launch.
 //
 //   warp 0      copies: block tables -> tensor-map copies of code tiles, and the work list that the other warps follow
 //   warps 1, 2  one thread of each issues a stream's products
+//   warp 3      the queries of rows' own tiles, ahead of the softmax
 //   warps 4-11  softmax, one thread per query row; four warps per stream
-//   warps 12-15 codes -> f16
+//   warps 12-19 codes -> f16, four warps to a tile
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -34,7 +36,9 @@ namespace {
 constexpr int kTile = 128;         // query rows and cache rows of a product
 constexpr int kPlanThreads = 1024;
 constexpr int kFewGroups = 1024;
-constexpr int kThreads = 512;
+constexpr int kThreads = 640;
+constexpr int kHalf = 64;            // columns of a half step
+constexpr int kSoftmaxRegs = 144, kOtherRegs = 64;  // a thread, of eight and of twelve warps
 constexpr int kSharedCtas = 160;   // parts are reserved for this many
 constexpr int kDescs = 4;
 constexpr float kWeightScale = 128.0f;  // weights of up to 2^8 (the maximum is followed lazily) stay below f16's largest
@@ -294,16 +298,14 @@ __device__ __forceinline__ void tm_load(uint32_t at, uint32_t (&r)[32]) {
         : "r"(at)
         : "memory");
 }
-__device__ __forceinline__ void tm_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tm_store32(uint32_t at, const uint32_t (&v)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
-        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]),
-        "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]),
-        "r"(v[29]), "r"(v[30]), "r"(v[31])
-        : "memory");
+__device__ __forceinline__ void tm_load16(uint32_t at, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]),
+                   "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at)
+                 : "memory");
 }
+__device__ __forceinline__ void tm_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_store16(uint32_t at, const uint32_t (&v)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
                  "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
@@ -331,6 +333,28 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return d;
 }
 
+// Queries: a row is scaled by the power of two that brings its largest magnitude to 2^8 .. 2^9; bf16 values then fit f16 without loss down to 2^-22 of it.
+// (Magnitudes by their bits: infinity and NaN are above all others, exponent 255.)
+__device__ __forceinline__ uint32_t largest_bits(const uint4& v) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    uint32_t most = 0u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) most = max(most, max((u[e] << 16) & 0x7fffffffu, u[e] & 0x7fff0000u));
+    return most;
+}
+__device__ __forceinline__ int query_exponent(uint32_t most) { return max((int)(most >> 23), 9); }
+__device__ __forceinline__ float query_up(uint32_t most) { return __int_as_float((262 - query_exponent(most)) << 23); }
+// what scores are multiplied by; a row that is not finite gives NaN
+__device__ __forceinline__ float query_down(int exponent) { return exponent == 255 ? NAN : __int_as_float((exponent - 8) << 23); }
+// eight queries, the `unit`-th sixteen bytes of row r of a Q tile
+__device__ __forceinline__ void store_queries(uint32_t tile, int r, int unit, const uint4& v, float up) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    uint32_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * up, __uint_as_float(u[e] & 0xffff0000u) * up);
+    sts128(tile + (uint32_t)r * 128u + (uint32_t)(unit >> 3) * kHalfTile + (uint32_t)(((unit & 7) ^ (r & 7)) << 4), h[0], h[1], h[2], h[3]);
+}
+
 __device__ __forceinline__ void code_rows(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(0), "r"(row), "r"(bar)
                  : "memory");
@@ -348,23 +372,26 @@ struct Side {
     int cache_rows;         // of the tile, those that any query row uses
     int lost;               // bit i: cache rows 16 i .. 16 i + 15 belong to no block
     int part;               // where the result goes
+    int lower, upper;       // kOwn: the cache rows that the row uses
 };
 struct __align__(16) Desc {
     float ks[2][8], vs[2][8];  // scales of each sixteen rows
     Side side[2];
-    int end, common, pad[2];   // no more steps; both streams use the first one's cache rows
+    int end, common;           // no more steps; both streams use the first one's cache rows
+    int pad[2];
 };
 
 template <int D>
 struct SharedSmem {
-    static constexpr int kOperands = D == 128 ? 3 : 4;  // tiles of f16
-    static constexpr int kStages = D == 128 ? 4 : 8;    // tiles of codes
+    static constexpr int kOperands = D == 128 ? 4 : 6;  // tiles of f16
+    static constexpr int kStages = D == 128 ? 2 : 8;    // tiles of codes
     static constexpr uint32_t kOperandBytes = kTile * D * 2, kCodeBytes = kTile * D;
     // what is small lies in front of the tiles
-    static constexpr uint32_t descs = 0, bars = descs + kDescs * sizeof(Desc);
+    static constexpr uint32_t exponents = 0, descs = 2 * 2 * kTile, bars = descs + kDescs * sizeof(Desc);
     // barriers
     static constexpr int code_full = 0, code_empty = code_full + kStages, op_full = code_empty + kStages, op_empty = op_full + kOperands, desc_full = op_empty + kOperands,
-                         desc_empty = desc_full + kDescs, q_full = desc_empty + kDescs, s_full = q_full + 2, p_full = s_full + 2, o_full = p_full + 2, turn = o_full + 2, n_bars = turn + 2;
+                         desc_empty = desc_full + kDescs, q_full = desc_empty + kDescs, q_free = q_full + 2, s_full = q_free + 2, p_full = s_full + 4, o_full = p_full + 4,
+                         pv_done = o_full + 2, n_bars = pv_done + 2;
     static constexpr uint32_t small = bars + n_bars * 8 + 8, q = (small + 1023) / 1024 * 1024, operands = q + 2 * kOperandBytes, codes = operands + kOperands * kOperandBytes;
     static constexpr uint32_t total = codes + kStages * kCodeBytes;
 };
@@ -387,14 +414,14 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         *abort_flag = 0;
         for (int i = 0; i < L::kStages; ++i) mbar_init(bar(L::code_full + i), 1), mbar_init(bar(L::code_empty + i), 4);
         for (int i = 0; i < L::kOperands; ++i) mbar_init(bar(L::op_full + i), 4), mbar_init(bar(L::op_empty + i), 2);
-        for (int i = 0; i < kDescs; ++i) mbar_init(bar(L::desc_full + i), 1 + 32), mbar_init(bar(L::desc_empty + i), 2 + 4 + 8);
+        for (int i = 0; i < kDescs; ++i) mbar_init(bar(L::desc_full + i), 1 + 32), mbar_init(bar(L::desc_empty + i), 2 + 1 + 8 + 8);
         for (int s = 0; s < 2; ++s) {
             mbar_init(bar(L::q_full + s), 4);
-            mbar_init(bar(L::s_full + s), 1);
-            mbar_init(bar(L::p_full + s), 4);
+            mbar_init(bar(L::q_free + s), 1);
             mbar_init(bar(L::o_full + s), 1);
-            mbar_init(bar(L::turn + s), 1);
+            mbar_init(bar(L::pv_done + s), 1);
         }
+        for (int i = 0; i < 4; ++i) mbar_init(bar(L::s_full + i), 1), mbar_init(bar(L::p_full + i), 4);
         mbar_init_fence();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
@@ -422,140 +449,300 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 
     // All roles walk the steps in the same order of products: S of step 0 (both streams), then for every step and stream O, and S of the step behind.
     // Operand tiles are made and used in that order.
+    if (warp >= 4 && warp < 12) {
+        // The softmax holds 64 scores in registers: its eight warps take what the other twelve leave of the launch's (256 * 144 + 384 * 64 of 640 * 96).
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        // ------------------------------------------------------------------ softmax
+        const int s = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
+        const uint32_t ts = tm_s(s) + lane_at, to = tm_o(s) + lane_at;
+        float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+        int lower = 0, upper = 0;
+        uint32_t s_phase = 0, o_phase = 0, item = 0, halves = 0;  // items, half steps so far
+        for (int p = 0; !aborted(); ++p) {
+            const int slot = p % kDescs;
+            wait(L::desc_full + slot, (uint32_t)(p / kDescs) & 1u);
+            const Desc& d = descs[slot];
+            if (d.end) break;
+            const Side& x = d.side[s];
+            const int flags = x.flags;
+            if (!(flags & kLive)) {
+                if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
+                continue;
+            }
+            const int n_rows = x.rows, part_at = x.part, base = x.base, lost = x.lost;
+            const bool mine = r < n_rows, any = quad * 32 < n_rows;
+            if (flags & kFirst) {
+                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+                if (flags & kOwn) {
+                    lower = x.lower, upper = x.upper;
+                } else {
+                    if (mine) {
+                        const int flat = x.row0 + r, m = flat / a.group, j = flat - m * a.group;
+                        lower = 0, upper = a.rows[m].x;
+                        const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D);
+                        uint4 v[D / 8];
+                        uint32_t most = 0u;
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) v[i] = __ldg(src + i);
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) most = max(most, largest_bits(v[i]));
+                        const float up = query_up(most);
+#pragma unroll
+                        for (int i = 0; i < D / 8; ++i) store_queries(base_s + L::q + (uint32_t)s * L::kOperandBytes, r, i, v[i], up);
+                        f = query_down(query_exponent(most)) * a.scale_log2;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(L::q_full + s));
+                }
+            }
+            // what this row uses of the tile
+            const int lo = max(lower - base, 0), hi = min(upper - base, kTile);
+            const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && lost == 0));
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h, ++halves) {
+                wait(L::s_full + 2 * s + h, s_phase);
+                tc_fence_after();
+                if ((flags & (kFirst | kOwn)) == (kFirst | kOwn) && h == 0 && mine) f = query_down(smem[L::exponents + (s * 2 + (item & 1u)) * kTile + r]) * a.scale_log2;
+                if (any) {
+                    uint32_t v[2][32];
+                    tm_load(ts + kHalf * h, v[0]);
+                    tm_load(ts + kHalf * h + 32, v[1]);
+                    float ks[4], rs[4];
+                    {
+                        const float4 k = *reinterpret_cast<const float4*>(&d.ks[s][4 * h]), w = *reinterpret_cast<const float4*>(&d.vs[s][4 * h]);
+                        ks[0] = k.x * f, ks[1] = k.y * f, ks[2] = k.z * f, ks[3] = k.w * f;
+                        rs[0] = w.x, rs[1] = w.y, rs[2] = w.z, rs[3] = w.w;
+                    }
+                    tm_load_wait();
+                    if (!all_used) {  // what the row does not use scores -infinity, whatever lies there; its scales count for nothing
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const int l = max(lo - 32 * c - kHalf * h, 0), n = min(max(hi - 32 * c - kHalf * h, 0), 32);
+                            uint32_t live = n > l ? (uint32_t)((1ull << n) - (1ull << l)) : 0u;
+                            if ((lost >> (4 * h + 2 * c)) & 1) live &= 0xffff0000u;
+                            if ((lost >> (4 * h + 2 * c + 1)) & 1) live &= 0x0000ffffu;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((live >> e) & 1u)) v[c][e] = 0xff800000u;
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const bool none = (live & (i ? 0xffff0000u : 0x0000ffffu)) == 0u;
+                                if (none || ks[2 * c + i] == 0.0f) ks[2 * c + i] = 1e-30f;  // -infinity times a scale of zero would be NaN; finite scores stay next to zero
+                                if (none) rs[2 * c + i] = 0.0f;
+                            }
+                        }
+                    }
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float t = __uint_as_float(v[i >> 1][16 * (i & 1)]);
+#pragma unroll
+                        for (int e = 1; e < 16; ++e) t = fmaxf(t, __uint_as_float(v[i >> 1][16 * (i & 1) + e]));
+                        top = fmaxf(top, t * ks[i]);
+                    }
+                    const float vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
+                    // The maximum is followed only where it grows by more than 2^8: weights stay within f16, and the accumulator is rarely scaled.
+                    const bool grows = top > m_run + 8.0f || (m_run == -INFINITY && top > -INFINITY), wider = vs > v_ref;
+                    if (__any_sync(0xffffffffu, grows || wider)) {
+                        const float n = grows ? top : m_run, nv = fmaxf(v_ref, vs);
+                        const float c = m_run == -INFINITY ? 0.0f : ex2(m_run - n);  // (nothing there yet: zeros)
+                        const float fo = nv > 0.0f ? c * (v_ref / nv) : c;
+                        l_run *= c;
+                        if (!(flags & kFirst) || h == 1) {
+                            wait(L::pv_done + s, (halves - 1u) & 1u);  // (the half in front of the last is in, or these scores would not be here)
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int i = 0; i < D / 16; ++i) {
+                                uint32_t o[16];
+                                tm_load16(to + 16 * i, o);
+                                tm_load_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fo);
+                                tm_store16(to + 16 * i, o);
+                            }
+                        }
+                        m_run = n;
+                        v_ref = nv;
+                    }
+                    const float per_ref = v_ref > 0.0f ? __fdividef(kWeightScale, v_ref) : 0.0f;
+                    // Weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost; their sum takes them unrounded.
+                    // They go over the scores.
+                    float2 sum = make_float2(0.0f, 0.0f);
+                    const float2 bb = splat(m_run == -INFINITY ? 0.0f : -m_run);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float2 kk = splat(ks[2 * c + i]), ww = splat(rs[2 * c + i] * per_ref);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                float2 t = fma2(make_float2(__uint_as_float(v[c][16 * i + e]), __uint_as_float(v[c][16 * i + e + 1])), kk, bb);
+                                t.x = ex2(t.x), t.y = ex2(t.y);
+                                sum = add2(sum, t);
+                                t = mul2(t, ww);
+                                w[8 * i + e / 2] = pack_f16(t.x, t.y);
+                            }
+                        }
+                        tm_store16(ts + kHalf * h + 16 * c, w);
+                    }
+                    l_run += sum.x + sum.y;
+                    tm_store_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::p_full + 2 * s + h));
+            }
+            s_phase ^= 1u;
+            if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
+            if (flags & kLast) {
+                wait(L::o_full + s, o_phase);
+                o_phase ^= 1u;
+                tc_fence_after();
+                ++item;
+                if (any) {
+                    const int rows = flags & kOwn ? a.group : kTile;
+                    float* part = (flags & kOwn ? a.parts_s : a.parts_w) + (size_t)part_at * part_floats(rows, D);
+                    const float unscale = v_ref * (1.0f / kWeightScale);
+#pragma unroll 1
+                    for (int i = 0; i < D / 32; ++i) {
+                        uint32_t v[32];
+                        tm_load(to + 32 * i, v);
+                        tm_load_wait();
+                        if (mine)
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<float4*>(part + (size_t)r * D + 32 * i + e) =
+                                    make_float4(__uint_as_float(v[e]) * unscale, __uint_as_float(v[e + 1]) * unscale, __uint_as_float(v[e + 2]) * unscale,
+                                                __uint_as_float(v[e + 3]) * unscale);
+                    }
+                    if (mine) *reinterpret_cast<float2*>(part + (size_t)rows * D + 2 * r) = make_float2(m_run, l_run);
+                    tc_fence_before();
+                }
+            }
+        }
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 0) {
         // ------------------------------------------------------------------ copies and the work list
+        // Half of the lanes keep the books of either stream.
+        const int s = lane >> 4, l16 = lane & 15;
         const int units = a.totals[1], tiles = a.totals[2];
-        const EqualRuns runs(2 * units + tiles, gridDim.x);
-        const Share share(runs, units, cta);
-        // the entry of cum[0 .. n] (not decreasing) that holds `at`: the last one that is not above it
-        auto find = [&](const int* cum, int n, int at) {
-            int lo = 0, hi = n;  // cum[lo] <= at < cum[hi]
-            while (hi - lo > 1) {
-                const int step = max(1, (hi - lo) / 32), probe = min(lo + step * (lane + 1), hi);
-                const unsigned above = __ballot_sync(0xffffffffu, probe >= hi || cum[probe] > at);
-                const int i = __ffs((int)above) - 1;  // (lane 31 may probe below hi)
-                if (i < 0) lo = lo + 32 * step;
-                else {
-                    const int l = lo;
-                    lo = l + step * i;
-                    hi = min(l + step * (i + 1), hi);
+        const Share share(EqualRuns(2 * units + tiles, gridDim.x), units, cta);
+        // the entry of cum[0 .. n] (not decreasing) that holds `at`, the last one that is not above it; in a half whose `wanted` is false: 0
+        auto find = [&](const int* cum, int n, int at, bool wanted) {
+            int lo = 0, hi = wanted ? n : 1;  // cum[lo] <= at < cum[hi]
+            while (__any_sync(0xffffffffu, hi - lo > 1)) {
+                const int step = max(1, (hi - lo) / 16), probe = min(lo + step * (l16 + 1), hi);
+                const bool past = probe >= hi || cum[probe] > at;
+                const unsigned above = (__ballot_sync(0xffffffffu, past) >> (16 * s)) & 0xffffu;
+                if (hi - lo > 1) {
+                    const int i = __ffs((int)above) - 1;  // (the last lane may probe below hi)
+                    if (i < 0) lo += 16 * step;
+                    else {
+                        hi = min(lo + step * (i + 1), hi);
+                        lo += step * i;
+                    }
                 }
             }
             return lo;
         };
-        // units of pairs
-        int wu = share.w0, pair = 0, w_head = 0, w_unit = 0, w_units = 1;
+        // units of pairs, the same for both streams
+        int wu = share.w0, w_head = 0, w_unit = 0, w_units = 1;
+        int pair = find(a.cum_pairs, a.totals[0], wu, wu < share.w1);
         int4 pair_info = make_int4(0, 0, 0, 0);
         if (wu < share.w1) {
-            pair = find(a.cum_pairs, a.totals[0], wu);
             const int c = a.cum_pairs[pair];
             w_units = (a.cum_pairs[pair + 1] - c) / a.n_kv;
             w_head = (wu - c) / w_units;
             w_unit = wu - c - w_head * w_units;
             pair_info = a.pairs[pair];
         }
-        // tiles of rows, of each stream
-        int su[2] = {share.s0, share.middle()}, s_end[2] = {share.middle(), share.s1}, m[2] = {0, 0}, s_head[2] = {0, 0}, s_tile[2] = {0, 0}, s_tiles[2] = {1, 1};
-        int4 row_info[2] = {};
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (su[s] < s_end[s]) {
-                m[s] = find(a.cum_rows, a.M, su[s]);
-                const int c = a.cum_rows[m[s]];
-                s_tiles[s] = (a.cum_rows[m[s] + 1] - c) / a.n_kv;
-                s_head[s] = (su[s] - c) / s_tiles[s];
-                s_tile[s] = su[s] - c - s_head[s] * s_tiles[s];
-                row_info[s] = a.rows[m[s]];
-            }
+        // tiles of rows
+        const int s_begin = s ? share.middle() : share.s0, s_end = s ? share.s1 : share.middle();
+        int su = s_begin, s_head = 0, s_tile = 0, s_tiles = 1, seq = 0;
+        int m = find(a.cum_rows, a.M, su, su < s_end);
+        int2 row = make_int2(0, 0);  // cache rows shared, length
+        auto enter_row = [&] {
+            s_tiles = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv;
+            const int4 info = a.rows[m];
+            row = make_int2(info.x, info.y);
+            seq = a.seq_ids ? a.seq_ids[m] : m;
+        };
+        if (su < s_end) {
+            enter_row();
+            const int at = su - a.cum_rows[m];
+            s_head = at / s_tiles;
+            s_tile = at - s_head * s_tiles;
+        }
         const int per_tile = kTile >> a.log2_rows;  // blocks
-        struct Tiles {  // of a step: lane l has block l of each stream's tile
-            int id[2], head[2];
-            bool there[2];
+        struct Tile {  // of a step and stream: lane i has block i
+            int id, head;
+            bool there;
         };
         int made = 0;  // code tiles so far
         // publishes step p; false at the end
-        auto publish = [&](int p, Tiles& now) {
+        auto publish = [&](int p, Tile& now) {
             const int slot = p % kDescs;
             if (p >= kDescs) wait(L::desc_empty + slot, (uint32_t)(p / kDescs - 1) & 1u);
             Desc& d = descs[slot];
-            const bool pairs_left = wu < share.w1;
-            const bool end = !pairs_left && su[0] >= s_end[0] && su[1] >= s_end[1];
-            const bool common = pairs_left && pair_info.y > kTile;
-            Side side[2] = {};
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                Side& x = side[s];
-                if (pairs_left) {
-                    const int tile = common ? w_unit : 2 * w_unit + s, rows = pair_info.w;
-                    const bool first = wu == share.w0 || w_unit == 0, last = wu == share.w1 - 1 || (tile + (common ? 1 : 2)) * kTile >= rows;
-                    x.flags = tile * kTile < rows ? kLive | (first ? kFirst : 0) | (last ? kLast : 0) : 0;
-                    x.row0 = pair_info.x + (common ? s * kTile : 0);
-                    x.rows = common ? (s ? pair_info.y - kTile : kTile) : pair_info.y;
-                    x.head = w_head;
-                    x.base = tile * kTile;
-                    x.cache_rows = min(rows - x.base, kTile);
-                    x.part = (pair * a.n_kv + w_head + cta) * 2 + s;
-                } else if (su[s] < s_end[s]) {
-                    const bool first = s_tile[s] == 0 || su[s] == (s ? share.middle() : share.s0), last = s_tile[s] == s_tiles[s] - 1 || su[s] == s_end[s] - 1;
-                    x.flags = kLive | kOwn | (first ? kFirst : 0) | (last ? kLast : 0);
-                    x.row0 = m[s] * a.group;
-                    x.rows = a.group;
-                    x.head = s_head[s];
-                    x.base = ((row_info[s].x >> a.log2_rows) << a.log2_rows) + s_tile[s] * kTile;
-                    x.cache_rows = min(row_info[s].y - x.base, kTile);
-                    x.part = m[s] * a.n_kv + s_head[s] + 2 * cta + s;
-                }
-                const bool live = x.flags & kLive;
-                // the blocks of the tile
-                const bool loads = live && !(common && s == 1);
-                int id = -1;
-                if (loads) {
-                    const int b = (x.base >> a.log2_rows) + lane;
-                    const int seq = pairs_left ? pair_info.z : a.seq_ids ? a.seq_ids[m[s]] : m[s];
-                    if (lane < per_tile && (lane << a.log2_rows) < x.cache_rows) id = a.tables[(size_t)seq * a.max_blocks + b];
-                    if (id >= a.n_blocks) id = -1;
-                }
-                now.id[s] = id;
-                now.head[s] = x.head;
-                now.there[s] = loads;
+            const bool pairs_left = wu < share.w1, row_left = !pairs_left && su < s_end;
+            const bool end = !__any_sync(0xffffffffu, pairs_left || row_left), common = pairs_left && pair_info.y > kTile;
+            Side x = {};
+            if (pairs_left) {
+                const int tile = common ? w_unit : 2 * w_unit + s, rows = pair_info.w;
+                const bool first = wu == share.w0 || w_unit == 0, last = wu == share.w1 - 1 || (tile + (common ? 1 : 2)) * kTile >= rows;
+                x.flags = tile * kTile < rows ? kLive | (first ? kFirst : 0) | (last ? kLast : 0) : 0;
+                x.row0 = pair_info.x + (common ? s * kTile : 0);
+                x.rows = common ? (s ? pair_info.y - kTile : kTile) : pair_info.y;
+                x.head = w_head;
+                x.base = tile * kTile;
+                x.cache_rows = min(rows - x.base, kTile);
+                x.part = (pair * a.n_kv + w_head + cta) * 2 + s;
+            } else if (row_left) {
+                x.flags = kLive | kOwn | (s_tile == 0 || su == s_begin ? kFirst : 0) | (s_tile == s_tiles - 1 || su == s_end - 1 ? kLast : 0);
+                x.row0 = m * a.group;
+                x.rows = a.group;
+                x.head = s_head;
+                x.base = ((row.x >> a.log2_rows) << a.log2_rows) + s_tile * kTile;
+                x.cache_rows = min(row.y - x.base, kTile);
+                x.part = m * a.n_kv + s_head + 2 * cta + s;
+                x.lower = row.x, x.upper = row.y;
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int from = common ? 0 : s;
-                int lost = 0;
-                if (side[s].flags & kLive) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int id = __shfl_sync(0xffffffffu, from ? now.id[1] : now.id[0], (16 * i) >> a.log2_rows);
-                        if (id < 0) lost |= 1 << i;
-                    }
-                }
-                side[s].lost = lost;
+            const bool live = x.flags & kLive;
+            now.there = live && !(common && s == 1);
+            now.head = x.head;
+            now.id = -1;
+            if (now.there && l16 < per_tile && (l16 << a.log2_rows) < x.cache_rows) {
+                const int id = a.tables[(size_t)(pairs_left ? pair_info.z : seq) * a.max_blocks + (x.base >> a.log2_rows) + l16];
+                now.id = id < a.n_blocks ? id : -1;
             }
-            // scales: lane 16 s + 8 v + i brings that of cache rows 16 i .. of stream s, of keys or values
+            const int from = common ? 0 : 16 * s;
+            const unsigned have = __ballot_sync(0xffffffffu, now.id >= 0) >> from;
+            if (live) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (!((have >> ((16 * i) >> a.log2_rows)) & 1u)) x.lost |= 1 << i;
+            }
+            // scales: the lower eight lanes of a half bring those of cache rows 16 i .. of the keys, the upper ones of the values
             {
-                const int s = lane >> 4, v = (lane >> 3) & 1, i = lane & 7;
-                const int id0 = __shfl_sync(0xffffffffu, now.id[0], (16 * i) >> a.log2_rows), id1 = __shfl_sync(0xffffffffu, now.id[1], (16 * i) >> a.log2_rows);
-                const int id = s && !common ? id1 : id0;
-                const int head = s && !common ? now.head[1] : now.head[0];
-                const uint32_t to = smem_u32(v ? &d.vs[s][i] : &d.ks[s][i]);
+                const int i = l16 & 7, id = __shfl_sync(0xffffffffu, now.id, from + ((16 * i) >> a.log2_rows));
+                float* to = &(l16 >> 3 ? d.vs : d.ks)[s][i];
                 if (id >= 0) {
-                    const float* src = (v ? a.v_scale : a.k_scale) + (size_t)id * a.n_kv + head;
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(src) : "memory");
+                    const float* src = (l16 >> 3 ? a.v_scale : a.k_scale) + (size_t)id * a.n_kv + x.head;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to)), "l"(src) : "memory");
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar(L::desc_full + slot)) : "memory");
                 } else {
-                    (v ? d.vs : d.ks)[s][i] = 0.0f;
+                    *to = 0.0f;
                     mbar_arrive(bar(L::desc_full + slot));
                 }
             }
-            if (lane == 0) {
-                d.side[0] = side[0];
-                d.side[1] = side[1];
-                d.end = end;
-                d.common = common;
-                mbar_arrive(bar(L::desc_full + slot));
-            }
+            if (l16 == 0) d.side[s] = x;
+            if (lane == 0) d.end = end, d.common = common;
             __syncwarp();
+            if (lane == 0) mbar_arrive(bar(L::desc_full + slot));
             // on to the next step
             if (pairs_left) {
                 ++wu;
@@ -569,45 +756,43 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                         pair_info = a.pairs[pair];
                     }
                 }
-            } else {
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-                    if (su[s] < s_end[s]) {
-                        ++su[s];
-                        if (++s_tile[s] == s_tiles[s] && su[s] < s_end[s]) {
-                            s_tile[s] = 0;
-                            if (++s_head[s] == a.n_kv) {
-                                s_head[s] = 0;
-                                do ++m[s];
-                                while (a.cum_rows[m[s] + 1] == a.cum_rows[m[s]]);
-                                s_tiles[s] = (a.cum_rows[m[s] + 1] - a.cum_rows[m[s]]) / a.n_kv;
-                                row_info[s] = a.rows[m[s]];
-                            }
-                        }
+            } else if (row_left) {
+                ++su;
+                if (++s_tile == s_tiles && su < s_end) {
+                    s_tile = 0;
+                    if (++s_head == a.n_kv) {
+                        s_head = 0;
+                        do ++m;
+                        while (a.cum_rows[m + 1] == a.cum_rows[m]);
+                        enter_row();
                     }
+                }
             }
+            __syncwarp();
             return !end;
         };
-        auto load = [&](const Tiles& now, int s, const CUtensorMap* map) {
-            if (!now.there[s]) return;
+        auto load = [&](const Tile& now, int which, const CUtensorMap* map) {
+            if (!__shfl_sync(0xffffffffu, (int)now.there, 16 * which)) return;
             const int place = made % L::kStages;
             if (made >= L::kStages) wait(L::code_empty + place, (uint32_t)(made / L::kStages - 1) & 1u);
             ++made;
-            const unsigned present = __ballot_sync(0xffffffffu, now.id[s] >= 0);
+            const bool mine = s == which && now.id >= 0;
+            const unsigned present = __ballot_sync(0xffffffffu, mine);
             const uint32_t full = bar(L::code_full + place), block_bytes = (uint32_t)D << a.log2_rows;
             if (lane == 0) mbar_expect_tx(full, (uint32_t)__popc(present) * block_bytes);
             __syncwarp();
-            if (now.id[s] >= 0)
-                code_rows(base_s + L::codes + (uint32_t)place * L::kCodeBytes + (uint32_t)lane * block_bytes, map, (now.id[s] * a.n_kv + now.head[s]) << a.log2_rows, full);
+            if (mine) code_rows(base_s + L::codes + (uint32_t)place * L::kCodeBytes + (uint32_t)l16 * block_bytes, map, (now.id * a.n_kv + now.head) << a.log2_rows, full);
         };
-        Tiles now = {{-1, -1}, {0, 0}, {false, false}}, next;
+        Tile now = {-1, 0, false}, next = now;
+        bool ended = false;
         for (int p = -1; !aborted(); ++p) {
-            load(now, 0, &map_v);
-            const bool more = publish(p + 1, next);
-            if (more) load(next, 0, &map_k);
-            load(now, 1, &map_v);
-            if (!more) break;
-            load(next, 1, &map_k);
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i) {  // values of step p, keys of the next, for either stream
+                load(now, i, &map_v);
+                if (i == 0 && !publish(p + 1, next)) next.there = false, ended = true;
+                load(next, i, &map_k);
+            }
+            if (ended) break;
             now = next;
         }
     } else if (warp <= 2) {
@@ -615,12 +800,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         // (What the instructions take is made the same for all lanes first: they want it in uniform registers.)
         const int s = __shfl_sync(0xffffffffu, warp - 1, 0);
         const uint32_t scores_at = __shfl_sync(0xffffffffu, tm_s(s), 0), sums_at = __shfl_sync(0xffffffffu, tm_o(s), 0);
-        const uint32_t s_full = __shfl_sync(0xffffffffu, bar(L::s_full + s), 0), o_full = __shfl_sync(0xffffffffu, bar(L::o_full + s), 0);
-        constexpr uint32_t kScores = instruction(kTile, false), kValues = instruction(D, true);
+        const uint32_t s_full = __shfl_sync(0xffffffffu, bar(L::s_full + 2 * s), 0), o_full = __shfl_sync(0xffffffffu, bar(L::o_full + s), 0);
+        const uint32_t q_free = __shfl_sync(0xffffffffu, bar(L::q_free + s), 0), pv_done = __shfl_sync(0xffffffffu, bar(L::pv_done + s), 0);
+        constexpr uint32_t kScores = instruction(kHalf, false), kValues = instruction(D, true);
         const uint64_t q_tile = operand(__shfl_sync(0xffffffffu, base_s + L::q + (uint32_t)s * L::kOperandBytes, 0), 16);
-        uint32_t q_phase = 0, p_phase = 0, turn_phase = s == 0 ? 1u : 0u;  // (the first turn is the first stream's)
-        int made = 0;                            // operand tiles so far, of both streams
-        int now = 0, other_now = 0;              // flags of step p, this stream's and the other's
+        uint32_t q_phase = 0, p_phase = 0;
+        int made = 0;                // operand tiles so far, of both streams
+        int now = 0, other_now = 0;  // flags of step p, this stream's and the other's
         bool common_now = false;
         auto filled = [&](int tile) { wait(L::op_full + tile % L::kOperands, (uint32_t)(tile / L::kOperands) & 1u); };
         // the other stream's tile: one is free when both warps have passed it
@@ -628,14 +814,14 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             filled(tile);
             if (lane == 0) mbar_arrive(bar(L::op_empty + tile % L::kOperands));
         };
-        // Step p's values, then the scores of the next, of this stream.  All that the second needs is looked up before the first's weights are waited for.
+        // Half by half, step p's values, then the scores of the next, of this stream.
         for (int p = -1; !aborted(); ++p) {
             const int slot = (p + 1) % kDescs;
             wait(L::desc_full + slot, (uint32_t)((p + 1) / kDescs) & 1u);
             const Desc& d = descs[slot];
             const bool more = !d.end, common = d.common;
             const int next = __shfl_sync(0xffffffffu, d.side[s].flags, 0), other = __shfl_sync(0xffffffffu, d.side[1 - s].flags, 0);
-            // tiles in the order of all products: values of the first stream, its next scores, the second's values, its next scores
+            // tiles in the order in which they are made: values of the first stream, its next keys, the second's values, its next keys
             const bool v0 = (s ? other_now : now) & kLive, k0 = (s ? other : next) & kLive, v1 = ((s ? now : other_now) & kLive) && !common_now, k1 = ((s ? next : other) & kLive) && !common;
             const int tile_v0 = made, tile_k0 = tile_v0 + v0, tile_v1 = tile_k0 + k0, tile_k1 = tile_v1 + v1;
             made = tile_k1 + k1;
@@ -646,48 +832,57 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             }
             const bool has_value = now & kLive, has_key = next & kLive;
             const uint32_t tiles_at = base_s + L::operands;
-            const uint32_t v_at = __shfl_sync(0xffffffffu, tiles_at + (uint32_t)(value % L::kOperands) * L::kOperandBytes, 0);
-            const uint32_t k_at = __shfl_sync(0xffffffffu, tiles_at + (uint32_t)(key % L::kOperands) * L::kOperandBytes, 0);
+            const uint64_t v_tile = operand(__shfl_sync(0xffffffffu, tiles_at + (uint32_t)(value % L::kOperands) * L::kOperandBytes, 0), kHalfTile);
+            const uint64_t k_tile = operand(__shfl_sync(0xffffffffu, tiles_at + (uint32_t)(key % L::kOperands) * L::kOperandBytes, 0), 16);
             const uint32_t v_done = __shfl_sync(0xffffffffu, bar(L::op_empty + value % L::kOperands), 0), k_done = __shfl_sync(0xffffffffu, bar(L::op_empty + key % L::kOperands), 0);
             const bool one = elect_one();
-            if (has_value) {
-                filled(value);
-                wait(L::p_full + s, p_phase);
-                p_phase ^= 1u;
-            }
-            const bool key_there = has_key && __all_sync(0xffffffffu, mbar_try_wait(bar(L::op_full + key % L::kOperands), (uint32_t)(key / L::kOperands) & 1u));
-            // The streams take turns at the tensor cores, so that one's softmax runs beside the other's products; without, both did the same at a time.
-            wait(L::turn + s, turn_phase);
-            turn_phase ^= 1u;
-            tc_fence_after();
-            if (has_value && one) {
-                const uint64_t v_tile = operand(v_at, kHalfTile);
+            if (has_value) filled(value);
+            // (A pair's queries come from softmax threads that first finish what is under way: then both halves' values go first.)
+            const bool late = has_key && (next & (kFirst | kOwn)) == kFirst;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                const int h = late ? i & 1 : i >> 1;
+                const bool values = late ? i < 2 : !(i & 1);
+                const uint32_t at = __shfl_sync(0xffffffffu, scores_at + kHalf * h, 0), rows = __shfl_sync(0xffffffffu, 512 * h, 0);  // (64 rows of 128 bytes, in sixteens)
+                const uint32_t full = __shfl_sync(0xffffffffu, s_full + 8 * h, 0);
+                if (values && has_value) {
+                    wait(L::p_full + 2 * s + h, p_phase);
+                    tc_fence_after();
+                    if (one) {
 #pragma unroll
-                for (int k = 0; k < kTile / 16; ++k) mma_ts(sums_at, scores_at + 8 * k, v_tile + 128u * k, kValues, !((now & kFirst) && k == 0));
-                if (now & kLast) tc_commit(o_full);
-                tc_commit(v_done);
-            }
-            if (has_key) {
-                if (!key_there) filled(key);
-                if (next & kFirst) {
-                    wait(L::q_full + s, q_phase);
-                    q_phase ^= 1u;
-                }
-                if (one) {
-                    const uint64_t k_tile = operand(k_at, 16);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
-                        mma_ss(scores_at, q_tile + off, k_tile + off, kScores, k > 0);
+                        for (int k = 0; k < kHalf / 16; ++k) mma_ts(sums_at, at + 8 * k, v_tile + rows + 128u * k, kValues, !((now & kFirst) && h == 0 && k == 0));
+                        tc_commit(pv_done);
+                        if (h == 1) {
+                            if (now & kLast) tc_commit(o_full);
+                            tc_commit(v_done);
+                        }
                     }
-                    tc_commit(s_full);
-                    tc_commit(k_done);
                 }
+                if (!values && has_key) {
+                    if (h == 0) {
+                        filled(key);
+                        if (next & kFirst) {
+                            wait(L::q_full + s, q_phase);
+                            q_phase ^= 1u;
+                        }
+                    }
+                    if (one) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = ((uint32_t)(k / 4) * kHalfTile + (uint32_t)(k % 4) * 32u) >> 4;
+                            mma_ss(at, q_tile + off, k_tile + rows + off, kScores, k > 0);
+                        }
+                        tc_commit(full);
+                        if (h == 1) {
+                            tc_commit(k_done);
+                            if (next & kLast) tc_commit(q_free);
+                        }
+                    }
+                }
+                __syncwarp();
             }
-            if (lane == 0) {
-                mbar_arrive(bar(L::turn + 1 - s));
-                if (p >= 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
-            }
+            if (has_value) p_phase ^= 1u;
+            if (p >= 0 && lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
             __syncwarp();
             if (!more) break;
             if (s == 0) {
@@ -696,9 +891,47 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             }
             now = next, other_now = other, common_now = common;
         }
+    } else if (warp == 3) {
+        // ------------------------------------------------------------------ queries of rows' own tiles
+        uint32_t items[2] = {0u, 0u};
+        for (int p = 0; !aborted(); ++p) {
+            const int slot = p % kDescs;
+            wait(L::desc_full + slot, (uint32_t)(p / kDescs) & 1u);
+            const Desc& d = descs[slot];
+            if (d.end) break;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const Side& x = d.side[s];
+                if ((x.flags & (kLive | kFirst)) != (kLive | kFirst)) continue;
+                const uint32_t item = items[s]++;
+                if (item > 0) wait(L::q_free + s, (item - 1u) & 1u);  // the scores of the item in front are made
+                if (!(x.flags & kOwn)) continue;                      // (a pair's: its 128 rows' softmax threads bring one each)
+                const int r = lane >> 2, c = lane & 3;  // four lanes to a row, eight rows at most
+                uint4 v[D / 32];
+                uint32_t most = 0u;
+                if (r < x.rows) {
+                    const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)x.row0 + (size_t)(x.row0 / a.group) * (a.n_q - a.group) + (size_t)x.head * a.group + r) * D) + c * (D / 32);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) v[i] = __ldg(src + i), most = max(most, largest_bits(v[i]));
+                }
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+                if (r < x.rows) {
+                    const float up = query_up(most);
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) store_queries(base_s + L::q + (uint32_t)s * L::kOperandBytes, r, c * (D / 32) + i, v[i], up);
+                    if (c == 0) smem[L::exponents + (s * 2 + (item & 1u)) * kTile + r] = (uint8_t)query_exponent(most);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane < 4) mbar_arrive(bar(L::q_full + s));
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
+        }
     } else if (warp >= 12) {
         // ------------------------------------------------------------------ codes -> f16
-        const int t = tid - 12 * 32;
+        const int t = tid & 127, mine = (warp - 12) >> 2;  // of every two tiles, the first four warps take one, the others the next
         // A thread takes sixteen codes of every 16th (32nd) row, always of the same columns.  Eight neighbouring lanes read eight different sixteen-byte columns
         // of the banks and write eight: four pieces of a row, the other four of its neighbour (which the swizzle moves by one sixteen-byte unit).
         const int chunk = t % (D / 16), row = D == 128 ? (t / 8) ^ (chunk >> 2) : t / 4;
@@ -709,6 +942,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             const Desc& d = descs[p % kDescs];
             const Side& x = d.side[s];
             if (!(x.flags & kLive) || (d.common && s == 1)) return;
+            if ((made & 1) != mine) {
+                ++made;
+                return;
+            }
             const int from = made % L::kStages, to = made % L::kOperands;
             wait(L::code_full + from, (uint32_t)(made / L::kStages) & 1u);
             if (made >= L::kOperands) wait(L::op_empty + to, (uint32_t)(made / L::kOperands - 1) & 1u);
@@ -762,217 +999,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             if (p >= 0 && lane == 0) mbar_arrive(bar(L::desc_empty + p % kDescs));
             if (!more) break;
         }
-    } else if (warp >= 4) {
-        // ------------------------------------------------------------------ softmax
-        const int s = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
-        const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
-        const uint32_t ts = tm_s(s) + lane_at, to = tm_o(s) + lane_at;
-        float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
-        int lower = 0, upper = 0;
-        uint32_t s_phase = 0, o_phase = 0;
-        for (int p = 0; !aborted(); ++p) {
-            const int slot = p % kDescs;
-            wait(L::desc_full + slot, (uint32_t)(p / kDescs) & 1u);
-            const Desc& d = descs[slot];
-            if (d.end) break;
-            const Side x = d.side[s];
-            if (!(x.flags & kLive)) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
-                continue;
-            }
-            const bool mine = r < x.rows, any = quad * 32 < x.rows;
-            if (x.flags & kFirst) {
-                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
-                if (mine) {
-                    const int flat = x.row0 + r, m = flat / a.group, j = flat - m * a.group;
-                    const int4 info = a.rows[m];
-                    lower = x.flags & kOwn ? info.x : 0;
-                    upper = x.flags & kOwn ? info.y : info.x;
-                    const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D);
-                    uint4 v[D / 8];
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) v[i] = __ldg(src + i);
-                    uint32_t most = 0u;  // the largest magnitude by its bits: infinity and NaN are above all others
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) most = max(most, max((u[e] << 16) & 0x7fffffffu, u[e] & 0x7fff0000u));
-                    }
-                    // the power of two that brings the largest magnitude to 2^8 .. 2^9: bf16 values then fit f16 without loss down to 2^-22 of it
-                    const int be = max((int)(most >> 23), 9);
-                    const float up = __int_as_float((262 - be) << 23), down = __int_as_float((be - 8) << 23);
-                    const uint32_t line = base_s + L::q + (uint32_t)s * L::kOperandBytes + (uint32_t)r * 128u;
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                        uint32_t h[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * up, __uint_as_float(u[e] & 0xffff0000u) * up);
-                        sts128(line + (uint32_t)(i >> 3) * kHalfTile + (uint32_t)(((i & 7) ^ (r & 7)) << 4), h[0], h[1], h[2], h[3]);
-                    }
-                    f = most >= 0x7f800000u ? NAN : down * a.scale_log2;  // a row that is not finite gives NaN
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(L::q_full + s));
-            }
-            // what this row uses of the tile
-            const int lo = max(lower - x.base, 0), hi = min(upper - x.base, kTile);
-            const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && x.lost == 0));
-            auto used = [&](int c) {  // of columns 32 c .. 32 c + 31
-                const int l = max(lo - 32 * c, 0), h = min(max(hi - 32 * c, 0), 32);
-                uint32_t w = h > l ? (uint32_t)((1ull << h) - (1ull << l)) : 0u;
-                if ((x.lost >> (2 * c)) & 1) w &= 0xffff0000u;
-                if ((x.lost >> (2 * c + 1)) & 1) w &= 0x0000ffffu;
-                return w;
-            };
-            float vs = 0.0f;  // the largest scale of values that the row uses
-            if (all_used) {
-                const float4 w0 = *reinterpret_cast<const float4*>(&d.vs[s][0]), w1 = *reinterpret_cast<const float4*>(&d.vs[s][4]);
-                vs = fmaxf(fmaxf(fmaxf(w0.x, w0.y), fmaxf(w0.z, w0.w)), fmaxf(fmaxf(w1.x, w1.y), fmaxf(w1.z, fmaxf(w1.w, 0.0f))));
-            }
-            wait(L::s_full + s, s_phase);
-            s_phase ^= 1u;
-            tc_fence_after();
-            if (any) {
-                // The loops over columns stay loops: with all of them unrolled, the roles' code did not fit the instruction caches, and a warp waited for
-                // instructions longer than for anything else (444 us for 2173 rows of two chunks, 0.3 instructions a cycle).
-                float top = -INFINITY;  // the largest score
-                if (all_used) {
-#pragma unroll 1
-                    for (int c = 0; c < 4; c += 2) {
-                        uint32_t v[2][32];
-                        tm_load(ts + 32 * c, v[0]);
-                        tm_load(ts + 32 * c + 32, v[1]);
-                        const float4 k = *reinterpret_cast<const float4*>(&d.ks[s][2 * c]);
-                        tm_load_wait();
-                        float t[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) t[i] = __uint_as_float(v[i >> 1][16 * (i & 1)]);
-#pragma unroll
-                        for (int e = 1; e < 16; ++e)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) t[i] = fmaxf(t[i], __uint_as_float(v[i >> 1][16 * (i & 1) + e]));
-                        top = fmaxf(top, fmaxf(fmaxf(t[0] * (k.x * f), t[1] * (k.y * f)), fmaxf(t[2] * (k.z * f), t[3] * (k.w * f))));
-                    }
-                } else {
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32];
-                        tm_load(ts + 32 * c, v);
-                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), w = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
-                        const uint32_t live = used(c);
-                        tm_load_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if ((live >> e) & 1u) top = fmaxf(top, __uint_as_float(v[e]) * ((e < 16 ? k.x : k.y) * f));
-                        if (live & 0x0000ffffu) vs = fmaxf(vs, w.x);
-                        if (live & 0xffff0000u) vs = fmaxf(vs, w.y);
-                    }
-                }
-                // The maximum is followed only where it grows by more than 2^8: weights stay within f16, and the accumulator is rarely scaled.
-                const bool grows = top > m_run + 8.0f || (m_run == -INFINITY && top > -INFINITY), wider = vs > v_ref;
-                if (__any_sync(0xffffffffu, grows || wider)) {
-                    const float n = grows ? top : m_run, nv = fmaxf(v_ref, vs);
-                    const float c = m_run == -INFINITY ? 0.0f : ex2(m_run - n);  // (nothing there yet: zeros)
-                    const float fo = nv > 0.0f ? c * (v_ref / nv) : c;
-                    l_run *= c;
-                    if (!(x.flags & kFirst)) {
-#pragma unroll 1
-                        for (int i = 0; i < D / 32; ++i) {
-                            uint32_t v[32];
-                            tm_load(to + 32 * i, v);
-                            tm_load_wait();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fo);
-                            tm_store32(to + 32 * i, v);
-                        }
-                    }
-                    m_run = n;
-                    v_ref = nv;
-                }
-                const float b = m_run == -INFINITY ? 0.0f : m_run;
-                const float per_ref = v_ref > 0.0f ? __fdividef(kWeightScale, v_ref) : 0.0f;
-                // Weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost; their sum takes them unrounded.
-                // They go over scores that have been read.
-                if (all_used) {
-                    float2 sum = make_float2(0.0f, 0.0f);
-                    const float2 bb = splat(-b);
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32], w[16];
-                        tm_load(ts + 32 * c, v);
-                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), r2 = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
-                        tm_load_wait();
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float2 kk = splat((i ? k.y : k.x) * f), ww = splat((i ? r2.y : r2.x) * per_ref);
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                float2 t = fma2(make_float2(__uint_as_float(v[16 * i + e]), __uint_as_float(v[16 * i + e + 1])), kk, bb);
-                                t.x = ex2(t.x), t.y = ex2(t.y);
-                                sum = add2(sum, t);
-                                t = mul2(t, ww);
-                                w[8 * i + e / 2] = pack_f16(t.x, t.y);
-                            }
-                        }
-                        tm_store16(ts + 16 * c, w);
-                    }
-                    l_run += sum.x + sum.y;
-                } else {
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32], w[16];
-                        tm_load(ts + 32 * c, v);
-                        const float2 k = *reinterpret_cast<const float2*>(&d.ks[s][2 * c]), r2 = *reinterpret_cast<const float2*>(&d.vs[s][2 * c]);
-                        const uint32_t live = used(c);
-                        tm_load_wait();
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float kk = (e < 16 ? k.x : k.y) * f, ww = (e < 16 ? r2.x : r2.y) * per_ref;
-                            const float p0 = (live >> e) & 1u ? ex2(fmaf(__uint_as_float(v[e]), kk, -b)) : 0.0f;
-                            const float p1 = (live >> (e + 1)) & 1u ? ex2(fmaf(__uint_as_float(v[e + 1]), kk, -b)) : 0.0f;
-                            l_run += p0 + p1;
-                            w[e / 2] = pack_f16((live >> e) & 1u ? p0 * ww : 0.0f, (live >> (e + 1)) & 1u ? p1 * ww : 0.0f);
-                        }
-                        tm_store16(ts + 16 * c, w);
-                    }
-                }
-                tm_store_wait();
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(bar(L::p_full + s));
-                mbar_arrive(bar(L::desc_empty + slot));
-            }
-            if (x.flags & kLast) {
-                wait(L::o_full + s, o_phase);
-                o_phase ^= 1u;
-                tc_fence_after();
-                if (any) {
-                    const int rows = x.flags & kOwn ? a.group : kTile;
-                    float* part = (x.flags & kOwn ? a.parts_s : a.parts_w) + (size_t)x.part * part_floats(rows, D);
-                    const float unscale = v_ref * (1.0f / kWeightScale);
-#pragma unroll 1
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t v[32];
-                        tm_load(to + 32 * i, v);
-                        tm_load_wait();
-                        if (mine)
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<float4*>(part + (size_t)r * D + 32 * i + e) =
-                                    make_float4(__uint_as_float(v[e]) * unscale, __uint_as_float(v[e + 1]) * unscale, __uint_as_float(v[e + 2]) * unscale,
-                                                __uint_as_float(v[e + 3]) * unscale);
-                    }
-                    if (mine) *reinterpret_cast<float2*>(part + (size_t)rows * D + 2 * r) = make_float2(m_run, l_run);
-                    tc_fence_before();
-                }
-            }
-        }
+    }
     }
     tc_fence_before();
     __syncthreads();
@@ -1176,6 +1203,10 @@ int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const Shar
         std::lock_guard<std::mutex> lock(mu);
         if (!done[dev]) {
             if (cudaFuncSetAttribute(shared_attention_kernel<D, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes) != cudaSuccess) return finish(cudaErrorUnknown);
+            // the warps' register split waits for ever unless the launch brings all of it
+            cudaFuncAttributes attr;
+            if (cudaFuncGetAttributes(&attr, shared_attention_kernel<D, KIND>) != cudaSuccess || attr.numRegs * kThreads < 256 * kSoftmaxRegs + (kThreads - 256) * kOtherRegs)
+                return finish(cudaErrorUnknown);
             done[dev] = true;
         }
     }
