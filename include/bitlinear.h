@@ -620,7 +620,7 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
  *   Definition, types, limits, status word and what becomes of rows without a length as for bitlinear_attention_decode_kv8, with these exceptions:
  *   queries are scaled by a power of two per head and enter the tensor cores as f16, exactly down to 2^-22 of the head's largest magnitude, and products
  *   are summed in fp32 over either kind of pool; scales must not be negative; a NaN among the e4m3 codes of a value that one row of a group uses may show in the others.
- *   M * n_kv * (max_blocks * block_rows / 128 + 3) < 2^30, n_groups <= 65535.  ws (device, 16-byte aligned) at least
+ *   M * n_kv * (max_blocks * block_rows / 128 + 4) < 2^30, M * n_q < 2^30, n_groups <= 65535.  ws (device, 16-byte aligned) at least
  *   bitlinear_attention_shared_kv8_workspace_bytes(...) bytes (0 for unsupported sizes; it grows with M and n_groups); contents need not survive, calls that share one must not overlap.
  *   Three launches.
  */

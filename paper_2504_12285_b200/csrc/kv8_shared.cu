@@ -45,7 +45,7 @@ constexpr float kWeightScale = 128.0f;  // weights of up to 2^8 (the maximum is 
 
 // Workspace.  A part: fp32 values of its query rows, then (max, sum) of each.
 struct SharedLayout {
-    size_t rows, pairs, cum_pairs, cum_rows, starts, firsts, pair_rows, totals, parts_w, parts_s, total;
+    size_t rows, pairs, cum_pairs, cum_rows, starts, firsts, pair_rows, item_ctas, totals, parts_w, parts_s, total;
     int max_pairs;
 };
 struct SharedArgs {
@@ -63,10 +63,11 @@ struct SharedArgs {
     int4* rows;       // of each row: cache rows it shares, its length, its group's first pair (-1: none), that group's first query row
     int4* pairs;      // of each pair of query tiles: its first query row, query rows, sequence, cache rows
     int* cum_pairs;   // units of the pairs in front, all heads
-    int* cum_rows;    // tiles of the rows' own parts in front, all heads
+    int* cum_rows;    // tiles of the rows' own parts in front, and a place for each part's start, all heads
     int* starts;      // group_starts, in range and not decreasing
     int* firsts;      // of each group: its first row with something in the cache
     int* pair_rows;   // of each pair: cache rows
+    int4* item_ctas;  // of each pair and head: its first unit, the first and last CTA that have some of it
     int* totals;      // pairs, units of pairs, tiles of rows
     float* parts_w;
     float* parts_s;
@@ -141,7 +142,7 @@ __device__ __forceinline__ int block_max_scan(int x, int* warp_sums) {  // inclu
 }
 
 // One CTA: which rows share what, the pairs of query tiles, and how many units lie in front of each pair and row.
-__global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedArgs a) {
+__global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedArgs a, int ctas) {
     __shared__ int warp_sums[32];
     __shared__ int few[3][kFewGroups + 1];
     __shared__ int few_pairs[kFewGroups];
@@ -215,6 +216,7 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
             }
             a.rows[m] = info;
             if (len > info.x) tiles = (len - ((info.x >> a.log2_rows) << a.log2_rows) + kTile - 1) / kTile * a.n_kv;
+            if (tiles > 0) tiles += a.n_kv;  // a place for each head's start
         }
         int total;
         const int at = tiles_before + block_exclusive_scan(tiles, warp_sums, total);
@@ -244,6 +246,12 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
         a.cum_pairs[n_pairs] = units_before;
         a.cum_rows[a.M] = tiles_before;
         a.totals[0] = n_pairs, a.totals[1] = units_before, a.totals[2] = tiles_before;
+    }
+    __syncthreads();
+    const EqualRuns runs(2 * units_before + tiles_before, ctas);
+    for (int i = tid; i < n_pairs * a.n_kv; i += kPlanThreads) {
+        const int p = i / a.n_kv, h = i - p * a.n_kv, c = a.cum_pairs[p], n = (a.cum_pairs[p + 1] - c) / a.n_kv, u0 = c + h * n;
+        a.item_ctas[i] = make_int4(u0, runs.owner(2 * u0), runs.owner(2 * (u0 + max(n, 1) - 1)), 0);
     }
 }
 
@@ -459,43 +467,91 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
         int lower = 0, upper = 0;
         uint32_t s_phase = 0, o_phase = 0, item = 0, halves = 0;  // items, half steps so far
+        // A finished item's accumulator is read after the next item's queries are on their way.
+        bool finished = false;
+        float* part = nullptr;
+        int part_rows = 0;
+        bool in_part = false, any_in_part = false;
+        auto hand_over = [&] {
+            finished = false;
+            wait(L::o_full + s, o_phase);
+            o_phase ^= 1u;
+            tc_fence_after();
+            if (any_in_part) {
+                const float unscale = v_ref * (1.0f / kWeightScale);
+#pragma unroll 1
+                for (int i = 0; i < D / 16; ++i) {
+                    uint32_t o[16];
+                    tm_load16(to + 16 * i, o);
+                    tm_load_wait();
+                    if (in_part) {
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4)  // (four dims of all rows lie together, so that a warp writes whole lines)
+                            *reinterpret_cast<float4*>(part + (size_t)((4 * i + e / 4) * part_rows + r) * 4) =
+                                make_float4(__uint_as_float(o[e]) * unscale, __uint_as_float(o[e + 1]) * unscale, __uint_as_float(o[e + 2]) * unscale,
+                                            __uint_as_float(o[e + 3]) * unscale);
+                    }
+                }
+                if (in_part) *reinterpret_cast<float2*>(part + (size_t)part_rows * D + 2 * r) = make_float2(m_run, l_run);
+            }
+            tc_fence_before();
+        };
         for (int p = 0; !aborted(); ++p) {
             const int slot = p % kDescs;
             wait(L::desc_full + slot, (uint32_t)(p / kDescs) & 1u);
             const Desc& d = descs[slot];
-            if (d.end) break;
+            if (d.end) {
+                if (finished) hand_over();
+                break;
+            }
             const Side& x = d.side[s];
             const int flags = x.flags;
             if (!(flags & kLive)) {
+                if (finished) hand_over();
                 if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
                 continue;
             }
             const int n_rows = x.rows, part_at = x.part, base = x.base, lost = x.lost;
             const bool mine = r < n_rows, any = quad * 32 < n_rows;
             if (flags & kFirst) {
-                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
                 if (flags & kOwn) {
                     lower = x.lower, upper = x.upper;
                 } else {
-                    if (mine) {
-                        const int flat = x.row0 + r, m = flat / a.group, j = flat - m * a.group;
-                        lower = 0, upper = a.rows[m].x;
-                        const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D);
-                        uint4 v[D / 8];
-                        uint32_t most = 0u;
+                    // sixteen (eight) lanes bring a row together, eight loads in flight (a row to each lane took the L1 cache 32 lines a load: 8,000 cycles for a tile)
+                    constexpr int LANES = D / 8, AT_ONCE = 32 / LANES;
+                    const int unit = lane % LANES;
+                    uint8_t* exponents = smem + L::exponents + (s * 2 + (item & 1u)) * kTile;
+                    if (any) {
+#pragma unroll 1
+                        for (int i0 = 0; i0 < LANES; i0 += 8) {
+                            uint4 v[8];
 #pragma unroll
-                        for (int i = 0; i < D / 8; ++i) v[i] = __ldg(src + i);
+                            for (int i = 0; i < 8; ++i) {
+                                const int row = quad * 32 + (i0 + i) * AT_ONCE + lane / LANES, flat = x.row0 + min(row, n_rows - 1), m = flat / a.group, j = flat - m * a.group;
+                                v[i] = __ldg(reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D) + unit);
+                            }
 #pragma unroll
-                        for (int i = 0; i < D / 8; ++i) most = max(most, largest_bits(v[i]));
-                        const float up = query_up(most);
+                            for (int i = 0; i < 8; ++i) {
+                                const int row = quad * 32 + (i0 + i) * AT_ONCE + lane / LANES;
+                                uint32_t most = largest_bits(v[i]);
 #pragma unroll
-                        for (int i = 0; i < D / 8; ++i) store_queries(base_s + L::q + (uint32_t)s * L::kOperandBytes, r, i, v[i], up);
-                        f = query_down(query_exponent(most)) * a.scale_log2;
+                                for (int off = LANES / 2; off > 0; off >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, off));
+                                store_queries(base_s + L::q + (uint32_t)s * L::kOperandBytes, row, unit, v[i], query_up(most));
+                                if (unit == 0) exponents[row] = (uint8_t)query_exponent(most);
+                            }
+                        }
+                        __syncwarp();
+                        if (mine) {
+                            lower = 0, upper = a.rows[(x.row0 + r) / a.group].x;
+                            f = query_down(exponents[r]) * a.scale_log2;
+                        }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(L::q_full + s));
                 }
+                if (finished) hand_over();
+                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
             }
             // what this row uses of the tile
             const int lo = max(lower - base, 0), hi = min(upper - base, kTile);
@@ -537,10 +593,11 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     float top = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float t = __uint_as_float(v[i >> 1][16 * (i & 1)]);
+                        const uint32_t* x16 = v[i >> 1] + 16 * (i & 1);
+                        float t = __uint_as_float(x16[15]);
 #pragma unroll
-                        for (int e = 1; e < 16; ++e) t = fmaxf(t, __uint_as_float(v[i >> 1][16 * (i & 1) + e]));
-                        top = fmaxf(top, t * ks[i]);
+                        for (int e = 0; e < 14; e += 2) t = fmaxf(fmaxf(t, __uint_as_float(x16[e])), __uint_as_float(x16[e + 1]));
+                        top = fmaxf(top, fmaxf(t, __uint_as_float(x16[14])) * ks[i]);
                     }
                     const float vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
                     // The maximum is followed only where it grows by more than 2^8: weights stay within f16, and the accumulator is rarely scaled.
@@ -598,29 +655,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             s_phase ^= 1u;
             if (lane == 0) mbar_arrive(bar(L::desc_empty + slot));
             if (flags & kLast) {
-                wait(L::o_full + s, o_phase);
-                o_phase ^= 1u;
-                tc_fence_after();
                 ++item;
-                if (any) {
-                    const int rows = flags & kOwn ? a.group : kTile;
-                    float* part = (flags & kOwn ? a.parts_s : a.parts_w) + (size_t)part_at * part_floats(rows, D);
-                    const float unscale = v_ref * (1.0f / kWeightScale);
-#pragma unroll 1
-                    for (int i = 0; i < D / 32; ++i) {
-                        uint32_t v[32];
-                        tm_load(to + 32 * i, v);
-                        tm_load_wait();
-                        if (mine)
-#pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<float4*>(part + (size_t)r * D + 32 * i + e) =
-                                    make_float4(__uint_as_float(v[e]) * unscale, __uint_as_float(v[e + 1]) * unscale, __uint_as_float(v[e + 2]) * unscale,
-                                                __uint_as_float(v[e + 3]) * unscale);
-                    }
-                    if (mine) *reinterpret_cast<float2*>(part + (size_t)rows * D + 2 * r) = make_float2(m_run, l_run);
-                    tc_fence_before();
-                }
+                finished = true, in_part = mine, any_in_part = any;
+                part_rows = flags & kOwn ? a.group : kTile;
+                part = (flags & kOwn ? a.parts_s : a.parts_w) + (size_t)part_at * part_floats(part_rows, D);
             }
         }
     } else {
@@ -663,10 +701,11 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         // tiles of rows
         const int s_begin = s ? share.middle() : share.s0, s_end = s ? share.s1 : share.middle();
         int su = s_begin, s_head = 0, s_tile = 0, s_tiles = 1, seq = 0;
+        bool fresh = true;  // the next tile is its item's first of this run
         int m = find(a.cum_rows, a.M, su, su < s_end);
         int2 row = make_int2(0, 0);  // cache rows shared, length
         auto enter_row = [&] {
-            s_tiles = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv;
+            s_tiles = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv - 1;
             const int4 info = a.rows[m];
             row = make_int2(info.x, info.y);
             seq = a.seq_ids ? a.seq_ids[m] : m;
@@ -674,8 +713,9 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         if (su < s_end) {
             enter_row();
             const int at = su - a.cum_rows[m];
-            s_head = at / s_tiles;
-            s_tile = at - s_head * s_tiles;
+            s_head = at / (s_tiles + 1);
+            s_tile = at - s_head * (s_tiles + 1) - 1;
+            if (s_tile < 0) s_tile = 0, ++su;  // the place that stands for the start
         }
         const int per_tile = kTile >> a.log2_rows;  // blocks
         struct Tile {  // of a step and stream: lane i has block i
@@ -702,7 +742,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 x.cache_rows = min(rows - x.base, kTile);
                 x.part = (pair * a.n_kv + w_head + cta) * 2 + s;
             } else if (row_left) {
-                x.flags = kLive | kOwn | (s_tile == 0 || su == s_begin ? kFirst : 0) | (s_tile == s_tiles - 1 || su == s_end - 1 ? kLast : 0);
+                x.flags = kLive | kOwn | (fresh ? kFirst : 0) | (s_tile == s_tiles - 1 || su == s_end - 1 ? kLast : 0);
+                fresh = false;
                 x.row0 = m * a.group;
                 x.rows = a.group;
                 x.head = s_head;
@@ -758,8 +799,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 }
             } else if (row_left) {
                 ++su;
-                if (++s_tile == s_tiles && su < s_end) {
-                    s_tile = 0;
+                if (++s_tile == s_tiles && ++su < s_end) {
+                    s_tile = 0, fresh = true;
                     if (++s_head == a.n_kv) {
                         s_head = 0;
                         do ++m;
@@ -1017,10 +1058,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 // ---------------------------------------------------------------------------------------------- the parts of a row
 
 // A query head's parts, by WARPS warps: warp w takes parts w, w + WARPS, ... of each of the two kinds.  Lane l first finds the l-th of a round's parts and weighs it;
-// then all lanes add up the rounds' values, a few dims each, eight parts' loads in flight.
+// then all lanes add up the rounds' values, a few dims each, four or eight parts' loads in flight.
 template <int D, int WARPS>
-__global__ void __launch_bounds__(128) shared_combine_kernel(const SharedArgs a, int ctas) {
-    constexpr int DIMS = D / 32;
+__global__ void __launch_bounds__(128, WARPS == 1 ? 12 : 6) shared_combine_kernel(const SharedArgs a, int ctas) {
+    constexpr int DIMS = D / 32, AT_ONCE = WARPS == 1 ? 4 : 8;  // (many heads: latency is hidden by more warps, not by more loads)
     __shared__ float2 joined[4];
     __shared__ float values[4][D];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -1032,15 +1073,15 @@ __global__ void __launch_bounds__(128) shared_combine_kernel(const SharedArgs a,
     const EqualRuns runs(2 * units + tiles, ctas);
     const int4 row = there ? a.rows[m] : make_int4(0, 0, -1, 0);
     float top = -INFINITY, l = 0.0f, acc[DIMS] = {};
-    // parts first .. last (a lane finds its own by `find`: nullptr where it is none; its query rows, and which of them)
-    auto gather = [&](int n, auto find) {
+    // n parts of n_rows query rows (a lane finds its own by `find`: nullptr where it is none; which of the rows)
+    auto gather = [&](int n, int n_rows, auto find) {
         for (int i0 = 32 * w; i0 < n; i0 += 32 * WARPS) {
             const float* part = nullptr;
-            int rows = 0, r = 0;
-            if (i0 + lane < n) part = find(i0 + lane, rows, r);
+            int r = 0;
+            if (i0 + lane < n) part = find(i0 + lane, r);
             float2 ml = make_float2(-INFINITY, 0.0f);
-            if (part) ml = *reinterpret_cast<const float2*>(part + (size_t)rows * D + 2 * r);
-            const float* mine = part ? part + (size_t)r * D : nullptr;
+            if (part) ml = *reinterpret_cast<const float2*>(part + (size_t)n_rows * D + 2 * r);
+            const float* mine = part ? part + 4 * r : nullptr;
             float most = ml.x;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
@@ -1056,15 +1097,15 @@ __global__ void __launch_bounds__(128) shared_combine_kernel(const SharedArgs a,
             for (int e = 0; e < DIMS; ++e) acc[e] *= f0;
             unsigned have = __ballot_sync(0xffffffffu, mine != nullptr && !(f == 0.0f));
             while (have) {
-                float v[8][DIMS], g[8];
+                float v[AT_ONCE][DIMS], g[AT_ONCE];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < AT_ONCE; ++k) {
                     const int src = have ? __ffs((int)have) - 1 : 0;
                     const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)mine, src));
                     g[k] = have ? __shfl_sync(0xffffffffu, f, src) : 0.0f;
                     if (have) {
-                        if constexpr (DIMS == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(p + 4 * lane);
-                        else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(p + 2 * lane);
+                        if constexpr (DIMS == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(p + (size_t)(4 * lane) * n_rows);
+                        else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(p + (size_t)(4 * (lane >> 1)) * n_rows + 2 * (lane & 1));
                     } else {
 #pragma unroll
                         for (int e = 0; e < DIMS; ++e) v[k][e] = 0.0f;
@@ -1072,7 +1113,7 @@ __global__ void __launch_bounds__(128) shared_combine_kernel(const SharedArgs a,
                     have &= have - 1;
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < AT_ONCE; ++k)
 #pragma unroll
                     for (int e = 0; e < DIMS; ++e) acc[e] = fmaf(v[k][e], g[k], acc[e]);
             }
@@ -1082,27 +1123,29 @@ __global__ void __launch_bounds__(128) shared_combine_kernel(const SharedArgs a,
         const int in_group = m * a.group + j - row.w, pair = row.z + in_group / (2 * kTile), r0 = in_group % (2 * kTile);
         const int4 info = a.pairs[pair];
         const bool two = info.y > kTile;
-        const int n = (a.cum_pairs[pair + 1] - a.cum_pairs[pair]) / a.n_kv, u0 = a.cum_pairs[pair] + h * n;
-        const int c0 = runs.owner(2 * u0), c1 = runs.owner(2 * (u0 + n - 1));
-        gather((c1 - c0 + 1) * (two ? 1 : 2), [&](int i, int& rows, int& r) -> const float* {
+        const int4 where = a.item_ctas[pair * a.n_kv + h];  // its first unit, the first and last CTA that have some of it
+        const int u0 = where.x, c0 = where.y, c1 = where.z;
+        gather((c1 - c0 + 1) * (two ? 1 : 2), kTile, [&](int i, int& r) -> const float* {
             const int c = c0 + (two ? i : i >> 1), s = two ? r0 / kTile : i & 1;
-            rows = kTile, r = r0 % kTile;
-            const Share share(runs, units, c);
-            if (share.w0 >= share.w1) return nullptr;                                                      // (a CTA with one place may have the second half of a unit's)
-            if (!two && s == 1 && (2 * max(share.w0 - u0, 0) + 1) * kTile >= info.w) return nullptr;  // the second stream had no tile
+            r = r0 % kTile;
+            if (!two || runs.each < 2) {
+                const Share share(runs, units, c);
+                if (share.w0 >= share.w1) return nullptr;                                                      // (a CTA with one place may have the second half of a unit's)
+                if (!two && s == 1 && (2 * max(share.w0 - u0, 0) + 1) * kTile >= info.w) return nullptr;  // the second stream had no tile
+            }
             return a.parts_w + ((size_t)(pair * a.n_kv + h + c) * 2 + s) * part_floats(kTile, D);
         });
     }
     if (row.y > row.x) {
-        const int n = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv, t0 = a.cum_rows[m] + h * n;
+        const int n = (a.cum_rows[m + 1] - a.cum_rows[m]) / a.n_kv - 1, t0 = a.cum_rows[m] + h * (n + 1) + 1;
         auto worker = [&](int t) {
             const int c = runs.owner(2 * units + t);
             return 2 * c + (t >= Share(runs, units, c).middle() ? 1 : 0);
         };
         const int first = worker(t0), last = worker(t0 + n - 1);
-        gather(last - first + 1, [&](int i, int& rows, int& r) -> const float* {
+        gather(last - first + 1, a.group, [&](int i, int& r) -> const float* {
             const int k = first + i;
-            rows = a.group, r = j;
+            r = j;
             const Share share(runs, units, k >> 1);
             if (((k & 1) ? share.s1 - share.middle() : share.middle() - share.s0) <= 0) return nullptr;  // (the second stream of a CTA with one tile)
             return a.parts_s + (size_t)(m * a.n_kv + h + k) * part_floats(a.group, D);
@@ -1162,6 +1205,7 @@ SharedLayout shared_layout(int M, int n_groups, int n_q, int n_kv, int D) {
     l.starts = room(((size_t)n_groups + 1) * sizeof(int));
     l.firsts = room(((size_t)n_groups + 1) * sizeof(int));
     l.pair_rows = room((size_t)l.max_pairs * sizeof(int));
+    l.item_ctas = room((size_t)l.max_pairs * n_kv * sizeof(int4));
     l.totals = room(3 * sizeof(int));
     l.parts_w = room(l.max_pairs == 0 ? 0 : ((size_t)l.max_pairs * n_kv + kSharedCtas) * 2 * part_floats(kTile, D) * sizeof(float));
     l.parts_s = room(((size_t)M * n_kv + 2 * kSharedCtas) * part_floats(group, D) * sizeof(float));
@@ -1219,7 +1263,7 @@ int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const Shar
     cfg.numAttrs = 1;
     cfg.gridDim = dim3(1);
     cfg.blockDim = dim3(kPlanThreads);
-    if (const int rc = finish(cudaLaunchKernelEx(&cfg, shared_plan_kernel, a))) return rc;
+    if (const int rc = finish(cudaLaunchKernelEx(&cfg, shared_plan_kernel, a, ctas))) return rc;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kBytes;
@@ -1252,7 +1296,7 @@ int bitlinear_attention_shared_kv8(const void* q_bf16, const void* k_cache, cons
     if (kv_dtype != BITLINEAR_KV_INT8 && kv_dtype != BITLINEAR_KV_E4M3) return BITLINEAR_ERR_DTYPE;
     if (!shared_sizes_ok(M, n_groups, n_q_heads, n_kv_heads, head_dim) || n_seq <= 0 || max_blocks <= 0 ||
         !kv8_dims_ok(n_q_heads, n_kv_heads, head_dim, kv_dtype, n_blocks, block_rows) || (long long)max_blocks * block_rows > (1ll << 30) || (!seq_ids && n_seq < M) ||
-        (double)M * n_kv_heads * (((double)max_blocks * block_rows + block_rows) / kTile + 2) * 2 > 2147483000.0)
+        (double)M * n_kv_heads * ((double)max_blocks * block_rows / kTile + 4) * 2 > 2147483000.0)
         return BITLINEAR_ERR_SHAPE;
     if (M == 0) return BITLINEAR_OK;
     if (!q_bf16 || !k_cache || !v_cache || !k_scale || !v_scale || !tables || !lengths || !group_starts || (n_groups > 0 && !shared_rows) || !out_bf16) return BITLINEAR_ERR_NULL;
@@ -1268,7 +1312,7 @@ int bitlinear_attention_shared_kv8(const void* q_bf16, const void* k_cache, cons
     SharedArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, group_starts, shared_rows, M, n_groups, n_q_heads, n_kv_heads,
                     n_q_heads / n_kv_heads, n_seq, max_blocks, log2_of(block_rows), n_blocks, 1.4426950408889634f / sqrtf((float)head_dim), static_cast<__nv_bfloat16*>(out_bf16),
                     reinterpret_cast<int4*>(w + l.rows), reinterpret_cast<int4*>(w + l.pairs), reinterpret_cast<int*>(w + l.cum_pairs), reinterpret_cast<int*>(w + l.cum_rows),
-                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.firsts), reinterpret_cast<int*>(w + l.pair_rows), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
+                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.firsts), reinterpret_cast<int*>(w + l.pair_rows), reinterpret_cast<int4*>(w + l.item_ctas), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
                     l.max_pairs, device_status_word()};
     const int ctas = std::min(sm_count, kSharedCtas);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
