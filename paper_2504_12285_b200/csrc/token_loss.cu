@@ -66,6 +66,9 @@ struct Vec<float> {
     static __device__ __forceinline__ uint4 join(const float (&x)[4]) {
         return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
+    static __device__ __forceinline__ float most(const uint4& v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
     static __device__ __forceinline__ float load(const float* p) { return *p; }
     static __device__ __forceinline__ void store(float* p, float x) { *p = x; }
 };
@@ -89,6 +92,13 @@ struct Vec<__nv_bfloat16> {
         }
         return make_uint4(u[0], u[1], u[2], u[3]);
     }
+    static __device__ __forceinline__ float most(const uint4& v) {  // (a NaN counts only where nothing else stands)
+        uint32_t a, b;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+        return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    }
     static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
@@ -102,6 +112,30 @@ __device__ __forceinline__ float ex2(float x) {
 // exp(x - m) for x <= m: the difference is rounded once, so what weighs most is off least
 __device__ __forceinline__ float exp_below(float x, float m) { return ex2((x - m) * kLog2e); }
 
+// Two fp32 operations an instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
+
+// The same exponentials by one multiply-add, for many elements of a row: 2^(x log2(e) - c) with c = fl(m log2(e)).  That is off from exp(x - m) by
+// the factor 2^(m log2(e) - c), the same for all elements, which is put right once (`residue`).  For |m| of 2^20 and more that factor leaves the range of
+// a float sooner or later: such rows go through exp_below.
+constexpr float kPlain = 1048576.0f;
+__device__ __forceinline__ float residue(float m, float c) { return ex2(-fmaf(m, kLog2e, -c)); }
+template <int N>
+__device__ __forceinline__ void exps(const float (&x)[N], float c, float (&e)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+        const float2 t = fma2(make_float2(x[j], x[j + 1]), splat(kLog2e), splat(-c));
+        e[j] = ex2(t.x), e[j + 1] = ex2(t.y);
+    }
+}
+
 // A row's elements before its first 16-byte border, and the number of whole 16-byte units behind that.
 template <typename T>
 struct RowShape {
@@ -112,11 +146,64 @@ struct RowShape {
     }
 };
 
+// f exp(l - m) of sixteen bytes of logits
+template <typename T>
+struct RowWeights {
+    float m, f, c, g;
+    bool plain;
+    __device__ __forceinline__ RowWeights(float m, float f) : m(m), f(f), c(m * kLog2e), g(f * residue(m, m * kLog2e)), plain(fabsf(m) < kPlain) {}
+};
+template <typename T>
+__device__ __forceinline__ void weigh(const uint4& raw, float (&v)[Vec<T>::N], const RowWeights<T>& w) {
+    constexpr int N = Vec<T>::N;
+    float x[N];
+    Vec<T>::split(raw, x);
+    if (w.plain) {
+        exps(x, w.c, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] *= w.g;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = exp_below(x[j], w.m) * w.f;
+    }
+}
+
 // a running maximum and the sum of exp(x - maximum); one that met nothing is (kLowest, 0)
 __device__ __forceinline__ void join_stats(float& m, float& s, float m2, float s2) {
     const float n = fmaxf(m, m2);
     s = s * exp_below(m, n) + s2 * exp_below(m2, n);
     m = n;
+}
+
+// A thread's statistics while it goes over a row: the running maximum, itself and in base 2, and the sum in two halves.
+struct Running {
+    float m = kLowest, c = kLowest;
+    float2 sum = make_float2(0.0f, 0.0f);
+    template <typename T>
+    __device__ __forceinline__ void add(const uint4& raw) {
+        constexpr int N = Vec<T>::N;
+        float v[N], e[N];
+        Vec<T>::split(raw, v);
+        const float top = Vec<T>::most(raw);
+        if (top > m) {
+            const float next = top * kLog2e;
+            sum.x *= ex2(c - next), sum.y *= ex2(c - next);
+            m = top, c = next;
+        }
+        exps(v, c, e);
+#pragma unroll
+        for (int j = 0; j < N; j += 2) sum.x += e[j], sum.y += e[j + 1];
+    }
+    __device__ __forceinline__ bool plain() const { return fabsf(m) < kPlain; }  // else the thread goes over its elements again, with exp_below and m
+    __device__ __forceinline__ float total() const { return (sum.x + sum.y) * (m > kLowest ? residue(m, c) : 1.0f); }
+};
+template <typename T>
+__device__ __forceinline__ float sum_below(const uint4& raw, float m) {
+    float v[Vec<T>::N], s = 0.0f;
+    Vec<T>::split(raw, v);
+#pragma unroll
+    for (int j = 0; j < Vec<T>::N; ++j) s += exp_below(v[j], m);
+    return s;
 }
 
 // The policy loss of one token and its slope with the log probability: r = exp(logp - old),
@@ -186,25 +273,18 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
         }
         const float chosen = Vec<T>::load(x + target);  // (before the cluster meets: the gradient may go where the logits are)
         if (single >= 0) xs = Vec<T>::load(x + single);
-        float m = kLowest, s = 0.0f;
-        if (single >= 0) join_stats(m, s, xs, xs > kLowest ? 1.0f : exp_below(xs, kLowest));
+        Running run;
         for (int p = 0, at = 0; at < n; ++p, at += a.piece) {
             if (!mbar_wait(smem_u32(bars + p), 0, &abort_flag)) break;
             const int end = min(at + a.piece, n);
-            for (int i = at + tid; i < end; i += kThreads) {
-                float v[N];
-                Vec<T>::split(*reinterpret_cast<const uint4*>(part_s + 16 * (size_t)i), v);
-                float top = v[0];
-#pragma unroll
-                for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
-                if (top > m) {
-                    s *= exp_below(m, top);
-                    m = top;
-                }
-#pragma unroll
-                for (int j = 0; j < N; ++j) s += exp_below(v[j], m);
-            }
+            for (int i = at + tid; i < end; i += kThreads) run.add<T>(*reinterpret_cast<const uint4*>(part_s + 16 * (size_t)i));
         }
+        float m = run.m, s = run.total();
+        if (!run.plain()) {
+            s = 0.0f;
+            for (int i = tid; i < n; i += kThreads) s += sum_below<T>(*reinterpret_cast<const uint4*>(part_s + 16 * (size_t)i), m);
+        }
+        if (single >= 0) join_stats(m, s, xs, xs > kLowest ? 1.0f : exp_below(xs, kLowest));
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) {
             const float m2 = __shfl_xor_sync(0xffffffffu, m, off), s2 = __shfl_xor_sync(0xffffffffu, s, off);
@@ -252,14 +332,13 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
         if (d != nullptr) {
             const bool live = counts && (weight != 0.0f);
             const float f = live ? -slope / all.y : 0.0f, at_target = -slope * expm1f(logp);
+            const RowWeights<T> weights(all.x, f);
             T* to = d + shape.head;
             const bool aligned = ((reinterpret_cast<uintptr_t>(to)) & 15) == 0;
             for (int i = tid; i < n; i += kThreads) {
                 float v[N];
                 if (live) {
-                    Vec<T>::split(*reinterpret_cast<const uint4*>(part_s + 16 * (size_t)i), v);
-#pragma unroll
-                    for (int j = 0; j < N; ++j) v[j] = exp_below(v[j], all.x) * f;
+                    weigh(*reinterpret_cast<const uint4*>(part_s + 16 * (size_t)i), v, weights);
                 } else {
 #pragma unroll
                     for (int j = 0; j < N; ++j) v[j] = 0.0f;
@@ -282,6 +361,125 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
     if (counts) cluster.barrier_wait();  // no CTA leaves while another reads its shared memory
     if (abort_flag && tid == 0 && a.status != nullptr) atomicExch(a.status, BITLINEAR_ERR_TIMEOUT);
     if (abort_flag) abort_drain();
+}
+
+// Many rows: a CTA to a row, which it streams from memory for the statistics and, for the gradient, once more from L2 - the rows under way are 128 bytes for each
+// of the vocabulary and SM at most, which L2 holds.  No CTA waits for another, so that loads and stores of several rows are under way at any time.
+constexpr int kStreamThreads = 512, kStreamUnits = 4;
+
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kStreamThreads, 2) token_stream_kernel(const RowArgs a) {
+    constexpr int N = Vec<T>::N, kWarpsHere = kStreamThreads / 32;
+    __shared__ float2 warp_stats[kWarpsHere];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.stride;
+    T* d = MODE == kPolicy && a.dlogits ? static_cast<T*>(a.dlogits) + (size_t)row * a.d_stride : nullptr;
+    const RowShape<T> shape(x, a.V);
+    const T* body = x + shape.head;
+    int single = -1;  // the elements at the row's ends: lane l of warp 0 has one at most
+    if (warp == 0) {
+        const int tail = shape.head + shape.units * N + lane - 16;
+        single = lane < 16 ? (lane < shape.head ? lane : -1) : tail < a.V ? tail : -1;
+    }
+    const int target = a.targets[row];
+    const bool counts = target >= 0 && target < a.V;  // else the row is not read: 0 all over
+    float weight = 1.0f, old = 0.0f, adv = 0.0f, ref = 0.0f;
+    if constexpr (MODE == kPolicy) {
+        if (a.weights) weight = a.weights[row];
+        old = a.old[row], adv = a.advantages[row], ref = a.ref ? a.ref[row] : 0.0f;
+    }
+    float slope = 0.0f, logp = 0.0f, loss = 0.0f, xs = kLowest;
+    float2 all = make_float2(0.0f, 1.0f);
+    if (counts) {
+        const float chosen = Vec<T>::load(x + target);  // (before the CTA meets: the gradient may go where the logits are)
+        if (single >= 0) xs = Vec<T>::load(x + single);
+        Running run;
+        for (int i0 = tid; i0 < shape.units; i0 += kStreamUnits * kStreamThreads) {
+            uint4 raw[kStreamUnits];
+#pragma unroll
+            for (int k = 0; k < kStreamUnits; ++k) {
+                const int i = i0 + k * kStreamThreads;
+                if (i < shape.units) raw[k] = MODE == kPolicy ? *(reinterpret_cast<const uint4*>(body) + i) : __ldcs(reinterpret_cast<const uint4*>(body) + i);
+            }
+#pragma unroll
+            for (int k = 0; k < kStreamUnits; ++k)
+                if (i0 + k * kStreamThreads < shape.units) run.add<T>(raw[k]);
+        }
+        float m = run.m, s = run.total();
+        if (!run.plain()) {
+            s = 0.0f;
+            for (int i = tid; i < shape.units; i += kStreamThreads) s += sum_below<T>(*(reinterpret_cast<const uint4*>(body) + i), m);
+        }
+        if (single >= 0) join_stats(m, s, xs, xs > kLowest ? 1.0f : exp_below(xs, kLowest));
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, m, off), s2 = __shfl_xor_sync(0xffffffffu, s, off);
+            join_stats(m, s, m2, s2);
+        }
+        if (lane == 0) warp_stats[warp] = make_float2(m, s);
+        __syncthreads();
+        all = warp_stats[lane % kWarpsHere];  // every warp joins all in the same order
+#pragma unroll
+        for (int off = kWarpsHere / 2; off > 0; off >>= 1) {
+            const float m2 = __shfl_xor_sync(0xffffffffu, all.x, off), s2 = __shfl_xor_sync(0xffffffffu, all.y, off);
+            join_stats(all.x, all.y, m2, s2);
+        }
+        all.x = __shfl_sync(0xffffffffu, all.x, 0), all.y = __shfl_sync(0xffffffffu, all.y, 0);
+        logp = (chosen - all.x) - logf(all.y);
+    }
+    if constexpr (MODE == kPolicy) {
+        if (counts && weight != 0.0f) {  // a token of weight 0 counts for nothing, whatever stands beside it
+            policy_token(logp, old, adv, ref, a.clip_low, a.clip_high, a.kl, loss, slope);
+            loss *= weight, slope *= weight;
+        }
+    }
+    if (tid == 0) {
+        a.logprobs[row] = logp;
+        if (a.stats) a.stats[row] = all;
+        if (a.grad) a.grad[row] = 0.0f;
+        if (MODE == kPolicy) a.token_loss[row] = loss;
+    }
+    if constexpr (MODE == kPolicy) {
+        if (d == nullptr) return;
+        const bool live = counts && weight != 0.0f;
+        const float f = live ? -slope / all.y : 0.0f, at_target = -slope * expm1f(logp);
+        const RowWeights<T> weights(all.x, f);
+        T* to = d + shape.head;
+        const bool aligned = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+        for (int i0 = tid; i0 < shape.units; i0 += kStreamUnits * kStreamThreads) {
+            uint4 raw[kStreamUnits];
+#pragma unroll
+            for (int k = 0; k < kStreamUnits; ++k) {
+                const int i = i0 + k * kStreamThreads;
+                if (live && i < shape.units) raw[k] = __ldcs(reinterpret_cast<const uint4*>(body) + i);
+            }
+#pragma unroll
+            for (int k = 0; k < kStreamUnits; ++k) {
+                const int i = i0 + k * kStreamThreads;
+                if (i >= shape.units) break;
+                float v[N];
+                if (live) {
+                    weigh(raw[k], v, weights);
+                    const int hit = target - shape.head - i * N;
+                    if (hit >= 0 && hit < N) {
+#pragma unroll
+                        for (int j = 0; j < N; ++j)
+                            if (j == hit) v[j] = at_target;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) v[j] = 0.0f;
+                }
+                if (aligned) __stcs(reinterpret_cast<uint4*>(to) + i, Vec<T>::join(v));
+                else
+#pragma unroll
+                    for (int j = 0; j < N; ++j) Vec<T>::store(to + (size_t)i * N + j, v[j]);
+            }
+        }
+        if (single >= 0) Vec<T>::store(d + single, !live ? 0.0f : single == target ? at_target : exp_below(xs, all.x) * f);
+    }
 }
 
 // The gradient from statistics that are there: every element on its own.  A CTA takes 256 x 4 units of a row, all loads in flight.
@@ -314,6 +512,7 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(const GradArgs a) 
     const float f = live ? -g / st.y : 0.0f;
     // 1 - p of the target from its own logit, which the thread that holds it has read: the gradient may go where the logits are
     auto at_target = [&](float l) { return -g * expm1f((l - st.x) - logf(st.y)); };
+    const RowWeights<T> weights(st.x, f);
     const T* body = x + shape.head;
     T* to = d + shape.head;
     const bool aligned = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
@@ -328,16 +527,20 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(const GradArgs a) 
         const int u = (slab * kGradUnits + k) * kThreads + tid;
         if (u >= shape.units) break;
         float v[N];
-        Vec<T>::split(raw[k], v);
-        const int hit = target - shape.head - u * N;
-        float there = 0.0f;
-        if (live && hit >= 0 && hit < N) {
+        if (live) {
+            weigh(raw[k], v, weights);
+            const int hit = target - shape.head - u * N;
+            if (hit >= 0 && hit < N) {
+                float x[N];
+                Vec<T>::split(raw[k], x);
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (j == hit) there = at_target(v[j]);
+                for (int j = 0; j < N; ++j)
+                    if (j == hit) v[j] = at_target(x[j]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = 0.0f;
         }
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = !live ? 0.0f : j == hit ? there : exp_below(v[j], st.x) * f;
         if (aligned) __stcs(reinterpret_cast<uint4*>(to) + u, Vec<T>::join(v));
         else
 #pragma unroll
@@ -443,6 +646,15 @@ int launch_rows(RowArgs a, int rows, int sm_count, cudaStream_t st) {
         }
     }
     const long long units = (long long)a.V * (int)sizeof(T) / 16;
+    if (rows >= sm_count) {
+        cudaLaunchAttribute attr[2];
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)rows);
+        cfg.blockDim = dim3(kStreamThreads);
+        cfg.stream = st;
+        launch_dependent(cfg, attr, 1);
+        return finish(cudaLaunchKernelEx(&cfg, token_stream_kernel<T, MODE>, a));
+    }
     int ranks = 1;
     auto part = [&] { return (units + ranks - 1) / ranks; };
     while (ranks < kMaxRanks && part() * 16 > kPartBytes) ranks *= 2;
