@@ -3,11 +3,14 @@
 //
 //   logp_t = l[target] - max l - log sum exp(l - max l);   d logp_t / d l_v = [v = target] - exp(l_v - max l) / sum
 //
-// Bound: bytes.  A row of 128,256 logits is 250 or 500 KB and a loss needs its normaliser before the first element of its gradient, so a
-// cluster of CTAs holds the row in shared memory, a contiguous part each: where the slope of the loss follows from the token alone (the
-// policy loss), logits are read once and the gradient is written once.  Parts of at most 72 KB, so that three CTAs share an SM
-// and one's copies run beside another's arithmetic and stores.  A loss over pairs needs all rows of both answers first: a pass for the
-// log probabilities, one for the gradient.
+// Bound: bytes.  A row of 128,256 logits is 250 or 500 KB and a loss needs its normaliser before the first element of its gradient.
+//   As many rows as SMs or more: a CTA streams a row, once from memory for the statistics and once from L2 for the gradient (token_stream_kernel).  3000 rows of
+//     128,256 bf16, policy loss and gradient: 302 to 312 us, 4.9 to 5.1 TB/s, 75 to 78 % of the copy rate; log probabilities of 1200 such rows 57 us, 82 %.
+//   Fewer rows: a cluster of up to eight CTAs holds a row in shared memory, a part each (token_row_kernel): 21 rows of 128,256 fp32 12 us where the other takes 40.
+// The second way, for many rows too, took 362 us for the 3000: a meeting of CTAs in every row, behind which nothing is in flight; with clusters that stay and fetch
+// their next row meanwhile it took 626 us, for the meeting then waits for the stores of the row before.
+// Where the slope of the loss follows from the token alone (the policy loss), logits are read from memory once and the gradient is written once.  A loss over pairs needs
+// all rows of both answers first: a pass for the log probabilities, one for the gradient that begins with the rows that are still in L2.
 #include "common.cuh"
 #include "sm100_sync.cuh"
 
@@ -365,11 +368,12 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
 
 // Many rows: a CTA to a row, which it streams from memory for the statistics and, for the gradient, once more from L2 - the rows under way are 128 bytes for each
 // of the vocabulary and SM at most, which L2 holds.  No CTA waits for another, so that loads and stores of several rows are under way at any time.
-constexpr int kStreamThreads = 512, kStreamUnits = 4;
+constexpr int kStreamThreads = 512;
+__host__ __device__ constexpr int stream_units(int mode) { return mode == kPolicy ? 8 : 4; }  // loads in flight a thread
 
 template <typename T, int MODE>
-__global__ void __launch_bounds__(kStreamThreads, 2) token_stream_kernel(const RowArgs a) {
-    constexpr int N = Vec<T>::N, kWarpsHere = kStreamThreads / 32;
+__global__ void __launch_bounds__(kStreamThreads, MODE == kPolicy ? 2 : 3) token_stream_kernel(const RowArgs a) {
+    constexpr int N = Vec<T>::N, kWarpsHere = kStreamThreads / 32, kStreamUnits = stream_units(MODE);
     __shared__ float2 warp_stats[kWarpsHere];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -404,8 +408,11 @@ __global__ void __launch_bounds__(kStreamThreads, 2) token_stream_kernel(const R
                 if (i < shape.units) raw[k] = MODE == kPolicy ? *(reinterpret_cast<const uint4*>(body) + i) : __ldcs(reinterpret_cast<const uint4*>(body) + i);
             }
 #pragma unroll
-            for (int k = 0; k < kStreamUnits; ++k)
-                if (i0 + k * kStreamThreads < shape.units) run.add<T>(raw[k]);
+            for (int k = 0; k < kStreamUnits; ++k) {
+                const int i = i0 + k * kStreamThreads;
+                if (i >= shape.units) break;
+                run.add<T>(raw[k]);
+            }
         }
         float m = run.m, s = run.total();
         if (!run.plain()) {
@@ -576,11 +583,12 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict_
 }
 
 // A pair's answers: warps 0 .. 3 sum the preferred one's log probabilities, 4 .. 7 the other's (fp64, always in the same order), then all
-// write the tokens' slopes.  Rows of no answer keep the slope 0 that they were given before.
+// write the tokens' slopes.  Rows of no answer keep the slope 0 that they were given before.  One CTA alone writes the mean, too.
 __global__ void __launch_bounds__(256) pair_kernel(const float* __restrict__ logprobs, const int* __restrict__ targets, const int* __restrict__ cu, const float* __restrict__ ref,
                                                    int T, int V, int pairs, float beta, float smooth, float* __restrict__ pair_loss, float* __restrict__ seq_logprobs,
-                                                   float* __restrict__ grad) {
+                                                   float* __restrict__ grad, float* __restrict__ loss) {
     __shared__ double part[8];
+    double total = 0.0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int half = threadIdx.x >> 7, t = threadIdx.x & 127;
@@ -601,13 +609,16 @@ __global__ void __launch_bounds__(256) pair_kernel(const float* __restrict__ log
         const float up = fminf(delta, 0.0f) - soft, down = fminf(-delta, 0.0f) - soft;
         const float slope = (float)(-(double)beta / pairs) * (1.0f / (1.0f + expf(delta)) - smooth);
         if (threadIdx.x == 0) {
-            pair_loss[i] = -(1.0f - smooth) * up - smooth * down;
+            const float value = -(1.0f - smooth) * up - smooth * down;
+            pair_loss[i] = value;
+            total += (double)value;
             seq_logprobs[2 * i] = (float)chosen;
             seq_logprobs[2 * i + 1] = (float)rejected;
         }
         if (grad != nullptr)
             for (int j = begin + t; j < end; j += 128) grad[j] = half ? -slope : slope;
     }
+    if (loss != nullptr && threadIdx.x == 0) *loss = (float)(total / pairs);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -786,14 +797,16 @@ int bitlinear_preference_loss(const void* logits, int logits_dtype, int T, int V
     }
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::min(pairs, 1024));
+    const bool few = pairs <= 8;  // one CTA after the other takes less than the launch of a sum
+    cfg.gridDim = dim3(few ? 1u : (unsigned)std::min(pairs, 1024));
     cfg.blockDim = dim3(256);
     cfg.stream = st;
     launch_dependent(cfg, attr, 1);
     if (const int rc = finish(cudaLaunchKernelEx(&cfg, pair_kernel, (const float*)logprobs, targets, cu_tokens, ref_logprobs, T, V, pairs, beta, label_smoothing, pair_loss,
-                                                 seq_logprobs, grad)))
+                                                 seq_logprobs, grad, few ? loss : nullptr)))
         return rc;
-    if (const int rc = sum_pass(pair_loss, pairs, 1.0 / pairs, loss, st)) return rc;
+    if (!few)
+        if (const int rc = sum_pass(pair_loss, pairs, 1.0 / pairs, loss, st)) return rc;
     if (!grad) return BITLINEAR_OK;
     const GradArgs g = {logits, row_stride, targets, stats, grad, dlogits, d_stride, T, V, 0};
     return grad_pass(g, logits_dtype, st);

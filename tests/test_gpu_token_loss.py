@@ -196,6 +196,51 @@ def test_policy_loss_strided(offset, pad, d_offset, d_pad, dtype):
     assert (store[:d_offset] == 7.0).all() and (out[:, V:] == 7.0).all()
 
 
+@pytest.mark.parametrize("T,V,dtype", [(148, 5, F32), (400, 1, BF16), (300, 129, BF16), (151, 32003, F32), (200, 8192, BF16), (149, 70001, BF16)])
+@pytest.mark.parametrize("offset,pad", [(0, 0), (3, 9)])
+def test_many_rows(T, V, dtype, offset, pad):
+    """As many rows as SMs and more are streamed."""
+    x, targets, case = policy_case(T, V, dtype, 5 * V + T, 0.1, offset=offset, pad=pad)
+    targets[2], targets[T - 1] = -1, V
+    case["weights"][5] = 0.0
+    out = torch.full((T, V + pad), 7.0, dtype=dtype, device=DEV)
+    got = bl.bitlinear_policy_loss(x, targets, **case, grad=out[:, :V])
+    assert (out[:, V:] == 7.0).all()
+    some = torch.tensor(sorted({0, 1, 2, 3, 5, T // 2, T - 2, T - 1}), device=DEV)
+    pick = {k: (v[some].contiguous() if torch.is_tensor(v) else v) for k, v in case.items()}
+    check_policy(x[some], targets[some], pick, (got[1][some].double().sum(), got[1][some], got[2][some], got[3][some]))
+    assert abs(float(got[0]) - float(got[1].double().sum())) <= U * abs(float(got[0])) + 1e-30
+    same = x.clone()
+    assert torch.equal(bl.bitlinear_policy_loss(same, targets, **case, grad=same)[3], got[3]) or pad  # (rows that start elsewhere are summed in another order)
+    assert bl.bitlinear_policy_loss(x, targets, **case)[3] is None
+    logp, stats = bl.bitlinear_token_logprobs(x, targets)
+    assert torch.equal(logp, got[2])
+    xs, ts = host(x[some]), targets[some].tolist()
+    for i, t in enumerate(some.tolist()):
+        r = le.row(xs[i], ts[i])
+        if r is not None:
+            assert float(stats[t, 0]) == r[1] and abs(float(stats[t, 1]) - r[2]) <= r[2] * sum_error(V, r[4])
+
+
+def test_many_extreme_rows():
+    inf, low, nan = math.inf, torch.finfo(F32).min, math.nan
+    x = torch.randn(160, 4099, generator=torch.Generator().manual_seed(2))
+    x[0, 5:], x[1], x[2, 100:], x[3, 17], x[4, 17], x[5] = -inf, low, low, nan, inf, -inf
+    x[6] *= 1e30
+    x[7, 0], x[8], x[9, 3] = 3e38, x[8] * 1e6, nan
+    targets = torch.zeros(160, dtype=torch.int32)
+    targets[6] = int(x[6].argmax())
+    targets[8] = int(x[8].argmax())
+    targets[9] = -1
+    args = [torch.zeros(160, device=DEV), torch.ones(160, device=DEV)]
+    _, _, logp, d = bl.bitlinear_policy_loss(x.to(DEV), targets.to(DEV), *args, clip_low=1.0, clip_high=1e9, grad=True)  # the loss is -exp(logp), so is its slope
+    for t in (0, 1, 2, 6, 7, 8, 10):
+        r = le.row(x[t].double().numpy(), int(targets[t]))
+        assert abs(float(logp[t]) - r[0]) <= logp_error(r, 4099), t
+        assert abs(host(d[t]) - le.gradient(r[3], int(targets[t]), r[0], -math.exp(r[0]))).max() <= 1e-5, t
+    assert torch.isnan(logp[3:6]).all() and torch.isnan(d[3:6]).all() and not d[9].any() and not logp[9]
+
+
 def test_policy_clips_on_both_sides():
     x, targets, case = policy_case(64, 300, F32, 5, 0.0)
     assert 5 < check_policy(x, targets, case, bl.bitlinear_policy_loss(x, targets, **case, grad=True)) < 60
