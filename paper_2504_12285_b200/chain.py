@@ -193,14 +193,21 @@ class PagedDecodeStep:
     {q/k/v BitLinear, rotary embedding + append, attention, o, gate/up, down}, output head, and the draw of the next tokens.
 
     A step carries up to `rows` tokens: new_tokens[p] of the request in place p (more than one for a prompt or for drafted tokens, none
-    for an idle place, -1 for one that has finished and gives its blocks back), in the order of the places."""
+    for an idle place, -1 for one that has finished and gives its blocks back), in the order of the places.
+
+    With `groups`, several answers to one prompt read its cache rows once for all: the prompt goes to one place, fork() lets the places behind it begin with its
+    whole blocks, and group g is places group_places[g] .. group_places[g + 1] - 1, which share their first shared_rows[g] rows.  A place gives back the blocks it
+    did not borrow; the one they were borrowed from must not finish before the others."""
 
     def __init__(self, layers, embedding: torch.Tensor, rows: int, places: int, n_blocks: int, block_rows: int, max_blocks: int, hidden: int, ffn: int,
                  n_q_heads: int, n_kv_heads: int, head_dim: int, kv_dtype=torch.int8, rms_eps: float = 1e-5, rope_base: float = 500000.0,
-                 device="cuda:0"):
-        """layers, embedding: as for DecodeStep; rows at most 16 (the output head's limit); kv_dtype: torch.int8 or torch.float8_e4m3fn."""
+                 device="cuda:0", groups: int = 0):
+        """layers, embedding: as for DecodeStep; rows at most 16 (the output head's limit); kv_dtype: torch.int8 or torch.float8_e4m3fn; groups: of places
+        that may share cache rows."""
         if not 1 <= rows <= 16:
             raise ValueError(f"rows must be 1 to 16, not {rows}")
+        if not 0 <= groups <= places:
+            raise ValueError(f"groups must be 0 to {places}, not {groups}")
         dev = torch.device(device)
         self.rows, self.dims, self.block_rows, self.table = rows, (n_q_heads, n_kv_heads, head_dim), block_rows, embedding
         kv = n_kv_heads * head_dim
@@ -225,13 +232,36 @@ class PagedDecodeStep:
         # how each place draws its tokens: temperature (0: the likeliest), top_k (0: off), top_p (1: off), min_p (0: off)
         self.temperature, self.top_k = torch.ones(places, **f32), torch.zeros(places, **i32)
         self.top_p, self.min_p = torch.ones(places, **f32), torch.zeros(places, **f32)
-        self.attn_ws = torch.empty(bl.bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim), dtype=torch.uint8, device=dev)
+        # groups of places, as they share cache rows: which places, how many rows; the blocks at the head of each place's table that it has borrowed
+        self.groups = groups
+        self.group_places, self.shared_rows = torch.zeros(groups + 1, **i32), torch.zeros(groups, **i32)
+        self.borrowed, self.columns = torch.zeros(places, dtype=torch.int64, device=dev), torch.arange(max_blocks, device=dev)
+        ws_bytes = (bl.bitlinear_attention_shared_kv8_workspace_bytes(rows, groups, n_q_heads, n_kv_heads, head_dim) if groups else
+                    bl.bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim))
+        self.attn_ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
         self.ids, self.logprobs, self.row_numbers = torch.zeros(rows, **i32), torch.zeros(rows, **f32), torch.arange(rows, device=dev)
         with torch.cuda.device(dev):
             self.calls = _token_calls(self, layers, rms_eps, dev)
             # a step that places nothing: sizes and types that one of the calls refuses are refused here, before there is a state to spoil
             self.step(torch.zeros(rows, **i32), torch.zeros(rows, **f32))
         torch.cuda.synchronize(dev)
+
+    def fork(self, source: int, first: int, count: int) -> int:
+        """Places first .. first + count - 1, which must be empty, begin with the whole blocks of the rows that place `source` has in the cache (between steps; the
+        tokens behind them are brought as any others).  Returns how many rows that is, of all layers: what shared_rows says of a group of them."""
+        if not self.groups:
+            raise ValueError("places share nothing without groups")
+        places = self.lengths.shape[0]
+        if not (0 <= source < places and 0 <= first and count >= 1 and first + count <= places) or first <= source < first + count:
+            raise ValueError(f"no such places: {source}, {first} .. {first + count - 1} of {places}")
+        to = slice(first, first + count)
+        if int(self.lengths[to].max()) > 0 or int(self.borrowed[to].max()) > 0:
+            raise ValueError(f"places {first} .. {first + count - 1} are not empty")
+        blocks = int(self.lengths[source]) // self.block_rows
+        self.tables[to, :blocks] = self.tables[source, :blocks]
+        self.lengths[to] = blocks * self.block_rows
+        self.borrowed[to] = blocks
+        return blocks * self.block_rows
 
     def step(self, token_ids: torch.Tensor, u: torch.Tensor):
         """token_ids: int32 [rows] (device), the tokens that the places bring in this step, in the order of the places (those of a place that is
@@ -253,17 +283,27 @@ class PagedDecodeStep:
         brought = self.new_tokens.clamp(min=0)
         ends = brought.cumsum(0)
         new_tokens = self.new_tokens.masked_fill((ends > self.rows).logical_and_(brought > 0), 2 ** 31 - 1)
+        if self.groups:  # a finished place first lets go of what it borrowed: its own blocks move to the head of its table
+            drop = self.borrowed.masked_fill(new_tokens >= 0, 0)
+            self.tables.copy_(self.tables.gather(1, (self.columns + drop[:, None]).clamp_(max=self.tables.shape[1] - 1)))
+            self.lengths.sub_((drop * self.block_rows).to(torch.int32))
+            self.borrowed.sub_(drop)
         (_, _, self.served, self.cu_tokens, self.seq_ids, self.positions, self.row_lengths, self.slots) = bl.bitlinear_block_tables(
             self.lengths, new_tokens, self.tables, self.free_blocks, self.n_free, self.block_rows, self.rows, lengths_out=self.lengths,
             n_free_out=self.n_free)
         place = self.seq_ids.clamp(min=0)
+        group_starts = self.cu_tokens.index_select(0, self.group_places) if self.groups else None
         ahead = ends.sub_(brought).sub_(self.cu_tokens[:-1])  # tokens in front of a place that have no row
         bl.bitlinear_embed(token_ids.index_select(0, ahead.index_select(0, place).add_(self.row_numbers)), self.table, out=self.h_in)
         for (qkv, o, gu, down), cache in zip(self.calls, self.cache):
             bl.bitlinear_forward_batch(*qkv, reuse_plan=True)
             bl.bitlinear_rope_kv8(self.q, self.k, self.v, self.positions, self.slots, self.rope_table, *cache, n_q, n_kv, hd, q_out=self.q_rot)
-            bl.bitlinear_attention_decode_kv8(self.q_rot, *cache, self.tables, self.row_lengths, n_q, n_kv, hd, seq_ids=self.seq_ids, out=self.attn,
-                                              ws=self.attn_ws)
+            if self.groups:
+                bl.bitlinear_attention_shared_kv8(self.q_rot, *cache, self.tables, self.row_lengths, group_starts, self.shared_rows, n_q, n_kv, hd, seq_ids=self.seq_ids,
+                                                  out=self.attn, ws=self.attn_ws)
+            else:
+                bl.bitlinear_attention_decode_kv8(self.q_rot, *cache, self.tables, self.row_lengths, n_q, n_kv, hd, seq_ids=self.seq_ids, out=self.attn,
+                                                  ws=self.attn_ws)
             for batch, ws in (o, gu, down):
                 bl.bitlinear_forward_batch(batch, ws, reuse_plan=True)
         bl.bitlinear_glue_residual_add(self.h_mid, self.dn)  # the last layer's residual

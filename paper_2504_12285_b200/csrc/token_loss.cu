@@ -5,8 +5,9 @@
 //
 // Bound: bytes.  A row of 128,256 logits is 250 or 500 KB and a loss needs its normaliser before the first element of its gradient.
 //   As many rows as SMs or more: a CTA streams a row, once from memory for the statistics and once from L2 for the gradient (token_stream_kernel).  3000 rows of
-//     128,256 bf16, policy loss and gradient: 302 to 312 us, 4.9 to 5.1 TB/s, 75 to 78 % of the copy rate; log probabilities of 1200 such rows 57 us, 82 %.
-//   Fewer rows: a cluster of up to eight CTAs holds a row in shared memory, a part each (token_row_kernel): 21 rows of 128,256 fp32 12 us where the other takes 40.
+//     128,256 bf16, policy loss and gradient: 300 us, 5.1 TB/s, 78 % of the copy rate; log probabilities of 1200 such rows 56 us, 84 %.
+//   Fewer rows: a cluster of up to eight CTAs holds a row in shared memory, a part each (token_row_kernel): 21 rows of 128,256 fp32 12 us (streamed 24), 120 rows 35
+//     (39), log probabilities of 7 rows 5 (10).
 // The second way, for many rows too, took 362 us for the 3000: a meeting of CTAs in every row, behind which nothing is in flight; with clusters that stay and fetch
 // their next row meanwhile it took 626 us, for the meeting then waits for the stores of the row before.
 // Where the slope of the loss follows from the token alone (the policy loss), logits are read from memory once and the gradient is written once.  A loss over pairs needs

@@ -85,3 +85,33 @@ def test_oracle_pins():
     for s in (0.0, 0.2):
         up, down = le.pair(1.0 + h, 0.3, 0.7, s, 1)[0], le.pair(1.0 - h, 0.3, 0.7, s, 1)[0]
         assert abs((up - down) / (2 * h) - le.pair(1.0, 0.3, 0.7, s, 1)[1]) < 1e-9
+
+
+def shared_call(M=4, G=2, n_q=20, n_kv=5, D=128, kind=0, n_blocks=8, rows=64, n_seq=4, max_blocks=4, ws=FAKE, ws_bytes=1 << 40, seq_ids=FAKE, **p):
+    a = [p.get(n, FAKE) for n in ("q", "k_cache", "v_cache", "k_scale", "v_scale", "tables", "lengths")]
+    return bl.lib().bitlinear_attention_shared_kv8(*a, seq_ids, p.get("starts", FAKE), p.get("shared", FAKE), M, G, n_q, n_kv, D, kind, n_blocks, rows, n_seq, max_blocks,
+                                                   p.get("out", FAKE), ws, ws_bytes, None)
+
+
+def test_shared_attention_refusals():
+    assert shared_call(kind=-1) == 5 and shared_call(kind=2) == 5
+    for bad in (dict(M=-1), dict(M=65536), dict(G=-1), dict(G=65536), dict(n_q=21), dict(n_q=45), dict(D=96), dict(rows=8), dict(rows=24), dict(n_blocks=0), dict(n_blocks=1 << 26),
+                dict(n_seq=0), dict(max_blocks=0), dict(max_blocks=1 << 25), dict(seq_ids=None, M=5), dict(M=65535, max_blocks=1 << 19), dict(M=65535, n_q=40000, n_kv=5000)):
+        assert shared_call(**bad) == 2, bad
+    assert shared_call(M=0) == 0
+    for name in ("q", "k_cache", "v_cache", "k_scale", "v_scale", "tables", "lengths", "starts", "shared", "out"):
+        assert shared_call(**{name: None}) == 1, name
+    for name in ("q", "k_cache", "v_cache", "out"):
+        assert shared_call(**{name: FAKE + 8}) == 3, name
+    need = bl.bitlinear_attention_shared_kv8_workspace_bytes(4, 2, 20, 5, 128)
+    assert need > 0 and shared_call(ws_bytes=need - 1) == 4 and shared_call(ws=None) == 4 and shared_call(ws=FAKE + 8) == 4
+    for bad in ((-1, 2, 20, 5, 128), (4, -1, 20, 5, 128), (4, 2, 20, 6, 128), (4, 2, 45, 5, 128), (4, 2, 20, 5, 96), (65536, 2, 20, 5, 128)):
+        assert bl.bitlinear_attention_shared_kv8_workspace_bytes(*bad) == 0, bad
+
+
+def test_shared_step_wants_no_more_groups_than_places():
+    from paper_2504_12285_b200 import chain as gpu_chain
+
+    for groups in (-1, 5):
+        with pytest.raises(ValueError):
+            gpu_chain.PagedDecodeStep([], torch.zeros(50, 64, dtype=torch.bfloat16), 4, 4, 8, 16, 4, 64, 128, 1, 1, 64, device="cpu", groups=groups)
