@@ -36,6 +36,7 @@ namespace {
 constexpr int kTile = 128;         // query rows and cache rows of a product
 constexpr int kPlanThreads = 1024;
 constexpr int kFewGroups = 1024;
+constexpr int kPlanRows = 4;  // a thread and round
 constexpr int kThreads = 640;
 constexpr int kHalf = 64;            // columns of a half step
 constexpr int kSoftmaxRegs = 144, kOtherRegs = 64;  // a thread, of eight and of twelve warps
@@ -190,12 +191,22 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
     }
     __syncthreads();
     int tiles_before = 0;
-    for (int m0 = 0; m0 < a.M; m0 += kPlanThreads) {
-        const int m = m0 + tid;
-        int tiles = 0;
-        if (m < a.M) {
-            const int seq = a.seq_ids ? a.seq_ids[m] : m;
-            const int len = seq < 0 || seq >= a.n_seq ? 0 : min(max(a.lengths[m], 0), cap);
+    const int each = a.M > kPlanThreads ? kPlanRows : 1;
+    for (int m0 = 0; m0 < a.M; m0 += each * kPlanThreads) {
+        const int m1 = m0 + each * tid, m2 = min(m1 + each, a.M);  // this thread's rows, their loads in flight together
+        int seqs[kPlanRows], lens[kPlanRows], tiles[kPlanRows], sum = 0;
+#pragma unroll
+        for (int k = 0; k < kPlanRows; ++k) {
+            const int m = m1 + k;
+            seqs[k] = m < m2 ? (a.seq_ids ? a.seq_ids[m] : m) : -1;
+            lens[k] = m < m2 ? a.lengths[m] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kPlanRows; ++k) {
+            const int m = m1 + k;
+            tiles[k] = 0;
+            if (m >= m2) break;
+            const int len = seqs[k] < 0 || seqs[k] >= a.n_seq ? 0 : min(max(lens[k], 0), cap);
             // the last group that begins at or before the row, if the row is not behind its end
             int lo = 0, hi = a.n_groups;
             while (lo < hi) {
@@ -215,12 +226,18 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
                 }
             }
             a.rows[m] = info;
-            if (len > info.x) tiles = (len - ((info.x >> a.log2_rows) << a.log2_rows) + kTile - 1) / kTile * a.n_kv;
-            if (tiles > 0) tiles += a.n_kv;  // a place for each head's start
+            // a place for each head's start, too
+            if (len > info.x) tiles[k] = ((len - ((info.x >> a.log2_rows) << a.log2_rows) + kTile - 1) / kTile + 1) * a.n_kv;
+            sum += tiles[k];
         }
         int total;
-        const int at = tiles_before + block_exclusive_scan(tiles, warp_sums, total);
-        if (m < a.M) a.cum_rows[m] = at;
+        int at = tiles_before + block_exclusive_scan(sum, warp_sums, total);
+#pragma unroll
+        for (int k = 0; k < kPlanRows; ++k) {
+            if (m1 + k >= m2) break;
+            a.cum_rows[m1 + k] = at;
+            at += tiles[k];
+        }
         tiles_before += total;
     }
     __syncthreads();
@@ -464,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         const int s = (warp - 4) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lane_at = (uint32_t)(quad * 32) << 16;
         const uint32_t ts = tm_s(s) + lane_at, to = tm_o(s) + lane_at;
-        float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+        float f = 0.0f, m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f, per_ref = 0.0f;  // per_ref: the weights' scale by v_ref
         int lower = 0, upper = 0;
         uint32_t s_phase = 0, o_phase = 0, item = 0, halves = 0;  // items, half steps so far
         // A finished item's accumulator is read after the next item's queries are on their way.
@@ -551,13 +568,16 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     if (lane == 0) mbar_arrive(bar(L::q_full + s));
                 }
                 if (finished) hand_over();
-                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+                m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f, per_ref = 0.0f;
             }
             // what this row uses of the tile
             const int lo = max(lower - base, 0), hi = min(upper - base, kTile);
             const bool all_used = __all_sync(0xffffffffu, !mine || (lo == 0 && hi == kTile && lost == 0));
 #pragma unroll 1
             for (int h = 0; h < 2; ++h, ++halves) {
+                // what does not hang on the scores comes before them
+                const float4 k4 = *reinterpret_cast<const float4*>(&d.ks[s][4 * h]), w4 = *reinterpret_cast<const float4*>(&d.vs[s][4 * h]);
+                float ks[4] = {k4.x, k4.y, k4.z, k4.w}, rs[4] = {w4.x, w4.y, w4.z, w4.w};
                 wait(L::s_full + 2 * s + h, s_phase);
                 tc_fence_after();
                 if ((flags & (kFirst | kOwn)) == (kFirst | kOwn) && h == 0 && mine) f = query_down(smem[L::exponents + (s * 2 + (item & 1u)) * kTile + r]) * a.scale_log2;
@@ -565,12 +585,12 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                     uint32_t v[2][32];
                     tm_load(ts + kHalf * h, v[0]);
                     tm_load(ts + kHalf * h + 32, v[1]);
-                    float ks[4], rs[4];
-                    {
-                        const float4 k = *reinterpret_cast<const float4*>(&d.ks[s][4 * h]), w = *reinterpret_cast<const float4*>(&d.vs[s][4 * h]);
-                        ks[0] = k.x * f, ks[1] = k.y * f, ks[2] = k.z * f, ks[3] = k.w * f;
-                        rs[0] = w.x, rs[1] = w.y, rs[2] = w.z, rs[3] = w.w;
-                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ks[i] *= f;
+                    float vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
+                    float ww[4];  // the weights' factors, if the largest scale of values stays
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ww[i] = rs[i] * per_ref;
                     tm_load_wait();
                     if (!all_used) {  // what the row does not use scores -infinity, whatever lies there; its scales count for nothing
 #pragma unroll
@@ -586,9 +606,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                             for (int i = 0; i < 2; ++i) {
                                 const bool none = (live & (i ? 0xffff0000u : 0x0000ffffu)) == 0u;
                                 if (none || ks[2 * c + i] == 0.0f) ks[2 * c + i] = 1e-30f;  // -infinity times a scale of zero would be NaN; finite scores stay next to zero
-                                if (none) rs[2 * c + i] = 0.0f;
+                                if (none) rs[2 * c + i] = ww[2 * c + i] = 0.0f;
                             }
                         }
+                        vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
                     }
                     float top = -INFINITY;
 #pragma unroll
@@ -599,7 +620,6 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                         for (int e = 0; e < 14; e += 2) t = fmaxf(fmaxf(t, __uint_as_float(x16[e])), __uint_as_float(x16[e + 1]));
                         top = fmaxf(top, fmaxf(t, __uint_as_float(x16[14])) * ks[i]);
                     }
-                    const float vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
                     // The maximum is followed only where it grows by more than 2^8: weights stay within f16, and the accumulator is rarely scaled.
                     const bool grows = top > m_run + 8.0f || (m_run == -INFINITY && top > -INFINITY), wider = vs > v_ref;
                     if (__any_sync(0xffffffffu, grows || wider)) {
@@ -622,8 +642,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                         }
                         m_run = n;
                         v_ref = nv;
+                        per_ref = v_ref > 0.0f ? __fdividef(kWeightScale, v_ref) : 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) ww[i] = rs[i] * per_ref;
                     }
-                    const float per_ref = v_ref > 0.0f ? __fdividef(kWeightScale, v_ref) : 0.0f;
                     // Weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost; their sum takes them unrounded.
                     // They go over the scores.
                     float2 sum = make_float2(0.0f, 0.0f);
@@ -633,13 +655,13 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                         uint32_t w[16];
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const float2 kk = splat(ks[2 * c + i]), ww = splat(rs[2 * c + i] * per_ref);
+                            const float2 kk = splat(ks[2 * c + i]), factor = splat(ww[2 * c + i]);
 #pragma unroll
                             for (int e = 0; e < 16; e += 2) {
                                 float2 t = fma2(make_float2(__uint_as_float(v[c][16 * i + e]), __uint_as_float(v[c][16 * i + e + 1])), kk, bb);
                                 t.x = ex2(t.x), t.y = ex2(t.y);
                                 sum = add2(sum, t);
-                                t = mul2(t, ww);
+                                t = mul2(t, factor);
                                 w[8 * i + e / 2] = pack_f16(t.x, t.y);
                             }
                         }
@@ -845,6 +867,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         const uint32_t q_free = __shfl_sync(0xffffffffu, bar(L::q_free + s), 0), pv_done = __shfl_sync(0xffffffffu, bar(L::pv_done + s), 0);
         constexpr uint32_t kScores = instruction(kHalf, false), kValues = instruction(D, true);
         const uint64_t q_tile = operand(__shfl_sync(0xffffffffu, base_s + L::q + (uint32_t)s * L::kOperandBytes, 0), 16);
+        const uint32_t at1 = __shfl_sync(0xffffffffu, scores_at + kHalf, 0), rows1 = __shfl_sync(0xffffffffu, 512, 0);  // the second half: 64 rows of 128 bytes, in sixteens
+        const uint32_t full1 = __shfl_sync(0xffffffffu, s_full + 8, 0);
         uint32_t q_phase = 0, p_phase = 0;
         int made = 0;                // operand tiles so far, of both streams
         int now = 0, other_now = 0;  // flags of step p, this stream's and the other's
@@ -884,8 +908,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             for (int i = 0; i < 4; ++i) {
                 const int h = late ? i & 1 : i >> 1;
                 const bool values = late ? i < 2 : !(i & 1);
-                const uint32_t at = __shfl_sync(0xffffffffu, scores_at + kHalf * h, 0), rows = __shfl_sync(0xffffffffu, 512 * h, 0);  // (64 rows of 128 bytes, in sixteens)
-                const uint32_t full = __shfl_sync(0xffffffffu, s_full + 8 * h, 0);
+                const uint32_t at = h ? at1 : scores_at, rows = h ? rows1 : 0u, full = h ? full1 : s_full;
                 if (values && has_value) {
                     wait(L::p_full + 2 * s + h, p_phase);
                     tc_fence_after();
@@ -1058,10 +1081,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 // ---------------------------------------------------------------------------------------------- the parts of a row
 
 // A query head's parts, by WARPS warps: warp w takes parts w, w + WARPS, ... of each of the two kinds.  Lane l first finds the l-th of a round's parts and weighs it;
-// then all lanes add up the rounds' values, a few dims each, four or eight parts' loads in flight.
+// then all lanes add up the rounds' values, a few dims each, eight parts' loads in flight.
 template <int D, int WARPS>
-__global__ void __launch_bounds__(128, WARPS == 1 ? 12 : 6) shared_combine_kernel(const SharedArgs a, int ctas) {
-    constexpr int DIMS = D / 32, AT_ONCE = WARPS == 1 ? 4 : 8;  // (many heads: latency is hidden by more warps, not by more loads)
+__global__ void __launch_bounds__(128, 6) shared_combine_kernel(const SharedArgs a, int ctas) {
+    constexpr int DIMS = D / 32, AT_ONCE = 8;
     __shared__ float2 joined[4];
     __shared__ float values[4][D];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -1186,6 +1209,122 @@ __global__ void __launch_bounds__(128, WARPS == 1 ? 12 : 6) shared_combine_kerne
     else *reinterpret_cast<uint32_t*>(dst) = out[0];
 }
 
+// The same for many rows: a warp takes all query heads of a row and KV head, which have the same parts, so that what leads to them is looked up once (a warp to a
+// query head: 27 us for 2173 rows of 20 heads).
+template <int D>
+__global__ void __launch_bounds__(128) shared_combine_rows_kernel(const SharedArgs a, int ctas) {
+    constexpr int DIMS = D / 32, HEADS = 4;  // query heads at a time
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int item = (int)blockIdx.x * 4 + warp, m = item / a.n_kv, h = item - m * a.n_kv;
+    if (m >= a.M) return;
+    const int4 row = a.rows[m];
+    const int units = a.totals[1], tiles = a.totals[2];
+    const EqualRuns runs(2 * units + tiles, ctas);
+    const int c_row0 = a.cum_rows[m], c_row1 = a.cum_rows[m + 1];
+    for (int j0 = 0, nj; j0 < a.group; j0 += nj) {
+        // heads j0 .. j0 + nj - 1: of one pair of query tiles, and of one tile
+        nj = min(HEADS, a.group - j0);
+        int r0 = 0, pair = 0;
+        const bool shares = row.z >= 0 && row.x > 0;
+        if (shares) {
+            const int in_group = m * a.group + j0 - row.w;
+            pair = row.z + in_group / (2 * kTile), r0 = in_group % (2 * kTile);
+            nj = min(nj, kTile - r0 % kTile);
+        }
+        float top[HEADS], l[HEADS], acc[HEADS][DIMS];
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            top[k] = -INFINITY, l[k] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < DIMS; ++e) acc[k][e] = 0.0f;
+        }
+        auto gather = [&](int n, int n_rows, int first_row, auto find) {
+            for (int i0 = 0; i0 < n; i0 += 32) {
+                const float* part = i0 + lane < n ? find(i0 + lane) : nullptr;
+                float2 ml[HEADS];
+                float f[HEADS];
+#pragma unroll
+                for (int k = 0; k < HEADS; ++k) ml[k] = part && k < nj ? *reinterpret_cast<const float2*>(part + (size_t)n_rows * D + 2 * (first_row + k)) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+                for (int k = 0; k < HEADS; ++k) {
+                    float most = ml[k].x;
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+                    const float now = fmaxf(top[k], most), f0 = top[k] == -INFINITY ? 0.0f : ex2(top[k] - now);
+                    f[k] = ml[k].x == -INFINITY ? (ml[k].y == ml[k].y ? 0.0f : NAN) : ex2(ml[k].x - now);
+                    float sum = ml[k].y * f[k];
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                    l[k] = l[k] * f0 + sum;
+                    top[k] = now;
+#pragma unroll
+                    for (int e = 0; e < DIMS; ++e) acc[k][e] *= f0;
+                }
+                for (unsigned left = __ballot_sync(0xffffffffu, part != nullptr); left; left &= left - 1) {
+                    const int src = __ffs((int)left) - 1;
+                    const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, (unsigned long long)part, src));
+                    float v[HEADS][DIMS];
+#pragma unroll
+                    for (int k = 0; k < HEADS; ++k) {
+                        const float* at = p + 4 * (size_t)(first_row + min(k, nj - 1));
+                        if constexpr (DIMS == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(at + (size_t)(4 * lane) * n_rows);
+                        else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(at + (size_t)(4 * (lane >> 1)) * n_rows + 2 * (lane & 1));
+                    }
+#pragma unroll
+                    for (int k = 0; k < HEADS; ++k) {
+                        const float w = __shfl_sync(0xffffffffu, f[k], src);
+#pragma unroll
+                        for (int e = 0; e < DIMS; ++e) acc[k][e] = w == 0.0f ? acc[k][e] : fmaf(v[k][e], w, acc[k][e]);  // (what weighs nothing may hold anything)
+                    }
+                }
+            }
+        };
+        if (shares) {
+            const int4 info = a.pairs[pair], where = a.item_ctas[pair * a.n_kv + h];  // its first unit, the first and last CTA that have some of it
+            const bool two = info.y > kTile;
+            gather((where.z - where.y + 1) * (two ? 1 : 2), kTile, r0 % kTile, [&](int i) -> const float* {
+                const int c = where.y + (two ? i : i >> 1), s = two ? r0 / kTile : i & 1;
+                if (!two || runs.each < 2) {
+                    const Share share(runs, units, c);
+                    if (share.w0 >= share.w1) return nullptr;
+                    if (!two && s == 1 && (2 * max(share.w0 - where.x, 0) + 1) * kTile >= info.w) return nullptr;
+                }
+                return a.parts_w + ((size_t)(pair * a.n_kv + h + c) * 2 + s) * part_floats(kTile, D);
+            });
+        }
+        if (row.y > row.x) {
+            const int n = (c_row1 - c_row0) / a.n_kv - 1, t0 = c_row0 + h * (n + 1) + 1;
+            auto worker = [&](int t) {
+                const int c = runs.owner(2 * units + t);
+                return 2 * c + (t >= Share(runs, units, c).middle() ? 1 : 0);
+            };
+            const int first = worker(t0), last = worker(t0 + n - 1);
+            gather(last - first + 1, a.group, j0, [&](int i) -> const float* {
+                const int k = first + i;
+                const Share share(runs, units, k >> 1);
+                if (((k & 1) ? share.s1 - share.middle() : share.middle() - share.s0) <= 0) return nullptr;
+                return a.parts_s + (size_t)(m * a.n_kv + h + k) * part_floats(a.group, D);
+            });
+        }
+#pragma unroll
+        for (int k = 0; k < HEADS; ++k) {
+            if (k >= nj) break;
+            const float inv = l[k] == 0.0f ? 0.0f : 1.0f / l[k];  // no row: zeros; a sum that is NaN stays one
+            uint32_t out[DIMS / 2];
+#pragma unroll
+            for (int e = 0; e < DIMS; e += 2) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(acc[k][e] * inv, acc[k][e + 1] * inv);
+                out[e / 2] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            __nv_bfloat16* dst = a.out + ((size_t)m * a.n_q + (size_t)h * a.group + j0 + k) * D + DIMS * lane;
+            if constexpr (DIMS == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
+            else *reinterpret_cast<uint32_t*>(dst) = out[0];
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- host side
 
 SharedLayout shared_layout(int M, int n_groups, int n_q, int n_kv, int D) {
@@ -1268,13 +1407,17 @@ int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const Shar
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kBytes;
     if (const int rc = finish(cudaLaunchKernelEx(&cfg, shared_attention_kernel<D, KIND>, map_k, map_v, a))) return rc;
-    // a warp per query head where there are enough of them, else four
-    const long long heads = (long long)a.M * a.n_q;
-    const bool many = heads >= 32ll * ctas;
-    cfg.gridDim = dim3((unsigned)(many ? (heads + 3) / 4 : heads));
+    // four warps per query head; one per row and KV head where there are thousands of rows, which have few parts each (2173 rows: 27 us with a warp per query head, 22 so;
+    // but 144 rows of six groups 17 and 25)
+    const long long heads = (long long)a.M * a.n_q, items = (long long)a.M * a.n_kv;
     cfg.blockDim = dim3(128);
     cfg.dynamicSmemBytes = 0;
-    return finish(many ? cudaLaunchKernelEx(&cfg, shared_combine_kernel<D, 1>, a, ctas) : cudaLaunchKernelEx(&cfg, shared_combine_kernel<D, 4>, a, ctas));
+    if (heads >= 128ll * ctas) {
+        cfg.gridDim = dim3((unsigned)((items + 3) / 4));
+        return finish(cudaLaunchKernelEx(&cfg, shared_combine_rows_kernel<D>, a, ctas));
+    }
+    cfg.gridDim = dim3((unsigned)heads);
+    return finish(cudaLaunchKernelEx(&cfg, shared_combine_kernel<D, 4>, a, ctas));
 }
 
 }  // namespace

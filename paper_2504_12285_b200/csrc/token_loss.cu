@@ -195,8 +195,12 @@ struct Running {
             m = top, c = next;
         }
         exps(v, c, e);
+        // sixteen bytes' terms among themselves first: fewer roundings at the size of the sum
 #pragma unroll
-        for (int j = 0; j < N; j += 2) sum.x += e[j], sum.y += e[j + 1];
+        for (int w = N / 2; w > 1; w /= 2)
+#pragma unroll
+            for (int j = 0; j < w; ++j) e[j] += e[j + w];
+        sum.x += e[0], sum.y += e[1];
     }
     __device__ __forceinline__ bool plain() const { return fabsf(m) < kPlain; }  // else the thread goes over its elements again, with exp_below and m
     __device__ __forceinline__ float total() const { return (sum.x + sum.y) * (m > kLowest ? residue(m, c) : 1.0f); }
@@ -210,17 +214,37 @@ __device__ __forceinline__ float sum_below(const uint4& raw, float m) {
     return s;
 }
 
+// A log probability in two parts, chosen - m - log(sum): rounded to fp32 alone it is off by a part in 2^24 of log(sum), which is ten or more, and the ratio of two
+// models' probabilities by as much.  log(sum) = k ln 2 + log(rest), rest about 1; k times the upper bits of ln 2 is exact.
+struct LogProb {
+    float hi, lo;
+};
+// x - y and what its rounding took
+__device__ __forceinline__ float difference(float x, float y, float& lost) {
+    const float d = __fsub_rn(x, y), z = __fsub_rn(d, x);
+    lost = __fsub_rn(__fsub_rn(x, __fsub_rn(d, z)), __fadd_rn(y, z));
+    return d;
+}
+__device__ __forceinline__ LogProb log_prob(float chosen, float m, float sum) {
+    const int bits = __float_as_int(sum), k = (bits - 0x3f3504f3) >> 23;  // rest between sqrt(1/2) and sqrt(2)
+    const float rest = __int_as_float(bits - (k << 23)), big = (float)k * 0x1.62e4p-1f;  // (fifteen bits)
+    const float small = fmaf((float)k, 0x1.7f7d1cp-20f, logf(sum > 0.0f && sum < INFINITY ? rest : sum));
+    float a_lo, b_lo, c_lo;
+    const float hi = difference(difference(difference(chosen, m, a_lo), big, b_lo), small, c_lo), lo = a_lo + b_lo + c_lo;
+    return {hi, fabsf(hi) < 1e30f && fabsf(lo) < 1.0f ? lo : 0.0f};
+}
+
 // The policy loss of one token and its slope with the log probability: r = exp(logp - old),
 //   -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(ref - logp) - (ref - logp) - 1).
-__device__ __forceinline__ void policy_token(float logp, float old, float adv, float ref, float low, float high, float kl, float& loss, float& slope) {
-    const float r = expf(logp - old);
+__device__ __forceinline__ void policy_token(LogProb logp, float old, float adv, float ref, float low, float high, float kl, float& loss, float& slope) {
+    const float r = expf((logp.hi - old) + logp.lo);
     const float free = r * adv, cut = fminf(fmaxf(r, 1.0f - low), 1.0f + high) * adv;
     const bool inside = free <= cut;
     loss = inside ? -free : -cut;
     slope = inside ? -free : 0.0f;
     if (free != free) loss = slope = free;
     if (kl != 0.0f) {
-        const float d = ref - logp, e = expm1f(d);
+        const float d = (ref - logp.hi) - logp.lo, e = expm1f(d);
         // e - d cancels for small d: the series there, its first term left out (d^8 / 8! of d^2 / 2) below 2^-26
         const float near = d * d * fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.0f / 5040.0f, 1.0f / 720.0f), 1.0f / 120.0f), 1.0f / 24.0f), 1.0f / 6.0f), 0.5f);
         loss = fmaf(kl, fabsf(d) < 0.25f ? near : e - d, loss);
@@ -261,7 +285,8 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
     const int target = a.targets[row];
     const float weight = MODE == kPolicy && a.weights ? a.weights[row] : 1.0f;
     const bool counts = target >= 0 && target < a.V;  // else the row is not read: 0 all over
-    float slope = 0.0f, logp = 0.0f;
+    float slope = 0.0f;
+    LogProb logp = {0.0f, 0.0f};
     float2 all = make_float2(0.0f, 1.0f);
     float xs = kLowest;
     if (counts) {
@@ -317,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
                 if (r < ranks) join_stats(all.x, all.y, o[r].x, o[r].y);
         }
         cluster.barrier_arrive();
-        logp = (chosen - all.x) - logf(all.y);
+        logp = log_prob(chosen, all.x, all.y);
     }
     float loss = 0.0f;
     if constexpr (MODE == kPolicy) {
@@ -327,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
         }
     }
     if (rank == 0 && tid == 0) {
-        a.logprobs[row] = logp;
+        a.logprobs[row] = logp.hi;
         if (a.stats) a.stats[row] = all;
         if (a.grad) a.grad[row] = 0.0f;
         if (MODE == kPolicy) a.token_loss[row] = loss;
@@ -335,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
     if constexpr (MODE == kPolicy) {
         if (d != nullptr) {
             const bool live = counts && (weight != 0.0f);
-            const float f = live ? -slope / all.y : 0.0f, at_target = -slope * expm1f(logp);
+            const float f = live ? -slope / all.y : 0.0f, at_target = -slope * expm1f(logp.hi);
             const RowWeights<T> weights(all.x, f);
             T* to = d + shape.head;
             const bool aligned = ((reinterpret_cast<uintptr_t>(to)) & 15) == 0;
@@ -395,7 +420,8 @@ __global__ void __launch_bounds__(kStreamThreads, MODE == kPolicy ? 2 : 3) token
         if (a.weights) weight = a.weights[row];
         old = a.old[row], adv = a.advantages[row], ref = a.ref ? a.ref[row] : 0.0f;
     }
-    float slope = 0.0f, logp = 0.0f, loss = 0.0f, xs = kLowest;
+    float slope = 0.0f, loss = 0.0f, xs = kLowest;
+    LogProb logp = {0.0f, 0.0f};
     float2 all = make_float2(0.0f, 1.0f);
     if (counts) {
         const float chosen = Vec<T>::load(x + target);  // (before the CTA meets: the gradient may go where the logits are)
@@ -435,7 +461,7 @@ __global__ void __launch_bounds__(kStreamThreads, MODE == kPolicy ? 2 : 3) token
             join_stats(all.x, all.y, m2, s2);
         }
         all.x = __shfl_sync(0xffffffffu, all.x, 0), all.y = __shfl_sync(0xffffffffu, all.y, 0);
-        logp = (chosen - all.x) - logf(all.y);
+        logp = log_prob(chosen, all.x, all.y);
     }
     if constexpr (MODE == kPolicy) {
         if (counts && weight != 0.0f) {  // a token of weight 0 counts for nothing, whatever stands beside it
@@ -444,7 +470,7 @@ __global__ void __launch_bounds__(kStreamThreads, MODE == kPolicy ? 2 : 3) token
         }
     }
     if (tid == 0) {
-        a.logprobs[row] = logp;
+        a.logprobs[row] = logp.hi;
         if (a.stats) a.stats[row] = all;
         if (a.grad) a.grad[row] = 0.0f;
         if (MODE == kPolicy) a.token_loss[row] = loss;
@@ -452,7 +478,7 @@ __global__ void __launch_bounds__(kStreamThreads, MODE == kPolicy ? 2 : 3) token
     if constexpr (MODE == kPolicy) {
         if (d == nullptr) return;
         const bool live = counts && weight != 0.0f;
-        const float f = live ? -slope / all.y : 0.0f, at_target = -slope * expm1f(logp);
+        const float f = live ? -slope / all.y : 0.0f, at_target = -slope * expm1f(logp.hi);
         const RowWeights<T> weights(all.x, f);
         T* to = d + shape.head;
         const bool aligned = (reinterpret_cast<uintptr_t>(to) & 15) == 0;
