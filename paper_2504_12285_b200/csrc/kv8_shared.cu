@@ -410,6 +410,7 @@ template <int D>
 struct SharedSmem {
     static constexpr int kOperands = D == 128 ? 4 : 6;  // tiles of f16
     static constexpr int kStages = D == 128 ? 2 : 8;    // tiles of codes
+    static_assert(kOperands % 2 == 0 && kStages % 2 == 0, "a place belongs to the same four conversion warps every time, which then wait for each of its phases");
     static constexpr uint32_t kOperandBytes = kTile * D * 2, kCodeBytes = kTile * D;
     // what is small lies in front of the tiles
     static constexpr uint32_t exponents = 0, descs = 2 * 2 * kTile, bars = descs + kDescs * sizeof(Desc);
@@ -485,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         int lower = 0, upper = 0;
         uint32_t s_phase = 0, o_phase = 0, item = 0, halves = 0;  // items, half steps so far
         // A finished item's accumulator is read after the next item's queries are on their way.
-        bool finished = false;
+        bool finished = false, after_pairs = false;
         float* part = nullptr;
         int part_rows = 0;
         bool in_part = false, any_in_part = false;
@@ -533,7 +534,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             if (flags & kFirst) {
                 if (flags & kOwn) {
                     lower = x.lower, upper = x.upper;
+                    if (after_pairs && quad == 0 && lane == 0) mbar_arrive(bar(L::q_free + s));
+                    after_pairs = false;
                 } else {
+                    after_pairs = true;
                     // sixteen (eight) lanes bring a row together, eight loads in flight (a row to each lane took the L1 cache 32 lines a load: 8,000 cycles for a tile)
                     constexpr int LANES = D / 8, AT_ONCE = 32 / LANES;
                     const int unit = lane % LANES;
@@ -939,7 +943,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                         tc_commit(full);
                         if (h == 1) {
                             tc_commit(k_done);
-                            if (next & kLast) tc_commit(q_free);
+                            if ((next & (kLast | kOwn)) == (kLast | kOwn)) tc_commit(q_free);
                         }
                     }
                 }
@@ -957,7 +961,10 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         }
     } else if (warp == 3) {
         // ------------------------------------------------------------------ queries of rows' own tiles
-        uint32_t items[2] = {0u, 0u};
+        // q_free completes once for each of a stream's own items, when its scores are made, and once before the first of them if pairs' items are in front, when the softmax
+        // has seen the last one's scores.  This warp waits for every one in turn: it may fall steps behind a stream's pairs, and a barrier that moved on by two phases
+        // meanwhile would look as if it had not moved.
+        uint32_t items[2] = {0u, 0u}, freed[2] = {0u, 0u};
         for (int p = 0; !aborted(); ++p) {
             const int slot = p % kDescs;
             wait(L::desc_full + slot, (uint32_t)(p / kDescs) & 1u);
@@ -968,8 +975,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 const Side& x = d.side[s];
                 if ((x.flags & (kLive | kFirst)) != (kLive | kFirst)) continue;
                 const uint32_t item = items[s]++;
-                if (item > 0) wait(L::q_free + s, (item - 1u) & 1u);  // the scores of the item in front are made
-                if (!(x.flags & kOwn)) continue;                      // (a pair's: its 128 rows' softmax threads bring one each)
+                if (!(x.flags & kOwn)) continue;  // (a pair's: its rows' softmax warps bring them)
+                if (item > 0) wait(L::q_free + s, freed[s]++ & 1u);  // the scores of the item in front are made
                 const int r = lane >> 2, c = lane & 3;  // four lanes to a row, eight rows at most
                 uint4 v[D / 32];
                 uint32_t most = 0u;
