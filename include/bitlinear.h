@@ -597,19 +597,20 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
  * overlap them otherwise.  V <= BITLINEAR_SAMPLE_MAX_VOCAB, T <= 2^24.
  *
  * bitlinear_token_logprobs: logprobs[t] = l[targets[t]] - max l - log(sum exp(l - max l)); stats [T][2] receives (max l, the sum), 8-byte aligned.
- *   One launch; exponentials to 2^-22, sums in fp32 over at most V / 256 terms a thread, joined in a fixed order.
+ *   One launch; exponentials to 2^-22, sums in fp32 (a thread's sixteen bytes of logits first, then its own, then the row's, in a fixed order); the terms of a log
+ *   probability are added in two fp32 numbers and rounded once.
  * bitlinear_token_logprobs_backward: dlogits[t][v] = grad[t] * ((v == targets[t]) - exp(l_v - max) / sum) from those stats; grad [T] fp32, the slope of any
  *   loss with logprobs.  A row whose grad is 0 gets zeros and is not read.
  * bitlinear_policy_loss: with r = exp(logp - old_logprobs[t]), A = advantages[t],
  *     token_loss[t] = weights[t] * ( -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1) ),  d = ref_logprobs[t] - logp,
- *   loss [1] their sum (fp64, fixed order), dlogits (nullable) its gradient; logits are read once.  weights NULL: 1; ref_logprobs may be NULL where kl_coef is 0.  A token
+ *   loss [1] their sum (fp64, fixed order), dlogits (nullable) its gradient.  Two launches.  weights NULL: 1; ref_logprobs may be NULL where kl_coef is 0.  A token
  *   of weight 0 adds no loss and no gradient, whatever else stands in its place.  clip_low, clip_high >= 0.
  * bitlinear_preference_loss: rows cu_tokens[i] .. cu_tokens[i+1]-1 (int32 [2 * pairs + 1], device) belong to answer i; answer 2j is preferred to answer 2j + 1.  With s_i
  *   the sum of answer i's log probabilities (fp64, fixed order) and ref_logprobs [2 * pairs] the same sums of the reference model,
  *     delta_j     = beta ((s_2j - ref_2j) - (s_2j+1 - ref_2j+1))
  *     pair_loss_j = -(1 - label_smoothing) log sigma(delta_j) - label_smoothing log sigma(-delta_j);      loss [1] = their mean,
  *   seq_logprobs [2 * pairs] = s, dlogits (nullable) the gradient of loss.  Offsets are clamped to 0 .. T and must not decrease; rows of no answer
- *   get a gradient of zeros.  ws (device, 16-byte aligned) at least bitlinear_preference_loss_workspace_bytes(T) bytes.
+ *   get a gradient of zeros.  Two to four launches.  ws (device, 16-byte aligned) at least bitlinear_preference_loss_workspace_bytes(T) bytes.
  *
  * bitlinear_attention_shared_kv8: bitlinear_attention_decode_kv8 for rows that share cache rows, which are then read and multiplied once for all of them.
  *   Rows group_starts[g] .. group_starts[g+1]-1 (int32 [n_groups + 1], device, not decreasing; clamped to 0 .. M) are group g, and its rows' first
