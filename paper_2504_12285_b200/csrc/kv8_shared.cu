@@ -13,11 +13,17 @@
 // cache rows (which are then converted once); else they take different cache rows.  What a row does not share is work of the same kind, with the few
 // query rows of that row alone.  All of it is cut into equal runs, one per CTA, whatever the lengths; parts of a row meet in a last launch.
 //
-//   warp 0      copies: block tables -> tensor-map copies of code tiles, and the work list that the other warps follow
+//   warp 0      the queries of rows' own tiles, ahead of the softmax
 //   warps 1, 2  one thread of each issues a stream's products
-//   warp 3      the queries of rows' own tiles, ahead of the softmax
+//   warp 3      copies: block tables -> tensor-map copies of code tiles, and the work list that the other warps follow (not on the scheduler of the softmax warps that
+//               have the first rows: where a tile has few query rows they have all the work)
 //   warps 4-11  softmax, one thread per query row; four warps per stream
 //   warps 12-19 codes -> f16, four warps to a tile
+//
+// Bound by its instruction caches: five warps of different roles to a scheduler, and two of them at any time wait for instructions.  So loops stay loops wherever a round
+// of them hides its own latency, and one loop does for whole and for partial tiles (conversion unrolled by four, once for either: ragged groups 86 -> 84 us, 64 answers over
+// 32,768 shared rows 100 -> 95).  A half step of 64 cache rows takes 3000 to 3500 cycles, of which the tensor cores need 1280: 64 answers over 32,768 rows 95 us (floor 13),
+// two chunks of 900 .. 1100 tokens behind 3000 .. 6000 222 us (71), 531 Tflop/s.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -586,35 +592,39 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 tc_fence_after();
                 if ((flags & (kFirst | kOwn)) == (kFirst | kOwn) && h == 0 && mine) f = query_down(smem[L::exponents + (s * 2 + (item & 1u)) * kTile + r]) * a.scale_log2;
                 if (any) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ks[i] *= f;
+                    if (!all_used) {  // what the row does not use scores -infinity, whatever lies there; its scales count for nothing
+                        const int l = max(lo - kHalf * h, 0), n = min(max(hi - kHalf * h, 0), kHalf);
+                        unsigned long long live = n > l ? (~0ull >> (64 - n)) & (~0ull << l) : 0ull;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if ((lost >> (4 * h + i)) & 1) live &= ~(0xffffull << (16 * i));
+                            const bool none = ((uint32_t)(live >> (16 * i)) & 0xffffu) == 0u;
+                            if (none || ks[i] == 0.0f) ks[i] = 1e-30f;  // -infinity times a scale of zero would be NaN; finite scores stay next to zero
+                            if (none) rs[i] = 0.0f;
+                        }
+#pragma unroll 1
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t x[16];
+                            tm_load16(ts + kHalf * h + 16 * i, x);
+                            const uint32_t used = (uint32_t)(live >> (16 * i));
+                            tm_load_wait();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (!((used >> e) & 1u)) x[e] = 0xff800000u;
+                            tm_store16(ts + kHalf * h + 16 * i, x);
+                        }
+                        tm_store_wait();
+                    }
                     uint32_t v[2][32];
                     tm_load(ts + kHalf * h, v[0]);
                     tm_load(ts + kHalf * h + 32, v[1]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) ks[i] *= f;
-                    float vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
+                    const float vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
                     float ww[4];  // the weights' factors, if the largest scale of values stays
 #pragma unroll
                     for (int i = 0; i < 4; ++i) ww[i] = rs[i] * per_ref;
                     tm_load_wait();
-                    if (!all_used) {  // what the row does not use scores -infinity, whatever lies there; its scales count for nothing
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const int l = max(lo - 32 * c - kHalf * h, 0), n = min(max(hi - 32 * c - kHalf * h, 0), 32);
-                            uint32_t live = n > l ? (uint32_t)((1ull << n) - (1ull << l)) : 0u;
-                            if ((lost >> (4 * h + 2 * c)) & 1) live &= 0xffff0000u;
-                            if ((lost >> (4 * h + 2 * c + 1)) & 1) live &= 0x0000ffffu;
-#pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (!((live >> e) & 1u)) v[c][e] = 0xff800000u;
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const bool none = (live & (i ? 0xffff0000u : 0x0000ffffu)) == 0u;
-                                if (none || ks[2 * c + i] == 0.0f) ks[2 * c + i] = 1e-30f;  // -infinity times a scale of zero would be NaN; finite scores stay next to zero
-                                if (none) rs[2 * c + i] = ww[2 * c + i] = 0.0f;
-                            }
-                        }
-                        vs = fmaxf(fmaxf(rs[0], rs[1]), fmaxf(rs[2], fmaxf(rs[3], 0.0f)));
-                    }
                     float top = -INFINITY;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -689,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
         }
     } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 0) {
+    if (warp == 3) {
         // ------------------------------------------------------------------ copies and the work list
         // Half of the lanes keep the books of either stream.
         const int s = lane >> 4, l16 = lane & 15;
@@ -862,7 +872,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             if (ended) break;
             now = next;
         }
-    } else if (warp <= 2) {
+    } else if (warp == 1 || warp == 2) {
         // ------------------------------------------------------------------ products, a warp for each stream: one thread starts a product every 55 cycles at most
         // (What the instructions take is made the same for all lanes first: they want it in uniform registers.)
         const int s = __shfl_sync(0xffffffffu, warp - 1, 0);
@@ -959,7 +969,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             }
             now = next, other_now = other, common_now = common;
         }
-    } else if (warp == 3) {
+    } else if (warp == 0) {
         // ------------------------------------------------------------------ queries of rows' own tiles
         // q_free completes once for each of a stream's own items, when its scores are made, and once before the first of them if pairs' items are in front, when the softmax
         // has seen the last one's scores.  This warp waits for every one in turn: it may fall steps behind a stream's pairs, and a barrier that moved on by two phases
@@ -1026,28 +1036,18 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
             const bool whole = !value || (cache_rows == kTile && lost == 0);
             const uint32_t in = src + in_at, out0 = dst + out_at, out1 = dst + (out_at ^ 16u);
             constexpr int STEP = 128 * 16 / D;  // rows from a thread's piece to its next
-            if (whole) {
-#pragma unroll 4
-                for (int i = 0; i < D / 16; ++i) {
-                    uint32_t w[4], h[8];
-                    lds128(in + i * STEP * D, w);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
-                    sts128(out0 + i * STEP * 128, h[0], h[1], h[2], h[3]);
-                    sts128(out1 + i * STEP * 128, h[4], h[5], h[6], h[7]);
-                }
-            } else {
+            // Values of no one's rows become 0: they may hold NaN, and zero times NaN is NaN.
+            const int there = whole ? kTile : cache_rows, gone = whole ? 0 : lost;
 #pragma unroll 1
-                for (int i = 0; i < D / 16; ++i) {
-                    uint32_t w[4], h[8];
-                    const int r = row + i * STEP;
-                    lds128(in + i * STEP * D, w);
-                    if (r >= cache_rows || ((lost >> (r >> 4)) & 1)) w[0] = w[1] = w[2] = w[3] = 0u;  // rows of no one may hold NaN, and zero times NaN is NaN
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t w[4], h[8];
+                const int r = row + i * STEP;
+                lds128(in + i * STEP * D, w);
+                if (r >= there || ((gone >> (r >> 4)) & 1)) w[0] = w[1] = w[2] = w[3] = 0u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
-                    sts128(out0 + i * STEP * 128, h[0], h[1], h[2], h[3]);
-                    sts128(out1 + i * STEP * 128, h[4], h[5], h[6], h[7]);
-                }
+                for (int j = 0; j < 4; ++j) codes_to_f16<KIND>(w[j], h[2 * j], h[2 * j + 1]);
+                sts128(out0 + i * STEP * 128, h[0], h[1], h[2], h[3]);
+                sts128(out1 + i * STEP * 128, h[4], h[5], h[6], h[7]);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
