@@ -292,7 +292,7 @@ class PagedDecodeStep:
             self.lengths, new_tokens, self.tables, self.free_blocks, self.n_free, self.block_rows, self.rows, lengths_out=self.lengths,
             n_free_out=self.n_free)
         place = self.seq_ids.clamp(min=0)
-        group_starts = self.cu_tokens.index_select(0, self.group_places) if self.groups else None
+        group_starts = self.cu_tokens.index_select(0, self.group_places.clamp(0, self.lengths.shape[0])) if self.groups else None
         ahead = ends.sub_(brought).sub_(self.cu_tokens[:-1])  # tokens in front of a place that have no row
         bl.bitlinear_embed(token_ids.index_select(0, ahead.index_select(0, place).add_(self.row_numbers)), self.table, out=self.h_in)
         for (qkv, o, gu, down), cache in zip(self.calls, self.cache):

@@ -181,3 +181,13 @@ def test_sampled_answers_are_learned_from():
         r = le.row(xs[int(order[t])], int(drawn[order[t]]))
         want = le.gradient(r[3], int(drawn[order[t]]), r[0], (-1 if (t // 3) % 2 == 0 else 1) * 0.5 / 2 / 2)
         assert np.abs(out[4][t].double().cpu().numpy() - want).max() <= 1e-4
+
+
+def test_group_places_outside_the_places():
+    # they count as the nearest place there is: one group of all places, one of none
+    st = make_step(sv.INT8)
+    gen = torch.Generator().manual_seed(64)
+    st.group_places.copy_(torch.tensor([-5, 99, 2 ** 31 - 1], dtype=torch.int32))
+    for new in ([3, 2, 0, 1, 0, 1, 1], [1, 1, 2, 1, 1, 1, 1]):
+        bring(st, new, gen)
+        check_last_layer(st, sv.INT8)
