@@ -823,8 +823,8 @@ def _dlogits(dlogits, logits):
     if dlogits is None or dlogits is False:
         return None, 0
     if dlogits is True:
-        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    elif dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != logits.device:
+        return torch.empty_like(logits), logits.shape[1]  # (rows without gaps, whatever lies between those of logits)
+    if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.device != logits.device:
         raise ValueError("the gradient must have the type, shape and device of logits")
     return dlogits, _logits(dlogits, "the gradient")[3]
 
