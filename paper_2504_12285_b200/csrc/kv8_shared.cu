@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const int row = quad * 32 + (i0 + i) * AT_ONCE + lane / LANES, flat = x.row0 + min(row, n_rows - 1), m = flat / a.group, j = flat - m * a.group;
-                                v[i] = __ldg(reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D) + unit);
+                                v[i] = *(reinterpret_cast<const uint4*>(a.q + ((size_t)m * a.n_q + (size_t)x.head * a.group + j) * D) + unit);
                             }
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
@@ -993,7 +993,7 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
                 if (r < x.rows) {
                     const uint4* src = reinterpret_cast<const uint4*>(a.q + ((size_t)x.row0 + (size_t)(x.row0 / a.group) * (a.n_q - a.group) + (size_t)x.head * a.group + r) * D) + c * (D / 32);
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) v[i] = __ldg(src + i), most = max(most, largest_bits(v[i]));
+                    for (int i = 0; i < D / 32; ++i) v[i] = src[i], most = max(most, largest_bits(v[i]));
                 }
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
                 most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));

@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(kThreads) token_grad_kernel(const GradArgs a) 
 }
 
 // sum of n numbers times scale in fp64, always in the same order: thread t adds every 1024th from t on, then a tree
-__global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict__ x, int n, double scale, float* __restrict__ out) {
+__global__ void __launch_bounds__(1024) loss_sum_kernel(const float* x, int n, double scale, float* out) {
     __shared__ double part[32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -611,9 +611,9 @@ __global__ void __launch_bounds__(1024) loss_sum_kernel(const float* __restrict_
 
 // A pair's answers: warps 0 .. 3 sum the preferred one's log probabilities, 4 .. 7 the other's (fp64, always in the same order), then all
 // write the tokens' slopes.  Rows of no answer keep the slope 0 that they were given before.  One CTA alone writes the mean, too.
-__global__ void __launch_bounds__(256) pair_kernel(const float* __restrict__ logprobs, const int* __restrict__ targets, const int* __restrict__ cu, const float* __restrict__ ref,
-                                                   int T, int V, int pairs, float beta, float smooth, float* __restrict__ pair_loss, float* __restrict__ seq_logprobs,
-                                                   float* __restrict__ grad, float* __restrict__ loss) {
+__global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const int* targets, const int* cu, const float* ref,
+                                                   int T, int V, int pairs, float beta, float smooth, float* pair_loss, float* seq_logprobs,
+                                                   float* grad, float* loss) {
     __shared__ double part[8];
     double total = 0.0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
