@@ -190,7 +190,9 @@ struct Running {
         Vec<T>::split(raw, v);
         const float top = Vec<T>::most(raw);
         if (top > m) {
-            const float next = top * kLog2e;
+            // Rounded up, c is nowhere below the product, and finite below -2^127: no element's exponential passes 1, whatever c's rounding is worth under a maximum of large
+            // magnitude (masked tokens in front of others). To the nearest, such a sum became infinite, and NaN with the next factor of 0.
+            const float next = __fmul_ru(top, kLog2e);
             sum.x *= ex2(c - next), sum.y *= ex2(c - next);
             m = top, c = next;
         }
