@@ -608,7 +608,7 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
  * bitlinear_preference_loss: rows cu_tokens[i] .. cu_tokens[i+1]-1 (int32 [2 * pairs + 1], device) belong to answer i; answer 2j is preferred to answer 2j + 1.  With s_i
  *   the sum of answer i's log probabilities (fp64, fixed order) and ref_logprobs [2 * pairs] the same sums of the reference model,
  *     delta_j     = beta ((s_2j - ref_2j) - (s_2j+1 - ref_2j+1))
- *     pair_loss_j = -(1 - label_smoothing) log sigma(delta_j) - label_smoothing log sigma(-delta_j);      loss [1] = their mean,
+ *     pair_loss_j = -(1 - label_smoothing) log sigma(delta_j) - label_smoothing log sigma(-delta_j)   (a term whose factor is 0 is 0, also where an answer's probability is);      loss [1] = their mean,
  *   seq_logprobs [2 * pairs] = s, dlogits (nullable) the gradient of loss.  Offsets are clamped to 0 .. T and must not decrease; rows of no answer
  *   get a gradient of zeros.  Two to four launches.  ws (device, 16-byte aligned) at least bitlinear_preference_loss_workspace_bytes(T) bytes.
  *

@@ -41,6 +41,6 @@ def policy_token(logp, old, adv, low, high, kl=0.0, ref=0.0):
 def pair(chosen, rejected, beta, smooth, pairs):
     """(loss of a pair whose answers are `chosen` and `rejected` above their references, slope of the mean over `pairs` with chosen)."""
     delta = beta * (chosen - rejected)
-    loss = (1.0 - smooth) * np.logaddexp(0.0, -delta) + smooth * np.logaddexp(0.0, delta)
+    loss = sum(f * np.logaddexp(0.0, x) for f, x in ((1.0 - smooth, -delta), (smooth, delta)) if f)  # a factor of 0 leaves nothing of an infinite term
     sigma = 1.0 / (1.0 + math.exp(-delta)) if delta >= 0 else math.exp(delta) / (1.0 + math.exp(delta))
     return float(loss), -beta / pairs * ((1.0 - smooth) * (1.0 - sigma) - smooth * sigma)

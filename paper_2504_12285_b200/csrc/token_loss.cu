@@ -638,7 +638,8 @@ __global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const 
         const float up = fminf(delta, 0.0f) - soft, down = fminf(-delta, 0.0f) - soft;
         const float slope = (float)(-(double)beta / pairs) * (1.0f / (1.0f + expf(delta)) - smooth);
         if (threadIdx.x == 0) {
-            const float value = -(1.0f - smooth) * up - smooth * down;
+            // (an answer of probability zero makes one of the two infinite: times a factor of 0 it would be NaN)
+            const float value = (smooth < 1.0f ? -(1.0f - smooth) * up : 0.0f) - (smooth > 0.0f ? smooth * down : 0.0f);
             pair_loss[i] = value;
             total += (double)value;
             seq_logprobs[2 * i] = (float)chosen;
