@@ -603,8 +603,8 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
  *   loss with logprobs.  A row whose grad is 0 gets zeros and is not read.
  * bitlinear_policy_loss: with r = exp(logp - old_logprobs[t]), A = advantages[t],
  *     token_loss[t] = weights[t] * ( -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(d) - d - 1) ),  d = ref_logprobs[t] - logp,
- *   loss [1] their sum (fp64, fixed order), dlogits (nullable) its gradient.  Two launches.  weights NULL: 1; ref_logprobs may be NULL where kl_coef is 0.  A token
- *   of weight 0 adds no loss and no gradient, whatever else stands in its place.  clip_low, clip_high >= 0.
+ *   loss [1] their sum (fp64, fixed order), dlogits (nullable) its gradient.  Two launches.  weights NULL: 1; ref_logprobs may be NULL where kl_coef is 0.  Where A
+ *   is 0 the first term is 0, however large r.  A token of weight 0 adds no loss and no gradient, whatever else stands in its place.  clip_low, clip_high >= 0.
  * bitlinear_preference_loss: rows cu_tokens[i] .. cu_tokens[i+1]-1 (int32 [2 * pairs + 1], device) belong to answer i; answer 2j is preferred to answer 2j + 1.  With s_i
  *   the sum of answer i's log probabilities (fp64, fixed order) and ref_logprobs [2 * pairs] the same sums of the reference model,
  *     delta_j     = beta ((s_2j - ref_2j) - (s_2j+1 - ref_2j+1))

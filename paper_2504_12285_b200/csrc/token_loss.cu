@@ -239,7 +239,8 @@ __device__ __forceinline__ LogProb log_prob(float chosen, float m, float sum) {
 // The policy loss of one token and its slope with the log probability: r = exp(logp - old),
 //   -min(r A, clip(r, 1 - low, 1 + high) A) + kl (exp(ref - logp) - (ref - logp) - 1).
 __device__ __forceinline__ void policy_token(LogProb logp, float old, float adv, float ref, float low, float high, float kl, float& loss, float& slope) {
-    const float r = expf((logp.hi - old) + logp.lo);
+    float r = expf((logp.hi - old) + logp.lo);
+    if (adv == 0.0f && r == INFINITY) r = 0.0f;  // 0 times a ratio past fp32 is 0
     const float free = r * adv, cut = fminf(fmaxf(r, 1.0f - low), 1.0f + high) * adv;
     const bool inside = free <= cut;
     loss = inside ? -free : -cut;

@@ -7,7 +7,7 @@ import torch
 
 from oracle import learning as le
 from paper_2504_12285_b200 import binding as bl
-from test_gpu_token_loss import DEV, F32, check_gradient, host
+from test_gpu_token_loss import DEV, F32, U, check_gradient, host, logp_error
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +47,34 @@ def test_answers_of_probability_zero(pairs, smooth):
     assert values[0] == (0.0 if smooth == 0 else math.inf) and values[1] == (0.0 if smooth == 1 else math.inf)
     want = math.fsum(values) / pairs if all(map(math.isfinite, values)) else math.inf
     assert float(loss) == want if math.isinf(want) else abs(float(loss) - want) <= 1e-5 * (1 + want)
+
+
+@pytest.mark.parametrize("T", [5, 160])
+def test_advantages_of_zero(T):
+    """Answers that are all rewarded alike have advantages of 0: the ratio, which leaves fp32 where a token was all but impossible when it was drawn, is multiplied by it."""
+    V = 700
+    x = torch.randn(T, V, generator=torch.Generator().manual_seed(T))
+    targets = torch.arange(T, dtype=torch.int32)
+    rows = [le.row(host(x[t]), t) for t in range(T)]
+    old = torch.tensor([r[0] for r in rows], dtype=F32) + 0.05
+    old[1], old[2], old[3] = -150.0, -1e10, -150.0
+    adv = torch.ones(T)
+    adv[:3], adv[3] = 0.0, 2.0
+    ref = torch.tensor([r[0] for r in rows], dtype=F32) - 0.3
+    for kl in (0.0, 0.25):
+        loss, token_loss, logp, d = bl.bitlinear_policy_loss(x.to(DEV), targets.to(DEV), old.to(DEV), adv.to(DEV), kl_coef=kl, ref_logprobs=ref.to(DEV), grad=True)
+        low = float(np.float32(0.2))
+        for t in range(T):
+            if t in (1, 2):  # (the ratio is multiplied by 0; one of the two is past 64 bits as well)
+                value, slope = le.policy_token(rows[t][0], rows[t][0], 0.0, low, low, kl, float(ref[t]))
+            else:
+                value, slope = le.policy_token(rows[t][0], float(old[t]), float(adv[t]), low, low, kl, float(ref[t]))
+            tol = (abs(float(adv[t])) * 1.2 + kl) * (logp_error(rows[t], V) + 10 * U) + abs(value) * 6 * U
+            assert abs(float(token_loss[t]) - value) <= tol, t
+            check_gradient(host(d[t]), le.gradient(rows[t][3], t, rows[t][0], slope), rows[t], V, t, F32, slope, tol)
+        assert abs(float(loss) - float(token_loss.double().sum())) <= U * abs(float(loss))
+    # what is not a number stays one
+    old[0] = math.nan
+    assert torch.isnan(bl.bitlinear_policy_loss(x.to(DEV), targets.to(DEV), old.to(DEV), adv.to(DEV))[1][0])
+    old[0], x[0, 5] = 0.0, math.nan
+    assert torch.isnan(bl.bitlinear_policy_loss(x.to(DEV), targets.to(DEV), old.to(DEV), adv.to(DEV))[1][0])
