@@ -614,8 +614,8 @@ int bitlinear_sample(const void* logits, int logits_dtype, int M, int V, long lo
  *
  * bitlinear_attention_shared_kv8: bitlinear_attention_decode_kv8 for rows that share cache rows, which are then read and multiplied once for all of them.
  *   Rows group_starts[g] .. group_starts[g+1]-1 (int32 [n_groups + 1], device, not decreasing; clamped to 0 .. M) are group g, and its rows' first
- *   shared_rows[g] cache rows (int32 [n_groups], device) are the same rows of the pool: their sequences' tables agree there (not checked; they are read by the table
- *   of the group's first row that has a length).  Answers to one prompt, each a sequence of its own, share the prompt's blocks; the tokens of a
+ *   shared_rows[g] cache rows (int32 [n_groups], device) are the same rows of the pool: their sequences' tables agree there, each as far as its
+ *   row's length (not checked; they are read by the tables of rows that reach furthest among them).  Answers to one prompt, each a sequence of its own, share the prompt's blocks; the tokens of a
  *   prompt's chunk are rows of one sequence with lengths position + 1, and share all of it.  A row uses none but the cache rows in front of its own length, shared
  *   or not; shared_rows need not be a multiple of anything, and may be longer than some rows of the group.  Rows of no group share nothing.
  *   Definition, types, limits, status word and what becomes of rows without a length as for bitlinear_attention_decode_kv8, with these exceptions:

@@ -52,7 +52,7 @@ constexpr float kWeightScale = 128.0f;  // weights of up to 2^8 (the maximum is 
 
 // Workspace.  A part: fp32 values of its query rows, then (max, sum) of each.
 struct SharedLayout {
-    size_t rows, pairs, cum_pairs, cum_rows, starts, firsts, pair_rows, item_ctas, totals, parts_w, parts_s, total;
+    size_t rows, pairs, cum_pairs, cum_rows, starts, pair_rows, item_ctas, totals, parts_w, parts_s, total;
     int max_pairs;
 };
 struct SharedArgs {
@@ -72,7 +72,6 @@ struct SharedArgs {
     int* cum_pairs;   // units of the pairs in front, all heads
     int* cum_rows;    // tiles of the rows' own parts in front, and a place for each part's start, all heads
     int* starts;      // group_starts, in range and not decreasing
-    int* firsts;      // of each group: its first row with something in the cache
     int* pair_rows;   // of each pair: cache rows
     int4* item_ctas;  // of each pair and head: its first unit, the first and last CTA that have some of it
     int* totals;      // pairs, units of pairs, tiles of rows
@@ -151,15 +150,14 @@ __device__ __forceinline__ int block_max_scan(int x, int* warp_sums) {  // inclu
 // One CTA: which rows share what, the pairs of query tiles, and how many units lie in front of each pair and row.
 __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedArgs a, int ctas) {
     __shared__ int warp_sums[32];
-    __shared__ int few[3][kFewGroups + 1];
+    __shared__ int few[2][kFewGroups + 1];
     __shared__ int few_pairs[kFewGroups];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, cap = a.max_blocks << a.log2_rows;
     // what the phases hand on lies in shared memory where it fits: a phase costs a microsecond less than by way of L2
     int* const starts = a.n_groups <= kFewGroups ? few[0] : a.starts;
-    int* const firsts = a.n_groups <= kFewGroups ? few[1] : a.firsts;
-    int* const first_pairs = a.n_groups <= kFewGroups ? few[2] : a.cum_pairs;  // (overwritten later)
+    int* const first_pairs = a.n_groups <= kFewGroups ? few[1] : a.cum_pairs;  // (overwritten later)
     int* const pair_rows = a.max_pairs <= kFewGroups ? few_pairs : a.pair_rows;
     // the groups' borders
     int carry = 0;
@@ -172,7 +170,7 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
         carry = starts[min(g0 + kPlanThreads - 1, a.n_groups)];
     }
     __syncthreads();
-    // the groups' pairs; a row on its own shares nothing.  pairs[].z holds the group for now; pair_rows: the most that a pair's rows share
+    // the groups' pairs; a row on its own shares nothing.  pair_rows: the most that a pair's rows share
     int n_pairs = 0;
     for (int g0 = 0; g0 < a.n_groups; g0 += kPlanThreads) {
         const int g = g0 + tid;
@@ -186,13 +184,10 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
         int total;
         const int at = n_pairs + block_exclusive_scan(n, warp_sums, total);
         for (int i = 0; i < n; ++i) {
-            a.pairs[at + i] = make_int4(first * a.group + i * 2 * kTile, min(2 * kTile, query_rows - i * 2 * kTile), g, 0);
+            a.pairs[at + i] = make_int4(first * a.group + i * 2 * kTile, min(2 * kTile, query_rows - i * 2 * kTile), 0, 0);
             pair_rows[at + i] = 0;
         }
-        if (g < a.n_groups) {
-            first_pairs[g] = n > 0 ? at : -1;
-            firsts[g] = a.M;
-        }
+        if (g < a.n_groups) first_pairs[g] = n > 0 ? at : -1;
         n_pairs += total;
     }
     __syncthreads();
@@ -224,11 +219,10 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
             if (lo < a.n_groups && starts[lo] <= m && first_pairs[lo] >= 0) {
                 const int flat0 = starts[lo] * a.group;
                 info = make_int4(min(len, a.shared_rows[lo]), len, first_pairs[lo], flat0);
-                if (len > 0) {
+                if (info.x > 0) {
                     const int p0 = info.z + (m * a.group - flat0) / (2 * kTile), p1 = info.z + (m * a.group + a.group - 1 - flat0) / (2 * kTile);
                     for (int p = p0; p <= p1; ++p)
                         if (pair_rows[p] < info.x) atomicMax(&pair_rows[p], info.x);
-                    if (firsts[lo] > m) atomicMin(&firsts[lo], m);
                 }
             }
             a.rows[m] = info;
@@ -256,8 +250,27 @@ __global__ void __launch_bounds__(kPlanThreads) shared_plan_kernel(const SharedA
             info.w = pair_rows[p];
             const int span = info.y > kTile ? kTile : 2 * kTile;  // a unit: one tile of cache rows for two query tiles, or two for one
             units = (info.w + span - 1) / span * a.n_kv;
-            const int first = firsts[info.z];
-            info.z = first < a.M ? (a.seq_ids ? a.seq_ids[first] : first) : 0;  // (no row has anything in the cache: no units)
+            // It is read by the table of a row that has all of its cache rows; others' tables may end before.  The last row of a chunk is one, and any row of answers behind
+            // their prompt, so the search begins at the end (with the maximum and its row in one 64-bit atomic the plan of two chunks took 10 us more).
+            int row = 0;
+            if (info.w > 0) {
+                row = (info.x + info.y - 1) / a.group;
+                for (bool found = a.rows[row].x == info.w; !found;) {
+                    constexpr int AT_ONCE = 8;
+                    const int from = row, first = info.x / a.group;
+                    int x[AT_ONCE];
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) x[k] = a.rows[max(from - 1 - k, first)].x;
+#pragma unroll
+                    for (int k = AT_ONCE - 1; k >= 0; --k)
+                        if (x[k] == info.w) row = max(from - 1 - k, first), found = true;
+                    if (!found) {
+                        row = max(from - AT_ONCE, first);
+                        found = row == first;  // (never without one)
+                    }
+                }
+            }
+            info.z = a.seq_ids ? a.seq_ids[row] : row;  // (no row has anything in the cache: no units)
             a.pairs[p] = info;
         }
         int total;
@@ -1349,7 +1362,6 @@ SharedLayout shared_layout(int M, int n_groups, int n_q, int n_kv, int D) {
     l.cum_pairs = room(((size_t)std::max(l.max_pairs, n_groups) + 1) * sizeof(int));
     l.cum_rows = room(((size_t)M + 1) * sizeof(int));
     l.starts = room(((size_t)n_groups + 1) * sizeof(int));
-    l.firsts = room(((size_t)n_groups + 1) * sizeof(int));
     l.pair_rows = room((size_t)l.max_pairs * sizeof(int));
     l.item_ctas = room((size_t)l.max_pairs * n_kv * sizeof(int4));
     l.totals = room(3 * sizeof(int));
@@ -1462,7 +1474,7 @@ int bitlinear_attention_shared_kv8(const void* q_bf16, const void* k_cache, cons
     SharedArgs a = {static_cast<const __nv_bfloat16*>(q_bf16), k_scale, v_scale, tables, lengths, seq_ids, group_starts, shared_rows, M, n_groups, n_q_heads, n_kv_heads,
                     n_q_heads / n_kv_heads, n_seq, max_blocks, log2_of(block_rows), n_blocks, 1.4426950408889634f / sqrtf((float)head_dim), static_cast<__nv_bfloat16*>(out_bf16),
                     reinterpret_cast<int4*>(w + l.rows), reinterpret_cast<int4*>(w + l.pairs), reinterpret_cast<int*>(w + l.cum_pairs), reinterpret_cast<int*>(w + l.cum_rows),
-                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.firsts), reinterpret_cast<int*>(w + l.pair_rows), reinterpret_cast<int4*>(w + l.item_ctas), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
+                    reinterpret_cast<int*>(w + l.starts), reinterpret_cast<int*>(w + l.pair_rows), reinterpret_cast<int4*>(w + l.item_ctas), reinterpret_cast<int*>(w + l.totals), reinterpret_cast<float*>(w + l.parts_w), reinterpret_cast<float*>(w + l.parts_s),
                     l.max_pairs, device_status_word()};
     const int ctas = std::min(sm_count, kSharedCtas);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
