@@ -197,7 +197,7 @@ class PagedDecodeStep:
 
     With `groups`, several answers to one prompt read its cache rows once for all: the prompt goes to one place, fork() lets the places behind it begin with its
     whole blocks, and group g is places group_places[g] .. group_places[g + 1] - 1, which share their first shared_rows[g] rows.  A place gives back the blocks it
-    did not borrow; the one they were borrowed from must not finish before the others."""
+    did not borrow; one whose blocks others still read is left out of a step in which it would finish (served 0: it finishes with the last of them, or later)."""
 
     def __init__(self, layers, embedding: torch.Tensor, rows: int, places: int, n_blocks: int, block_rows: int, max_blocks: int, hidden: int, ffn: int,
                  n_q_heads: int, n_kv_heads: int, head_dim: int, kv_dtype=torch.int8, rms_eps: float = 1e-5, rope_base: float = 500000.0,
@@ -232,10 +232,12 @@ class PagedDecodeStep:
         # how each place draws its tokens: temperature (0: the likeliest), top_k (0: off), top_p (1: off), min_p (0: off)
         self.temperature, self.top_k = torch.ones(places, **f32), torch.zeros(places, **i32)
         self.top_p, self.min_p = torch.ones(places, **f32), torch.zeros(places, **f32)
-        # groups of places, as they share cache rows: which places, how many rows; the blocks at the head of each place's table that it has borrowed
+        # groups of places, as they share cache rows: which places, how many rows; the blocks at the head of each place's table that it has borrowed,
+        # and [p, q]: some of them belong to place q
         self.groups = groups
         self.group_places, self.shared_rows = torch.zeros(groups + 1, **i32), torch.zeros(groups, **i32)
         self.borrowed, self.columns = torch.zeros(places, dtype=torch.int64, device=dev), torch.arange(max_blocks, device=dev)
+        self.lenders = torch.zeros(places, places, dtype=torch.bool, device=dev)
         ws_bytes = (bl.bitlinear_attention_shared_kv8_workspace_bytes(rows, groups, n_q_heads, n_kv_heads, head_dim) if groups else
                     bl.bitlinear_attention_kv8_workspace_bytes(n_q_heads, n_kv_heads, head_dim))
         self.attn_ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
@@ -261,6 +263,9 @@ class PagedDecodeStep:
         self.tables[to, :blocks] = self.tables[source, :blocks]
         self.lengths[to] = blocks * self.block_rows
         self.borrowed[to] = blocks
+        if blocks:
+            self.lenders[to] = self.lenders[source]
+            self.lenders[to, source] = blocks > int(self.borrowed[source])
         return blocks * self.block_rows
 
     def step(self, token_ids: torch.Tensor, u: torch.Tensor):
@@ -268,7 +273,7 @@ class PagedDecodeStep:
         left out among them: a place whose tokens end beyond the rows is left out); u: fp32 [rows], a random number for each row.
         -> (ids int32 [rows], logprobs fp32 [rows]): the token drawn behind each row; the last row of place p is row
         cu_tokens[p + 1] - 1, and rows from cu_tokens[-1] on mean nothing.  served[p] is 0 where the pool, the rows or the place's table did
-        not suffice and the place's tokens were left out."""
+        not suffice and the place's tokens were left out, and where a place would have finished whose blocks others still read."""
         n_q, n_kv, hd = self.dims
         # all that a later call would refuse, before the first one changes the state
         bl._tensors((token_ids, torch.int32, (self.rows,), "token_ids"), (u, torch.float32, (self.rows,), "u"))
@@ -283,7 +288,13 @@ class PagedDecodeStep:
         brought = self.new_tokens.clamp(min=0)
         ends = brought.cumsum(0)
         new_tokens = self.new_tokens.masked_fill((ends > self.rows).logical_and_(brought > 0), 2 ** 31 - 1)
-        if self.groups:  # a finished place first lets go of what it borrowed: its own blocks move to the head of its table
+        if self.groups:
+            # a place that lent blocks stays while one that does not finish has them (who borrowed from a borrower has the first lender among its own)
+            finished = new_tokens < 0
+            read = (self.lenders & ~finished[:, None]).any(0)
+            new_tokens.masked_fill_(finished & read, 2 ** 31 - 1)
+            self.lenders.masked_fill_((new_tokens < 0)[:, None], False)
+            # a finished place first lets go of what it borrowed: its own blocks move to the head of its table
             drop = self.borrowed.masked_fill(new_tokens >= 0, 0)
             self.tables.copy_(self.tables.gather(1, (self.columns + drop[:, None]).clamp_(max=self.tables.shape[1] - 1)))
             self.lengths.sub_((drop * self.block_rows).to(torch.int32))
