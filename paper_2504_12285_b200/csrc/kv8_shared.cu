@@ -1100,25 +1100,25 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 
 // ---------------------------------------------------------------------------------------------- the parts of a row
 
-// A query head's parts, by WARPS warps: warp w takes parts w, w + WARPS, ... of each of the two kinds.  Lane l first finds the l-th of a round's parts and weighs it;
+// A query head's parts, by four warps: each takes 32 parts in turn of each of the two kinds.  Lane l first finds the l-th of a round's parts and weighs it;
 // then all lanes add up the rounds' values, a few dims each, eight parts' loads in flight.
-template <int D, int WARPS>
-__global__ void __launch_bounds__(128, 6) shared_combine_kernel(const SharedArgs a, int ctas) {
+constexpr int kJoinWarps = 4;
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinWarps, 6) shared_combine_kernel(const SharedArgs a, int ctas) {
     constexpr int DIMS = D / 32, AT_ONCE = 8;
-    __shared__ float2 joined[4];
-    __shared__ float values[4][D];
+    __shared__ float2 joined[kJoinWarps];
+    __shared__ float values[kJoinWarps][D];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int item = (int)blockIdx.x * (4 / WARPS) + warp / WARPS, m = item / a.n_q, head = item - m * a.n_q, h = head / a.group, j = head - h * a.group, w = warp % WARPS;
-    const bool there = m < a.M;
+    const int item = (int)blockIdx.x, m = item / a.n_q, head = item - m * a.n_q, h = head / a.group, j = head - h * a.group;
     const int units = a.totals[1], tiles = a.totals[2];
     const EqualRuns runs(2 * units + tiles, ctas);
-    const int4 row = there ? a.rows[m] : make_int4(0, 0, -1, 0);
+    const int4 row = a.rows[m];
     float top = -INFINITY, l = 0.0f, acc[DIMS] = {};
     // n parts of n_rows query rows (a lane finds its own by `find`: nullptr where it is none; which of the rows)
     auto gather = [&](int n, int n_rows, auto find) {
-        for (int i0 = 32 * w; i0 < n; i0 += 32 * WARPS) {
+        for (int i0 = 32 * warp; i0 < n; i0 += 32 * kJoinWarps) {
             const float* part = nullptr;
             int r = 0;
             if (i0 + lane < n) part = find(i0 + lane, r);
@@ -1194,29 +1194,26 @@ __global__ void __launch_bounds__(128, 6) shared_combine_kernel(const SharedArgs
             return a.parts_s + (size_t)(m * a.n_kv + h + k) * part_floats(a.group, D);
         });
     }
-    if constexpr (WARPS > 1) {
-        if (lane == 0) joined[warp] = make_float2(top, l);
+    if (lane == 0) joined[warp] = make_float2(top, l);
 #pragma unroll
-        for (int e = 0; e < DIMS; ++e) values[warp][DIMS * lane + e] = acc[e];
-        __syncthreads();
-        if (w != 0) return;
-        float most = top;
+    for (int e = 0; e < DIMS; ++e) values[warp][DIMS * lane + e] = acc[e];
+    __syncthreads();
+    if (warp != 0) return;
+    float most = top;
 #pragma unroll
-        for (int k = 1; k < WARPS; ++k) most = fmaxf(most, joined[warp + k].x);
-        const float f0 = top == -INFINITY ? (l == l ? 0.0f : NAN) : ex2(top - most);
-        l *= f0;
+    for (int k = 1; k < kJoinWarps; ++k) most = fmaxf(most, joined[k].x);
+    const float f0 = top == -INFINITY ? (l == l ? 0.0f : NAN) : ex2(top - most);
+    l *= f0;
 #pragma unroll
-        for (int e = 0; e < DIMS; ++e) acc[e] *= f0;
+    for (int e = 0; e < DIMS; ++e) acc[e] *= f0;
 #pragma unroll
-        for (int k = 1; k < WARPS; ++k) {
-            const float2 o = joined[warp + k];
-            const float f = o.x == -INFINITY ? (o.y == o.y ? 0.0f : NAN) : ex2(o.x - most);
-            l = fmaf(o.y, f, l);
+    for (int k = 1; k < kJoinWarps; ++k) {
+        const float2 o = joined[k];
+        const float f = o.x == -INFINITY ? (o.y == o.y ? 0.0f : NAN) : ex2(o.x - most);
+        l = fmaf(o.y, f, l);
 #pragma unroll
-            for (int e = 0; e < DIMS; ++e) acc[e] = fmaf(values[warp + k][DIMS * lane + e], f, acc[e]);
-        }
+        for (int e = 0; e < DIMS; ++e) acc[e] = fmaf(values[k][DIMS * lane + e], f, acc[e]);
     }
-    if (!there) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no row: zeros; a sum that is NaN stays one
     uint32_t out[DIMS / 2];
 #pragma unroll
@@ -1429,14 +1426,14 @@ int shared_launch(const CUtensorMap& map_k, const CUtensorMap& map_v, const Shar
     // four warps per query head; one per row and KV head where there are thousands of rows, which have few parts each (2173 rows: 27 us with a warp per query head, 22 so;
     // but 144 rows of six groups 17 and 25)
     const long long heads = (long long)a.M * a.n_q, items = (long long)a.M * a.n_kv;
-    cfg.blockDim = dim3(128);
+    cfg.blockDim = dim3(32 * kJoinWarps);
     cfg.dynamicSmemBytes = 0;
     if (heads >= 128ll * ctas) {
         cfg.gridDim = dim3((unsigned)((items + 3) / 4));
         return finish(cudaLaunchKernelEx(&cfg, shared_combine_rows_kernel<D>, a, ctas));
     }
     cfg.gridDim = dim3((unsigned)heads);
-    return finish(cudaLaunchKernelEx(&cfg, shared_combine_kernel<D, 4>, a, ctas));
+    return finish(cudaLaunchKernelEx(&cfg, shared_combine_kernel<D>, a, ctas));
 }
 
 }  // namespace

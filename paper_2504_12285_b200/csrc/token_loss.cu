@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(256) pair_kernel(const float* logprobs, const 
 
 int dtype_bytes(int dtype) { return dtype == BITLINEAR_F32 ? 4 : dtype == BITLINEAR_BF16 ? 2 : 0; }
 
-cudaError_t launch_dependent(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int clusters) {
+void launch_dependent(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int clusters) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
@@ -664,7 +664,6 @@ cudaError_t launch_dependent(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = clusters > 1 ? 2 : 1;
-    return cudaSuccess;
 }
 
 int finish(cudaError_t rc) {
@@ -781,7 +780,7 @@ int bitlinear_token_logprobs_backward(const void* logits, int logits_dtype, int 
     if (logits == dlogits && d_stride != row_stride) return BITLINEAR_ERR_SHAPE;
     if (!element_aligned(logits, logits_dtype) || !element_aligned(dlogits, logits_dtype) || reinterpret_cast<uintptr_t>(stats) % 8) return BITLINEAR_ERR_ALIGN;
     int sm_count = 0;
-    if (const int rc = device_sm_count(&sm_count)) return rc;
+    if (const int rc = device_sm_count(&sm_count)) return rc;  // (for the device's architecture; the grid does not hang on the number)
     const GradArgs a = {logits, row_stride, targets, reinterpret_cast<const float2*>(stats), grad, dlogits, d_stride, T, V, 0};
     return grad_pass(a, logits_dtype, static_cast<cudaStream_t>(stream));
 }
