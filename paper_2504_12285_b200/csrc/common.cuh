@@ -123,6 +123,13 @@ int int8_mma_rate_probe(int n_mma, double* ops_out, cudaStream_t st);
 // SM count of the current device (cached per device; BITLINEAR_ERR_ARCH unless it is compute capability 10.x).
 int device_sm_count(int* sm_count);
 
+// The status of a launch; its error does not stay for the next one.
+inline int finish(cudaError_t rc) {
+    if (rc == cudaSuccess) return BITLINEAR_OK;
+    cudaGetLastError();
+    return BITLINEAR_ERR_CUDA;
+}
+
 // Sticky device-side status word (set by kernels whose bounded waits ran out).
 int* device_status_word();
 

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "bitlinear.h"
+#include "fp32_math.cuh"
 
 namespace bitlinear {
 
@@ -19,12 +20,6 @@ inline int log2_of(int block_rows) { return block_rows == 16 ? 4 : block_rows ==
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
-}
-// 2^x to two units in the last place; results below 2^-126 are 0
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 
 // Four codes of a word -> two pairs of f16, exactly.  int8: the code plus 128 becomes the low bits of 1024 + x, and

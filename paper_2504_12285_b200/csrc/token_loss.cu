@@ -13,6 +13,7 @@
 // Where the slope of the loss follows from the token alone (the policy loss), logits are read from memory once and the gradient is written once.  A loss over pairs needs
 // all rows of both answers first: a pass for the log probabilities, one for the gradient that begins with the rows that are still in L2.
 #include "common.cuh"
+#include "fp32_math.cuh"
 #include "sm100_sync.cuh"
 
 #include <cooperative_groups.h>
@@ -107,24 +108,8 @@ struct Vec<__nv_bfloat16> {
     static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 };
 
-// 2^x to two units in the last place; results below 2^-126 are 0
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // exp(x - m) for x <= m: the difference is rounded once, so what weighs most is off least
 __device__ __forceinline__ float exp_below(float x, float m) { return ex2((x - m) * kLog2e); }
-
-// Two fp32 operations an instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 d;
-    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 splat(float x) { return make_float2(x, x); }
 
 // The same exponentials by one multiply-add, for many elements of a row: 2^(x log2(e) - c) with c = fl(m log2(e)).  That is off from exp(x - m) by
 // the factor 2^(m log2(e) - c), the same for all elements, which is put right once (`residue`).  For |m| of 2^20 and more that factor leaves the range of
@@ -664,12 +649,6 @@ void launch_dependent(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], i
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = clusters > 1 ? 2 : 1;
-}
-
-int finish(cudaError_t rc) {
-    if (rc == cudaSuccess) return BITLINEAR_OK;
-    cudaGetLastError();
-    return BITLINEAR_ERR_CUDA;
 }
 
 template <typename T, int MODE>
