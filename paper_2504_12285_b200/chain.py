@@ -283,6 +283,13 @@ class PagedDecodeStep:
                 raise TypeError(f"{name} must be of {dtype} and on the step's device")
             if t.dim() != 1 or t.shape[0] < self.new_tokens.shape[0]:
                 raise ValueError(f"{name} must have an entry for each place")
+        for name, dtypes, n in (("new_tokens", (torch.int32,), self.lengths.shape[0]), ("group_places", (torch.int32, torch.int64), self.groups + 1)):
+            t = getattr(self, name)
+            if t.dtype not in dtypes or t.get_device() != u.get_device():
+                raise TypeError(f"{name} must be of {' or '.join(map(str, dtypes))} and on the step's device")
+            if t.shape != (n,):
+                raise ValueError(f"{name} must be ({n},), not {tuple(t.shape)}")
+        bl._tensors((self.shared_rows, torch.int32, (self.groups,), "shared_rows"))
         # a place that outgrows its table is left out and those behind it are not: each place keeps its tokens, and one whose tokens are not
         # all among token_ids asks for more than any table holds
         brought = self.new_tokens.clamp(min=0)
