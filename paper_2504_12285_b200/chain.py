@@ -197,7 +197,9 @@ class PagedDecodeStep:
 
     With `groups`, several answers to one prompt read its cache rows once for all: the prompt goes to one place, fork() lets the places behind it begin with its
     whole blocks, and group g is places group_places[g] .. group_places[g + 1] - 1, which share their first shared_rows[g] rows.  A place gives back the blocks it
-    did not borrow; one whose blocks others still read is left out of a step in which it would finish (served 0: it finishes with the last of them, or later)."""
+    did not borrow; one whose blocks others still read is left out of a step in which it would finish (served 0: it finishes with the last of them, or later).
+    Groups save memory at any length; time they save from about 150,000 cache rows on that a step's rows use in all.  A recorded step of 16 places on 2B sizes takes, without and
+    with a group of all of them, 2.12 and 2.57 ms behind a prompt of 1024 tokens, 2.48 and 3.01 behind 4096, 5.20 and 3.52 behind 32,768."""
 
     def __init__(self, layers, embedding: torch.Tensor, rows: int, places: int, n_blocks: int, block_rows: int, max_blocks: int, hidden: int, ffn: int,
                  n_q_heads: int, n_kv_heads: int, head_dim: int, kv_dtype=torch.int8, rms_eps: float = 1e-5, rope_base: float = 500000.0,

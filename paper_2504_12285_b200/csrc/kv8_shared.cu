@@ -23,7 +23,7 @@
 // Bound by its instruction caches: five warps of different roles to a scheduler, and two of them at any time wait for instructions.  So loops stay loops wherever a round
 // of them hides its own latency, and one loop does for whole and for partial tiles (conversion unrolled by four, once for either: ragged groups 86 -> 84 us, 64 answers over
 // 32,768 shared rows 100 -> 95).  A half step of 64 cache rows takes 3000 to 3500 cycles, of which the tensor cores need 1280: 64 answers over 32,768 rows 95 us (floor 13),
-// two chunks of 900 .. 1100 tokens behind 3000 .. 6000 222 us (71), 531 Tflop/s.
+// two chunks of 900 .. 1100 tokens behind 3000 .. 6000 223 us (71), 530 Tflop/s.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -653,7 +653,8 @@ __global__ void __launch_bounds__(kThreads, 1) shared_attention_kernel(const __g
 #pragma unroll
                         for (int i = 0; i < 4; ++i) ww[i] = rs[i] * per_ref;
                     }
-                    // Weights are rounded to f16, up to 2^-11 of each, an eighth of what the result's rounding to bf16 may cost; their sum takes them unrounded.
+                    // Weights, times their rows' scale of values, are rounded to f16 in units of the largest scale met so far: up to 2^-11 of each, an eighth of what the result's
+                    // rounding to bf16 may cost, and below 2^-21 of those units, where f16 has no more normal numbers, up to 2^-32 of them.  Their sum takes them unrounded.
                     // They go over the scores.
                     float2 sum = make_float2(0.0f, 0.0f);
                     const float2 bb = splat(m_run == -INFINITY ? 0.0f : -m_run);

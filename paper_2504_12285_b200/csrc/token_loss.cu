@@ -380,8 +380,9 @@ __global__ void __launch_bounds__(kThreads, 3) token_row_kernel(const RowArgs a)
     if (abort_flag) abort_drain();
 }
 
-// Many rows: a CTA to a row, which it streams from memory for the statistics and, for the gradient, once more from L2 - the rows under way are 128 bytes for each
-// of the vocabulary and SM at most, which L2 holds.  No CTA waits for another, so that loads and stores of several rows are under way at any time.
+// Many rows: a CTA to a row, which it streams from memory for the statistics and, for the gradient, once more - from L2, as far as that holds the rows under way, two to
+// an SM: 76 MB of 128,256 bf16 logits, but 152 MB of as many in fp32, of which some come from memory again (1500 rows 367 us; the same bytes as 3000 rows of bf16 325, of
+// 64,128 fp32 305; in slices for the clusters of the other kernel 468).  No CTA waits for another, so that loads and stores of several rows are under way at any time.
 constexpr int kStreamThreads = 512;
 __host__ __device__ constexpr int stream_units(int mode) { return mode == kPolicy ? 8 : 4; }  // loads in flight a thread
 
