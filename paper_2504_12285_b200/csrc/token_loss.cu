@@ -682,7 +682,8 @@ int launch_rows(RowArgs a, int rows, int sm_count, cudaStream_t st) {
     // few rows: more CTAs to each while SMs are idle and a part keeps 4 KB
     while (ranks < kMaxRanks && (long long)rows * ranks * 2 <= sm_count && part() >= 512) ranks *= 2;
     a.part = (int)std::max(part(), 1ll);
-    a.piece = std::max(512, (a.part + kMaxPieces - 1) / kMaxPieces);
+    // (whole rounds of the CTA's threads: a thread that goes over the part again without regard to pieces meets the units whose maximum it has)
+    a.piece = std::max(512, ((a.part + kMaxPieces - 1) / kMaxPieces + kThreads - 1) / kThreads * kThreads);
     if (a.part * 16 > kMost || (long long)rows * ranks > 0x7fffffffll) return BITLINEAR_ERR_SHAPE;
     cudaLaunchAttribute attr[2];
     cudaLaunchConfig_t cfg = {};

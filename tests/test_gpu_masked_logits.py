@@ -127,3 +127,25 @@ def test_masked_targets(V, copies, dtype):
     logp, stats = bl.bitlinear_token_logprobs(xd, td)
     d = bl.bitlinear_token_logprobs_backward(xd, td, stats, torch.ones(3 * copies, device=DEV))
     check_rows(x, td.cpu()[:3], logp, stats, d, [1.0] * 3, dtype)
+
+
+@pytest.mark.parametrize("V", [196609, 300001, 360448])
+@pytest.mark.parametrize("free", [40, 3000])
+def test_masked_rows_of_a_large_vocabulary(V, free):
+    """Few tokens are free, so that most threads meet masks alone and go over their part twice, next to threads that do not; masks of several sizes stand among each other."""
+    gen = torch.Generator().manual_seed(V + free)
+    levels = torch.tensor([-1e7, -1e10, -1e30, -1e38, -3e38, torch.finfo(F32).min, -math.inf])
+    x = levels[torch.randint(0, 7, (4, V), generator=gen)]
+    for t in range(4):
+        some = torch.randperm(V, generator=gen)[:free]
+        x[t, some] = torch.randn(free, generator=gen) * 3.0
+    x[3] = torch.where(x[3] > -1e6, torch.tensor(-1e7), x[3])  # none is free: those of the highest level share all
+    targets = x.argmax(1).to(torch.int32)
+    xd, td = x.to(DEV), targets.to(DEV)
+    logp, stats = bl.bitlinear_token_logprobs(xd, td)
+    d = bl.bitlinear_token_logprobs_backward(xd, td, stats, torch.ones(4, device=DEV))
+    check_rows(x, targets, logp, stats, d, [1.0] * 4, F32)
+    want = [le.row(host(x[t]), int(targets[t]))[0] for t in range(4)]
+    old = torch.tensor(want, dtype=F32)
+    got = bl.bitlinear_policy_loss(xd, td, old.to(DEV), torch.ones(4, device=DEV), grad=True)
+    check_rows(x, targets, got[2], None, got[3], [-math.exp(w - float(o)) for w, o in zip(want, old)], F32)
